@@ -507,6 +507,117 @@ void tb_registry_free(tb_registry* r);
  */
 int tb_unregister_model_noalloc(tb_registry* r, int32_t id, void* hip_stream);
 
+/*
+ * Row operators: what a program asks of rows of logits next to their decoding.
+ * They need no arena. A row z[0..V] at temperature tau > 0 has u = z / tau,
+ * p = softmax(u) and lse = log-sum-exp(u).
+ *
+ * Arguments shared by all of them
+ *
+ *   logits        device, element type dtype (TB_F32, TB_BF16), row i at
+ *                 i * row_stride elements (row_stride >= V+1; the rows of
+ *                 logits[T,B,K,:] in order); 4-byte / 2-byte aligned
+ *   n_rows        rows, in [0, 2^40]; 0 is a no-op that touches no buffer
+ *   v_plus_blank  V + 1, in [2, TB_MAX_ROW]: also wider than the step calls take
+ *   temperature   in [1e-4, 1e4]
+ *   workspace     device, 16-byte aligned, tb_rows_workspace_bytes(...) bytes
+ *                 (TB_ENOMEM when smaller); that is 0, and workspace may be
+ *                 NULL, unless rows are cut into segments. It is free again
+ *                 once the stream has passed the call.
+ *
+ * A list holds up to TB_MAX_LIST token ids per row, -1 for an unused place (at
+ * any place). Any other id outside [0, V] is never dereferenced and makes what
+ * depends on it NaN. Outputs may share memory neither with one another nor with
+ * inputs (TB_EINVAL), except that a gradient may take the logits' own place
+ * (same pointer and stride).
+ *
+ * A token at -inf has probability 0 (a token at the type's lowest value as
+ * well, unless all are). A row whose every value is -inf is empty: lse -inf,
+ * log probabilities -inf, entropy 0, no alternatives, a loss of +inf where the
+ * teacher has any mass, gradients 0. A row that holds a NaN or +inf has NaN
+ * lse, log probabilities, entropy, loss and gradients. Sums are float32
+ * relative to the row's maximum; gradients are rounded once to dtype.
+ */
+enum { TB_MAX_LIST = 64, TB_MAX_ROW = 1 << 20 };
+
+/*
+ * tb_rows_workspace_bytes — bytes a row operator needs for rows of this type,
+ * count and width and n_alt alternatives (0 for the gradients and tb_distill);
+ * -1 for arguments the operators reject.
+ */
+int64_t tb_rows_workspace_bytes(int32_t dtype, int64_t n_rows, int32_t v_plus_blank,
+                                int32_t n_alt);
+
+/*
+ * tb_token_logprobs — per row the log probabilities of n_tok given tokens, the
+ * log-sum-exp, the entropy and the n_alt best alternatives (confidences of
+ * decoded tokens, blank against label, a teacher's lists for tb_distill).
+ *
+ *   tokens            device int32[n_rows * n_tok]
+ *   out_logprob       device float[n_rows * n_tok]: u[token] - lse; 0 for -1
+ *   out_lse           device float[n_rows], or NULL
+ *   out_entropy       device float[n_rows], or NULL: -sum p log p, in nats
+ *   out_alt           device int32[n_rows * n_alt]: the tokens of the largest z in
+ *                     descending order, ties to the lowest id; only tokens above
+ *                     -inf (a NaN never is one), then -1
+ *   out_alt_logprob   device float[n_rows * n_alt]: theirs, -inf for -1
+ *
+ * n_tok and n_alt may be 0 (their buffers are then not touched).
+ */
+int tb_token_logprobs(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus_blank,
+                      int64_t row_stride, float temperature, const int32_t* tokens,
+                      int32_t n_tok, float* out_logprob, float* out_lse, float* out_entropy,
+                      int32_t n_alt, int32_t* out_alt, float* out_alt_logprob, void* workspace,
+                      int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * tb_token_logprobs_grad — the gradient of a scalar with respect to the logits,
+ * from its gradients g, g_L and g_H with respect to the log probabilities of
+ * tokens (alternatives count as given tokens), lse and entropy:
+ *
+ *   dz[v] = (p[v] * (g_L - sum_j g_j - g_H * (log p[v] + entropy))
+ *            + sum of g_j over the j with tokens[j] = v) / tau
+ *
+ *   d_logprob        device float[n_rows * n_tok]
+ *   d_lse, d_entropy device float[n_rows], or NULL (0)
+ *   grad             device, dtype, row i at i * grad_stride elements; the
+ *                    values between rows are not touched
+ *
+ * A row to which no gradient comes (all 0) gets 0 whatever it holds.
+ */
+int tb_token_logprobs_grad(const void* logits, int32_t dtype, int64_t n_rows,
+                           int32_t v_plus_blank, int64_t row_stride, float temperature,
+                           const int32_t* tokens, int32_t n_tok, const float* d_logprob,
+                           const float* d_lse, const float* d_entropy, void* grad,
+                           int64_t grad_stride, void* workspace, int64_t workspace_bytes,
+                           void* hip_stream);
+
+/*
+ * tb_distill — the loss of a student's rows against a teacher's top logits, its
+ * gradient, or both in one pass. The teacher's list of a row has n_teacher
+ * places (token, score); q is
+ *
+ *   tail = 0: softmax(score / tau) over the list (scores: logits, or log
+ *             probabilities of any normalisation);
+ *             loss = sum_k q_k (log q_k - log p[token_k]); an empty list: 0
+ *   tail = 1: exp(score): the scores are log probabilities at the temperature
+ *             of the call. All other tokens are one event, of probability q_r =
+ *             max(0, 1 - sum q) and p_r = the sum of p outside the list;
+ *             loss = sum_k q_k (log q_k - log p[token_k]) + q_r (log q_r - log p_r)
+ *
+ *   teacher_tok    device int32[n_rows * n_teacher], teacher_score device float
+ *   weight         device float[n_rows], or NULL (1): multiplies the row's loss;
+ *                  0 gives loss and gradient 0 whatever the row holds
+ *   out_loss       device float[n_rows], or NULL
+ *   grad           device, dtype, or NULL: gradient of the sum of out_loss, row i
+ *                  at i * grad_stride elements
+ */
+int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus_blank,
+               int64_t row_stride, float temperature, const int32_t* teacher_tok,
+               const float* teacher_score, int32_t n_teacher, int32_t tail, const float* weight,
+               float* out_loss, void* grad, int64_t grad_stride, void* workspace,
+               int64_t workspace_bytes, void* hip_stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* tb_last_error(void);
 

@@ -21,7 +21,9 @@ HIP_SOURCES = ["capi.hip", "greedy.hip", "greedy_seg.hip",
                "greedy_seg_1_8.hip", "greedy_seg_9_16.hip", "greedy_seg_17_24.hip",
                "greedy_seg_25_32.hip", "greedy_wide.hip", "greedy_list_f32.hip",
                "greedy_list_bf16.hip", "beam.hip", "beam_list_f32.hip",
-               "beam_list_bf16.hip", "state.hip", "registry.hip"]
+               "beam_list_bf16.hip", "state.hip", "registry.hip",
+               "rows.hip", "rows_score_f32.hip", "rows_score_bf16.hip", "rows_grad_f32.hip",
+               "rows_grad_bf16.hip", "rows_distill_f32.hip", "rows_distill_bf16.hip"]
 CXX_SOURCES = ["compiler.cpp", "variative.cpp", "cache.cpp", "errors.cpp"]
 
 HIPCC_FLAGS = [

@@ -23,6 +23,7 @@ TB_F32, TB_BF16 = 0, 1
 TB_COMMIT, TB_PURE_POTENTIAL = 0, 1
 TB_STATE_NONE, TB_STATE_INVALID, TB_STATE_TIMEOUT = -1, -2, -3
 TB_MAX_BEAM = 32
+TB_MAX_LIST, TB_MAX_ROW = 64, 1 << 20
 # tb_debug_select_kernels choices
 GREEDY_AUTO, GREEDY_REF = 0, 1
 BEAM_AUTO, BEAM_REF, BEAM_NO_PIPE = 0, 1, 2
@@ -86,6 +87,11 @@ def _load() -> C.CDLL:
         "tb_debug_select_kernels": [I32, I32],
         "tb_debug_set_spin_limit": [C.c_uint32],
         "tb_debug_launch_empty": [I32, I32, I32, P],
+        "tb_token_logprobs": [P, I32, I64, I32, I64, C.c_float, P, I32, P, P, P, I32, P, P, P, I64,
+                              P],
+        "tb_token_logprobs_grad": [P, I32, I64, I32, I64, C.c_float, P, I32, P, P, P, P, I64, P,
+                                   I64, P],
+        "tb_distill": [P, I32, I64, I32, I64, C.c_float, P, P, I32, I32, P, P, P, I64, P, I64, P],
         "tb_registry_layout": [I32, I64, I32, C.POINTER(tb_arena_layout)],
         "tb_registry_create": [I32, I64, P, I32, P, I64, P, C.POINTER(C.c_void_p)],
         "tb_registry_arena": [P, C.POINTER(tb_arena)],
@@ -114,6 +120,8 @@ def _load() -> C.CDLL:
         getattr(lib, name).restype = C.c_int64
     lib.tb_registry_used_states.argtypes = [P]
     lib.tb_unregister_workspace_bytes.argtypes = [P, I32]
+    lib.tb_rows_workspace_bytes.restype = C.c_int64
+    lib.tb_rows_workspace_bytes.argtypes = [I32, I64, I32, I32]
     lib.tb_last_error.argtypes = []
     lib.tb_last_error.restype = C.c_char_p
     return lib
@@ -130,7 +138,9 @@ EXPORTED = ("tb_compile_graphs", "tb_graphs_layout", "tb_graphs_host_image", "tb
             "tb_unregister_model", "tb_registry_free", "tb_unregister_model_noalloc",
             "tb_init_beam_stream", "tb_boost_step_beam_stream", "tb_compile_variative",
             "tb_graphs_cache_create", "tb_graphs_cache_compile", "tb_graphs_cache_stats",
-            "tb_graphs_cache_free", "tb_graphs_save", "tb_graphs_load")
+            "tb_graphs_cache_free", "tb_graphs_save", "tb_graphs_load",
+            "tb_rows_workspace_bytes", "tb_token_logprobs", "tb_token_logprobs_grad",
+            "tb_distill")
 
 
 def _check(code: int) -> None:
@@ -534,6 +544,163 @@ def tb_boost_step_beam_stream(arena: Arena, logits, model_ids, states, scores, h
         _dptr(out_parent, torch.int32, "out_parent"), _dptr(out_state, torch.int32, "out_state"),
         _dptr(out_step, torch.float32, "out_step"), _dptr(out_cum, torch.float32, "out_cum"),
         _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# row operators
+
+
+def _rows(x, name: str = "logits"):
+    """(rows, V+1, row stride) of a tensor [..., V+1] whose rows are evenly spaced."""
+    shape = x.shape
+    n = len(shape)
+    if n < 1 or shape[-1] < 2:
+        raise ValueError(f"{name} must be [..., V+1] with V+1 >= 2")
+    strides = x.stride()
+    if strides[-1] != 1:
+        raise ValueError(f"{name} rows must be contiguous")
+    rows, step = 1, 0
+    for d in range(n - 2, -1, -1):
+        size = shape[d]
+        if size == 1:
+            continue
+        if step == 0:
+            step = strides[d]
+        elif strides[d] != rows * step:
+            raise ValueError(f"{name} rows must be evenly spaced")
+        rows *= size
+    if rows > 1 and step < shape[-1]:
+        raise ValueError(f"{name} rows overlap")
+    return rows, shape[-1], step if rows > 1 else max(step, shape[-1])
+
+
+def _per_row(t, rows: int, dtype, name: str) -> int:
+    """Values a row of a contiguous per-row device tensor [rows..., n] (None: 0)."""
+    if t is None:
+        return 0
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    k = t.shape[-1] if t.dim() else 1
+    if t.numel() != rows * k:
+        raise ValueError(f"{name} holds {t.numel()} elements, needs [{rows}, n]")
+    return k
+
+
+def _one_per_row(t, rows: int, name: str) -> Optional[int]:
+    """Device pointer of a float32 tensor of one value a row (None passes NULL)."""
+    if t is None:
+        return None
+    import torch
+    _need(t, rows, name)
+    return _dptr(t, torch.float32, name)
+
+
+def _rows_in(logits, n_alt: int, workspace):
+    """(arguments of the rows, workspace arguments, device workspace) of a call.
+    A workspace that the call needs and the caller did not pass is allocated on
+    the current stream."""
+    import torch
+    n, V1, rs = _rows(logits)
+    dt = TB_F32 if logits.dtype == torch.float32 else TB_BF16
+    if dt == TB_BF16 and logits.dtype != torch.bfloat16:
+        raise ValueError("logits must be float32 or bfloat16")
+    ptr = _logits_ptr(logits)
+    if workspace is None:
+        need = LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    if workspace is None:
+        return (ptr, dt, n, V1, rs), (None, 0), None
+    return ((ptr, dt, n, V1, rs),
+            (_dptr(workspace, name="workspace"), workspace.numel() * workspace.element_size()),
+            workspace)
+
+
+def _grad_args(grad, logits):
+    """(device pointer, row stride) of a gradient (None passes NULL)."""
+    if grad is None:
+        return None, 0
+    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+        raise ValueError("grad must have the logits' shape and dtype")
+    if not grad.is_cuda:
+        raise ValueError("grad must be a device tensor")
+    return grad.data_ptr(), _rows(grad, "grad")[2]
+
+
+def tb_rows_workspace_bytes(logits, n_alt: int = 0) -> int:
+    """Workspace bytes of a row operator on these logits (0: none)."""
+    import torch
+    n, V1, _ = _rows(logits)
+    dt = TB_F32 if logits.dtype == torch.float32 else TB_BF16
+    return int(LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt))
+
+
+def tb_token_logprobs(logits, tokens=None, out_logprob=None, out_lse=None, out_entropy=None,
+                      out_alt=None, out_alt_logprob=None, temperature: float = 1.0,
+                      workspace=None, stream=None) -> None:
+    """logits: [..., V+1] device tensor with evenly spaced rows; tokens and
+    out_logprob [..., n_tok]; out_lse and out_entropy one value a row; out_alt
+    and out_alt_logprob [..., n_alt]."""
+    import torch
+    i32, f32 = torch.int32, torch.float32
+    M = 0 if out_alt is None else out_alt.shape[-1]
+    rows, ws, keep = _rows_in(logits, M, workspace)
+    n = rows[2]
+    J = _per_row(tokens, n, i32, "tokens")
+    if _per_row(out_logprob, n, f32, "out_logprob") != J:
+        raise ValueError("out_logprob must hold one value per token")
+    _per_row(out_alt, n, i32, "out_alt")
+    if _per_row(out_alt_logprob, n, f32, "out_alt_logprob") != M:
+        raise ValueError("out_alt_logprob must hold one value per alternative")
+    _check(LIB.tb_token_logprobs(*rows, temperature, tokens.data_ptr() if J else None, J,
+                                 out_logprob.data_ptr() if J else None,
+                                 _one_per_row(out_lse, n, "out_lse"),
+                                 _one_per_row(out_entropy, n, "out_entropy"), M,
+                                 out_alt.data_ptr() if M else None,
+                                 out_alt_logprob.data_ptr() if M else None, *ws,
+                                 _stream(stream)))
+
+
+def tb_token_logprobs_grad(logits, tokens, d_logprob, grad, d_lse=None, d_entropy=None,
+                           temperature: float = 1.0, workspace=None, stream=None) -> None:
+    """grad: like logits (or the logits themselves); tokens and d_logprob
+    [..., n_tok] or None; d_lse and d_entropy one value a row or None."""
+    import torch
+    rows, ws, keep = _rows_in(logits, 0, workspace)
+    n = rows[2]
+    J = _per_row(tokens, n, torch.int32, "tokens")
+    if _per_row(d_logprob, n, torch.float32, "d_logprob") != J:
+        raise ValueError("d_logprob must hold one value per token")
+    if grad is None:
+        raise ValueError("grad is required")
+    _check(LIB.tb_token_logprobs_grad(*rows, temperature, tokens.data_ptr() if J else None, J,
+                                      d_logprob.data_ptr() if J else None,
+                                      _one_per_row(d_lse, n, "d_lse"),
+                                      _one_per_row(d_entropy, n, "d_entropy"),
+                                      *_grad_args(grad, logits), *ws, _stream(stream)))
+
+
+def tb_distill(logits, teacher_tok, teacher_score, out_loss=None, grad=None, weight=None,
+               temperature: float = 1.0, tail: bool = False, workspace=None,
+               stream=None) -> None:
+    """teacher_tok and teacher_score: [..., n_teacher]; weight and out_loss one
+    value a row or None; grad: like logits (or the logits themselves) or None."""
+    import torch
+    rows, ws, keep = _rows_in(logits, 0, workspace)
+    n = rows[2]
+    if teacher_tok is None or teacher_score is None:
+        raise ValueError("teacher_tok and teacher_score are required")
+    K = _per_row(teacher_tok, n, torch.int32, "teacher_tok")
+    if _per_row(teacher_score, n, torch.float32, "teacher_score") != K:
+        raise ValueError("teacher_score must hold one value per teacher token")
+    _check(LIB.tb_distill(*rows, temperature, teacher_tok.data_ptr(), teacher_score.data_ptr(), K,
+                          1 if tail else 0, _one_per_row(weight, n, "weight"),
+                          _one_per_row(out_loss, n, "out_loss"), *_grad_args(grad, logits), *ws,
+                          _stream(stream)))
 
 
 def tb_reset_stream(arena: Arena, b: int, new_model_id: int, K: int, model_ids, states,

@@ -1,0 +1,460 @@
+// Rows of logits kept in registers: loading, softmax statistics, and the sums
+// over a row's segments. Shared by the row operators (log probabilities of
+// given tokens, distillation from a teacher's top logits, their gradients).
+//
+// A row z[0..C) at temperature tau has u = z / tau, m = max z and, in units of
+// log2, the exponents t_v = (z_v - m) log2(e) / tau <= 0. The operators need
+//
+//   S = sum 2^t,  D = sum 2^t t   (entropy = ln S - ln 2 D / S),
+//   R = sum of 2^t over the tokens outside a list.
+//
+// One row takes one wave, four or sixteen waves (by its length, instance()
+// below), each lane holding NP pieces of 16 bytes, so that every operator reads
+// a row once, also one that writes its gradient. Rows longer than the registers
+// of a workgroup are cut into segments: a first launch leaves every segment's
+// (m, S, D, R) in the caller's workspace, a second one joins them.
+#pragma once
+
+#include <climits>
+
+#include "device.hpp"
+#include "launch.hpp"
+
+namespace tbias {
+namespace rows {
+
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kThreads = 256;  // of a workgroup whose rows take one or four waves
+constexpr int kMaxSeg = 64;    // segments of a row: one lane each when they are joined
+
+// Sixteen bytes at the alignment of one element: rows start at any element.
+template <class LT>
+struct __attribute__((packed, aligned(sizeof(LT)))) Quad {
+  uint32_t w[4];
+};
+
+template <class LT>
+struct Elem;
+template <>
+struct Elem<float> {
+  static constexpr int PV = 4;  // values in 16 bytes
+  static constexpr uint32_t kFill = 0xff800000u;  // -inf
+  __device__ static inline float get(const uint32_t* w, int e) { return __uint_as_float(w[e]); }
+  __device__ static inline float widen(float x) { return x; }
+  __device__ static inline float narrow(float x) { return x; }
+  __device__ static inline void pack(const float* v, uint32_t* w) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(v[e]);
+  }
+};
+template <>
+struct Elem<uint16_t> {
+  static constexpr int PV = 8;
+  static constexpr uint32_t kFill = 0xff80ff80u;
+  __device__ static inline float get(const uint32_t* w, int e) {
+    return __uint_as_float((e & 1) ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+  __device__ static inline float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+  // to the nearest, ties to even; the one rounding of a bfloat16 gradient
+  __device__ static inline uint32_t pair(float a, float b) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 h2 __attribute__((ext_vector_type(2)));
+    const f2 v = {a, b};
+    const h2 h = __builtin_convertvector(v, h2);
+    return __builtin_bit_cast(uint32_t, h);
+  }
+  __device__ static inline uint16_t narrow(float x) { return (uint16_t)pair(x, x); }
+  __device__ static inline void pack(const float* v, uint32_t* w) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = pair(v[2 * e], v[2 * e + 1]);
+  }
+};
+
+// The rows of a call and how they are cut.
+struct Rows {
+  const void* z;
+  int64_t stride;   // elements from row to row
+  int64_t row0;     // first row of this launch
+  int64_t n_rows;   // rows of the call
+  int32_t C;        // values of a row
+  int32_t n_seg;    // segments of a row (1: the row is kept whole)
+  int32_t seg;      // values of a segment (the last may be shorter)
+  float c;          // log2(e) / tau
+  float inv_tau;
+  float4* part;     // [n_rows, n_seg] segments' (m, S, D, R)
+};
+
+struct Stats {
+  float m, S, D, R;
+};
+
+// How t_v is computed: one fused multiply-add per value, z c - M, where M = m c
+// rounded; the exponents are then delta = m c - M too small, all by the same,
+// which the callers take out of what they report. Where |m c| is so large that
+// delta is not small (masks of the type's lowest value) the maximum is
+// subtracted first and delta is 0.
+struct Basis {
+  float c, m, M, delta;
+  bool big;
+  __device__ static inline Basis of(float m, float c) {
+    Basis b;
+    b.c = c;
+    b.m = m == kNegInf ? 0.f : m;  // no value above -inf: every term is 0
+    b.M = b.m * c;
+    b.big = !(__builtin_fabsf(b.M) < 65536.f);
+    b.delta = b.big ? 0.f : __builtin_fmaf(b.m, c, -b.M);
+    return b;
+  }
+  template <bool BIG>
+  __device__ inline float t(float z) const {
+    return BIG ? (z - m) * c : __builtin_fmaf(z, c, -M);
+  }
+  __device__ inline float t(float z) const { return big ? t<true>(z) : t<false>(z); }
+};
+
+__device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_exp2f(t); }
+
+// max of three without the quieting of loaded values (a NaN operand is passed over)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+
+// Reductions over the NWR waves of a row; `box` holds NWR words that no other
+// reduction of the kernel uses.
+template <int NWR>
+__device__ __forceinline__ float row_max(float v, float* box, int q) {
+  v = wave_max_dpp(v);
+  if (NWR == 1) return v;
+  if (__lane_id() == 0) box[q] = v;
+  __syncthreads();
+  float r = box[0];
+#pragma unroll
+  for (int i = 1; i < NWR; ++i) r = __builtin_fmaxf(r, box[i]);
+  return r;
+}
+template <int NWR, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float* box, int q) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = wave_sum_dpp(v[k]);
+  if (NWR == 1) return;
+  if (__lane_id() == 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) box[k * NWR + q] = v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    float r = 0.f;
+#pragma unroll
+    for (int i = 0; i < NWR; ++i) r += box[k * NWR + i];
+    v[k] = r;
+  }
+}
+
+// n values of a row from `row` on, in the registers of NWR waves: NP pieces of
+// PV values a lane, and up to PV - 1 values that fill no piece, one per lane of
+// wave 0. Places past the end hold -inf.
+template <class LT, int NWR, int NP>
+struct Tile {
+  static constexpr int PV = Elem<LT>::PV;
+  Quad<LT> w[NP];
+  float tail;
+  int32_t lane, q, n;
+
+  __device__ inline int32_t first(int p) const { return ((p * NWR + q) * 64 + lane) * PV; }
+  __device__ inline int32_t tail_at() const { return n - n % PV + lane; }
+  __device__ inline bool has_tail() const { return q == 0 && lane < n % PV; }
+  __device__ inline bool has(int p) const { return first(p) + PV <= n; }
+
+  __device__ inline void load(const LT* row, int32_t n_, int lane_, int q_) {
+    n = n_;
+    lane = lane_;
+    q = q_;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      if (has(p)) {
+        w[p] = *reinterpret_cast<const Quad<LT>*>(row + first(p));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[p].w[k] = Elem<LT>::kFill;
+      }
+    }
+    tail = kNegInf;
+    if (has_tail()) tail = Elem<LT>::widen(row[tail_at()]);
+  }
+  __device__ inline float at(int p, int e) const { return Elem<LT>::get(w[p].w, e); }
+  // Between two passes over the values: bfloat16 pairs are taken apart again
+  // in each pass instead of being held widened, in twice the registers (142 of
+  // them instead of 8 values in 4, and scratch memory in the longest rows).
+  __device__ inline void repack() {
+    if (PV == 8) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(w[p].w[k]));
+    }
+  }
+
+  // largest value of this lane's
+  __device__ inline float lane_max() const {
+    float m = tail;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int e = 0; e < PV; e += 2) m = max3(m, at(p, e), at(p, e + 1));
+    return m;
+  }
+
+  // This lane's sums of 2^t, of 2^t t (ENT) and of 2^t outside the list whose
+  // members are set in `bits` (LIST), a piece at a time: less rounding than one
+  // chain. t is held at -200, where 2^t is 0, so that -inf adds 0 to D.
+  template <bool BIG, bool ENT, bool LIST>
+  __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3]) const {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      float a = 0.f, d = 0.f, r = 0.f;
+      const int32_t f = first(p);
+      const uint32_t mask = LIST && has(p) ? bits[f >> 5] >> (f & 31) : 0u;
+#pragma unroll
+      for (int e = 0; e < PV; ++e) {
+        const float t = b.t<BIG>(at(p, e));
+        const float x = exp2_fast(t);
+        a += x;
+        if (ENT) d = __builtin_fmaf(x, __builtin_fmaxf(t, -200.f), d);
+        if (LIST) r += (mask >> e) & 1 ? 0.f : x;
+      }
+      s[0] += a;
+      if (ENT) s[1] += d;
+      if (LIST) s[2] += r;
+    }
+    const float t = b.t<BIG>(tail), x = exp2_fast(t);
+    s[0] += x;
+    if (ENT) s[1] = __builtin_fmaf(x, __builtin_fmaxf(t, -200.f), s[1]);
+    if (LIST) {
+      const int32_t i = tail_at();
+      s[2] += has_tail() && ((bits[i >> 5] >> (i & 31)) & 1) ? 0.f : x;
+    }
+  }
+
+  // Writes f(t, 2^t) in place of every value.
+  template <bool BIG, class F>
+  __device__ inline void store(LT* out, const Basis& b, F f) const {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      float v[PV];
+#pragma unroll
+      for (int e = 0; e < PV; ++e) {
+        const float t = b.t<BIG>(at(p, e));
+        v[e] = f(t, exp2_fast(t));
+      }
+      if (has(p)) {
+        Quad<LT> o;
+        Elem<LT>::pack(v, o.w);
+        *reinterpret_cast<Quad<LT>*>(out + first(p)) = o;
+      }
+    }
+    if (has_tail()) {
+      const float t = b.t<BIG>(tail);
+      out[tail_at()] = Elem<LT>::narrow(f(t, exp2_fast(t)));
+    }
+  }
+
+  __device__ inline void store_zeros(LT* out) const {
+    Quad<LT> o = {{0u, 0u, 0u, 0u}};
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      if (has(p)) *reinterpret_cast<Quad<LT>*>(out + first(p)) = o;
+    if (has_tail()) out[tail_at()] = Elem<LT>::narrow(0.f);
+  }
+};
+
+// The row's statistics in the waves that hold it: relative to b's exponents (S,
+// D and R are 2^-delta times too large, D also off by delta S).
+// `box` holds 4 NWR words.
+template <bool ENT, bool LIST, class LT, int NWR, int NP>
+__device__ __forceinline__ Stats statistics(Tile<LT, NWR, NP>& x, float c, float lane_max,
+                                            const uint32_t* bits, float* box, Basis& b) {
+  const float m = row_max<NWR>(lane_max, box, x.q);
+  b = Basis::of(m, c);
+  x.repack();
+  float s[3] = {0.f, 0.f, 0.f};
+  if (b.big)
+    x.template sums<true, ENT, LIST>(b, bits, s);
+  else
+    x.template sums<false, ENT, LIST>(b, bits, s);
+  row_sum<NWR>(s, box + NWR, x.q);
+  x.repack();
+  return {m, s[0], s[1], s[2]};
+}
+
+// Statistics relative to the maximum itself, as segments are kept.
+__device__ __forceinline__ float4 to_part(const Stats& s, const Basis& b) {
+  const float f = exp2_fast(-b.delta);
+  return make_float4(s.m, f * s.S, f * (s.D - b.delta * s.S), f * s.R);
+}
+
+// All segments' statistics of a row, joined; every lane of the wave returns
+// them, relative to Basis::of(m, c).
+__device__ __forceinline__ Stats join(const float4* part, int32_t n_seg, float c, int lane,
+                                      Basis& b) {
+  float4 v = make_float4(kNegInf, 0.f, 0.f, 0.f);
+  if (lane < n_seg) v = part[lane];
+  const float m = wave_max_dpp(v.x);
+  b = Basis::of(m, c);
+  // a segment without a value above -inf adds nothing, but its NaN
+  const float a = v.x == kNegInf ? 0.f : (v.x - b.m) * c + b.delta;
+  const float f = exp2_fast(a);
+  const float t = __builtin_fmaxf(a, -200.f);
+  Stats s;
+  s.m = m;
+  s.S = wave_sum_dpp(f * v.y);
+  s.D = wave_sum_dpp(f * __builtin_fmaf(t, v.y, v.z));
+  s.R = wave_sum_dpp(f * v.w);
+  return s;
+}
+
+// ln of the sum of exp(u - u_max)
+__device__ __forceinline__ float log_sum(const Stats& s, const Basis& b) {
+  return logf(s.S) - kLn2 * b.delta;
+}
+// entropy in nats; a row without a value above -inf has none
+__device__ __forceinline__ float entropy(const Stats& s) {
+  if (s.m == kNegInf && s.S == 0.f) return 0.f;
+  const float h = logf(s.S) - kLn2 * (s.D / s.S);
+  return h < 0.f ? 0.f : h;
+}
+__device__ __forceinline__ bool empty(const Stats& s) { return s.m == kNegInf && s.S == 0.f; }
+
+// log probability of a value of the row
+__device__ __forceinline__ float log_prob(float z, const Basis& b, float log_s, float inv_tau) {
+  return z == kNegInf ? (log_s != log_s ? log_s : kNegInf) : (z - b.m) * inv_tau - log_s;
+}
+
+// ---- instances: waves per row and pieces per lane, by the values they hold
+
+struct Shape {
+  int nwr, np;
+};
+constexpr int capacity(Shape s, int pv) { return s.nwr * s.np * 64 * pv + pv - 1; }
+
+constexpr int kShapes = 9;
+// Shapes of a type whose pieces hold pv values, in ascending order of their capacity.
+constexpr Shape shape(int pv, int i) {
+  constexpr Shape f32[kShapes] = {{1, 1}, {1, 2}, {1, 4}, {1, 8}, {4, 4},
+                                  {4, 8}, {16, 4}, {16, 8}, {16, 16}};
+  constexpr Shape b16[kShapes] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4},
+                                  {4, 8}, {16, 4}, {16, 8}, {16, 16}};
+  return pv == 4 ? f32[i] : b16[i];
+}
+
+// Shapes that the segments of cut rows take.
+constexpr bool cuts(Shape s) { return s.nwr > 1 && s.np == 8; }
+
+struct Plan {
+  int shape;       // instance of the (whole or cut) rows
+  int32_t n_seg;   // segments of a row
+  int32_t seg;     // values of a segment
+};
+Plan plan(int32_t dtype, int64_t n_rows, int32_t C);
+
+// The segments' statistics, then their alternatives.
+inline int64_t workspace_bytes(const Plan& p, int64_t n_rows, int32_t n_alt) {
+  return p.n_seg > 1 ? n_rows * p.n_seg * (16 + 8 * (int64_t)n_alt) : 0;
+}
+
+// Calls f(Int<NWR>, Int<NP>) for an instance.
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
+template <class LT, int I = 0, class F>
+inline void with_shape(int i, F f) {
+  constexpr Shape s = shape(Elem<LT>::PV, I);
+  if (i == I) {
+    f(Int<s.nwr>(), Int<s.np>());
+  } else if constexpr (I + 1 < kShapes) {
+    with_shape<LT, I + 1>(i, f);
+  }
+}
+
+// Launches of whole rows, in ranges that one launch may hold; f(first row, grid).
+template <class F>
+inline void in_launches(int64_t n_rows, int rows_per_group, int threads, int32_t n_seg, F f) {
+  const int64_t most = most_groups(threads) / n_seg * rows_per_group;
+  for (int64_t r = 0; r < n_rows; r += most) {
+    const int64_t n = n_rows - r < most ? n_rows - r : most;
+    f(r, dim3((unsigned)((n + rows_per_group - 1) / rows_per_group), (unsigned)n_seg));
+  }
+}
+
+// Where a wave stands: its row, its part of it.
+template <int NWR>
+struct Place {
+  static constexpr int kWg = NWR * 64 > kThreads ? NWR * 64 : kThreads;
+  static constexpr int kRows = kWg / 64 / NWR;  // rows of a workgroup
+  int lane, q, slot;  // slot: row of the workgroup
+  int64_t row;
+  int32_t c0, n;      // first value and number of values of the segment
+  __device__ inline explicit Place(const Rows& a) {
+    lane = __lane_id();
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    q = wv % NWR;
+    slot = wv / NWR;
+    row = a.row0 + (int64_t)blockIdx.x * kRows + slot;
+    c0 = (int32_t)blockIdx.y * a.seg;
+    n = a.C - c0 < a.seg ? a.C - c0 : a.seg;
+  }
+};
+
+// Orders a wave's LDS writes before its later reads (one wave's LDS operations
+// are in order; this holds the compiler to it).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---- launchers (argument checks happen in the C ABI)
+
+struct ScoreIO {
+  const int32_t* tokens;
+  int32_t J;
+  float* logprob;
+  float* lse;
+  float* entropy;
+  int32_t M;
+  int32_t* alt;
+  float* alt_logprob;
+  int2* lists;  // [n_rows, n_seg, M] segments' alternatives: value bits, token
+};
+struct GradIO {
+  const int32_t* tokens;
+  int32_t J;
+  const float* d_logprob;
+  const float* d_lse;
+  const float* d_entropy;
+  void* grad;
+  int64_t grad_stride;
+};
+struct DistillIO {
+  const int32_t* tokens;
+  const float* score;
+  int32_t K;
+  int32_t tail;
+  float temperature;
+  const float* weight;
+  float* loss;
+  void* grad;
+  int64_t grad_stride;
+};
+hipError_t score_f32(const Rows& a, const ScoreIO& io, const Plan& p, hipStream_t st);
+hipError_t score_bf16(const Rows& a, const ScoreIO& io, const Plan& p, hipStream_t st);
+hipError_t grad_f32(const Rows& a, const GradIO& io, const Plan& p, hipStream_t st);
+hipError_t grad_bf16(const Rows& a, const GradIO& io, const Plan& p, hipStream_t st);
+hipError_t distill_f32(const Rows& a, const DistillIO& io, const Plan& p, hipStream_t st);
+hipError_t distill_bf16(const Rows& a, const DistillIO& io, const Plan& p, hipStream_t st);
+
+}  // namespace rows
+}  // namespace tbias

@@ -1,0 +1,348 @@
+// Gradients of the row operators with respect to the logits: of the log
+// probabilities of given tokens, the log-sum-exp and the entropy, and of the
+// distillation loss from a teacher's top logits, whose value is computed here
+// too (templates; instantiated in rows_grad_*.hip and rows_distill_*.hip).
+//
+// Every gradient is a multiple of the row's probabilities, with other values at
+// the few listed tokens:
+//
+//   log probabilities g_j of tokens t_j, log-sum-exp g_L, entropy g_H:
+//     dz_v = p_v (g_L - sum_j g_j - g_H (ln p_v + H)) / tau + sum_{t_j = v} g_j / tau
+//   distillation, weight w, teacher probabilities q_k of tokens t_k:
+//     dz_v = w p_v (Q - T) / tau  off the list,  w (Q p_v - sum_{t_k = v} q_k) / tau  on it,
+//     Q: the teacher's mass; T = q_rest / p_rest with the tail, 0 without.
+//
+// So a lane writes its values from registers, then the lanes of one wave write
+// the listed tokens over them (a token listed twice once, by its first place,
+// with the places summed in order). A row is read once and written once, and
+// the gradient may take the logits' own place.
+#pragma once
+
+#include "rows.hpp"
+
+namespace tbias {
+namespace rows {
+
+// Words of the membership bits of a row (or segment).
+template <class LT, int NWR, int NP>
+constexpr int list_words() {
+  return NWR * NP * 64 * Elem<LT>::PV / 32 + 1;
+}
+
+// Sum of g over the places with this lane's token, and whether this is the
+// first of them. Lanes below n take part.
+__device__ __forceinline__ float sum_same(int32_t id, float g, int n, int lane, bool& first) {
+  float sum = 0.f;
+  first = true;
+  for (int i = 0; i < n; ++i) {
+    const int32_t other = __builtin_amdgcn_readlane(id, i);
+    const float add = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), i));
+    if (other == id) {
+      sum += add;
+      if (i < lane) first = false;
+    }
+  }
+  return sum;
+}
+
+// The wave of a row that writes listed tokens has to come after all that the
+// row's waves wrote.
+template <int NWR>
+__device__ __forceinline__ void row_sync() {
+  if (NWR > 1)
+    __syncthreads();
+  else
+    wave_fence();
+}
+
+enum Pass { kWhole, kStats, kApply };
+
+// ---- gradient of log probabilities, log-sum-exp and entropy
+
+template <class LT, int NWR, int NP, bool ENT, Pass PASS>
+__global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io) {
+  __shared__ float box[4 * NWR];
+  lds_poison(box, sizeof(box));
+  const Place<NWR> at(a);
+  if (at.row >= a.n_rows) return;  // uniform over the row's waves
+  const LT* z = static_cast<const LT*>(a.z) + at.row * a.stride;
+  LT* out = static_cast<LT*>(io.grad) + at.row * io.grad_stride + at.c0;
+  Tile<LT, NWR, NP> x;
+  int32_t id = -1;
+  float g = 0.f, zj = kNegInf, gl = 0.f, gh = 0.f;
+  if (at.lane < io.J) {
+    id = io.tokens[at.row * io.J + at.lane];
+    g = io.d_logprob[at.row * io.J + at.lane];
+  }
+  if (io.d_lse) gl = io.d_lse[at.row];
+  if (ENT) gh = io.d_entropy[at.row];
+  x.load(z + at.c0, at.n, at.lane, at.q);
+  const bool ok = (uint32_t)id < (uint32_t)a.C;
+  const bool mine = ok && id >= at.c0 && id < at.c0 + at.n;
+  if (mine) zj = Elem<LT>::widen(z[id]);
+  const bool bad = __ballot(!ok && id != -1) != 0;
+  if (!ok) g = 0.f;
+  // no gradient comes in: none goes out, whatever the row holds
+  if (!bad && __ballot(g != 0.f) == 0 && gl == 0.f && gh == 0.f) {
+    if (PASS != kStats) x.store_zeros(out);
+    return;
+  }
+  Basis b;
+  Stats s;
+  if (PASS == kApply) {
+    s = join(a.part + at.row * a.n_seg, a.n_seg, a.c, at.lane, b);
+    row_sync<NWR>();  // zj is read before another wave may write there
+  } else {
+    s = statistics<ENT, false>(x, a.c, x.lane_max(), nullptr, box, b);
+  }
+  if (PASS == kStats) {
+    if (at.q == 0 && at.lane == 0) a.part[at.row * a.n_seg + blockIdx.y] = to_part(s, b);
+    return;
+  }
+  if (empty(s) && !bad) {
+    x.store_zeros(out);
+    return;
+  }
+  const float total = wave_sum_dpp(g);
+  const float f = a.inv_tau / s.S;
+  float k0 = (gl - total) * f, k1 = 0.f;
+  if (ENT) {
+    k0 -= gh * (entropy(s) - logf(s.S)) * f;
+    k1 = -gh * kLn2 * f;
+  }
+  if (bad) k0 = __builtin_nanf("");
+  auto slope = [&](float t, float e) {
+    return ENT ? e * __builtin_fmaf(k1, __builtin_fmaxf(t, -200.f), k0) : e * k0;
+  };
+  if (b.big)
+    x.template store<true>(out, b, slope);
+  else
+    x.template store<false>(out, b, slope);
+  row_sync<NWR>();
+  if (at.q != 0) return;
+  bool first;
+  const float sum = sum_same(id, g, io.J, at.lane, first);
+  if (mine && first) {
+    const float t = b.t(zj);
+    out[id - at.c0] = Elem<LT>::narrow(__builtin_fmaf(sum, a.inv_tau, slope(t, exp2_fast(t))));
+  }
+}
+
+// ---- distillation
+
+// A teacher's list, a token per lane.
+struct Teacher {
+  int32_t id;
+  bool ok, bad;      // bad: the row has a token out of range
+  float q, logq;
+  float mass, rest;  // of the list and (with the tail) of all else
+};
+__device__ __forceinline__ Teacher teacher(const DistillIO& io, int64_t row, int32_t C, float c,
+                                           int lane) {
+  Teacher t;
+  t.id = -1;
+  float sc = kNegInf;
+  if (lane < io.K) {
+    t.id = io.tokens[row * io.K + lane];
+    sc = io.score[row * io.K + lane];
+  }
+  t.ok = (uint32_t)t.id < (uint32_t)C;
+  t.bad = __ballot(!t.ok && t.id != -1) != 0;
+  if (!t.ok) sc = kNegInf;
+  t.rest = 0.f;
+  if (io.tail) {
+    t.q = expf(sc);
+    t.logq = sc;
+    const float sum = wave_sum_dpp(t.q);
+    const float rest = 1.f - sum;
+    t.rest = rest < 0.f ? 0.f : rest;  // (a NaN stays)
+    t.mass = sum + t.rest;
+  } else {
+    const float m = wave_max_dpp(sc);
+    const float x = sc - (m == kNegInf ? 0.f : m);
+    const float e = exp2_fast(x * c);
+    const float sum = wave_sum_dpp(e);
+    t.mass = sum == 0.f ? 0.f : 1.f;
+    t.q = sum == 0.f ? 0.f : e / sum;
+    t.logq = x * (c * kLn2) - logf(sum);
+    if (sum != sum) t.mass = sum;
+  }
+  return t;
+}
+
+__device__ __forceinline__ float distill_loss(const Teacher& t, float zk, const Stats& s,
+                                              const Basis& b, float inv_tau) {
+  const float log_s = log_sum(s, b);
+  const float lp = log_prob(zk, b, log_s, inv_tau);
+  // NaN scores give NaN terms
+  float loss = wave_sum_dpp(t.ok && t.q != 0.f ? t.q * (t.logq - lp) : 0.f);
+  if (t.rest != 0.f) {  // nothing outside the list (or an empty row): no mass for the rest
+    const float lr = s.R == 0.f ? kNegInf : logf(s.R) - logf(s.S);
+    loss += t.rest * (logf(t.rest) - lr);
+  }
+  return t.bad ? __builtin_nanf("") : loss;
+}
+
+// Sets the members of the list that lie in this part of the row.
+template <int NWR, int WORDS>
+__device__ __forceinline__ void set_bits(uint32_t* bits, const Teacher& t, int32_t c0, int32_t n,
+                                         int lane, int q) {
+  for (int i = q * 64 + lane; i < WORDS; i += NWR * 64) bits[i] = 0u;
+  row_sync<NWR>();
+  if (q == 0 && t.ok && t.id >= c0 && t.id < c0 + n)
+    atomicOr(&bits[(t.id - c0) >> 5], 1u << ((t.id - c0) & 31));
+  row_sync<NWR>();
+}
+
+template <class LT, int NWR, int NP, bool TAIL, Pass PASS>
+__global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, DistillIO io) {
+  constexpr int kWords = TAIL && PASS != kApply ? list_words<LT, NWR, NP>() : 1;
+  __shared__ float box[4 * NWR];
+  __shared__ uint32_t bits_all[Place<NWR>::kRows][kWords];
+  lds_poison(box, sizeof(box));
+  lds_poison(bits_all, sizeof(bits_all));
+  const Place<NWR> at(a);
+  if (at.row >= a.n_rows) return;  // uniform over the row's waves
+  const LT* z = static_cast<const LT*>(a.z) + at.row * a.stride;
+  LT* out = static_cast<LT*>(io.grad) + at.row * io.grad_stride + at.c0;
+  Tile<LT, NWR, NP> x;
+  x.load(z + at.c0, at.n, at.lane, at.q);
+  const float w = io.weight ? io.weight[at.row] : 1.f;
+  const Teacher t = teacher(io, at.row, a.C, a.c, at.lane);
+  const bool mine = t.ok && t.id >= at.c0 && t.id < at.c0 + at.n;
+  float zk = kNegInf;
+  if (mine) zk = Elem<LT>::widen(z[t.id]);
+  if (w == 0.f || (t.mass == 0.f && !t.bad)) {
+    if (PASS != kStats && io.grad) x.store_zeros(out);
+    if (PASS == kWhole && io.loss && at.q == 0 && at.lane == 0) io.loss[at.row] = 0.f;
+    return;
+  }
+  Basis b;
+  Stats s;
+  if (PASS == kApply) {
+    s = join(a.part + at.row * a.n_seg, a.n_seg, a.c, at.lane, b);
+    row_sync<NWR>();  // zk is read before another wave may write there
+  } else {
+    uint32_t* bits = bits_all[at.slot];
+    if (TAIL) set_bits<NWR, kWords>(bits, t, at.c0, at.n, at.lane, at.q);
+    s = statistics<false, TAIL>(x, a.c, x.lane_max(), bits, box, b);
+  }
+  if (PASS == kStats) {
+    if (at.q == 0 && at.lane == 0) a.part[at.row * a.n_seg + blockIdx.y] = to_part(s, b);
+    return;
+  }
+  if (PASS == kWhole && io.loss && at.q == 0) {
+    const float loss = distill_loss(t, zk, s, b, a.inv_tau);
+    if (at.lane == 0) io.loss[at.row] = w * loss;
+  }
+  if (!io.grad) return;
+  if (empty(s) && !t.bad) {
+    x.store_zeros(out);
+    return;
+  }
+  const float wt = w * a.inv_tau;
+  const float mass = t.bad ? __builtin_nanf("") : t.mass;
+  const float k_on = mass * wt / s.S;
+  float k_off = k_on;
+  if (TAIL && t.rest != 0.f && !(s.R == 0.f)) k_off = (mass - t.rest / (s.R / s.S)) * wt / s.S;
+  auto slope = [&](float, float e) { return e * k_off; };
+  if (b.big)
+    x.template store<true>(out, b, slope);
+  else
+    x.template store<false>(out, b, slope);
+  row_sync<NWR>();
+  if (at.q != 0) return;
+  bool first;
+  const float sum = sum_same(t.id, t.q, io.K, at.lane, first);
+  if (mine && first) {
+    const float e = exp2_fast(b.t(zk));
+    out[t.id - at.c0] = Elem<LT>::narrow(__builtin_fmaf(-sum, wt, e * k_on));
+  }
+}
+
+// The loss of rows in segments: one wave per row, before the gradient may take
+// the logits' place.
+template <class LT>
+__global__ __launch_bounds__(kThreads) void distill_loss_kernel(Rows a, DistillIO io) {
+  const int lane = __lane_id();
+  const int64_t row = a.row0 + (int64_t)blockIdx.x * (kThreads / 64) +
+                      __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (row >= a.n_rows) return;
+  const LT* z = static_cast<const LT*>(a.z) + row * a.stride;
+  const float w = io.weight ? io.weight[row] : 1.f;
+  const Teacher t = teacher(io, row, a.C, a.c, lane);
+  float loss = 0.f;
+  if (w != 0.f && (t.mass != 0.f || t.bad)) {
+    Basis b;
+    const Stats s = join(a.part + row * a.n_seg, a.n_seg, a.c, lane, b);
+    loss = w * distill_loss(t, t.ok ? Elem<LT>::widen(z[t.id]) : kNegInf, s, b, a.inv_tau);
+  }
+  if (lane == 0) io.loss[row] = loss;
+}
+
+// ---- launches
+
+template <class LT, class IO, class F>
+hipError_t grads_t(const Rows& a0, const Plan& p, F launch) {
+  Rows a = a0;
+  with_shape<LT>(p.shape, [&](auto nwr, auto np) {
+    constexpr int NWR = decltype(nwr)::value;
+    typedef Place<NWR> Pl;
+    in_launches(a.n_rows, Pl::kRows, Pl::kWg, p.n_seg, [&](int64_t r, dim3 grid) {
+      a.row0 = r;
+      launch(a, grid, dim3(Pl::kWg), nwr, np);
+    });
+  });
+  return hipGetLastError();
+}
+
+template <class LT>
+hipError_t grad_t(const Rows& a0, const GradIO& io, const Plan& p, hipStream_t st) {
+  auto pass = [&](auto pass_) {
+    constexpr Pass PASS = (Pass) decltype(pass_)::value;
+    return grads_t<LT, GradIO>(a0, p, [&](const Rows& a, dim3 grid, dim3 wg, auto nwr, auto np) {
+      constexpr int NWR = decltype(nwr)::value, NP = decltype(np)::value;
+      if constexpr (PASS == kWhole || cuts(Shape{NWR, NP})) {
+        if (io.d_entropy)
+          grad_kernel<LT, NWR, NP, true, PASS><<<grid, wg, 0, st>>>(a, io);
+        else
+          grad_kernel<LT, NWR, NP, false, PASS><<<grid, wg, 0, st>>>(a, io);
+      }
+    });
+  };
+  if (p.n_seg == 1) return pass(Int<kWhole>());
+  const hipError_t e = pass(Int<kStats>());
+  return e == hipSuccess ? pass(Int<kApply>()) : e;
+}
+
+template <class LT>
+hipError_t distill_t(const Rows& a0, const DistillIO& io, const Plan& p, hipStream_t st) {
+  auto pass = [&](auto pass_) {
+    constexpr Pass PASS = (Pass) decltype(pass_)::value;
+    return grads_t<LT, DistillIO>(
+        a0, p, [&](const Rows& a, dim3 grid, dim3 wg, auto nwr, auto np) {
+          constexpr int NWR = decltype(nwr)::value, NP = decltype(np)::value;
+          if constexpr (PASS == kWhole || cuts(Shape{NWR, NP})) {
+            if (io.tail)
+              distill_kernel<LT, NWR, NP, true, PASS><<<grid, wg, 0, st>>>(a, io);
+            else
+              distill_kernel<LT, NWR, NP, false, PASS><<<grid, wg, 0, st>>>(a, io);
+          }
+        });
+  };
+  if (p.n_seg == 1) return pass(Int<kWhole>());
+  hipError_t e = pass(Int<kStats>());
+  if (e == hipSuccess && io.loss) {
+    Rows a = a0;
+    in_launches(a.n_rows, kThreads / 64, kThreads, 1, [&](int64_t r, dim3 grid) {
+      a.row0 = r;
+      distill_loss_kernel<LT><<<grid, kThreads, 0, st>>>(a, io);
+    });
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && io.grad) e = pass(Int<kApply>());
+  return e;
+}
+
+}  // namespace rows
+}  // namespace tbias
