@@ -186,9 +186,8 @@ struct Tile {
     if (has_tail()) tail = Elem<LT>::widen(row[tail_at()]);
   }
   __device__ inline float at(int p, int e) const { return Elem<LT>::get(w[p].w, e); }
-  // Between two passes over the values: bfloat16 pairs are taken apart again
-  // in each pass instead of being held widened, in twice the registers (142 of
-  // them instead of 8 values in 4, and scratch memory in the longest rows).
+  // At the start of a pass over the values: bfloat16 pairs are taken apart again
+  // in each pass instead of being held widened, in twice the registers.
   __device__ inline void repack() {
     if (PV == 8) {
 #pragma unroll
@@ -198,21 +197,30 @@ struct Tile {
     }
   }
 
-  // largest value of this lane's
-  __device__ inline float lane_max() const {
-    float m = tail;
+  // largest value of this lane's (a NaN is passed over), also of two halves of them
+  __device__ inline void lane_max2(float& a, float& b) const {
+    a = tail;
+    b = kNegInf;
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int e = 0; e < PV; e += 2) m = max3(m, at(p, e), at(p, e + 1));
-    return m;
+      for (int e = 0; e < PV; e += 4) {
+        a = max3(a, at(p, e), at(p, e + 1));
+        b = max3(b, at(p, e + 2), at(p, e + 3));
+      }
+  }
+  __device__ inline float lane_max() const {
+    float a, b;
+    lane_max2(a, b);
+    return __builtin_fmaxf(a, b);
   }
 
   // This lane's sums of 2^t, of 2^t t (ENT) and of 2^t outside the list whose
   // members are set in `bits` (LIST), a piece at a time: less rounding than one
   // chain. t is held at -200, where 2^t is 0, so that -inf adds 0 to D.
   template <bool BIG, bool ENT, bool LIST>
-  __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3]) const {
+  __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3]) {
+    repack();
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       float a = 0.f, d = 0.f, r = 0.f;
@@ -241,7 +249,8 @@ struct Tile {
 
   // Writes f(t, 2^t) in place of every value.
   template <bool BIG, class F>
-  __device__ inline void store(LT* out, const Basis& b, F f) const {
+  __device__ inline void store(LT* out, const Basis& b, F f) {
+    repack();
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       float v[PV];
@@ -275,18 +284,16 @@ struct Tile {
 // D and R are 2^-delta times too large, D also off by delta S).
 // `box` holds 4 NWR words.
 template <bool ENT, bool LIST, class LT, int NWR, int NP>
-__device__ __forceinline__ Stats statistics(Tile<LT, NWR, NP>& x, float c, float lane_max,
-                                            const uint32_t* bits, float* box, Basis& b) {
-  const float m = row_max<NWR>(lane_max, box, x.q);
+__device__ __forceinline__ Stats statistics(Tile<LT, NWR, NP>& x, float c, const uint32_t* bits,
+                                            float* box, Basis& b) {
+  const float m = row_max<NWR>(x.lane_max(), box, x.q);
   b = Basis::of(m, c);
-  x.repack();
   float s[3] = {0.f, 0.f, 0.f};
   if (b.big)
     x.template sums<true, ENT, LIST>(b, bits, s);
   else
     x.template sums<false, ENT, LIST>(b, bits, s);
   row_sum<NWR>(s, box + NWR, x.q);
-  x.repack();
   return {m, s[0], s[1], s[2]};
 }
 

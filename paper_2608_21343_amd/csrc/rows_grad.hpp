@@ -93,7 +93,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io
     s = join(a.part + at.row * a.n_seg, a.n_seg, a.c, at.lane, b);
     row_sync<NWR>();  // zj is read before another wave may write there
   } else {
-    s = statistics<ENT, false>(x, a.c, x.lane_max(), nullptr, box, b);
+    s = statistics<ENT, false>(x, a.c, nullptr, box, b);
   }
   if (PASS == kStats) {
     if (at.q == 0 && at.lane == 0) a.part[at.row * a.n_seg + blockIdx.y] = to_part(s, b);
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, Distil
   } else {
     uint32_t* bits = bits_all[at.slot];
     if (TAIL) set_bits<NWR, kWords>(bits, t, at.c0, at.n, at.lane, at.q);
-    s = statistics<false, TAIL>(x, a.c, x.lane_max(), bits, box, b);
+    s = statistics<false, TAIL>(x, a.c, bits, box, b);
   }
   if (PASS == kStats) {
     if (at.q == 0 && at.lane == 0) a.part[at.row * a.n_seg + blockIdx.y] = to_part(s, b);

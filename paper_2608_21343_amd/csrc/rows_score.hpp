@@ -64,55 +64,251 @@ __device__ __forceinline__ void row_best(float& z, int32_t& id, float* box_z, in
   id = bi;
 }
 
+// ---- the M best values of a row
+//
+// A value t that M values reach bounds the M-th best from below. The maxima of
+// G >= 2 M groups of the row's values supply it: t is the M-th best of them (or
+// a bound of that), and about 1.4 M values reach it. Those are collected in LDS
+// and ranked against each other. Maxima are needed for the softmax anyway; the
+// rest costs a test per value and some ten operations per candidate, where one
+// argmax after the other costs four operations per value and alternative.
+
+// Floats in an order of whole numbers (-0 as 0), and back.
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_order(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+// A candidate: value first, then the lower token.
+__device__ __forceinline__ uint64_t candidate(float v, int32_t id) {
+  return (uint64_t)order_of(v) << 32 | (uint32_t)~id;
+}
+
+// Lanes whose values share a group, as a power of two; -1: a lane holds two.
+// 64 or 128 groups for M above 16 or 32 (rows of one and four waves: from 16
+// groups on).
+template <int NWR>
+__device__ __forceinline__ int group_log2(int M) {
+  const int most = NWR == 1 ? 2 : 4;
+  const int less = M > 32 ? 3 : M > 16 ? 2 : M > 8 ? 1 : 0;
+  return NWR == 16 ? (M > 32 ? 3 : 4) : most - less;
+}
+__device__ __forceinline__ float group_max(float v, int log2) {
+  if (log2 > 0) v = __builtin_fmaxf(v, dpp_f<0xB1, 0xf>(v, v));   // pairs
+  if (log2 > 1) v = __builtin_fmaxf(v, dpp_f<0x4E, 0xf>(v, v));   // quads
+  if (log2 > 2) v = __builtin_fmaxf(v, dpp_f<0x141, 0xf>(v, v));  // 8 lanes, mirrored
+  if (log2 > 3) v = __builtin_fmaxf(v, dpp_f<0x140, 0xf>(v, v));  // 16 lanes, mirrored
+  return v;
+}
+__device__ __forceinline__ float no_nan(float v) { return v == v ? v : kNegInf; }
+
+// A value that at least `need` of the lanes' a and b reach, few more if it can be:
+// bisection between their least and greatest in the order of whole numbers.
+__device__ __forceinline__ float reached_by(float a, float b, int need) {
+  const uint32_t ka = order_of(a), kb = order_of(b);
+  uint32_t lo = order_of(kNegInf), hi = order_of(wave_max_dpp(__builtin_fmaxf(a, b)));
+  // the greatest that all of a reach, if those are enough
+  const float least = -wave_max_dpp(-a);
+  if (least > kNegInf && need <= 64) lo = order_of(least);
+  while (lo < hi) {  // need lanes reach lo
+    const uint32_t mid = lo + (hi - lo) / 2 + 1;
+    const int n = __builtin_popcountll(__ballot(ka >= mid)) + __builtin_popcountll(__ballot(kb >= mid));
+    if (n < need) {
+      hi = mid - 1;
+    } else {
+      lo = mid;
+      if (n == need) break;
+    }
+  }
+  return of_order(lo);
+}
+
+// Candidates of a row: those of its waves, each in its own part of the list.
+template <int NWR>
+struct Found {
+  static constexpr int kCap = NWR == 1 ? 256 : NWR == 4 ? 128 : 64;  // of a wave
+  static constexpr int kMost = 256;                                  // of a row
+  uint64_t key[NWR][kCap];
+  int32_t n[NWR];
+};
+
+// Writes the M best of the row's candidates; one wave.
+template <int NWR, bool PART>
+__device__ __forceinline__ void rank(const Found<NWR>& f, const Rows& a, const ScoreIO& io,
+                                     int64_t row, int32_t c0, const Basis& b, float log_s,
+                                     int lane) {
+  int32_t total = 0, count[NWR];
+#pragma unroll
+  for (int w = 0; w < NWR; ++w) {
+    count[w] = __builtin_amdgcn_readfirstlane(f.n[w]);
+    total += count[w];
+  }
+  auto write = [&](uint64_t key, int at) {
+    if (at < io.M)
+      write_alt<PART>(a, io, row, at, of_order((uint32_t)(key >> 32)),
+                      c0 + (int32_t)~(uint32_t)key, b, log_s);
+  };
+  for (int base = 0; base < total; base += 64) {  // mostly once
+    uint64_t own = 0;
+    int32_t before = 0;
+#pragma unroll
+    for (int w = 0; w < NWR; ++w) {
+      const int32_t i = base + lane - before;
+      if (i >= 0 && i < count[w]) own = f.key[w][i];
+      before += count[w];
+    }
+    int at = 0;
+    if (total <= 64) {
+      for (int j = 0; j < total; ++j) {
+        const uint32_t hi = __builtin_amdgcn_readlane((int)(own >> 32), j);
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)own, j);
+        at += ((uint64_t)hi << 32 | lo) > own;
+      }
+    } else {
+#pragma unroll
+      for (int w = 0; w < NWR; ++w)
+        for (int j = 0; j < count[w]; ++j) at += f.key[w][j] > own;
+    }
+    if (base + lane < total) write(own, at);
+  }
+  if (lane >= total && lane < io.M)
+    write_alt<PART>(a, io, row, lane, kNegInf, -1, b, log_s);
+}
+
 template <class LT, int NWR, int NP, bool TOP, bool PART>
 __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO io) {
   typedef Tile<LT, NWR, NP> T;
   constexpr int PV = T::PV;
   __shared__ float box[4 * NWR], box_z[NWR];
   __shared__ int32_t box_id[NWR];
+  __shared__ float group[TOP && NWR > 1 ? 128 : 1];
+  __shared__ Found<TOP ? NWR : 1> found_all[TOP ? Place<NWR>::kRows : 1];
   lds_poison(box, sizeof(box));
+  lds_poison(group, sizeof(group));
+  lds_poison(found_all, sizeof(found_all));
   const Place<NWR> at(a);
   if (at.row >= a.n_rows) return;  // uniform over the row's waves
   const LT* z = static_cast<const LT*>(a.z) + at.row * a.stride;
   T x;
   x.load(z + at.c0, at.n, at.lane, at.q);
   Basis b;
-  const float lm = x.lane_max();
-  const Stats s = PART || io.entropy
-                      ? statistics<true, false>(x, a.c, lm, nullptr, box, b)
-                      : statistics<false, false>(x, a.c, lm, nullptr, box, b);
-  const float log_s = log_sum(s, b);
-  if (at.q == 0) {
+  Stats s;
+  const bool ent = PART || io.entropy;
+  auto finish = [&](float log_s) {  // one wave
     if (PART) {
       if (at.lane == 0) a.part[at.row * a.n_seg + blockIdx.y] = to_part(s, b);
     } else {
       write_scores(a, io, at.row, z, s, b, log_s, at.lane);
     }
-  }
-  if (!TOP) return;
-  // one alternative after the other: the best of those that come after the last
-  float lz = __builtin_huge_valf();
-  int32_t li = -1;
-  for (int i = 0; i < io.M; ++i) {
-    float bz = kNegInf;
-    int32_t bi = INT_MAX;
-    auto see = [&](float v, int32_t id) {
-      if ((v < lz || (v == lz && id > li)) && v > bz) {
-        bz = v;
-        bi = id;
-      }
+  };
+  if constexpr (!TOP) {
+    s = ent ? statistics<true, false>(x, a.c, nullptr, box, b)
+            : statistics<false, false>(x, a.c, nullptr, box, b);
+    if (at.q == 0) finish(log_sum(s, b));
+  } else {
+    // the row's maximum and a bound of its M-th best value
+    Found<NWR>& found = found_all[at.slot];
+    const int log2 = group_log2<NWR>(io.M);
+    float g0, g1;
+    x.lane_max2(g0, g1);
+    g0 = no_nan(g0);
+    g1 = no_nan(g1);
+    int need = io.M;
+    if (log2 >= 0) {
+      g0 = group_max(__builtin_fmaxf(g0, g1), log2);
+      g1 = kNegInf;
+    }
+    if (NWR == 1) {
+      need <<= log2 > 0 ? log2 : 0;  // every lane of a group has its value
+    } else {
+      const int per = 64 >> log2, G = per * NWR;  // 16, 32, 64 or 128 groups
+      if ((at.lane & ((1 << log2) - 1)) == 0) group[at.q * per + (at.lane >> log2)] = g0;
+      __syncthreads();
+      g0 = group[at.lane & (G - 1)];
+      if (G > 64)
+        g1 = group[64 + at.lane];
+      else
+        need *= 64 / G;
+    }
+    s.m = wave_max_dpp(__builtin_fmaxf(g0, g1));
+    b = Basis::of(s.m, a.c);
+    float bound = reached_by(g0, g1, need);
+    if (bound == kNegInf) bound = -__FLT_MAX__;  // only tokens above -inf
+    float v[3] = {0.f, 0.f, 0.f};
+    if (ent) {
+      if (b.big)
+        x.template sums<true, true, false>(b, nullptr, v);
+      else
+        x.template sums<false, true, false>(b, nullptr, v);
+    } else {
+      if (b.big)
+        x.template sums<true, false, false>(b, nullptr, v);
+      else
+        x.template sums<false, false, false>(b, nullptr, v);
+    }
+    x.repack();
+    int32_t n = 0;
+    auto see = [&](float val, int32_t id) {
+      const uint64_t hit = __ballot(val >= bound);
+      if (hit == 0) return;
+      const int32_t i = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32),
+                                                      __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+      if (val >= bound && i < Found<NWR>::kCap) found.key[at.q][i] = candidate(val, id);
+      n += __builtin_popcountll(hit);
     };
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
       for (int e = 0; e < PV; ++e) see(x.at(p, e), x.first(p) + e);
     see(x.tail, x.tail_at());
-    x.repack();
-    row_best<NWR>(bz, bi, box_z, box_id, at.q, at.lane);
-    if (at.q == 0 && at.lane == 0)
-      write_alt<PART>(a, io, at.row, i, bz, bz == kNegInf ? -1 : at.c0 + bi, b, log_s);
-    lz = bz;
-    li = bi;
+    if (at.lane == 0) found.n[at.q] = n;
+    if (NWR == 1) wave_fence();
+    row_sum<NWR>(v, box, at.q);  // the waves' candidates are in LDS after it, too
+    s.S = v[0];
+    s.D = v[1];
+    s.R = 0.f;
+    const float log_s = log_sum(s, b);
+    if (at.q == 0) finish(log_s);
+    bool over = false;
+    int32_t total = 0;
+#pragma unroll
+    for (int w = 0; w < NWR; ++w) {
+      const int32_t k = __builtin_amdgcn_readfirstlane(found.n[w]);
+      over |= k > Found<NWR>::kCap;
+      total += k;
+    }
+    if (!over && total <= Found<NWR>::kMost) {
+      if (at.q == NWR - 1)
+        rank<NWR, PART>(found, a, io, at.row, at.c0, b, log_s, at.lane);
+      return;
+    }
+    // Too many for the list (rows of few different values): one alternative after
+    // the other, the best of those that come after the last.
+    float lz = __builtin_huge_valf();
+    int32_t li = -1;
+    for (int i = 0; i < io.M; ++i) {
+      float bz = kNegInf;
+      int32_t bi = INT_MAX;
+      auto best = [&](float val, int32_t id) {
+        if ((val < lz || (val == lz && id > li)) && val > bz) {
+          bz = val;
+          bi = id;
+        }
+      };
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int e = 0; e < PV; ++e) best(x.at(p, e), x.first(p) + e);
+      best(x.tail, x.tail_at());
+      x.repack();
+      row_best<NWR>(bz, bi, box_z, box_id, at.q, at.lane);
+      if (at.q == 0 && at.lane == 0)
+        write_alt<PART>(a, io, at.row, i, bz, bz == kNegInf ? -1 : at.c0 + bi, b, log_s);
+      lz = bz;
+      li = bi;
+    }
   }
 }
 
