@@ -52,8 +52,16 @@ template <>
 struct Elem<uint16_t> {
   static constexpr int PV = 8;
   static constexpr uint32_t kFill = 0xff80ff80u;
+  // Volatile, so that every pass over a row takes the pairs apart again; held
+  // widened from pass to pass they take twice the registers (scratch memory in
+  // the longest rows).
   __device__ static inline float get(const uint32_t* w, int e) {
-    return __uint_as_float((e & 1) ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    float x;
+    if (e & 1)
+      asm volatile("v_and_b32 %0, %2, %1" : "=v"(x) : "v"(w[e / 2]), "s"(0xffff0000u));
+    else
+      asm volatile("v_lshlrev_b32 %0, 16, %1" : "=v"(x) : "v"(w[e / 2]));
+    return x;
   }
   __device__ static inline float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
   // to the nearest, ties to even; the one rounding of a bfloat16 gradient
@@ -115,11 +123,10 @@ struct Basis {
 
 __device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_exp2f(t); }
 
-// max of three without the quieting of loaded values (a NaN operand is passed over)
+// max of three in one instruction; a NaN stays (a maximum that passes it over
+// costs another instruction for every value loaded)
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-  return d;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 // Reductions over the NWR waves of a row; `box` holds NWR words that no other
@@ -186,33 +193,24 @@ struct Tile {
     if (has_tail()) tail = Elem<LT>::widen(row[tail_at()]);
   }
   __device__ inline float at(int p, int e) const { return Elem<LT>::get(w[p].w, e); }
-  // At the start of a pass over the values: bfloat16 pairs are taken apart again
-  // in each pass instead of being held widened, in twice the registers.
-  __device__ inline void repack() {
-    if (PV == 8) {
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(w[p].w[k]));
-    }
-  }
 
-  // largest value of this lane's (a NaN is passed over), also of two halves of them
-  __device__ inline void lane_max2(float& a, float& b) const {
+  // largest value of this lane's (or NaN), also of two halves of them
+  __device__ inline void lane_max2(float& a, float& b) {
     a = tail;
     b = kNegInf;
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p) {
 #pragma unroll
       for (int e = 0; e < PV; e += 4) {
         a = max3(a, at(p, e), at(p, e + 1));
         b = max3(b, at(p, e + 2), at(p, e + 3));
       }
+    }
   }
-  __device__ inline float lane_max() const {
+  __device__ inline float lane_max() {
     float a, b;
     lane_max2(a, b);
-    return __builtin_fmaxf(a, b);
+    return __builtin_elementwise_maximum(a, b);
   }
 
   // This lane's sums of 2^t, of 2^t t (ENT) and of 2^t outside the list whose
@@ -220,23 +218,32 @@ struct Tile {
   // chain. t is held at -200, where 2^t is 0, so that -inf adds 0 to D.
   template <bool BIG, bool ENT, bool LIST>
   __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3]) {
-    repack();
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      float a = 0.f, d = 0.f, r = 0.f;
-      const int32_t f = first(p);
-      const uint32_t mask = LIST && has(p) ? bits[f >> 5] >> (f & 31) : 0u;
+      float a = 0.f, d = 0.f, x[PV];
 #pragma unroll
       for (int e = 0; e < PV; ++e) {
         const float t = b.t<BIG>(at(p, e));
-        const float x = exp2_fast(t);
-        a += x;
-        if (ENT) d = __builtin_fmaf(x, __builtin_fmaxf(t, -200.f), d);
-        if (LIST) r += (mask >> e) & 1 ? 0.f : x;
+        x[e] = exp2_fast(t);
+        a += x[e];
+        if (ENT) d = __builtin_fmaf(x[e], __builtin_fmaxf(t, -200.f), d);
+      }
+      if (ENT) s[1] += d;
+      if (LIST) {
+        // (also past the row's end, where 2^t is 0: no test of it)
+        const int32_t f = first(p);
+        const uint32_t mask = bits[f >> 5] >> (f & 31) & ((1u << PV) - 1);
+        // the sums of this piece before the next one's values: registers
+        asm volatile("" : "+v"(a));
+        float r = a;
+        if (__ballot(mask != 0) != 0) {  // few pieces hold a listed token
+          r = 0.f;
+#pragma unroll
+          for (int e = 0; e < PV; ++e) r += (mask >> e) & 1 ? 0.f : x[e];
+        }
+        s[2] += r;
       }
       s[0] += a;
-      if (ENT) s[1] += d;
-      if (LIST) s[2] += r;
     }
     const float t = b.t<BIG>(tail), x = exp2_fast(t);
     s[0] += x;
@@ -250,7 +257,6 @@ struct Tile {
   // Writes f(t, 2^t) in place of every value.
   template <bool BIG, class F>
   __device__ inline void store(LT* out, const Basis& b, F f) {
-    repack();
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       float v[PV];

@@ -248,7 +248,6 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
       else
         x.template sums<false, false, false>(b, nullptr, v);
     }
-    x.repack();
     int32_t n = 0;
     auto see = [&](float val, int32_t id) {
       const uint64_t hit = __ballot(val >= bound);
@@ -259,9 +258,10 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
       n += __builtin_popcountll(hit);
     };
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p) {
 #pragma unroll
       for (int e = 0; e < PV; ++e) see(x.at(p, e), x.first(p) + e);
+    }
     see(x.tail, x.tail_at());
     if (at.lane == 0) found.n[at.q] = n;
     if (NWR == 1) wave_fence();
@@ -291,6 +291,9 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
     for (int i = 0; i < io.M; ++i) {
       float bz = kNegInf;
       int32_t bi = INT_MAX;
+      // the places are formed anew in each turn: held, they take a register a value
+      int32_t place = at.lane * PV;
+      asm volatile("" : "+v"(place));
       auto best = [&](float val, int32_t id) {
         if ((val < lz || (val == lz && id > li)) && val > bz) {
           bz = val;
@@ -298,11 +301,12 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
         }
       };
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
-#pragma unroll
-        for (int e = 0; e < PV; ++e) best(x.at(p, e), x.first(p) + e);
+      for (int p = 0; p < NP; ++p) {
+  #pragma unroll
+        for (int e = 0; e < PV; ++e)
+          best(x.at(p, e), place + (p * NWR + at.q) * 64 * PV + e);
+      }
       best(x.tail, x.tail_at());
-      x.repack();
       row_best<NWR>(bz, bi, box_z, box_id, at.q, at.lane);
       if (at.q == 0 && at.lane == 0)
         write_alt<PART>(a, io, at.row, i, bz, bz == kNegInf ? -1 : at.c0 + bi, b, log_s);
