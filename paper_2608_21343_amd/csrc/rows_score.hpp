@@ -67,11 +67,12 @@ __device__ __forceinline__ void row_best(float& z, int32_t& id, float* box_z, in
 // ---- the M best values of a row
 //
 // A value t that M values reach bounds the M-th best from below. The maxima of
-// G >= 2 M groups of the row's values supply it: t is the M-th best of them (or
-// a bound of that), and about 1.4 M values reach it. Those are collected in LDS
-// and ranked against each other. Maxima are needed for the softmax anyway; the
-// rest costs a test per value and some ten operations per candidate, where one
-// argmax after the other costs four operations per value and alternative.
+// 64 (M > 16: 128) groups of the row's values supply it: t is the M-th best of
+// them, and some 1.1 to 1.4 M values reach it. Those are collected in LDS and
+// ranked against each other. The maxima are needed for the softmax anyway; the
+// rest costs a test per value, some six operations per place of a lane at which
+// candidates lie and two per candidate, where one argmax after the other costs
+// four operations per value and alternative.
 
 // Floats in an order of whole numbers (-0 as 0), and back.
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -81,19 +82,11 @@ __device__ __forceinline__ uint32_t order_of(float v) {
 __device__ __forceinline__ float of_order(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
-// A candidate: value first, then the lower token.
-__device__ __forceinline__ uint64_t candidate(float v, int32_t id) {
-  return (uint64_t)order_of(v) << 32 | (uint32_t)~id;
-}
 
-// Lanes whose values share a group, as a power of two; -1: a lane holds two.
-// 64 or 128 groups for M above 16 or 32 (rows of one and four waves: from 16
-// groups on).
+// Lanes that share a group, as a power of two; -1: a lane holds two groups.
 template <int NWR>
 __device__ __forceinline__ int group_log2(int M) {
-  const int most = NWR == 1 ? 2 : 4;
-  const int less = M > 32 ? 3 : M > 16 ? 2 : M > 8 ? 1 : 0;
-  return NWR == 16 ? (M > 32 ? 3 : 4) : most - less;
+  return (NWR == 1 ? 0 : NWR == 4 ? 2 : 4) - (M > 16 ? 1 : 0);
 }
 __device__ __forceinline__ float group_max(float v, int log2) {
   if (log2 > 0) v = __builtin_fmaxf(v, dpp_f<0xB1, 0xf>(v, v));   // pairs
@@ -104,17 +97,17 @@ __device__ __forceinline__ float group_max(float v, int log2) {
 }
 __device__ __forceinline__ float no_nan(float v) { return v == v ? v : kNegInf; }
 
-// A value that at least `need` of the lanes' a and b reach, few more if it can be:
-// bisection between their least and greatest in the order of whole numbers.
-__device__ __forceinline__ float reached_by(float a, float b, int need) {
+// A value that at least `need` (at most 64) of the lanes' a (and, with two, b)
+// reach, and few more if it can be: bisection between their least and greatest
+// in the order of whole numbers.
+__device__ __forceinline__ float reached_by(float a, float b, bool two, int need, float most) {
+  if (need == 1) return most;
   const uint32_t ka = order_of(a), kb = order_of(b);
-  uint32_t lo = order_of(kNegInf), hi = order_of(wave_max_dpp(__builtin_fmaxf(a, b)));
-  // the greatest that all of a reach, if those are enough
-  const float least = -wave_max_dpp(-a);
-  if (least > kNegInf && need <= 64) lo = order_of(least);
-  while (lo < hi) {  // need lanes reach lo
+  uint32_t lo = order_of(-wave_max_dpp(-a)), hi = order_of(most);
+  while (lo < hi) {  // need values reach lo
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    const int n = __builtin_popcountll(__ballot(ka >= mid)) + __builtin_popcountll(__ballot(kb >= mid));
+    int n = __builtin_popcountll(__ballot(ka >= mid));
+    if (two) n += __builtin_popcountll(__ballot(kb >= mid));
     if (n < need) {
       hi = mid - 1;
     } else {
@@ -125,19 +118,25 @@ __device__ __forceinline__ float reached_by(float a, float b, int need) {
   return of_order(lo);
 }
 
-// Candidates of a row: those of its waves, each in its own part of the list.
+// Candidates of a row: those of its waves (value, place), each in its own part
+// of the list.
 template <int NWR>
 struct Found {
   static constexpr int kCap = NWR == 1 ? 256 : NWR == 4 ? 128 : 64;  // of a wave
   static constexpr int kMost = 256;                                  // of a row
-  uint64_t key[NWR][kCap];
+  static constexpr int kKeys = 128;  // ranked by words of 32 bits
+  int2 at[NWR][kCap];
+  uint4 key[kKeys / 4];
   int32_t n[NWR];
 };
 
-// Writes the M best of the row's candidates; one wave.
-template <int NWR, bool PART>
-__device__ __forceinline__ void rank(const Found<NWR>& f, const Rows& a, const ScoreIO& io,
-                                     int64_t row, int32_t c0, const Basis& b, float log_s,
+// Writes the M best of the row's candidates; one wave. The order is that of
+// (value, lower place) as one whole number: of 32 bits for bfloat16 rows of up
+// to 2^16 values, also for float32 where no two candidates are equal (which
+// shows in the sum of the ranks), else of 64.
+template <class LT, int NWR, bool PART>
+__device__ __forceinline__ void rank(Found<NWR>& f, const Rows& a, const ScoreIO& io, int64_t row,
+                                     int32_t c0, int32_t n, const Basis& b, float log_s,
                                      int lane) {
   int32_t total = 0, count[NWR];
 #pragma unroll
@@ -145,36 +144,67 @@ __device__ __forceinline__ void rank(const Found<NWR>& f, const Rows& a, const S
     count[w] = __builtin_amdgcn_readfirstlane(f.n[w]);
     total += count[w];
   }
-  auto write = [&](uint64_t key, int at) {
-    if (at < io.M)
-      write_alt<PART>(a, io, row, at, of_order((uint32_t)(key >> 32)),
-                      c0 + (int32_t)~(uint32_t)key, b, log_s);
-  };
-  for (int base = 0; base < total; base += 64) {  // mostly once
-    uint64_t own = 0;
-    int32_t before = 0;
+  auto candidate = [&](int32_t i) {  // of all waves'
+    int2 c = make_int2(0, 0);
 #pragma unroll
     for (int w = 0; w < NWR; ++w) {
-      const int32_t i = base + lane - before;
-      if (i >= 0 && i < count[w]) own = f.key[w][i];
-      before += count[w];
+      if (i >= 0 && i < count[w]) c = f.at[w][i];
+      i -= count[w];
     }
-    int at = 0;
-    if (total <= 64) {
-      for (int j = 0; j < total; ++j) {
-        const uint32_t hi = __builtin_amdgcn_readlane((int)(own >> 32), j);
-        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)own, j);
-        at += ((uint64_t)hi << 32 | lo) > own;
-      }
-    } else {
-#pragma unroll
-      for (int w = 0; w < NWR; ++w)
-        for (int j = 0; j < count[w]; ++j) at += f.key[w][j] > own;
-    }
-    if (base + lane < total) write(own, at);
-  }
+    return c;
+  };
+  auto write = [&](int2 c, int at) {
+    if (at < io.M)
+      write_alt<PART>(a, io, row, at, __int_as_float(c.x), c0 + c.y, b, log_s);
+  };
   if (lane >= total && lane < io.M)
     write_alt<PART>(a, io, row, lane, kNegInf, -1, b, log_s);
+  constexpr bool kShort = sizeof(LT) == 2;
+  if (total <= Found<NWR>::kKeys && (!kShort || n <= 65536)) {
+    int2 c[2];
+    uint32_t key[2];
+    int at[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      c[h] = make_int2(0, 0);
+      key[h] = 0;
+      at[h] = 0;
+      if (h * 64 >= total) continue;  // uniform
+      c[h] = candidate(h * 64 + lane);
+      const uint32_t o = order_of(__int_as_float(c[h].x));
+      if (h * 64 + lane < total) key[h] = kShort ? (o & 0xffff0000u) | (0xffff - c[h].y) : o;
+      reinterpret_cast<uint32_t*>(f.key)[h * 64 + lane] = key[h];
+    }
+    wave_fence();
+    for (int j = 0; j < total; j += 4) {
+      const uint4 k = f.key[j / 4];
+      at[0] += (k.x > key[0]) + (k.y > key[0]) + (k.z > key[0]) + (k.w > key[0]);
+      if (total > 64) at[1] += (k.x > key[1]) + (k.y > key[1]) + (k.z > key[1]) + (k.w > key[1]);
+    }
+    bool ties = false;
+    if (!kShort) {
+      int sum = (lane < total ? at[0] : 0) + (64 + lane < total ? at[1] : 0);
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      ties = sum != total * (total - 1) / 2;
+    }
+    if (!ties) {
+      if (lane < total) write(c[0], at[0]);
+      if (64 + lane < total) write(c[1], at[1]);
+      return;
+    }
+  }
+  auto whole = [](int2 c) {
+    return (uint64_t)order_of(__int_as_float(c.x)) << 32 | (uint32_t)~c.y;
+  };
+  for (int base = 0; base < total; base += 64) {
+    const int2 own = candidate(base + lane);
+    const uint64_t key = whole(own);
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < NWR; ++w)
+      for (int j = 0; j < count[w]; ++j) at += whole(f.at[w][j]) > key;
+    if (base + lane < total) write(own, at);
+  }
 }
 
 template <class LT, int NWR, int NP, bool TOP, bool PART>
@@ -211,30 +241,21 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
     // the row's maximum and a bound of its M-th best value
     Found<NWR>& found = found_all[at.slot];
     const int log2 = group_log2<NWR>(io.M);
+    const bool two = io.M > 16;
     float g0, g1;
     x.lane_max2(g0, g1);
     g0 = no_nan(g0);
     g1 = no_nan(g1);
-    int need = io.M;
-    if (log2 >= 0) {
-      g0 = group_max(__builtin_fmaxf(g0, g1), log2);
-      g1 = kNegInf;
-    }
-    if (NWR == 1) {
-      need <<= log2 > 0 ? log2 : 0;  // every lane of a group has its value
-    } else {
-      const int per = 64 >> log2, G = per * NWR;  // 16, 32, 64 or 128 groups
-      if ((at.lane & ((1 << log2) - 1)) == 0) group[at.q * per + (at.lane >> log2)] = g0;
+    if (log2 >= 0) g0 = group_max(__builtin_fmaxf(g0, g1), log2);
+    if (NWR > 1) {
+      if ((at.lane & ((1 << log2) - 1)) == 0) group[at.q * (64 >> log2) + (at.lane >> log2)] = g0;
       __syncthreads();
-      g0 = group[at.lane & (G - 1)];
-      if (G > 64)
-        g1 = group[64 + at.lane];
-      else
-        need *= 64 / G;
+      g0 = group[at.lane];
+      if (two) g1 = group[64 + at.lane];
     }
-    s.m = wave_max_dpp(__builtin_fmaxf(g0, g1));
+    s.m = wave_max_dpp(two ? __builtin_fmaxf(g0, g1) : g0);
     b = Basis::of(s.m, a.c);
-    float bound = reached_by(g0, g1, need);
+    float bound = reached_by(g0, g1, two, io.M, s.m);
     if (bound == kNegInf) bound = -__FLT_MAX__;  // only tokens above -inf
     float v[3] = {0.f, 0.f, 0.f};
     if (ent) {
@@ -252,10 +273,13 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
     auto see = [&](float val, int32_t id) {
       const uint64_t hit = __ballot(val >= bound);
       if (hit == 0) return;
-      const int32_t i = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32),
-                                                      __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
-      if (val >= bound && i < Found<NWR>::kCap) found.key[at.q][i] = candidate(val, id);
-      n += __builtin_popcountll(hit);
+      const int32_t more = n + __builtin_popcountll(hit);
+      if (more <= Found<NWR>::kCap && val >= bound) {
+        const int32_t i = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32),
+                                                    __builtin_amdgcn_mbcnt_lo((uint32_t)hit, n));
+        found.at[at.q][i] = make_int2(__float_as_int(val), id);
+      }
+      n = more;
     };
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -281,7 +305,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
     }
     if (!over && total <= Found<NWR>::kMost) {
       if (at.q == NWR - 1)
-        rank<NWR, PART>(found, a, io, at.row, at.c0, b, log_s, at.lane);
+        rank<LT, NWR, PART>(found, a, io, at.row, at.c0, at.n, b, log_s, at.lane);
       return;
     }
     // Too many for the list (rows of few different values): one alternative after
