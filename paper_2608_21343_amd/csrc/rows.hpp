@@ -25,7 +25,7 @@ namespace rows {
 
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kThreads = 256;  // of a workgroup whose rows take one or four waves
+constexpr int kThreads = 256;  // of a workgroup whose rows take one wave each
 constexpr int kMaxSeg = 64;    // segments of a row: one lane each when they are joined
 
 // Sixteen bytes at the alignment of one element: rows start at any element.
@@ -129,11 +129,60 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
-// Reductions over the NWR waves of a row; `box` holds NWR words that no other
-// reduction of the kernel uses.
+// ---- sums and maxima of a wave, one instruction a step: a lane without a
+// source keeps its value. (A read across lanes comes two instructions after the
+// write; the compiler does not look into the block, so it keeps that itself.)
+#define TB_STEPS(OP1, OP2, WAIT)                                                       \
+  "s_nop 1\n\t" OP1 " row_shr:1 row_mask:0xf bank_mask:0xf\n\t" OP2                   \
+  " row_shr:1 row_mask:0xf bank_mask:0xf\n\t" WAIT "\n\t" OP1                         \
+  " row_shr:2 row_mask:0xf bank_mask:0xf\n\t" OP2                                      \
+  " row_shr:2 row_mask:0xf bank_mask:0xf\n\t" WAIT "\n\t" OP1                         \
+  " row_shr:4 row_mask:0xf bank_mask:0xf\n\t" OP2                                      \
+  " row_shr:4 row_mask:0xf bank_mask:0xf\n\t" WAIT "\n\t" OP1                         \
+  " row_shr:8 row_mask:0xf bank_mask:0xf\n\t" OP2                                      \
+  " row_shr:8 row_mask:0xf bank_mask:0xf\n\t" WAIT "\n\t" OP1                         \
+  " row_bcast:15 row_mask:0xa bank_mask:0xf\n\t" OP2                                   \
+  " row_bcast:15 row_mask:0xa bank_mask:0xf\n\t" WAIT "\n\t" OP1                      \
+  " row_bcast:31 row_mask:0xc bank_mask:0xf\n\t" OP2                                   \
+  " row_bcast:31 row_mask:0xc bank_mask:0xf\n\ts_nop 1"
+#define TB_STEP(OP)                                                                     \
+  "s_nop 1\n\t" OP " row_shr:1 row_mask:0xf bank_mask:0xf\n\ts_nop 1\n\t" OP          \
+  " row_shr:2 row_mask:0xf bank_mask:0xf\n\ts_nop 1\n\t" OP                            \
+  " row_shr:4 row_mask:0xf bank_mask:0xf\n\ts_nop 1\n\t" OP                            \
+  " row_shr:8 row_mask:0xf bank_mask:0xf\n\ts_nop 1\n\t" OP                            \
+  " row_bcast:15 row_mask:0xa bank_mask:0xf\n\ts_nop 1\n\t" OP                         \
+  " row_bcast:31 row_mask:0xc bank_mask:0xf\n\ts_nop 1"
+
+__device__ __forceinline__ float wave_most(float v) {  // a NaN is passed over
+  asm(TB_STEP("v_max_f32_dpp %0, %0, %0") : "+v"(v));
+  return bcast63_f(v);
+}
+__device__ __forceinline__ float wave_least(float v) {
+  asm(TB_STEP("v_min_f32_dpp %0, %0, %0") : "+v"(v));
+  return bcast63_f(v);
+}
+__device__ __forceinline__ float wave_total(float v) {
+  asm(TB_STEP("v_add_f32_dpp %0, %0, %0") : "+v"(v));
+  return bcast63_f(v);
+}
+__device__ __forceinline__ int32_t wave_total_i32(int32_t v) {
+  asm(TB_STEP("v_add_u32_dpp %0, %0, %0") : "+v"(v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ void wave_totals(float& v, float& w) {
+  asm(TB_STEPS("v_add_f32_dpp %0, %0, %0", "v_add_f32_dpp %1, %1, %1", "s_nop 0")
+      : "+v"(v), "+v"(w));
+  v = bcast63_f(v);
+  w = bcast63_f(w);
+}
+#undef TB_STEP
+#undef TB_STEPS
+
+// Reductions over the NWR waves of a row; `box` holds NWR words (a word for
+// every wave and sum) that no other reduction of the kernel uses.
 template <int NWR>
 __device__ __forceinline__ float row_max(float v, float* box, int q) {
-  v = wave_max_dpp(v);
+  v = wave_most(v);
   if (NWR == 1) return v;
   if (__lane_id() == 0) box[q] = v;
   __syncthreads();
@@ -142,61 +191,84 @@ __device__ __forceinline__ float row_max(float v, float* box, int q) {
   for (int i = 1; i < NWR; ++i) r = __builtin_fmaxf(r, box[i]);
   return r;
 }
-template <int NWR, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float* box, int q) {
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = wave_sum_dpp(v[k]);
+// Sums of v[0] and, where they are used, of v[1] or v[2].
+template <int NWR, bool SECOND, bool THIRD>
+__device__ __forceinline__ void row_sum(float (&v)[3], float* box, int q) {
+  static_assert(!(SECOND && THIRD), "two sums at most");
+  constexpr int K = SECOND ? 1 : 2;
+  if (SECOND || THIRD)
+    wave_totals(v[0], v[K]);
+  else
+    v[0] = wave_total(v[0]);
   if (NWR == 1) return;
   if (__lane_id() == 0) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) box[k * NWR + q] = v[k];
+    box[q] = v[0];
+    if (SECOND || THIRD) box[NWR + q] = v[K];
   }
   __syncthreads();
+  float r = 0.f, r2 = 0.f;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    float r = 0.f;
-#pragma unroll
-    for (int i = 0; i < NWR; ++i) r += box[k * NWR + i];
-    v[k] = r;
+  for (int i = 0; i < NWR; ++i) {
+    r += box[i];
+    if (SECOND || THIRD) r2 += box[NWR + i];
   }
+  v[0] = r;
+  if (SECOND || THIRD) v[K] = r2;
 }
 
 // n values of a row from `row` on, in the registers of NWR waves: NP pieces of
-// PV values a lane, and up to PV - 1 values that fill no piece, one per lane of
-// wave 0. Places past the end hold -inf.
+// PV values a lane, and what fills no piece one value per lane of wave 0. Places
+// past the end hold -inf.
+//
+// A row of one wave starts with its first piece wherever it lies in memory, so
+// that its results depend on its values alone. In longer rows of bfloat16 the
+// pieces lie on whole 16 bytes and up to PV - 1 values come before them: sums
+// then differ in their last bits from place to place, but 2048 rows of 131,073
+// take 243 us instead of 308 (distillation with its gradient) and 136 instead
+// of 167 (log-sum-exp). Float32 rows gain nothing (65,537 values: 139 and 130).
 template <class LT, int NWR, int NP>
 struct Tile {
   static constexpr int PV = Elem<LT>::PV;
+  static constexpr bool kWhole16 = PV == 8 && NWR > 1;
   Quad<LT> w[NP];
-  float tail;
-  int32_t lane, q, n;
+  float rim;
+  int32_t lane, q;
+  int32_t n, pieces;  // values, whole pieces of the row
+  int32_t head;       // values before the first piece
 
-  __device__ inline int32_t first(int p) const { return ((p * NWR + q) * 64 + lane) * PV; }
-  __device__ inline int32_t tail_at() const { return n - n % PV + lane; }
-  __device__ inline bool has_tail() const { return q == 0 && lane < n % PV; }
-  __device__ inline bool has(int p) const { return first(p) + PV <= n; }
+  __device__ inline int32_t piece(int p) const { return (p * NWR + q) * 64 + lane; }
+  __device__ inline bool has(int p) const { return piece(p) < pieces; }
+  __device__ inline int32_t first(int p) const { return head + piece(p) * PV; }
+  __device__ inline int32_t rim_at() const { return lane < head ? lane : pieces * PV + lane; }
+  __device__ inline bool has_rim() const { return q == 0 && lane < n - pieces * PV; }
 
   __device__ inline void load(const LT* row, int32_t n_, int lane_, int q_) {
     n = n_;
     lane = lane_;
     q = q_;
+    head = kWhole16 ? (int32_t)((16 - ((uintptr_t)row & 15)) & 15) / (int32_t)sizeof(LT) : 0;
+    if (head > n) head = n;
+    pieces = (n - head) / PV;
+    const LT* aligned = row + head;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       if (has(p)) {
-        w[p] = *reinterpret_cast<const Quad<LT>*>(row + first(p));
+        w[p] = *reinterpret_cast<const Quad<LT>*>(aligned + piece(p) * PV);
       } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[p].w[k] = Elem<LT>::kFill;
       }
     }
-    tail = kNegInf;
-    if (has_tail()) tail = Elem<LT>::widen(row[tail_at()]);
+    rim = kNegInf;
+    if (has_rim()) rim = Elem<LT>::widen(row[rim_at()]);
   }
+  // Places of a value in membership bits: a piece's lie within one word.
+  __device__ inline int32_t bit(int32_t i) const { return i + PV - head; }
   __device__ inline float at(int p, int e) const { return Elem<LT>::get(w[p].w, e); }
 
   // largest value of this lane's (or NaN), also of two halves of them
   __device__ inline void lane_max2(float& a, float& b) {
-    a = tail;
+    a = rim;
     b = kNegInf;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -214,44 +286,53 @@ struct Tile {
   }
 
   // This lane's sums of 2^t, of 2^t t (ENT) and of 2^t outside the list whose
-  // members are set in `bits` (LIST), a piece at a time: less rounding than one
-  // chain. t is held at -200, where 2^t is 0, so that -inf adds 0 to D.
+  // members are set in `bits` (LIST), in four chains: less rounding than in one.
+  // t is held at -200, where 2^t is 0, so that -inf adds 0 to D.
   template <bool BIG, bool ENT, bool LIST>
   __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3]) {
+    float a[4], d[4];
+    {
+      const float t = b.t<BIG>(rim), x = exp2_fast(t);
+      a[0] = x;
+      a[1] = a[2] = a[3] = d[1] = d[2] = d[3] = 0.f;
+      d[0] = ENT ? x * __builtin_fmaxf(t, -200.f) : 0.f;
+      if (LIST) {
+        const int32_t i = bit(rim_at());
+        s[2] = has_rim() && ((bits[i >> 5] >> (i & 31)) & 1) ? 0.f : x;
+      }
+    }
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      float a = 0.f, d = 0.f, x[PV];
+      float x[PV];
 #pragma unroll
       for (int e = 0; e < PV; ++e) {
         const float t = b.t<BIG>(at(p, e));
         x[e] = exp2_fast(t);
-        a += x[e];
-        if (ENT) d = __builtin_fmaf(x[e], __builtin_fmaxf(t, -200.f), d);
+        if (!LIST) a[e & 3] += x[e];
+        if (ENT) d[e & 3] = __builtin_fmaf(x[e], __builtin_fmaxf(t, -200.f), d[e & 3]);
       }
-      if (ENT) s[1] += d;
+      // the sums of a bfloat16 piece before the next one's values: registers
+      if (!LIST && PV == 8) asm volatile("" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
       if (LIST) {
         // (also past the row's end, where 2^t is 0: no test of it)
-        const int32_t f = first(p);
+        const int32_t f = bit(first(p));
         const uint32_t mask = bits[f >> 5] >> (f & 31) & ((1u << PV) - 1);
-        // the sums of this piece before the next one's values: registers
-        asm volatile("" : "+v"(a));
-        float r = a;
+        float all = x[0];
+#pragma unroll
+        for (int e = 1; e < PV; ++e) all += x[e];
+        asm volatile("" : "+v"(all));  // (as above)
+        float r = all;
         if (__ballot(mask != 0) != 0) {  // few pieces hold a listed token
           r = 0.f;
 #pragma unroll
           for (int e = 0; e < PV; ++e) r += (mask >> e) & 1 ? 0.f : x[e];
         }
         s[2] += r;
+        a[p & 3] += all;
       }
-      s[0] += a;
     }
-    const float t = b.t<BIG>(tail), x = exp2_fast(t);
-    s[0] += x;
-    if (ENT) s[1] = __builtin_fmaf(x, __builtin_fmaxf(t, -200.f), s[1]);
-    if (LIST) {
-      const int32_t i = tail_at();
-      s[2] += has_tail() && ((bits[i >> 5] >> (i & 31)) & 1) ? 0.f : x;
-    }
+    s[0] = (a[0] + a[1]) + (a[2] + a[3]);
+    if (ENT) s[1] = (d[0] + d[1]) + (d[2] + d[3]);
   }
 
   // Writes f(t, 2^t) in place of every value.
@@ -265,15 +346,16 @@ struct Tile {
         const float t = b.t<BIG>(at(p, e));
         v[e] = f(t, exp2_fast(t));
       }
+      Quad<LT> o;
+      Elem<LT>::pack(v, o.w);
+      if (PV == 8) asm volatile("" : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(o.w[3]));
       if (has(p)) {
-        Quad<LT> o;
-        Elem<LT>::pack(v, o.w);
         *reinterpret_cast<Quad<LT>*>(out + first(p)) = o;
       }
     }
-    if (has_tail()) {
-      const float t = b.t<BIG>(tail);
-      out[tail_at()] = Elem<LT>::narrow(f(t, exp2_fast(t)));
+    if (has_rim()) {
+      const float t = b.t<BIG>(rim);
+      out[rim_at()] = Elem<LT>::narrow(f(t, exp2_fast(t)));
     }
   }
 
@@ -282,13 +364,13 @@ struct Tile {
 #pragma unroll
     for (int p = 0; p < NP; ++p)
       if (has(p)) *reinterpret_cast<Quad<LT>*>(out + first(p)) = o;
-    if (has_tail()) out[tail_at()] = Elem<LT>::narrow(0.f);
+    if (has_rim()) out[rim_at()] = Elem<LT>::narrow(0.f);
   }
 };
 
 // The row's statistics in the waves that hold it: relative to b's exponents (S,
 // D and R are 2^-delta times too large, D also off by delta S).
-// `box` holds 4 NWR words.
+// `box` holds 3 NWR words.
 template <bool ENT, bool LIST, class LT, int NWR, int NP>
 __device__ __forceinline__ Stats statistics(Tile<LT, NWR, NP>& x, float c, const uint32_t* bits,
                                             float* box, Basis& b) {
@@ -299,7 +381,7 @@ __device__ __forceinline__ Stats statistics(Tile<LT, NWR, NP>& x, float c, const
     x.template sums<true, ENT, LIST>(b, bits, s);
   else
     x.template sums<false, ENT, LIST>(b, bits, s);
-  row_sum<NWR>(s, box + NWR, x.q);
+  row_sum<NWR, ENT, LIST>(s, box + NWR, x.q);
   return {m, s[0], s[1], s[2]};
 }
 
@@ -315,7 +397,7 @@ __device__ __forceinline__ Stats join(const float4* part, int32_t n_seg, float c
                                       Basis& b) {
   float4 v = make_float4(kNegInf, 0.f, 0.f, 0.f);
   if (lane < n_seg) v = part[lane];
-  const float m = wave_max_dpp(v.x);
+  const float m = wave_most(v.x);
   b = Basis::of(m, c);
   // a segment without a value above -inf adds nothing, but its NaN
   const float a = v.x == kNegInf ? 0.f : (v.x - b.m) * c + b.delta;
@@ -323,9 +405,10 @@ __device__ __forceinline__ Stats join(const float4* part, int32_t n_seg, float c
   const float t = __builtin_fmaxf(a, -200.f);
   Stats s;
   s.m = m;
-  s.S = wave_sum_dpp(f * v.y);
-  s.D = wave_sum_dpp(f * __builtin_fmaf(t, v.y, v.z));
-  s.R = wave_sum_dpp(f * v.w);
+  s.S = wave_total(f * v.y);
+  s.D = f * __builtin_fmaf(t, v.y, v.z);
+  s.R = f * v.w;
+  wave_totals(s.D, s.R);
   return s;
 }
 
@@ -353,18 +436,11 @@ struct Shape {
 };
 constexpr int capacity(Shape s, int pv) { return s.nwr * s.np * 64 * pv + pv - 1; }
 
-constexpr int kShapes = 9;
-// Shapes of a type whose pieces hold pv values, in ascending order of their capacity.
-constexpr Shape shape(int pv, int i) {
-  constexpr Shape f32[kShapes] = {{1, 1}, {1, 2}, {1, 4}, {1, 8}, {4, 4},
-                                  {4, 8}, {16, 4}, {16, 8}, {16, 16}};
-  constexpr Shape b16[kShapes] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4},
-                                  {4, 8}, {16, 4}, {16, 8}, {16, 16}};
-  return pv == 4 ? f32[i] : b16[i];
-}
-
+constexpr int kShapes = 13;
+constexpr Shape kShape[kShapes] = {{1, 1}, {1, 2}, {1, 4}, {1, 8}, {1, 16}, {2, 16}, {4, 2},
+                                   {4, 4}, {4, 8}, {4, 16}, {16, 4}, {16, 8}, {16, 16}};
 // Shapes that the segments of cut rows take.
-constexpr bool cuts(Shape s) { return s.nwr > 1 && s.np == 8; }
+constexpr bool cuts(Shape s) { return s.nwr >= 4 && s.np == 8; }
 
 struct Plan {
   int shape;       // instance of the (whole or cut) rows
@@ -385,7 +461,7 @@ struct Int {
 };
 template <class LT, int I = 0, class F>
 inline void with_shape(int i, F f) {
-  constexpr Shape s = shape(Elem<LT>::PV, I);
+  constexpr Shape s = kShape[I];
   if (i == I) {
     f(Int<s.nwr>(), Int<s.np>());
   } else if constexpr (I + 1 < kShapes) {
@@ -406,7 +482,7 @@ inline void in_launches(int64_t n_rows, int rows_per_group, int threads, int32_t
 // Where a wave stands: its row, its part of it.
 template <int NWR>
 struct Place {
-  static constexpr int kWg = NWR * 64 > kThreads ? NWR * 64 : kThreads;
+  static constexpr int kWg = NWR > 1 ? NWR * 64 : kThreads;
   static constexpr int kRows = kWg / 64 / NWR;  // rows of a workgroup
   int lane, q, slot;  // slot: row of the workgroup
   int64_t row;

@@ -23,14 +23,16 @@
 namespace tbias {
 namespace rows {
 
-// Words of the membership bits of a row (or segment).
+// Words of a row's (or segment's) membership bits, one per value (Tile::bit).
 template <class LT, int NWR, int NP>
 constexpr int list_words() {
   return NWR * NP * 64 * Elem<LT>::PV / 32 + 1;
 }
 
-// Sum of g over the places with this lane's token, and whether this is the
-// first of them. Lanes below n take part.
+// A row's list: which lanes' tokens are the first of their kind, and the sum
+// of g over the places of each. Lists of up to four places are compared place
+// by place; for longer ones the lanes mark their tokens in bits, and only if one
+// is found marked the places are compared.
 __device__ __forceinline__ float sum_same(int32_t id, float g, int n, int lane, bool& first) {
   float sum = 0.f;
   first = true;
@@ -43,6 +45,22 @@ __device__ __forceinline__ float sum_same(int32_t id, float g, int n, int lane, 
     }
   }
   return sum;
+}
+constexpr int kFewPlaces = 4;
+// Marks a lane's token, at place i of the part's bits; whether two lanes have the
+// same (every lane returns it).
+__device__ __forceinline__ bool mark(uint32_t* bits, bool mine, int32_t i) {
+  bool twice = false;
+  if (mine) {
+    const uint32_t one = 1u << (i & 31);
+    twice = (atomicOr(&bits[i >> 5], one) & one) != 0;
+  }
+  return __ballot(twice) != 0;
+}
+__device__ __forceinline__ bool mark_fresh(uint32_t* bits, bool mine, int32_t i) {
+  if (mine) bits[i >> 5] = 0u;
+  wave_fence();
+  return mark(bits, mine, i);
 }
 
 // The wave of a row that writes listed tokens has to come after all that the
@@ -61,8 +79,10 @@ enum Pass { kWhole, kStats, kApply };
 
 template <class LT, int NWR, int NP, bool ENT, Pass PASS>
 __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io) {
-  __shared__ float box[4 * NWR];
+  __shared__ float box[3 * NWR];
+  __shared__ uint32_t bits_all[Place<NWR>::kRows][list_words<LT, NWR, NP>()];
   lds_poison(box, sizeof(box));
+  lds_poison(bits_all, sizeof(bits_all));
   const Place<NWR> at(a);
   if (at.row >= a.n_rows) return;  // uniform over the row's waves
   const LT* z = static_cast<const LT*>(a.z) + at.row * a.stride;
@@ -103,7 +123,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io
     x.store_zeros(out);
     return;
   }
-  const float total = wave_sum_dpp(g);
+  const float total = wave_total(g);
   const float f = a.inv_tau / s.S;
   float k0 = (gl - total) * f, k1 = 0.f;
   if (ENT) {
@@ -120,8 +140,10 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io
     x.template store<false>(out, b, slope);
   row_sync<NWR>();
   if (at.q != 0) return;
-  bool first;
-  const float sum = sum_same(id, g, io.J, at.lane, first);
+  bool first = true;
+  float sum = g;
+  if (io.J <= kFewPlaces || mark_fresh(bits_all[at.slot], mine, x.bit(id - at.c0)))
+    sum = sum_same(id, g, io.J, at.lane, first);
   if (mine && first) {
     const float t = b.t(zj);
     out[id - at.c0] = Elem<LT>::narrow(__builtin_fmaf(sum, a.inv_tau, slope(t, exp2_fast(t))));
@@ -153,15 +175,15 @@ __device__ __forceinline__ Teacher teacher(const DistillIO& io, int64_t row, int
   if (io.tail) {
     t.q = expf(sc);
     t.logq = sc;
-    const float sum = wave_sum_dpp(t.q);
+    const float sum = wave_total(t.q);
     const float rest = 1.f - sum;
     t.rest = rest < 0.f ? 0.f : rest;  // (a NaN stays)
     t.mass = sum + t.rest;
   } else {
-    const float m = wave_max_dpp(sc);
+    const float m = wave_most(sc);
     const float x = sc - (m == kNegInf ? 0.f : m);
     const float e = exp2_fast(x * c);
-    const float sum = wave_sum_dpp(e);
+    const float sum = wave_total(e);
     t.mass = sum == 0.f ? 0.f : 1.f;
     t.q = sum == 0.f ? 0.f : e / sum;
     t.logq = x * (c * kLn2) - logf(sum);
@@ -175,7 +197,7 @@ __device__ __forceinline__ float distill_loss(const Teacher& t, float zk, const 
   const float log_s = log_sum(s, b);
   const float lp = log_prob(zk, b, log_s, inv_tau);
   // NaN scores give NaN terms
-  float loss = wave_sum_dpp(t.ok && t.q != 0.f ? t.q * (t.logq - lp) : 0.f);
+  float loss = wave_total(t.ok && t.q != 0.f ? t.q * (t.logq - lp) : 0.f);
   if (t.rest != 0.f) {  // nothing outside the list (or an empty row): no mass for the rest
     const float lr = s.R == 0.f ? kNegInf : logf(s.R) - logf(s.S);
     loss += t.rest * (logf(t.rest) - lr);
@@ -183,21 +205,10 @@ __device__ __forceinline__ float distill_loss(const Teacher& t, float zk, const 
   return t.bad ? __builtin_nanf("") : loss;
 }
 
-// Sets the members of the list that lie in this part of the row.
-template <int NWR, int WORDS>
-__device__ __forceinline__ void set_bits(uint32_t* bits, const Teacher& t, int32_t c0, int32_t n,
-                                         int lane, int q) {
-  for (int i = q * 64 + lane; i < WORDS; i += NWR * 64) bits[i] = 0u;
-  row_sync<NWR>();
-  if (q == 0 && t.ok && t.id >= c0 && t.id < c0 + n)
-    atomicOr(&bits[(t.id - c0) >> 5], 1u << ((t.id - c0) & 31));
-  row_sync<NWR>();
-}
-
 template <class LT, int NWR, int NP, bool TAIL, Pass PASS>
 __global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, DistillIO io) {
-  constexpr int kWords = TAIL && PASS != kApply ? list_words<LT, NWR, NP>() : 1;
-  __shared__ float box[4 * NWR];
+  constexpr int kWords = list_words<LT, NWR, NP>();
+  __shared__ float box[3 * NWR];
   __shared__ uint32_t bits_all[Place<NWR>::kRows][kWords];
   lds_poison(box, sizeof(box));
   lds_poison(bits_all, sizeof(bits_all));
@@ -219,12 +230,18 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, Distil
   }
   Basis b;
   Stats s;
+  uint32_t* bits = bits_all[at.slot];
+  bool twice = false;  // a token is listed twice (in the wave that writes the list)
   if (PASS == kApply) {
     s = join(a.part + at.row * a.n_seg, a.n_seg, a.c, at.lane, b);
     row_sync<NWR>();  // zk is read before another wave may write there
   } else {
-    uint32_t* bits = bits_all[at.slot];
-    if (TAIL) set_bits<NWR, kWords>(bits, t, at.c0, at.n, at.lane, at.q);
+    if (TAIL) {
+      for (int i = at.q * 64 + at.lane; i < kWords; i += NWR * 64) bits[i] = 0u;
+      row_sync<NWR>();
+      if (at.q == 0) twice = mark(bits, mine, x.bit(t.id - at.c0));
+      row_sync<NWR>();
+    }
     s = statistics<false, TAIL>(x, a.c, bits, box, b);
   }
   if (PASS == kStats) {
@@ -252,8 +269,11 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, Distil
     x.template store<false>(out, b, slope);
   row_sync<NWR>();
   if (at.q != 0) return;
-  bool first;
-  const float sum = sum_same(t.id, t.q, io.K, at.lane, first);
+  if (!TAIL || PASS == kApply)
+    twice = io.K <= kFewPlaces || mark_fresh(bits, mine, x.bit(t.id - at.c0));
+  bool first = true;
+  float sum = t.q;
+  if (twice) sum = sum_same(t.id, t.q, io.K, at.lane, first);
   if (mine && first) {
     const float e = exp2_fast(b.t(zk));
     out[t.id - at.c0] = Elem<LT>::narrow(__builtin_fmaf(-sum, wt, e * k_on));

@@ -86,7 +86,7 @@ __device__ __forceinline__ float of_order(uint32_t k) {
 // Lanes that share a group, as a power of two; -1: a lane holds two groups.
 template <int NWR>
 __device__ __forceinline__ int group_log2(int M) {
-  return (NWR == 1 ? 0 : NWR == 4 ? 2 : 4) - (M > 16 ? 1 : 0);
+  return (NWR == 1 ? 0 : NWR == 2 ? 1 : NWR == 4 ? 2 : 4) - (M > 16 ? 1 : 0);
 }
 __device__ __forceinline__ float group_max(float v, int log2) {
   if (log2 > 0) v = __builtin_fmaxf(v, dpp_f<0xB1, 0xf>(v, v));   // pairs
@@ -103,7 +103,7 @@ __device__ __forceinline__ float no_nan(float v) { return v == v ? v : kNegInf; 
 __device__ __forceinline__ float reached_by(float a, float b, bool two, int need, float most) {
   if (need == 1) return most;
   const uint32_t ka = order_of(a), kb = order_of(b);
-  uint32_t lo = order_of(-wave_max_dpp(-a)), hi = order_of(most);
+  uint32_t lo = order_of(wave_least(a)), hi = order_of(most);
   while (lo < hi) {  // need values reach lo
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
     int n = __builtin_popcountll(__ballot(ka >= mid));
@@ -122,7 +122,7 @@ __device__ __forceinline__ float reached_by(float a, float b, bool two, int need
 // of the list.
 template <int NWR>
 struct Found {
-  static constexpr int kCap = NWR == 1 ? 256 : NWR == 4 ? 128 : 64;  // of a wave
+  static constexpr int kCap = NWR <= 2 ? 256 : NWR == 4 ? 128 : 64;  // of a wave
   static constexpr int kMost = 256;                                  // of a row
   static constexpr int kKeys = 128;  // ranked by words of 32 bits
   int2 at[NWR][kCap];
@@ -183,9 +183,8 @@ __device__ __forceinline__ void rank(Found<NWR>& f, const Rows& a, const ScoreIO
     }
     bool ties = false;
     if (!kShort) {
-      int sum = (lane < total ? at[0] : 0) + (64 + lane < total ? at[1] : 0);
-      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-      ties = sum != total * (total - 1) / 2;
+      const int sum = (lane < total ? at[0] : 0) + (64 + lane < total ? at[1] : 0);
+      ties = wave_total_i32(sum) != total * (total - 1) / 2;
     }
     if (!ties) {
       if (lane < total) write(c[0], at[0]);
@@ -211,7 +210,7 @@ template <class LT, int NWR, int NP, bool TOP, bool PART>
 __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO io) {
   typedef Tile<LT, NWR, NP> T;
   constexpr int PV = T::PV;
-  __shared__ float box[4 * NWR], box_z[NWR];
+  __shared__ float box[3 * NWR], box_z[NWR];
   __shared__ int32_t box_id[NWR];
   __shared__ float group[TOP && NWR > 1 ? 128 : 1];
   __shared__ Found<TOP ? NWR : 1> found_all[TOP ? Place<NWR>::kRows : 1];
@@ -253,7 +252,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
       g0 = group[at.lane];
       if (two) g1 = group[64 + at.lane];
     }
-    s.m = wave_max_dpp(two ? __builtin_fmaxf(g0, g1) : g0);
+    s.m = wave_most(two ? __builtin_fmaxf(g0, g1) : g0);
     b = Basis::of(s.m, a.c);
     float bound = reached_by(g0, g1, two, io.M, s.m);
     if (bound == kNegInf) bound = -__FLT_MAX__;  // only tokens above -inf
@@ -286,10 +285,13 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
 #pragma unroll
       for (int e = 0; e < PV; ++e) see(x.at(p, e), x.first(p) + e);
     }
-    see(x.tail, x.tail_at());
+    see(x.rim, x.rim_at());
     if (at.lane == 0) found.n[at.q] = n;
     if (NWR == 1) wave_fence();
-    row_sum<NWR>(v, box, at.q);  // the waves' candidates are in LDS after it, too
+    if (ent)  // the waves' candidates are in LDS after it, too
+      row_sum<NWR, true, false>(v, box, at.q);
+    else
+      row_sum<NWR, false, false>(v, box, at.q);
     s.S = v[0];
     s.D = v[1];
     s.R = 0.f;
@@ -316,10 +318,10 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
       float bz = kNegInf;
       int32_t bi = INT_MAX;
       // the places are formed anew in each turn: held, they take a register a value
-      int32_t place = at.lane * PV;
+      int32_t place = x.head + at.lane * PV;
       asm volatile("" : "+v"(place));
       auto best = [&](float val, int32_t id) {
-        if ((val < lz || (val == lz && id > li)) && val > bz) {
+        if ((val < lz || (val == lz && id > li)) && better(val, id, bz, bi) && val > kNegInf) {
           bz = val;
           bi = id;
         }
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
         for (int e = 0; e < PV; ++e)
           best(x.at(p, e), place + (p * NWR + at.q) * 64 * PV + e);
       }
-      best(x.tail, x.tail_at());
+      best(x.rim, x.rim_at());
       row_best<NWR>(bz, bi, box_z, box_id, at.q, at.lane);
       if (at.q == 0 && at.lane == 0)
         write_alt<PART>(a, io, at.row, i, bz, bz == kNegInf ? -1 : at.c0 + bi, b, log_s);
