@@ -287,9 +287,10 @@ struct Tile {
 
   // This lane's sums of 2^t, of 2^t t (ENT) and of 2^t outside the list whose
   // members are set in `bits` (LIST), in four chains: less rounding than in one.
-  // t is held at -200, where 2^t is 0, so that -inf adds 0 to D.
-  template <bool BIG, bool ENT, bool LIST>
-  __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3]) {
+  // t is held at -200, where 2^t is 0, so that -inf adds 0 to D. look(value,
+  // place) sees every value, too.
+  template <bool BIG, bool ENT, bool LIST, class F>
+  __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3], F look) {
     float a[4], d[4];
     {
       const float t = b.t<BIG>(rim), x = exp2_fast(t);
@@ -303,16 +304,21 @@ struct Tile {
     }
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      float x[PV];
+      float v[PV], x[PV];
 #pragma unroll
       for (int e = 0; e < PV; ++e) {
-        const float t = b.t<BIG>(at(p, e));
+        v[e] = at(p, e);
+        const float t = b.t<BIG>(v[e]);
         x[e] = exp2_fast(t);
         if (!LIST) a[e & 3] += x[e];
         if (ENT) d[e & 3] = __builtin_fmaf(x[e], __builtin_fmaxf(t, -200.f), d[e & 3]);
       }
-      // the sums of a bfloat16 piece before the next one's values: registers
-      if (!LIST && PV == 8) asm volatile("" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
+      // the sums of a piece before its values are looked at and before the next
+      // one's: put off, they hold registers
+      if (!LIST) asm volatile("" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
+      if (ENT) asm volatile("" : "+v"(d[0]), "+v"(d[1]), "+v"(d[2]), "+v"(d[3]));
+#pragma unroll
+      for (int e = 0; e < PV; ++e) look(v[e], first(p) + e);
       if (LIST) {
         // (also past the row's end, where 2^t is 0: no test of it)
         const int32_t f = bit(first(p));
@@ -331,6 +337,7 @@ struct Tile {
         a[p & 3] += all;
       }
     }
+    look(rim, rim_at());
     s[0] = (a[0] + a[1]) + (a[2] + a[3]);
     if (ENT) s[1] = (d[0] + d[1]) + (d[2] + d[3]);
   }
@@ -377,10 +384,11 @@ __device__ __forceinline__ Stats statistics(Tile<LT, NWR, NP>& x, float c, const
   const float m = row_max<NWR>(x.lane_max(), box, x.q);
   b = Basis::of(m, c);
   float s[3] = {0.f, 0.f, 0.f};
+  auto look = [](float, int32_t) {};
   if (b.big)
-    x.template sums<true, ENT, LIST>(b, bits, s);
+    x.template sums<true, ENT, LIST>(b, bits, s, look);
   else
-    x.template sums<false, ENT, LIST>(b, bits, s);
+    x.template sums<false, ENT, LIST>(b, bits, s, look);
   row_sum<NWR, ENT, LIST>(s, box + NWR, x.q);
   return {m, s[0], s[1], s[2]};
 }
@@ -419,7 +427,7 @@ __device__ __forceinline__ float log_sum(const Stats& s, const Basis& b) {
 // entropy in nats; a row without a value above -inf has none
 __device__ __forceinline__ float entropy(const Stats& s) {
   if (s.m == kNegInf && s.S == 0.f) return 0.f;
-  const float h = logf(s.S) - kLn2 * (s.D / s.S);
+  const float h = logf(s.S) - kLn2 * (s.D * __builtin_amdgcn_rcpf(s.S));
   return h < 0.f ? 0.f : h;
 }
 __device__ __forceinline__ bool empty(const Stats& s) { return s.m == kNegInf && s.S == 0.f; }

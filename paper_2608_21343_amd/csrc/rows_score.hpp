@@ -27,17 +27,42 @@ __device__ __forceinline__ void write_scores(const Rows& a, const ScoreIO& io, i
   }
 }
 
-// The i-th alternative of a row (or segment).
+// Where a row's (or segment's) alternatives are written.
 template <bool PART>
-__device__ __forceinline__ void write_alt(const Rows& a, const ScoreIO& io, int64_t row, int i,
-                                          float z, int32_t id, const Basis& b, float log_s) {
-  if (PART) {
-    io.lists[(row * a.n_seg + blockIdx.y) * io.M + i] = make_int2(__float_as_int(z), id);
-  } else {
-    io.alt[row * io.M + i] = id;
-    io.alt_logprob[row * io.M + i] = id < 0 ? kNegInf : log_prob(z, b, log_s, a.inv_tau);
+struct AltRow {
+  int32_t* id;
+  float* logprob;
+  int2* list;
+  float log_s, m, inv_tau;
+  __device__ inline AltRow(const Rows& a, const ScoreIO& io, int64_t row, const Basis& b,
+                           float log_s_) {
+    if (PART) {
+      list = io.lists + (row * a.n_seg + blockIdx.y) * io.M;
+    } else {
+      id = io.alt + row * io.M;
+      logprob = io.alt_logprob + row * io.M;
+    }
+    log_s = log_s_;
+    m = b.m;
+    inv_tau = a.inv_tau;
   }
-}
+  __device__ inline void write(int i, float z, int32_t token) const {
+    if (PART) {
+      list[i] = make_int2(__float_as_int(z), token);
+    } else {
+      id[i] = token;
+      logprob[i] = (z - m) * inv_tau - log_s;
+    }
+  }
+  __device__ inline void none(int i) const {
+    if (PART) {
+      list[i] = make_int2(__float_as_int(kNegInf), -1);
+    } else {
+      id[i] = -1;
+      logprob[i] = kNegInf;
+    }
+  }
+};
 
 // Best (z, id) over the row's waves of every wave's own best.
 template <int NWR>
@@ -135,9 +160,8 @@ struct Found {
 // to 2^16 values, also for float32 where no two candidates are equal (which
 // shows in the sum of the ranks), else of 64.
 template <class LT, int NWR, bool PART>
-__device__ __forceinline__ void rank(Found<NWR>& f, const Rows& a, const ScoreIO& io, int64_t row,
-                                     int32_t c0, int32_t n, const Basis& b, float log_s,
-                                     int lane) {
+__device__ __forceinline__ void rank(Found<NWR>& f, const AltRow<PART>& out, int M, int32_t c0,
+                                     int32_t n, int lane) {
   int32_t total = 0, count[NWR];
 #pragma unroll
   for (int w = 0; w < NWR; ++w) {
@@ -154,43 +178,48 @@ __device__ __forceinline__ void rank(Found<NWR>& f, const Rows& a, const ScoreIO
     return c;
   };
   auto write = [&](int2 c, int at) {
-    if (at < io.M)
-      write_alt<PART>(a, io, row, at, __int_as_float(c.x), c0 + c.y, b, log_s);
+    if (at < M) out.write(at, __int_as_float(c.x), c0 + c.y);
   };
-  if (lane >= total && lane < io.M)
-    write_alt<PART>(a, io, row, lane, kNegInf, -1, b, log_s);
+  if (total < M && lane >= total && lane < M) out.none(lane);
   constexpr bool kShort = sizeof(LT) == 2;
   if (total <= Found<NWR>::kKeys && (!kShort || n <= 65536)) {
-    int2 c[2];
-    uint32_t key[2];
-    int at[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      c[h] = make_int2(0, 0);
-      key[h] = 0;
-      at[h] = 0;
-      if (h * 64 >= total) continue;  // uniform
-      c[h] = candidate(h * 64 + lane);
-      const uint32_t o = order_of(__int_as_float(c[h].x));
-      if (h * 64 + lane < total) key[h] = kShort ? (o & 0xffff0000u) | (0xffff - c[h].y) : o;
-      reinterpret_cast<uint32_t*>(f.key)[h * 64 + lane] = key[h];
-    }
-    wave_fence();
-    for (int j = 0; j < total; j += 4) {
-      const uint4 k = f.key[j / 4];
-      at[0] += (k.x > key[0]) + (k.y > key[0]) + (k.z > key[0]) + (k.w > key[0]);
-      if (total > 64) at[1] += (k.x > key[1]) + (k.y > key[1]) + (k.z > key[1]) + (k.w > key[1]);
-    }
+    auto key_of = [&](int2 c) {
+      const uint32_t o = order_of(__int_as_float(c.x));
+      return kShort ? (o & 0xffff0000u) | (0xffff - c.y) : o;
+    };
+    uint32_t* keys = reinterpret_cast<uint32_t*>(f.key);
+    const int2 c = candidate(lane);
+    const uint32_t key = lane < total ? key_of(c) : 0;
+    keys[lane] = key;
     bool ties = false;
-    if (!kShort) {
-      const int sum = (lane < total ? at[0] : 0) + (64 + lane < total ? at[1] : 0);
-      ties = wave_total_i32(sum) != total * (total - 1) / 2;
+    if (total <= 64) {
+      int at = 0;
+      wave_fence();
+      for (int j = 0; j < total; j += 4) {
+        const uint4 k = f.key[j / 4];
+        at += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+      }
+      if (!kShort) ties = wave_total_i32(lane < total ? at : 0) != total * (total - 1) / 2;
+      if (!ties && lane < total) write(c, at);
+    } else {
+      const int2 c2 = candidate(64 + lane);
+      const uint32_t key2 = 64 + lane < total ? key_of(c2) : 0;
+      keys[64 + lane] = key2;
+      int at = 0, at2 = 0;
+      wave_fence();
+      for (int j = 0; j < total; j += 4) {
+        const uint4 k = f.key[j / 4];
+        at += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+        at2 += (k.x > key2) + (k.y > key2) + (k.z > key2) + (k.w > key2);
+      }
+      if (!kShort)
+        ties = wave_total_i32(at + (64 + lane < total ? at2 : 0)) != total * (total - 1) / 2;
+      if (!ties) {
+        write(c, at);
+        if (64 + lane < total) write(c2, at2);
+      }
     }
-    if (!ties) {
-      if (lane < total) write(c[0], at[0]);
-      if (64 + lane < total) write(c[1], at[1]);
-      return;
-    }
+    if (!ties) return;
   }
   auto whole = [](int2 c) {
     return (uint64_t)order_of(__int_as_float(c.x)) << 32 | (uint32_t)~c.y;
@@ -224,7 +253,6 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
   x.load(z + at.c0, at.n, at.lane, at.q);
   Basis b;
   Stats s;
-  const bool ent = PART || io.entropy;
   auto finish = [&](float log_s) {  // one wave
     if (PART) {
       if (at.lane == 0) a.part[at.row * a.n_seg + blockIdx.y] = to_part(s, b);
@@ -233,7 +261,8 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
     }
   };
   if constexpr (!TOP) {
-    s = ent ? statistics<true, false>(x, a.c, nullptr, box, b)
+    s = PART || io.entropy
+            ? statistics<true, false>(x, a.c, nullptr, box, b)
             : statistics<false, false>(x, a.c, nullptr, box, b);
     if (at.q == 0) finish(log_sum(s, b));
   } else {
@@ -256,18 +285,6 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
     b = Basis::of(s.m, a.c);
     float bound = reached_by(g0, g1, two, io.M, s.m);
     if (bound == kNegInf) bound = -__FLT_MAX__;  // only tokens above -inf
-    float v[3] = {0.f, 0.f, 0.f};
-    if (ent) {
-      if (b.big)
-        x.template sums<true, true, false>(b, nullptr, v);
-      else
-        x.template sums<false, true, false>(b, nullptr, v);
-    } else {
-      if (b.big)
-        x.template sums<true, false, false>(b, nullptr, v);
-      else
-        x.template sums<false, false, false>(b, nullptr, v);
-    }
     int32_t n = 0;
     auto see = [&](float val, int32_t id) {
       const uint64_t hit = __ballot(val >= bound);
@@ -280,18 +297,14 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
       }
       n = more;
     };
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-#pragma unroll
-      for (int e = 0; e < PV; ++e) see(x.at(p, e), x.first(p) + e);
-    }
-    see(x.rim, x.rim_at());
+    float v[3] = {0.f, 0.f, 0.f};
+    if (b.big)
+      x.template sums<true, true, false>(b, nullptr, v, see);
+    else
+      x.template sums<false, true, false>(b, nullptr, v, see);
     if (at.lane == 0) found.n[at.q] = n;
     if (NWR == 1) wave_fence();
-    if (ent)  // the waves' candidates are in LDS after it, too
-      row_sum<NWR, true, false>(v, box, at.q);
-    else
-      row_sum<NWR, false, false>(v, box, at.q);
+    row_sum<NWR, true, false>(v, box, at.q);  // the waves' candidates are in LDS then, too
     s.S = v[0];
     s.D = v[1];
     s.R = 0.f;
@@ -305,9 +318,9 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
       over |= k > Found<NWR>::kCap;
       total += k;
     }
+    const AltRow<PART> out(a, io, at.row, b, log_s);
     if (!over && total <= Found<NWR>::kMost) {
-      if (at.q == NWR - 1)
-        rank<LT, NWR, PART>(found, a, io, at.row, at.c0, at.n, b, log_s, at.lane);
+      if (at.q == NWR - 1) rank<LT, NWR, PART>(found, out, io.M, at.c0, at.n, at.lane);
       return;
     }
     // Too many for the list (rows of few different values): one alternative after
@@ -334,8 +347,12 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
       }
       best(x.rim, x.rim_at());
       row_best<NWR>(bz, bi, box_z, box_id, at.q, at.lane);
-      if (at.q == 0 && at.lane == 0)
-        write_alt<PART>(a, io, at.row, i, bz, bz == kNegInf ? -1 : at.c0 + bi, b, log_s);
+      if (at.q == 0 && at.lane == 0) {
+        if (bz == kNegInf)
+          out.none(i);
+        else
+          out.write(i, bz, at.c0 + bi);
+      }
       lz = bz;
       li = bi;
     }
@@ -354,6 +371,7 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(Rows a, ScoreIO io
   const Stats s = join(a.part + row * a.n_seg, a.n_seg, a.c, lane, b);
   const float log_s = log_sum(s, b);
   write_scores(a, io, row, z, s, b, log_s, lane);
+  const AltRow<false> out(a, io, row, b, log_s);
   // merge: every lane holds the best that its segment's list has left
   const int2* list = io.lists + (row * a.n_seg + lane) * io.M;
   int at = 0;
@@ -363,8 +381,12 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(Rows a, ScoreIO io
     float bz;
     int32_t bi;
     const int own = wave_argmax_dpp(__int_as_float(head.x), head.y < 0 ? INT_MAX : head.y, bz, bi);
-    if (lane == 0)
-      write_alt<false>(a, io, row, i, bz, bz == kNegInf ? -1 : bi, b, log_s);
+    if (lane == 0) {
+      if (bz == kNegInf)
+        out.none(i);
+      else
+        out.write(i, bz, bi);
+    }
     if (lane == own) {
       ++at;
       head = at < io.M && lane < a.n_seg ? list[at] : make_int2(__float_as_int(kNegInf), INT_MAX);
