@@ -24,7 +24,7 @@ namespace tbias {
 namespace rows {
 
 constexpr float kNegInf = -__builtin_huge_valf();
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256;  // of a workgroup whose rows take one wave each
 constexpr int kMaxSeg = 64;    // segments of a row: one lane each when they are joined
 
@@ -122,6 +122,8 @@ struct Basis {
 };
 
 __device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_exp2f(t); }
+// Natural logarithm of 0 or a normal number, to 1.5 units of the last place.
+__device__ __forceinline__ float ln(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 
 // max of three in one instruction; a NaN stays (a maximum that passes it over
 // costs another instruction for every value loaded)
@@ -422,12 +424,12 @@ __device__ __forceinline__ Stats join(const float4* part, int32_t n_seg, float c
 
 // ln of the sum of exp(u - u_max)
 __device__ __forceinline__ float log_sum(const Stats& s, const Basis& b) {
-  return logf(s.S) - kLn2 * b.delta;
+  return ln(s.S) - kLn2 * b.delta;
 }
 // entropy in nats; a row without a value above -inf has none
 __device__ __forceinline__ float entropy(const Stats& s) {
   if (s.m == kNegInf && s.S == 0.f) return 0.f;
-  const float h = logf(s.S) - kLn2 * (s.D * __builtin_amdgcn_rcpf(s.S));
+  const float h = ln(s.S) - kLn2 * (s.D * __builtin_amdgcn_rcpf(s.S));
   return h < 0.f ? 0.f : h;
 }
 __device__ __forceinline__ bool empty(const Stats& s) { return s.m == kNegInf && s.S == 0.f; }

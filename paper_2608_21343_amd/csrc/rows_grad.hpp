@@ -127,7 +127,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io
   const float f = a.inv_tau / s.S;
   float k0 = (gl - total) * f, k1 = 0.f;
   if (ENT) {
-    k0 -= gh * (entropy(s) - logf(s.S)) * f;
+    k0 -= gh * (entropy(s) - ln(s.S)) * f;
     k1 = -gh * kLn2 * f;
   }
   if (bad) k0 = __builtin_nanf("");
@@ -173,7 +173,7 @@ __device__ __forceinline__ Teacher teacher(const DistillIO& io, int64_t row, int
   if (!t.ok) sc = kNegInf;
   t.rest = 0.f;
   if (io.tail) {
-    t.q = expf(sc);
+    t.q = exp2_fast(sc * kLog2e);
     t.logq = sc;
     const float sum = wave_total(t.q);
     const float rest = 1.f - sum;
@@ -185,8 +185,8 @@ __device__ __forceinline__ Teacher teacher(const DistillIO& io, int64_t row, int
     const float e = exp2_fast(x * c);
     const float sum = wave_total(e);
     t.mass = sum == 0.f ? 0.f : 1.f;
-    t.q = sum == 0.f ? 0.f : e / sum;
-    t.logq = x * (c * kLn2) - logf(sum);
+    t.q = sum == 0.f ? 0.f : e * __builtin_amdgcn_rcpf(sum);
+    t.logq = x * (c * kLn2) - ln(sum);
     if (sum != sum) t.mass = sum;
   }
   return t;
@@ -199,8 +199,8 @@ __device__ __forceinline__ float distill_loss(const Teacher& t, float zk, const 
   // NaN scores give NaN terms
   float loss = wave_total(t.ok && t.q != 0.f ? t.q * (t.logq - lp) : 0.f);
   if (t.rest != 0.f) {  // nothing outside the list (or an empty row): no mass for the rest
-    const float lr = s.R == 0.f ? kNegInf : logf(s.R) - logf(s.S);
-    loss += t.rest * (logf(t.rest) - lr);
+    const float lr = s.R == 0.f ? kNegInf : ln(s.R) - ln(s.S);
+    loss += t.rest * (ln(t.rest) - lr);
   }
   return t.bad ? __builtin_nanf("") : loss;
 }
