@@ -129,6 +129,14 @@ def _load() -> C.CDLL:
 
 LIB = _load()
 
+
+def _types():
+    import torch
+    return torch.float32, torch.bfloat16, torch.int32
+
+
+_F32, _BF16, _I32 = _types()  # (objects of their own: compared by identity)
+
 EXPORTED = ("tb_compile_graphs", "tb_graphs_layout", "tb_graphs_host_image", "tb_graphs_upload",
             "tb_graphs_free", "tb_validate_image", "tb_init_states", "tb_boost_step_greedy",
             "tb_boost_step_beam", "tb_reset_stream", "tb_last_error",
@@ -549,14 +557,16 @@ def tb_boost_step_beam_stream(arena: Arena, logits, model_ids, states, scores, h
 # ---------------------------------------------------------------------------
 # row operators
 
+# rows of up to this many values are never cut into segments (tbias.h)
+_WHOLE_ROW = 1 << 15
+
 
 def _rows(x, name: str = "logits"):
     """(rows, V+1, row stride) of a tensor [..., V+1] whose rows are evenly spaced."""
-    shape = x.shape
+    shape, strides = x.shape, x.stride()
     n = len(shape)
     if n < 1 or shape[-1] < 2:
         raise ValueError(f"{name} must be [..., V+1] with V+1 >= 2")
-    strides = x.stride()
     if strides[-1] != 1:
         raise ValueError(f"{name} rows must be contiguous")
     rows, step = 1, 0
@@ -574,50 +584,56 @@ def _rows(x, name: str = "logits"):
     return rows, shape[-1], step if rows > 1 else max(step, shape[-1])
 
 
-def _per_row(t, rows: int, dtype, name: str) -> int:
-    """Values a row of a contiguous per-row device tensor [rows..., n] (None: 0)."""
+def _list(t, rows: int, dtype, name: str):
+    """(values a row, device pointer) of a contiguous tensor [rows..., n]; (0,
+    None) for None."""
     if t is None:
-        return 0
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+        return 0, None
     k = t.shape[-1] if t.dim() else 1
-    if t.numel() != rows * k:
+    if (t.dtype is not dtype or t.numel() != rows * k or not t.is_cuda
+            or not t.is_contiguous()):  # the first fault
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
         raise ValueError(f"{name} holds {t.numel()} elements, needs [{rows}, n]")
-    return k
+    return k, t.data_ptr()
 
 
-def _one_per_row(t, rows: int, name: str) -> Optional[int]:
+def _one(t, rows: int, name: str) -> Optional[int]:
     """Device pointer of a float32 tensor of one value a row (None passes NULL)."""
     if t is None:
         return None
-    import torch
-    _need(t, rows, name)
-    return _dptr(t, torch.float32, name)
+    if (t.dtype is not _F32 or t.numel() != rows or not t.is_cuda
+            or not t.is_contiguous()):  # the first fault
+        _need(t, rows, name)
+        _dptr(t, _F32, name)
+    return t.data_ptr()
 
 
 def _rows_in(logits, n_alt: int, workspace):
-    """(arguments of the rows, workspace arguments, device workspace) of a call.
-    A workspace that the call needs and the caller did not pass is allocated on
-    the current stream."""
-    import torch
+    """(arguments of the rows, workspace pointer, workspace bytes, device
+    workspace) of a call. A workspace that the call needs and the caller did not
+    pass is allocated on the current stream."""
     n, V1, rs = _rows(logits)
-    dt = TB_F32 if logits.dtype == torch.float32 else TB_BF16
-    if dt == TB_BF16 and logits.dtype != torch.bfloat16:
+    if logits.dtype == _F32:
+        dt = TB_F32
+    elif logits.dtype == _BF16:
+        dt = TB_BF16
+    else:
         raise ValueError("logits must be float32 or bfloat16")
     ptr = _logits_ptr(logits)
-    if workspace is None:
+    if workspace is None and V1 > _WHOLE_ROW:
+        import torch
         need = LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt)
         if need > 0:
             workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
     if workspace is None:
-        return (ptr, dt, n, V1, rs), (None, 0), None
-    return ((ptr, dt, n, V1, rs),
-            (_dptr(workspace, name="workspace"), workspace.numel() * workspace.element_size()),
-            workspace)
+        return (ptr, dt, n, V1, rs), None, 0, None
+    return ((ptr, dt, n, V1, rs), _dptr(workspace, name="workspace"),
+            workspace.numel() * workspace.element_size(), workspace)
 
 
 def _grad_args(grad, logits):
@@ -633,9 +649,9 @@ def _grad_args(grad, logits):
 
 def tb_rows_workspace_bytes(logits, n_alt: int = 0) -> int:
     """Workspace bytes of a row operator on these logits (0: none)."""
-    import torch
     n, V1, _ = _rows(logits)
-    dt = TB_F32 if logits.dtype == torch.float32 else TB_BF16
+    dt, _ = _logits_args(logits) if logits.dim() > 1 else (
+        TB_F32 if logits.dtype == _F32 else TB_BF16, 0)
     return int(LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt))
 
 
@@ -645,43 +661,37 @@ def tb_token_logprobs(logits, tokens=None, out_logprob=None, out_lse=None, out_e
     """logits: [..., V+1] device tensor with evenly spaced rows; tokens and
     out_logprob [..., n_tok]; out_lse and out_entropy one value a row; out_alt
     and out_alt_logprob [..., n_alt]."""
-    import torch
-    i32, f32 = torch.int32, torch.float32
     M = 0 if out_alt is None else out_alt.shape[-1]
-    rows, ws, keep = _rows_in(logits, M, workspace)
+    rows, ws, ws_bytes, keep = _rows_in(logits, M, workspace)
     n = rows[2]
-    J = _per_row(tokens, n, i32, "tokens")
-    if _per_row(out_logprob, n, f32, "out_logprob") != J:
+    J, p_tok = _list(tokens, n, _I32, "tokens")
+    J2, p_lp = _list(out_logprob, n, _F32, "out_logprob")
+    if J != J2:
         raise ValueError("out_logprob must hold one value per token")
-    _per_row(out_alt, n, i32, "out_alt")
-    if _per_row(out_alt_logprob, n, f32, "out_alt_logprob") != M:
+    M, p_alt = _list(out_alt, n, _I32, "out_alt")
+    M2, p_alt_lp = _list(out_alt_logprob, n, _F32, "out_alt_logprob")
+    if M != M2:
         raise ValueError("out_alt_logprob must hold one value per alternative")
-    _check(LIB.tb_token_logprobs(*rows, temperature, tokens.data_ptr() if J else None, J,
-                                 out_logprob.data_ptr() if J else None,
-                                 _one_per_row(out_lse, n, "out_lse"),
-                                 _one_per_row(out_entropy, n, "out_entropy"), M,
-                                 out_alt.data_ptr() if M else None,
-                                 out_alt_logprob.data_ptr() if M else None, *ws,
-                                 _stream(stream)))
+    _check(LIB.tb_token_logprobs(*rows, temperature, p_tok, J, p_lp, _one(out_lse, n, "out_lse"),
+                                 _one(out_entropy, n, "out_entropy"), M, p_alt, p_alt_lp, ws,
+                                 ws_bytes, _stream(stream)))
 
 
 def tb_token_logprobs_grad(logits, tokens, d_logprob, grad, d_lse=None, d_entropy=None,
                            temperature: float = 1.0, workspace=None, stream=None) -> None:
     """grad: like logits (or the logits themselves); tokens and d_logprob
     [..., n_tok] or None; d_lse and d_entropy one value a row or None."""
-    import torch
-    rows, ws, keep = _rows_in(logits, 0, workspace)
+    rows, ws, ws_bytes, keep = _rows_in(logits, 0, workspace)
     n = rows[2]
-    J = _per_row(tokens, n, torch.int32, "tokens")
-    if _per_row(d_logprob, n, torch.float32, "d_logprob") != J:
+    J, p_tok = _list(tokens, n, _I32, "tokens")
+    J2, p_d = _list(d_logprob, n, _F32, "d_logprob")
+    if J != J2:
         raise ValueError("d_logprob must hold one value per token")
     if grad is None:
         raise ValueError("grad is required")
-    _check(LIB.tb_token_logprobs_grad(*rows, temperature, tokens.data_ptr() if J else None, J,
-                                      d_logprob.data_ptr() if J else None,
-                                      _one_per_row(d_lse, n, "d_lse"),
-                                      _one_per_row(d_entropy, n, "d_entropy"),
-                                      *_grad_args(grad, logits), *ws, _stream(stream)))
+    _check(LIB.tb_token_logprobs_grad(*rows, temperature, p_tok, J, p_d, _one(d_lse, n, "d_lse"),
+                                      _one(d_entropy, n, "d_entropy"),
+                                      *_grad_args(grad, logits), ws, ws_bytes, _stream(stream)))
 
 
 def tb_distill(logits, teacher_tok, teacher_score, out_loss=None, grad=None, weight=None,
@@ -689,18 +699,17 @@ def tb_distill(logits, teacher_tok, teacher_score, out_loss=None, grad=None, wei
                stream=None) -> None:
     """teacher_tok and teacher_score: [..., n_teacher]; weight and out_loss one
     value a row or None; grad: like logits (or the logits themselves) or None."""
-    import torch
-    rows, ws, keep = _rows_in(logits, 0, workspace)
+    rows, ws, ws_bytes, keep = _rows_in(logits, 0, workspace)
     n = rows[2]
     if teacher_tok is None or teacher_score is None:
         raise ValueError("teacher_tok and teacher_score are required")
-    K = _per_row(teacher_tok, n, torch.int32, "teacher_tok")
-    if _per_row(teacher_score, n, torch.float32, "teacher_score") != K:
+    K, p_tok = _list(teacher_tok, n, _I32, "teacher_tok")
+    K2, p_score = _list(teacher_score, n, _F32, "teacher_score")
+    if K != K2:
         raise ValueError("teacher_score must hold one value per teacher token")
-    _check(LIB.tb_distill(*rows, temperature, teacher_tok.data_ptr(), teacher_score.data_ptr(), K,
-                          1 if tail else 0, _one_per_row(weight, n, "weight"),
-                          _one_per_row(out_loss, n, "out_loss"), *_grad_args(grad, logits), *ws,
-                          _stream(stream)))
+    _check(LIB.tb_distill(*rows, temperature, p_tok, p_score, K, 1 if tail else 0,
+                          _one(weight, n, "weight"), _one(out_loss, n, "out_loss"),
+                          *_grad_args(grad, logits), ws, ws_bytes, _stream(stream)))
 
 
 def tb_reset_stream(arena: Arena, b: int, new_model_id: int, K: int, model_ids, states,

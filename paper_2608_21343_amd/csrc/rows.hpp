@@ -479,7 +479,7 @@ inline void with_shape(int i, F f) {
   }
 }
 
-// Launches of whole rows, in ranges that one launch may hold; f(first row, grid).
+// Launches over all rows, in ranges that one launch may hold; f(first row, grid).
 template <class F>
 inline void in_launches(int64_t n_rows, int rows_per_group, int threads, int32_t n_seg, F f) {
   const int64_t most = most_groups(threads) / n_seg * rows_per_group;

@@ -302,9 +302,8 @@ __global__ __launch_bounds__(kThreads) void distill_loss_kernel(Rows a, DistillI
 
 // ---- launches
 
-template <class LT, class IO, class F>
-hipError_t grads_t(const Rows& a0, const Plan& p, F launch) {
-  Rows a = a0;
+template <class LT, class F>
+hipError_t in_shape(Rows a, const Plan& p, F launch) {
   with_shape<LT>(p.shape, [&](auto nwr, auto np) {
     constexpr int NWR = decltype(nwr)::value;
     typedef Place<NWR> Pl;
@@ -317,10 +316,10 @@ hipError_t grads_t(const Rows& a0, const Plan& p, F launch) {
 }
 
 template <class LT>
-hipError_t grad_t(const Rows& a0, const GradIO& io, const Plan& p, hipStream_t st) {
-  auto pass = [&](auto pass_) {
+hipError_t grad_t(const Rows& all, const GradIO& io, const Plan& p, hipStream_t st) {
+  auto pass = [&](const Rows& rows, auto pass_) {
     constexpr Pass PASS = (Pass) decltype(pass_)::value;
-    return grads_t<LT, GradIO>(a0, p, [&](const Rows& a, dim3 grid, dim3 wg, auto nwr, auto np) {
+    return in_shape<LT>(rows, p, [&](const Rows& a, dim3 grid, dim3 wg, auto nwr, auto np) {
       constexpr int NWR = decltype(nwr)::value, NP = decltype(np)::value;
       if constexpr (PASS == kWhole || cuts(Shape{NWR, NP})) {
         if (io.d_entropy)
@@ -330,38 +329,36 @@ hipError_t grad_t(const Rows& a0, const GradIO& io, const Plan& p, hipStream_t s
       }
     });
   };
-  if (p.n_seg == 1) return pass(Int<kWhole>());
-  const hipError_t e = pass(Int<kStats>());
-  return e == hipSuccess ? pass(Int<kApply>()) : e;
+  if (p.n_seg == 1) return pass(all, Int<kWhole>());
+  const hipError_t e = pass(all, Int<kStats>());
+  return e == hipSuccess ? pass(all, Int<kApply>()) : e;
 }
 
 template <class LT>
-hipError_t distill_t(const Rows& a0, const DistillIO& io, const Plan& p, hipStream_t st) {
-  auto pass = [&](auto pass_) {
+hipError_t distill_t(const Rows& all, const DistillIO& io, const Plan& p, hipStream_t st) {
+  auto pass = [&](const Rows& rows, auto pass_) {
     constexpr Pass PASS = (Pass) decltype(pass_)::value;
-    return grads_t<LT, DistillIO>(
-        a0, p, [&](const Rows& a, dim3 grid, dim3 wg, auto nwr, auto np) {
-          constexpr int NWR = decltype(nwr)::value, NP = decltype(np)::value;
-          if constexpr (PASS == kWhole || cuts(Shape{NWR, NP})) {
-            if (io.tail)
-              distill_kernel<LT, NWR, NP, true, PASS><<<grid, wg, 0, st>>>(a, io);
-            else
-              distill_kernel<LT, NWR, NP, false, PASS><<<grid, wg, 0, st>>>(a, io);
-          }
-        });
+    return in_shape<LT>(rows, p, [&](const Rows& a, dim3 grid, dim3 wg, auto nwr, auto np) {
+      constexpr int NWR = decltype(nwr)::value, NP = decltype(np)::value;
+      if constexpr (PASS == kWhole || cuts(Shape{NWR, NP})) {
+        if (io.tail)
+          distill_kernel<LT, NWR, NP, true, PASS><<<grid, wg, 0, st>>>(a, io);
+        else
+          distill_kernel<LT, NWR, NP, false, PASS><<<grid, wg, 0, st>>>(a, io);
+      }
+    });
   };
-  if (p.n_seg == 1) return pass(Int<kWhole>());
-  hipError_t e = pass(Int<kStats>());
+  if (p.n_seg == 1) return pass(all, Int<kWhole>());
+  hipError_t e = pass(all, Int<kStats>());
   if (e == hipSuccess && io.loss) {
-    Rows a = a0;
+    Rows a = all;
     in_launches(a.n_rows, kThreads / 64, kThreads, 1, [&](int64_t r, dim3 grid) {
       a.row0 = r;
       distill_loss_kernel<LT><<<grid, kThreads, 0, st>>>(a, io);
     });
     e = hipGetLastError();
   }
-  if (e == hipSuccess && io.grad) e = pass(Int<kApply>());
-  return e;
+  return e == hipSuccess && io.grad ? pass(all, Int<kApply>()) : e;
 }
 
 }  // namespace rows
