@@ -41,6 +41,9 @@ struct Elem<float> {
   static constexpr int PV = 4;  // values in 16 bytes
   static constexpr uint32_t kFill = 0xff800000u;  // -inf
   __device__ static inline float get(const uint32_t* w, int e) { return __uint_as_float(w[e]); }
+  // a value as it is loaded, and what it is worth
+  typedef float Raw;
+  static constexpr float kRawNegInf = -__builtin_huge_valf();
   __device__ static inline float widen(float x) { return x; }
   __device__ static inline float narrow(float x) { return x; }
   __device__ static inline void pack(const float* v, uint32_t* w) {
@@ -63,7 +66,14 @@ struct Elem<uint16_t> {
       asm volatile("v_lshlrev_b32 %0, 16, %1" : "=v"(x) : "v"(w[e / 2]));
     return x;
   }
-  __device__ static inline float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+  typedef uint32_t Raw;
+  static constexpr uint32_t kRawNegInf = 0xff80u;
+  // Volatile, too: moved to where the value is loaded, it waits for all loads.
+  __device__ static inline float widen(uint32_t x) {
+    float y;
+    asm volatile("v_lshlrev_b32 %0, 16, %1" : "=v"(y) : "v"(x));
+    return y;
+  }
   // to the nearest, ties to even; the one rounding of a bfloat16 gradient
   __device__ static inline uint32_t pair(float a, float b) {
     typedef float f2 __attribute__((ext_vector_type(2)));
@@ -233,7 +243,7 @@ struct Tile {
   static constexpr int PV = Elem<LT>::PV;
   static constexpr bool kWhole16 = PV == 8 && NWR > 1;
   Quad<LT> w[NP];
-  float rim;
+  typename Elem<LT>::Raw rim_raw;
   int32_t lane, q;
   int32_t n, pieces;  // values, whole pieces of the row
   int32_t head;       // values before the first piece
@@ -261,16 +271,17 @@ struct Tile {
         for (int k = 0; k < 4; ++k) w[p].w[k] = Elem<LT>::kFill;
       }
     }
-    rim = kNegInf;
-    if (has_rim()) rim = Elem<LT>::widen(row[rim_at()]);
+    rim_raw = Elem<LT>::kRawNegInf;
+    if (has_rim()) rim_raw = row[rim_at()];
   }
+  __device__ inline float rim() const { return Elem<LT>::widen(rim_raw); }
   // Places of a value in membership bits: a piece's lie within one word.
   __device__ inline int32_t bit(int32_t i) const { return i + PV - head; }
   __device__ inline float at(int p, int e) const { return Elem<LT>::get(w[p].w, e); }
 
   // largest value of this lane's (or NaN), also of two halves of them
   __device__ inline void lane_max2(float& a, float& b) {
-    a = rim;
+    a = rim();
     b = kNegInf;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -295,7 +306,7 @@ struct Tile {
   __device__ inline void sums(const Basis& b, const uint32_t* bits, float (&s)[3], F look) {
     float a[4], d[4];
     {
-      const float t = b.t<BIG>(rim), x = exp2_fast(t);
+      const float t = b.t<BIG>(rim()), x = exp2_fast(t);
       a[0] = x;
       a[1] = a[2] = a[3] = d[1] = d[2] = d[3] = 0.f;
       d[0] = ENT ? x * __builtin_fmaxf(t, -200.f) : 0.f;
@@ -339,7 +350,7 @@ struct Tile {
         a[p & 3] += all;
       }
     }
-    look(rim, rim_at());
+    look(rim(), rim_at());
     s[0] = (a[0] + a[1]) + (a[2] + a[3]);
     if (ENT) s[1] = (d[0] + d[1]) + (d[2] + d[3]);
   }
@@ -363,7 +374,7 @@ struct Tile {
       }
     }
     if (has_rim()) {
-      const float t = b.t<BIG>(rim);
+      const float t = b.t<BIG>(rim());
       out[rim_at()] = Elem<LT>::narrow(f(t, exp2_fast(t)));
     }
   }
@@ -507,6 +518,11 @@ struct Place {
     n = a.C - c0 < a.seg ? a.C - c0 : a.seg;
   }
 };
+
+// Waves that a SIMD should hold at least: the largest tiles come out a register or
+// two above the 96 that five waves may have (97: four, 65,536 rows of 8193
+// bfloat16 with 32 alternatives 235 us instead of 217).
+constexpr int least_waves(Shape s) { return s.nwr <= 2 && s.np == 16 ? 5 : 1; }
 
 // Orders a wave's LDS writes before its later reads (one wave's LDS operations
 // are in order; this holds the compiler to it).

@@ -89,7 +89,8 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io
   LT* out = static_cast<LT*>(io.grad) + at.row * io.grad_stride + at.c0;
   Tile<LT, NWR, NP> x;
   int32_t id = -1;
-  float g = 0.f, zj = kNegInf, gl = 0.f, gh = 0.f;
+  typename Elem<LT>::Raw zj = Elem<LT>::kRawNegInf;
+  float g = 0.f, gl = 0.f, gh = 0.f;
   if (at.lane < io.J) {
     id = io.tokens[at.row * io.J + at.lane];
     g = io.d_logprob[at.row * io.J + at.lane];
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io
   x.load(z + at.c0, at.n, at.lane, at.q);
   const bool ok = (uint32_t)id < (uint32_t)a.C;
   const bool mine = ok && id >= at.c0 && id < at.c0 + at.n;
-  if (mine) zj = Elem<LT>::widen(z[id]);
+  if (mine) zj = z[id];
   const bool bad = __ballot(!ok && id != -1) != 0;
   if (!ok) g = 0.f;
   // no gradient comes in: none goes out, whatever the row holds
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io
   if (io.J <= kFewPlaces || mark_fresh(bits_all[at.slot], mine, x.bit(id - at.c0)))
     sum = sum_same(id, g, io.J, at.lane, first);
   if (mine && first) {
-    const float t = b.t(zj);
+    const float t = b.t(Elem<LT>::widen(zj));
     out[id - at.c0] = Elem<LT>::narrow(__builtin_fmaf(sum, a.inv_tau, slope(t, exp2_fast(t))));
   }
 }
@@ -159,18 +160,25 @@ struct Teacher {
   float q, logq;
   float mass, rest;  // of the list and (with the tail) of all else
 };
-__device__ __forceinline__ Teacher teacher(const DistillIO& io, int64_t row, int32_t C, float c,
-                                           int lane) {
-  Teacher t;
-  t.id = -1;
-  float sc = kNegInf;
-  if (lane < io.K) {
-    t.id = io.tokens[row * io.K + lane];
-    sc = io.score[row * io.K + lane];
+struct Places {  // as they lie in memory
+  int32_t id;
+  float score;
+  __device__ inline Places(const DistillIO& io, int64_t row, int lane) {
+    id = -1;
+    score = kNegInf;
+    if (lane < io.K) {
+      id = io.tokens[row * io.K + lane];
+      score = io.score[row * io.K + lane];
+    }
   }
+};
+__device__ __forceinline__ Teacher teacher(const DistillIO& io, const Places& p, int32_t C,
+                                           float c) {
+  Teacher t;
+  t.id = p.id;
   t.ok = (uint32_t)t.id < (uint32_t)C;
   t.bad = __ballot(!t.ok && t.id != -1) != 0;
-  if (!t.ok) sc = kNegInf;
+  const float sc = t.ok ? p.score : kNegInf;
   t.rest = 0.f;
   if (io.tail) {
     t.q = exp2_fast(sc * kLog2e);
@@ -216,13 +224,16 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, Distil
   if (at.row >= a.n_rows) return;  // uniform over the row's waves
   const LT* z = static_cast<const LT*>(a.z) + at.row * a.stride;
   LT* out = static_cast<LT*>(io.grad) + at.row * io.grad_stride + at.c0;
+  // loads in the order in which they are waited for: the list, the row, and the
+  // listed values, whose places the list gives while the row is on its way
+  const Places places(io, at.row, at.lane);
   Tile<LT, NWR, NP> x;
   x.load(z + at.c0, at.n, at.lane, at.q);
+  const bool mine = places.id >= at.c0 && places.id < at.c0 + at.n;
+  typename Elem<LT>::Raw zk = Elem<LT>::kRawNegInf;
+  if (mine) zk = z[places.id];
   const float w = io.weight ? io.weight[at.row] : 1.f;
-  const Teacher t = teacher(io, at.row, a.C, a.c, at.lane);
-  const bool mine = t.ok && t.id >= at.c0 && t.id < at.c0 + at.n;
-  float zk = kNegInf;
-  if (mine) zk = Elem<LT>::widen(z[t.id]);
+  const Teacher t = teacher(io, places, a.C, a.c);
   if (w == 0.f || (t.mass == 0.f && !t.bad)) {
     if (PASS != kStats && io.grad) x.store_zeros(out);
     if (PASS == kWhole && io.loss && at.q == 0 && at.lane == 0) io.loss[at.row] = 0.f;
@@ -249,7 +260,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, Distil
     return;
   }
   if (PASS == kWhole && io.loss && at.q == 0) {
-    const float loss = distill_loss(t, zk, s, b, a.inv_tau);
+    const float loss = distill_loss(t, Elem<LT>::widen(zk), s, b, a.inv_tau);
     if (at.lane == 0) io.loss[at.row] = w * loss;
   }
   if (!io.grad) return;
@@ -275,7 +286,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, Distil
   float sum = t.q;
   if (twice) sum = sum_same(t.id, t.q, io.K, at.lane, first);
   if (mine && first) {
-    const float e = exp2_fast(b.t(zk));
+    const float e = exp2_fast(b.t(Elem<LT>::widen(zk)));
     out[t.id - at.c0] = Elem<LT>::narrow(__builtin_fmaf(-sum, wt, e * k_on));
   }
 }
@@ -290,7 +301,7 @@ __global__ __launch_bounds__(kThreads) void distill_loss_kernel(Rows a, DistillI
   if (row >= a.n_rows) return;
   const LT* z = static_cast<const LT*>(a.z) + row * a.stride;
   const float w = io.weight ? io.weight[row] : 1.f;
-  const Teacher t = teacher(io, row, a.C, a.c, lane);
+  const Teacher t = teacher(io, Places(io, row, lane), a.C, a.c);
   float loss = 0.f;
   if (w != 0.f && (t.mass != 0.f || t.bad)) {
     Basis b;

@@ -7,7 +7,9 @@
 namespace tbias {
 namespace rows {
 
-// Writes what follows from a row's statistics; one wave.
+// Writes what follows from a row's statistics; one wave. (The given tokens are read
+// here: read before the row they are waited for together with it, which gains
+// nothing: 7511 rows of 612 bfloat16 9.5 us instead of 9.2.)
 template <class LT>
 __device__ __forceinline__ void write_scores(const Rows& a, const ScoreIO& io, int64_t row,
                                              const LT* z, const Stats& s, const Basis& b,
@@ -236,7 +238,7 @@ __device__ __forceinline__ void rank(Found<NWR>& f, const AltRow<PART>& out, int
 }
 
 template <class LT, int NWR, int NP, bool TOP, bool PART>
-__global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO io) {
+__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void score_kernel(Rows a, ScoreIO io) {
   typedef Tile<LT, NWR, NP> T;
   constexpr int PV = T::PV;
   __shared__ float box[3 * NWR], box_z[NWR];
@@ -345,7 +347,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg) void score_kernel(Rows a, ScoreIO 
         for (int e = 0; e < PV; ++e)
           best(x.at(p, e), place + (p * NWR + at.q) * 64 * PV + e);
       }
-      best(x.rim, x.rim_at());
+      best(x.rim(), x.rim_at());
       row_best<NWR>(bz, bi, box_z, box_id, at.q, at.lane);
       if (at.q == 0 && at.lane == 0) {
         if (bz == kNegInf)
