@@ -348,6 +348,7 @@ struct Tile {
         }
         s[2] += r;
         a[p & 3] += all;
+        asm volatile("" : "+v"(s[2]), "+v"(a[p & 3]));
       }
     }
     look(rim(), rim_at());
@@ -519,10 +520,14 @@ struct Place {
   }
 };
 
-// Waves that a SIMD should hold at least: the largest tiles come out a register or
-// two above the 96 that five waves may have (97: four, 65,536 rows of 8193
-// bfloat16 with 32 alternatives 235 us instead of 217).
-constexpr int least_waves(Shape s) { return s.nwr <= 2 && s.np == 16 ? 5 : 1; }
+// Waves that a SIMD should hold at least: the largest tiles come out a few
+// registers above the 96 that five waves may have (97: four, 65,536 rows of 8193
+// bfloat16 with 32 alternatives 235 us instead of 217), tiles of eight pieces
+// above the 64 with which two workgroups of sixteen waves fit a CU (4096 rows of
+// 65,537 bfloat16, distillation with the tail and its gradient: X us).
+constexpr int least_waves(Shape s) {
+  return s.nwr == 16 ? (s.np == 8 ? 8 : 4) : s.np == 16 ? 5 : 1;
+}
 
 // Orders a wave's LDS writes before its later reads (one wave's LDS operations
 // are in order; this holds the compiler to it).

@@ -78,7 +78,7 @@ enum Pass { kWhole, kStats, kApply };
 // ---- gradient of log probabilities, log-sum-exp and entropy
 
 template <class LT, int NWR, int NP, bool ENT, Pass PASS>
-__global__ __launch_bounds__(Place<NWR>::kWg) void grad_kernel(Rows a, GradIO io) {
+__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void grad_kernel(Rows a, GradIO io) {
   __shared__ float box[3 * NWR];
   __shared__ uint32_t bits_all[Place<NWR>::kRows][list_words<LT, NWR, NP>()];
   lds_poison(box, sizeof(box));
@@ -214,7 +214,7 @@ __device__ __forceinline__ float distill_loss(const Teacher& t, float zk, const 
 }
 
 template <class LT, int NWR, int NP, bool TAIL, Pass PASS>
-__global__ __launch_bounds__(Place<NWR>::kWg) void distill_kernel(Rows a, DistillIO io) {
+__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void distill_kernel(Rows a, DistillIO io) {
   constexpr int kWords = list_words<LT, NWR, NP>();
   __shared__ float box[3 * NWR];
   __shared__ uint32_t bits_all[Place<NWR>::kRows][kWords];
