@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import sys
 from pathlib import Path
 from typing import Optional, Sequence, Tuple
 
@@ -196,7 +197,7 @@ def _fits(t, n: int, dtype, exact: bool = False) -> bool:
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream.cuda_stream
-    import torch
+    torch = sys.modules["torch"]  # (_load has imported it)
     # the handle of torch.cuda.current_stream() without making its object
     if torch.cuda.is_initialized():
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
@@ -570,6 +571,9 @@ def _rows(x, name: str = "logits"):
     if strides[-1] != 1:
         raise ValueError(f"{name} rows must be contiguous")
     rows, step = 1, 0
+    if n == 2 and shape[0] > 1:
+        rows, step = shape[0], strides[0]
+        n = 0
     for d in range(n - 2, -1, -1):
         size = shape[d]
         if size == 1:
