@@ -523,7 +523,7 @@ int tb_unregister_model_noalloc(tb_registry* r, int32_t id, void* hip_stream);
  *   workspace     device, 16-byte aligned, tb_rows_workspace_bytes(...) bytes
  *                 (TB_ENOMEM when smaller); that is 0, and workspace may be
  *                 NULL, unless rows are cut into segments (never rows of up
- *                 to 32768 values). It is free again once the stream has passed
+ *                 to 16384 values). It is free again once the stream has passed
  *                 the call.
  *
  * A list holds up to TB_MAX_LIST token ids per row, -1 for an unused place (at

@@ -559,7 +559,7 @@ def tb_boost_step_beam_stream(arena: Arena, logits, model_ids, states, scores, h
 # row operators
 
 # rows of up to this many values are never cut into segments (tbias.h)
-_WHOLE_ROW = 1 << 15
+_WHOLE_ROW = 1 << 14
 
 
 def _rows(x, name: str = "logits"):

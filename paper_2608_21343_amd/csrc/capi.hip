@@ -1,4 +1,5 @@
 // C ABI shim: synchronous argument checks, then asynchronous launches.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -303,9 +304,9 @@ int check_apart(const RowBuf (&b)[N], int n_out) {
 
 // The rows and their plan; workspace for rows in segments.
 int make_rows(const void* logits, int32_t dtype, int64_t n_rows, int32_t V1, int64_t row_stride,
-              float temperature, int32_t n_alt, void* workspace, int64_t workspace_bytes,
-              rows::Rows* a, rows::Plan* p) {
-  *p = rows::plan(dtype, n_rows, V1);
+              float temperature, bool grad, int32_t n_alt, void* workspace,
+              int64_t workspace_bytes, rows::Rows* a, rows::Plan* p) {
+  *p = rows::plan(dtype, n_rows, V1, grad);
   const int64_t need = rows::workspace_bytes(*p, n_rows, n_alt);
   if (need > 0) {
     if (!workspace || workspace_bytes < need)
@@ -329,7 +330,9 @@ extern "C" int64_t tb_rows_workspace_bytes(int32_t dtype, int64_t n_rows, int32_
     fail(TB_EINVAL, "bad dtype, n_rows, v_plus_blank or n_alt");
     return -1;
   }
-  return rows::workspace_bytes(rows::plan(dtype, n_rows, v_plus_blank), n_rows, n_alt);
+  return std::max(
+      rows::workspace_bytes(rows::plan(dtype, n_rows, v_plus_blank, false), n_rows, n_alt),
+      rows::workspace_bytes(rows::plan(dtype, n_rows, v_plus_blank, true), n_rows, 0));
 }
 
 extern "C" int tb_token_logprobs(const void* logits, int32_t dtype, int64_t n_rows,
@@ -352,7 +355,7 @@ extern "C" int tb_token_logprobs(const void* logits, int32_t dtype, int64_t n_ro
   if (n_alt > 0 && (r = check_i32(out_alt_logprob, "out_alt_logprob"))) return r;
   rows::Rows a;
   rows::Plan p;
-  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, n_alt,
+  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, false, n_alt,
                      workspace, workspace_bytes, &a, &p)))
     return r;
   const int64_t part = rows::workspace_bytes(p, n_rows, 0);
@@ -394,7 +397,7 @@ extern "C" int tb_token_logprobs_grad(const void* logits, int32_t dtype, int64_t
   if ((r = check_grad(grad, dtype, n_rows, grad_stride, v_plus_blank))) return r;
   rows::Rows a;
   rows::Plan p;
-  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, 0, workspace,
+  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, true, 0, workspace,
                      workspace_bytes, &a, &p)))
     return r;
   const bool in_place = grad == logits && grad_stride == row_stride;
@@ -434,7 +437,7 @@ extern "C" int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int
   if (grad && (r = check_grad(grad, dtype, n_rows, grad_stride, v_plus_blank))) return r;
   rows::Rows a;
   rows::Plan p;
-  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, 0, workspace,
+  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, grad != nullptr, 0, workspace,
                      workspace_bytes, &a, &p)))
     return r;
   const bool in_place = grad == logits && grad_stride == row_stride;

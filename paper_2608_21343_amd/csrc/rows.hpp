@@ -235,9 +235,9 @@ __device__ __forceinline__ void row_sum(float (&v)[3], float* box, int q) {
 // A row of one wave starts with its first piece wherever it lies in memory, so
 // that its results depend on its values alone. In longer rows of bfloat16 the
 // pieces lie on whole 16 bytes and up to PV - 1 values come before them: sums
-// then differ in their last bits from place to place, but 2048 rows of 131,073
-// take 243 us instead of 308 (distillation with its gradient) and 136 instead
-// of 167 (log-sum-exp). Float32 rows gain nothing (65,537 values: 139 and 130).
+// then differ in their last bits from place to place, but a distillation with its
+// gradient of 2048 rows of 131,073 takes 243 us instead of 308. Float32 rows gain
+// nothing (2048 of 65,537 values, 16 alternatives: 139 and 130).
 template <class LT, int NWR, int NP>
 struct Tile {
   static constexpr int PV = Elem<LT>::PV;
@@ -250,6 +250,23 @@ struct Tile {
 
   __device__ inline int32_t piece(int p) const { return (p * NWR + q) * 64 + lane; }
   __device__ inline bool has(int p) const { return piece(p) < pieces; }
+  // Passes over the pieces, f(p): of large tiles a row may need little more than
+  // half, so the second half is taken by groups that are skipped where the row has
+  // ended (4096 rows of 33,000 bfloat16 in segments of (4, 16): 78 us, 54 without the
+  // unused pieces). Tested piece by piece, full tiles lose more: 65,536 rows of
+  // 8193 with 32 alternatives 226 us instead of 217.
+  template <class F>
+  __device__ inline void each(F f) const {
+    constexpr int H = NP >= 8 ? NP / 2 : NP, G = NP >= 8 ? NP / 4 : 1;
+#pragma unroll
+    for (int p = 0; p < H; ++p) f(p);
+#pragma unroll
+    for (int g = H; g < NP; g += G) {
+      if ((g * NWR + q) * 64 >= pieces) continue;  // uniform
+#pragma unroll
+      for (int p = g; p < g + G; ++p) f(p);
+    }
+  }
   __device__ inline int32_t first(int p) const { return head + piece(p) * PV; }
   __device__ inline int32_t rim_at() const { return lane < head ? lane : pieces * PV + lane; }
   __device__ inline bool has_rim() const { return q == 0 && lane < n - pieces * PV; }
@@ -283,14 +300,13 @@ struct Tile {
   __device__ inline void lane_max2(float& a, float& b) {
     a = rim();
     b = kNegInf;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
+    each([&](int p) {
 #pragma unroll
       for (int e = 0; e < PV; e += 4) {
         a = max3(a, at(p, e), at(p, e + 1));
         b = max3(b, at(p, e + 2), at(p, e + 3));
       }
-    }
+    });
   }
   __device__ inline float lane_max() {
     float a, b;
@@ -315,8 +331,7 @@ struct Tile {
         s[2] = has_rim() && ((bits[i >> 5] >> (i & 31)) & 1) ? 0.f : x;
       }
     }
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
+    each([&](int p) {
       float v[PV], x[PV];
 #pragma unroll
       for (int e = 0; e < PV; ++e) {
@@ -350,7 +365,7 @@ struct Tile {
         a[p & 3] += all;
         asm volatile("" : "+v"(s[2]), "+v"(a[p & 3]));
       }
-    }
+    });
     look(rim(), rim_at());
     s[0] = (a[0] + a[1]) + (a[2] + a[3]);
     if (ENT) s[1] = (d[0] + d[1]) + (d[2] + d[3]);
@@ -359,8 +374,7 @@ struct Tile {
   // Writes f(t, 2^t) in place of every value.
   template <bool BIG, class F>
   __device__ inline void store(LT* out, const Basis& b, F f) {
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
+    each([&](int p) {
       float v[PV];
 #pragma unroll
       for (int e = 0; e < PV; ++e) {
@@ -373,7 +387,7 @@ struct Tile {
       if (has(p)) {
         *reinterpret_cast<Quad<LT>*>(out + first(p)) = o;
       }
-    }
+    });
     if (has_rim()) {
       const float t = b.t<BIG>(rim());
       out[rim_at()] = Elem<LT>::narrow(f(t, exp2_fast(t)));
@@ -462,14 +476,14 @@ constexpr int kShapes = 13;
 constexpr Shape kShape[kShapes] = {{1, 1}, {1, 2}, {1, 4}, {1, 8}, {1, 16}, {2, 16}, {4, 2},
                                    {4, 4}, {4, 8}, {4, 16}, {16, 4}, {16, 8}, {16, 16}};
 // Shapes that the segments of cut rows take.
-constexpr bool cuts(Shape s) { return s.nwr >= 4 && s.np == 8; }
+constexpr bool cuts(Shape s) { return s.nwr == 4 && s.np >= 8; }
 
 struct Plan {
   int shape;       // instance of the (whole or cut) rows
   int32_t n_seg;   // segments of a row
   int32_t seg;     // values of a segment
 };
-Plan plan(int32_t dtype, int64_t n_rows, int32_t C);
+Plan plan(int32_t dtype, int64_t n_rows, int32_t C, bool grad);
 
 // The segments' statistics, then their alternatives.
 inline int64_t workspace_bytes(const Plan& p, int64_t n_rows, int32_t n_alt) {
@@ -524,7 +538,8 @@ struct Place {
 // registers above the 96 that five waves may have (97: four, 65,536 rows of 8193
 // bfloat16 with 32 alternatives 235 us instead of 217), tiles of eight pieces
 // above the 64 with which two workgroups of sixteen waves fit a CU (4096 rows of
-// 65,537 bfloat16, distillation with the tail and its gradient: X us).
+// 65,537 bfloat16, distillation with the tail and its gradient, 219 us instead of
+// 240).
 constexpr int least_waves(Shape s) {
   return s.nwr == 16 ? (s.np == 8 ? 8 : 4) : s.np == 16 ? 5 : 1;
 }
