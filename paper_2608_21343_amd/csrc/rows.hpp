@@ -250,14 +250,15 @@ struct Tile {
 
   __device__ inline int32_t piece(int p) const { return (p * NWR + q) * 64 + lane; }
   __device__ inline bool has(int p) const { return piece(p) < pieces; }
-  // Passes over the pieces, f(p): of large tiles a row may need little more than
-  // half, so the second half is taken by groups that are skipped where the row has
-  // ended (4096 rows of 33,000 bfloat16 in segments of (4, 16): 78 us, 54 without the
-  // unused pieces). Tested piece by piece, full tiles lose more: 65,536 rows of
-  // 8193 with 32 alternatives 226 us instead of 217.
+  // Passes over the pieces, f(p): of tiles of four and more a row may need little
+  // more than half, so the second half is taken by groups that are skipped where the
+  // row has ended (131,072 rows of 1082 bfloat16 78 us, 70 without the unused pieces;
+  // 4096 of 33,000 in segments of (4, 16) 78 and 54). Tested piece by piece
+  // throughout, full tiles lose: 65,536 rows of 8193 with 32 alternatives 226 us
+  // instead of 211.
   template <class F>
   __device__ inline void each(F f) const {
-    constexpr int H = NP >= 8 ? NP / 2 : NP, G = NP >= 8 ? NP / 4 : 1;
+    constexpr int H = NP >= 4 ? NP / 2 : NP, G = NP >= 4 ? NP / 4 : 1;
 #pragma unroll
     for (int p = 0; p < H; ++p) f(p);
 #pragma unroll
