@@ -362,47 +362,68 @@ __global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void 
 }
 
 // Joins the segments of a row: one workgroup of one wave per row, the segments'
-// lists in its LDS (8 rows of 131,073 float32 with 64 alternatives 24.7 us,
-// 30.6 with the heads read from memory one by one).
+// lists in its LDS. The best of them are found as those of a row are: the first
+// J places of the n_seg lists hold at least M values, whose M-th best bounds the
+// row's. (Merged place by place, each place waits for the last: 8 rows of 131,073
+// float32 with 64 alternatives 24.7 us; so 18.4.)
 template <class LT>
 __global__ __launch_bounds__(64) void score_join_kernel(Rows a, ScoreIO io) {
   extern __shared__ int2 lists[];  // [n_seg, M]
+  __shared__ Found<1> found;
   lds_poison(lists, sizeof(int2) * a.n_seg * io.M);
+  lds_poison(&found, sizeof(found));
   const int lane = __lane_id();
   const int64_t row = a.row0 + blockIdx.x;
   if (row >= a.n_rows) return;
   const LT* z = static_cast<const LT*>(a.z) + row * a.stride;
-  const int2* all = io.lists + row * a.n_seg * io.M;
-  for (int i = lane; i < a.n_seg * io.M; i += 64) lists[i] = all[i];
+  const int M = io.M, n = a.n_seg * M;
+  const int2* all = io.lists + row * n;
+  for (int i = lane; i < n; i += 64) lists[i] = all[i];
   Basis b;
   const Stats s = join(a.part + row * a.n_seg, a.n_seg, a.c, lane, b);
   const float log_s = log_sum(s, b);
   write_scores(a, io, row, z, s, b, log_s, lane);
-  if (io.M == 0) return;
+  if (M == 0) return;
+  wave_fence();
+  // place i of list k is value i * n_seg + k of the first J places
+  const int J = M < 128 / a.n_seg ? M : 128 / a.n_seg, G = J * a.n_seg;
+  auto value = [&](int e) {
+    return e < G ? __int_as_float(lists[e % a.n_seg * M + e / a.n_seg].x) : kNegInf;
+  };
+  const float g0 = value(lane), g1 = value(64 + lane);
+  float bound = reached_by(g0, g1, true, M, wave_most(__builtin_fmaxf(g0, g1)));
+  if (bound == kNegInf) bound = -__FLT_MAX__;  // only tokens above -inf
+  int32_t count = 0;
+  for (int base = 0; base < n; base += 64) {
+    const int2 c = base + lane < n ? lists[base + lane] : make_int2(__float_as_int(kNegInf), -1);
+    const bool in = __int_as_float(c.x) >= bound;
+    const uint64_t hit = __ballot(in);
+    const int32_t more = count + __builtin_popcountll(hit);
+    if (more <= Found<1>::kCap && in)
+      found.at[0][__builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32),
+                                            __builtin_amdgcn_mbcnt_lo((uint32_t)hit, count))] = c;
+    count = more;
+  }
+  if (lane == 0) found.n[0] = count;
   wave_fence();
   const AltRow<false> out(a, io, row, b, log_s);
-  // merge: every lane holds the best that its segment's list has left
+  if (count <= Found<1>::kCap) {
+    rank<LT, 1, false>(found, out, M, 0, a.C, lane);
+    return;
+  }
+  // too many equal values: every lane holds the best that its list has left
   const int2 end = make_int2(__float_as_int(kNegInf), -1);
-  const int2* head = lists + lane * io.M;
-  const int2* last = head + io.M;
+  const int2* head = lists + lane * M;
+  const int2* last = head + M;
   int2 best = lane < a.n_seg ? *head : end;
-  int i = 0;
-  for (; i < io.M; ++i) {
+  for (int i = 0; i < M; ++i) {  // (there are more than M)
     const float v = __int_as_float(best.x), top = wave_most(v);
-    if (top == kNegInf) break;  // nothing left
-    const uint64_t hit = __ballot(v == top);
-    int own = (int)__builtin_ctzll(hit);
-    int32_t id = __builtin_amdgcn_readlane(best.y, own);
-    if (hit & (hit - 1)) {  // equal values: the lowest token
-      id = wave_min_i32_dpp(v == top ? best.y : INT_MAX);
-      own = (int)__builtin_ctzll(__ballot(v == top && best.y == id));
-    }
-    if (lane == own) {
+    const int32_t id = wave_min_i32_dpp(v == top ? best.y : INT_MAX);
+    if (v == top && best.y == id) {
       out.write(i, top, id);
       best = ++head < last ? *head : end;
     }
   }
-  if (lane >= i && lane < io.M) out.none(lane);
 }
 
 template <class LT>
