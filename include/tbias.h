@@ -537,7 +537,9 @@ int tb_unregister_model_noalloc(tb_registry* r, int32_t id, void* hip_stream);
  * log probabilities -inf, entropy 0, no alternatives, a loss of +inf where the
  * teacher has any mass, gradients 0. A row that holds a NaN or +inf has NaN
  * lse, log probabilities, entropy, loss and gradients. Sums are float32
- * relative to the row's maximum; gradients are rounded once to dtype.
+ * relative to the row's maximum; gradients are rounded once to dtype. Rows of up
+ * to 4096 (TB_F32) or 8192 (TB_BF16) values give the same bits wherever they lie
+ * and whatever else the call holds; longer ones may differ in their last bits.
  */
 enum { TB_MAX_LIST = 64, TB_MAX_ROW = 1 << 20 };
 

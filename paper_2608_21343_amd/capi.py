@@ -617,10 +617,10 @@ def _one(t, rows: int, name: str) -> Optional[int]:
     return t.data_ptr()
 
 
-def _rows_in(logits, n_alt: int, workspace):
+def _rows_in(logits, n_alt: int, workspace, stream):
     """(arguments of the rows, workspace pointer, workspace bytes, device
     workspace) of a call. A workspace that the call needs and the caller did not
-    pass is allocated on the current stream."""
+    pass is allocated on the call's stream, whose later work alone may reuse it."""
     n, V1, rs = _rows(logits)
     if logits.dtype == _F32:
         dt = TB_F32
@@ -633,7 +633,8 @@ def _rows_in(logits, n_alt: int, workspace):
         import torch
         need = LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt)
         if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+            with torch.cuda.stream(stream):  # (None: the current one)
+                workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
     if workspace is None:
         return (ptr, dt, n, V1, rs), None, 0, None
     return ((ptr, dt, n, V1, rs), _dptr(workspace, name="workspace"),
@@ -666,7 +667,7 @@ def tb_token_logprobs(logits, tokens=None, out_logprob=None, out_lse=None, out_e
     out_logprob [..., n_tok]; out_lse and out_entropy one value a row; out_alt
     and out_alt_logprob [..., n_alt]."""
     M = 0 if out_alt is None else out_alt.shape[-1]
-    rows, ws, ws_bytes, keep = _rows_in(logits, M, workspace)
+    rows, ws, ws_bytes, keep = _rows_in(logits, M, workspace, stream)
     n = rows[2]
     J, p_tok = _list(tokens, n, _I32, "tokens")
     J2, p_lp = _list(out_logprob, n, _F32, "out_logprob")
@@ -685,7 +686,7 @@ def tb_token_logprobs_grad(logits, tokens, d_logprob, grad, d_lse=None, d_entrop
                            temperature: float = 1.0, workspace=None, stream=None) -> None:
     """grad: like logits (or the logits themselves); tokens and d_logprob
     [..., n_tok] or None; d_lse and d_entropy one value a row or None."""
-    rows, ws, ws_bytes, keep = _rows_in(logits, 0, workspace)
+    rows, ws, ws_bytes, keep = _rows_in(logits, 0, workspace, stream)
     n = rows[2]
     J, p_tok = _list(tokens, n, _I32, "tokens")
     J2, p_d = _list(d_logprob, n, _F32, "d_logprob")
@@ -703,7 +704,7 @@ def tb_distill(logits, teacher_tok, teacher_score, out_loss=None, grad=None, wei
                stream=None) -> None:
     """teacher_tok and teacher_score: [..., n_teacher]; weight and out_loss one
     value a row or None; grad: like logits (or the logits themselves) or None."""
-    rows, ws, ws_bytes, keep = _rows_in(logits, 0, workspace)
+    rows, ws, ws_bytes, keep = _rows_in(logits, 0, workspace, stream)
     n = rows[2]
     if teacher_tok is None or teacher_score is None:
         raise ValueError("teacher_tok and teacher_score are required")
