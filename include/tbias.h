@@ -606,7 +606,8 @@ int tb_token_logprobs_grad(const void* logits, int32_t dtype, int64_t n_rows,
  *   tail = 1: exp(score): the scores are log probabilities at the temperature
  *             of the call. All other tokens are one event, of probability q_r =
  *             max(0, 1 - sum q) and p_r = the sum of p outside the list;
- *             loss = sum_k q_k (log q_k - log p[token_k]) + q_r (log q_r - log p_r)
+ *             loss = sum_k q_k (log q_k - log p[token_k]) + q_r (log q_r - log p_r);
+ *             a p_r of less than 2^-126 of the row's largest p counts as 0
  *
  *   teacher_tok    device int32[n_rows * n_teacher], teacher_score device float
  *   weight         device float[n_rows], or NULL (1): multiplies the row's loss;

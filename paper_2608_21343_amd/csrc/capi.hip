@@ -397,8 +397,8 @@ extern "C" int tb_token_logprobs_grad(const void* logits, int32_t dtype, int64_t
   if ((r = check_grad(grad, dtype, n_rows, grad_stride, v_plus_blank))) return r;
   rows::Rows a;
   rows::Plan p;
-  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, true, 0, workspace,
-                     workspace_bytes, &a, &p)))
+  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, true, 0,
+                     workspace, workspace_bytes, &a, &p)))
     return r;
   const bool in_place = grad == logits && grad_stride == row_stride;
   const RowBuf bufs[] = {
@@ -437,8 +437,8 @@ extern "C" int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int
   if (grad && (r = check_grad(grad, dtype, n_rows, grad_stride, v_plus_blank))) return r;
   rows::Rows a;
   rows::Plan p;
-  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, grad != nullptr, 0, workspace,
-                     workspace_bytes, &a, &p)))
+  if ((r = make_rows(logits, dtype, n_rows, v_plus_blank, row_stride, temperature, grad != nullptr,
+                     0, workspace, workspace_bytes, &a, &p)))
     return r;
   const bool in_place = grad == logits && grad_stride == row_stride;
   const RowBuf bufs[] = {

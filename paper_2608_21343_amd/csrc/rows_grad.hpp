@@ -78,7 +78,8 @@ enum Pass { kWhole, kStats, kApply };
 // ---- gradient of log probabilities, log-sum-exp and entropy
 
 template <class LT, int NWR, int NP, bool ENT, Pass PASS>
-__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void grad_kernel(Rows a, GradIO io) {
+__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void grad_kernel(
+    Rows a, GradIO io) {
   __shared__ float box[3 * NWR];
   __shared__ uint32_t bits_all[Place<NWR>::kRows][list_words<LT, NWR, NP>()];
   lds_poison(box, sizeof(box));
@@ -214,7 +215,8 @@ __device__ __forceinline__ float distill_loss(const Teacher& t, float zk, const 
 }
 
 template <class LT, int NWR, int NP, bool TAIL, Pass PASS>
-__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void distill_kernel(Rows a, DistillIO io) {
+__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void distill_kernel(
+    Rows a, DistillIO io) {
   constexpr int kWords = list_words<LT, NWR, NP>();
   __shared__ float box[3 * NWR];
   __shared__ uint32_t bits_all[Place<NWR>::kRows][kWords];
@@ -272,7 +274,12 @@ __global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void 
   const float mass = t.bad ? __builtin_nanf("") : t.mass;
   const float k_on = mass * wt / s.S;
   float k_off = k_on;
-  if (TAIL && t.rest != 0.f && !(s.R == 0.f)) k_off = (mass - t.rest / (s.R / s.S)) * wt / s.S;
+  if (TAIL && t.rest != 0.f && !(s.R == 0.f)) {
+    // (not by way of R / S, which may be too small a number for its inverse)
+    k_off = (mass / s.S - t.rest / s.R) * wt;
+    // a token of probability 0 among those outside gets 0, not 0 times infinity
+    if (__builtin_isinf(k_off)) k_off = __builtin_copysignf(__FLT_MAX__, k_off);
+  }
   auto slope = [&](float, float e) { return e * k_off; };
   if (b.big)
     x.template store<true>(out, b, slope);

@@ -238,7 +238,8 @@ __device__ __forceinline__ void rank(Found<NWR>& f, const AltRow<PART>& out, int
 }
 
 template <class LT, int NWR, int NP, bool TOP, bool PART>
-__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void score_kernel(Rows a, ScoreIO io) {
+__global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void score_kernel(
+    Rows a, ScoreIO io) {
   typedef Tile<LT, NWR, NP> T;
   constexpr int PV = T::PV;
   __shared__ float box[3 * NWR], box_z[NWR];
@@ -341,12 +342,11 @@ __global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void 
           bi = id;
         }
       };
+      x.each([&](int p) {
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-  #pragma unroll
         for (int e = 0; e < PV; ++e)
           best(x.at(p, e), place + (p * NWR + at.q) * 64 * PV + e);
-      }
+      });
       best(x.rim(), x.rim_at());
       row_best<NWR>(bz, bi, box_z, box_id, at.q, at.lane);
       if (at.q == 0 && at.lane == 0) {

@@ -67,3 +67,36 @@ def test_rows_of_one_wave_do_not_depend_on_place_or_number(dtype, C):
         bits = (lambda x: x.view(torch.int32 if x.dtype != torch.bfloat16 else torch.int16))
         np.testing.assert_array_equal(bits(a).repeat(*([700] + [1] * (a.dim() - 1))).numpy(),
                                       bits(b).numpy())
+
+
+@pytest.mark.parametrize("z_out", [-86.0, -87.2, -87.33, -100.0])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_tail_of_almost_no_mass(dtype, z_out):
+    """One token outside the list has the least probability that float32 holds
+    (or less), all others none: its gradient takes the teacher's whole rest, and
+    the tokens of probability 0 have none. Its exponential is within 3 roundings
+    of its exponent, 87 * 2^-22, of the true one, but the quotient by their sum,
+    which is itself, is exact; below 2^-126 it counts as 0 and the loss as inf."""
+    from paper_2608_21343_amd import capi
+    C = 300
+    z = torch.full((2, C), -float("inf"))
+    z[:, :40] = 0.0
+    z[:, 250] = z_out
+    z = z.to(dtype).cuda()
+    ids = torch.arange(40, dtype=torch.int32).repeat(2, 1).cuda()
+    sc = torch.full((2, 40), float(np.log(0.5 / 40))).cuda()
+    loss, grad = torch.empty(2, device="cuda"), torch.empty_like(z)
+    capi.tb_distill(z, ids, sc, loss, grad, tail=True)
+    g = grad.float().cpu().numpy()
+    low = float(z[0, 250]) < -87.336  # 126 ln 2
+    tol = 2.0 ** -8 if dtype == torch.bfloat16 else 1e-5
+    np.testing.assert_allclose(g[:, :40], 1 / 40 - 0.5 / 40, atol=1e-6 + tol / 80)
+    rest = np.delete(g[:, 40:], 210, 1)
+    assert (rest == 0).all()
+    if low:
+        assert np.isinf(loss.cpu().numpy()).all() and (np.abs(g[:, 250]) < 1e-30).all()
+    else:
+        np.testing.assert_allclose(g[:, 250], -0.5, atol=0.5 * tol + 1e-5)
+        want = 0.5 * (np.log(0.5 / 40) - np.log(1 / 40)) + 0.5 * (
+            np.log(0.5) - (float(z[0, 250]) - np.log(40)))
+        np.testing.assert_allclose(loss.cpu().numpy(), want, atol=5e-5)
