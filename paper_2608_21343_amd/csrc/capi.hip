@@ -450,8 +450,8 @@ extern "C" int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int
       {teacher_score, n_rows * n_teacher * 4, "teacher_score"},
       {weight, n_rows * 4, "weight"}};
   if ((r = check_apart(bufs, 3))) return r;
-  const rows::DistillIO io = {teacher_tok, teacher_score, n_teacher, tail, temperature, weight,
-                              out_loss, grad, grad_stride};
+  const rows::DistillIO io = {teacher_tok, teacher_score, n_teacher, tail, weight, out_loss,
+                              grad, grad_stride};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   hipError_t e =
       dtype == TB_F32 ? rows::distill_f32(a, io, p, st) : rows::distill_bf16(a, io, p, st);

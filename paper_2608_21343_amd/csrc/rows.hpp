@@ -475,9 +475,9 @@ struct Shape {
 };
 constexpr int capacity(Shape s, int pv) { return s.nwr * s.np * 64 * pv + pv - 1; }
 
-constexpr int kShapes = 13;
-constexpr Shape kShape[kShapes] = {{1, 1}, {1, 2}, {1, 4}, {1, 8}, {1, 16}, {2, 16}, {4, 2},
-                                   {4, 4}, {4, 8}, {4, 16}, {16, 4}, {16, 8}, {16, 16}};
+constexpr int kShapes = 11;
+constexpr Shape kShape[kShapes] = {{1, 1}, {1, 2},  {1, 4},  {1, 8},  {1, 16}, {2, 16},
+                                   {4, 8}, {4, 16}, {16, 4}, {16, 8}, {16, 16}};
 // Shapes that the segments of cut rows take.
 constexpr bool cuts(Shape s) { return s.nwr == 4 && s.np >= 8; }
 
@@ -581,7 +581,6 @@ struct DistillIO {
   const float* score;
   int32_t K;
   int32_t tail;
-  float temperature;
   const float* weight;
   float* loss;
   void* grad;
