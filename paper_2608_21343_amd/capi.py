@@ -632,8 +632,10 @@ def _rows_in(logits, n_alt: int, workspace, stream):
     if workspace is None and V1 > _WHOLE_ROW:
         import torch
         need = LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt)
-        if need > 0:
-            with torch.cuda.stream(stream):  # (None: the current one)
+        if need > 0 and stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+        elif need > 0:
+            with torch.cuda.stream(stream):
                 workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
     if workspace is None:
         return (ptr, dt, n, V1, rs), None, 0, None
