@@ -570,7 +570,7 @@ def _rows(x, name: str = "logits"):
         raise ValueError(f"{name} must be [..., V+1] with V+1 >= 2")
     if strides[-1] != 1:
         raise ValueError(f"{name} rows must be contiguous")
-    rows, step = 1, 0
+    rows, step = 1, None  # (0 is the stride of an expanded dimension)
     if n == 2 and shape[0] > 1:
         rows, step = shape[0], strides[0]
         n = 0
@@ -578,14 +578,14 @@ def _rows(x, name: str = "logits"):
         size = shape[d]
         if size == 1:
             continue
-        if step == 0:
+        if step is None:
             step = strides[d]
         elif strides[d] != rows * step:
             raise ValueError(f"{name} rows must be evenly spaced")
         rows *= size
     if rows > 1 and step < shape[-1]:
         raise ValueError(f"{name} rows overlap")
-    return rows, shape[-1], step if rows > 1 else max(step, shape[-1])
+    return rows, shape[-1], step if rows > 1 else shape[-1]
 
 
 def _list(t, rows: int, dtype, name: str):

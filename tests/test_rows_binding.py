@@ -1,0 +1,88 @@
+"""The binding of the row operators on tensors of host memory: how it reads
+shapes and strides (nothing is launched; a tensor's memory is never touched)."""
+
+import pytest
+import torch
+
+from paper_2608_21343_amd import capi, rowops
+
+V1 = 10
+
+
+def _spread(*shape):
+    """Logits of padded rows."""
+    return torch.zeros(*shape, V1 + 3)[..., :V1]
+
+
+def _last_place(x, rows, step):
+    return x.storage_offset() + (rows - 1) * step + V1 - 1
+
+
+# views whose rows are the same memory several times: inner, middle and outer
+# dimensions, and several of them
+EXPANDED = {
+    "inner": torch.zeros(4, 1, V1).expand(4, 3, V1),
+    "inner of one": torch.zeros(1, 1, V1).expand(1, 3, V1),
+    "outer": torch.zeros(1, 3, V1).expand(4, 3, V1),
+    "both": torch.zeros(1, 1, V1).expand(4, 3, V1),
+    "first of four": torch.zeros(1, 4, 3, V1).expand(2, 4, 3, V1),
+    "second of four": torch.zeros(2, 1, 3, V1).expand(2, 4, 3, V1),
+    "third of four": torch.zeros(2, 4, 1, V1).expand(2, 4, 3, V1),
+    "inner two of four": torch.zeros(2, 1, 1, V1).expand(2, 4, 3, V1),
+    "outer two of four": torch.zeros(1, 1, 3, V1).expand(2, 4, 3, V1),
+    "two dimensions": torch.zeros(1, V1).expand(3, V1),
+    "padded": _spread(4, 1).expand(4, 3, V1),
+    "between dimensions of one": torch.zeros(4, 1, 1, V1).expand(4, 3, 1, V1),
+    "transposed": torch.zeros(4, 1, V1).expand(4, 3, V1).transpose(0, 1),
+}
+
+
+@pytest.mark.parametrize("name", EXPANDED)
+def test_expanded_rows_are_refused_and_copied(name):
+    x = EXPANDED[name]
+    with pytest.raises(ValueError, match="overlap|evenly"):
+        capi._rows(x)
+    with pytest.raises(ValueError, match="grad rows"):
+        capi._rows(x, "grad")
+    y = rowops._even(x)
+    assert y.is_contiguous() and y.shape == x.shape
+    rows, width, step = capi._rows(y)
+    assert rows * width == x.numel() and step == width
+
+
+@pytest.mark.parametrize("x, want", [
+    (torch.zeros(V1), (1, V1, V1)),
+    (torch.zeros(3, V1), (3, V1, V1)),
+    (torch.zeros(4, 3, V1), (12, V1, V1)),
+    (torch.zeros(4, 1, 3, 1, V1), (12, V1, V1)),
+    (_spread(4, 3), (12, V1, V1 + 3)),
+    (_spread(2, 4, 3)[:, :1, :1], (2, V1, 12 * (V1 + 3))),
+    (_spread(2, 4, 3)[:, :, 1], (8, V1, 3 * (V1 + 3))),
+    (_spread(4, 3)[::2, 1], (2, V1, 6 * (V1 + 3))),
+    # expanded, but only by dimensions of size 1
+    (torch.zeros(4, 1, V1).expand(4, 1, V1), (4, V1, V1)),
+    (torch.zeros(4, 3, V1).expand(1, 4, 3, V1), (12, V1, V1)),
+])
+def test_rows_of_views(x, want):
+    assert capi._rows(x) == want
+    assert _last_place(x, want[0], want[2]) < x.untyped_storage().nbytes() // 4
+    assert rowops._even(x) is x
+
+
+def test_rows_address_what_the_view_addresses():
+    """Of views of every kind: accepted rows are those of the view, in order."""
+    import itertools
+    taken = 0
+    for shape in itertools.product((1, 2, 3), repeat=3):
+        for strides in itertools.product((0, 10, 13, 20, 30, 39, 60, 90), repeat=3):
+            x = torch.empty(600).as_strided((*shape, V1), (*strides, 1))
+            try:
+                rows, width, step = capi._rows(x)
+            except ValueError:
+                continue
+            want = [sum(i * s for i, s in zip(at, strides))
+                    for at in itertools.product(*map(range, shape))]
+            assert (rows, width) == (len(want), V1)
+            assert want == [i * step for i in range(rows)] and (rows == 1 or step >= V1)
+            taken += 1
+    assert taken > 100
