@@ -574,6 +574,8 @@ def _rows(x, name: str = "logits"):
     if n == 2 and shape[0] > 1:
         rows, step = shape[0], strides[0]
         n = 0
+    elif 0 in shape:
+        return 0, shape[-1], shape[-1]
     for d in range(n - 2, -1, -1):
         size = shape[d]
         if size == 1:

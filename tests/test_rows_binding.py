@@ -86,3 +86,23 @@ def test_rows_address_what_the_view_addresses():
             assert want == [i * step for i in range(rows)] and (rows == 1 or step >= V1)
             taken += 1
     assert taken > 100
+
+
+@pytest.mark.parametrize("shape", [(0, V1), (0, 3, V1), (2, 0, V1), (2, 3, 0, V1), (2, 0, 3, V1),
+                                   (0, 0, V1)])
+def test_no_rows_of_any_shape(shape):
+    assert capi._rows(torch.zeros(shape)) == (0, V1, V1)
+    assert capi._rows(torch.zeros(*shape[:-1], V1 + 3)[..., :V1]) == (0, V1, V1)
+    assert rowops._even(torch.zeros(shape)).shape == shape
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lead", [(2, 0), (0, 3), (2, 0, 3)])
+def test_calls_without_rows_of_any_shape(lead):
+    z = torch.zeros(*lead, V1, device="cuda", requires_grad=True)
+    tok = torch.zeros(*lead, 2, dtype=torch.int32, device="cuda")
+    got = rowops.token_scores(z, tok, 3)
+    assert got.logprob.shape == (*lead, 2) and got.alt.shape == (*lead, 3)
+    loss = rowops.distill_loss(z, tok, torch.zeros(*lead, 2, device="cuda"))
+    (loss.sum() + got.logprob.sum()).backward()
+    assert loss.shape == lead and z.grad.shape == z.shape
