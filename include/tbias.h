@@ -605,7 +605,8 @@ int tb_token_logprobs_grad(const void* logits, int32_t dtype, int64_t n_rows,
  *             loss = sum_k q_k (log q_k - log p[token_k]); an empty list: 0
  *   tail = 1: exp(score): the scores are log probabilities at the temperature
  *             of the call. All other tokens are one event, of probability q_r =
- *             max(0, 1 - sum q) and p_r = the sum of p outside the list;
+ *             1 - sum q (0 where that is below 2^-18, the rounding of a list
+ *             that sums to 1) and p_r = the sum of p outside the list;
  *             loss = sum_k q_k (log q_k - log p[token_k]) + q_r (log q_r - log p_r);
  *             a p_r of less than 2^-126 of the row's largest p counts as 0
  *

@@ -154,6 +154,13 @@ __global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void 
 
 // ---- distillation
 
+// A rest of less mass than this is the rounding of the scores and of their sum:
+// 64 half steps of float32, where a whole vocabulary's scores, H = -sum q s <=
+// ln 64, are off by 4 H + 15 half steps of their sum and the sum of their
+// exponentials by another 1.5 H + 8. (Taken as mass, it makes the loss infinite
+// where the student has none outside the list.)
+constexpr float kLeastRest = 0x1p-18f;
+
 // A teacher's list, a token per lane.
 struct Teacher {
   int32_t id;
@@ -186,7 +193,7 @@ __device__ __forceinline__ Teacher teacher(const DistillIO& io, const Places& p,
     t.logq = sc;
     const float sum = wave_total(t.q);
     const float rest = 1.f - sum;
-    t.rest = rest < 0.f ? 0.f : rest;  // (a NaN stays)
+    t.rest = rest < kLeastRest ? 0.f : rest;  // (a NaN stays)
     t.mass = sum + t.rest;
   } else {
     const float m = wave_most(sc);

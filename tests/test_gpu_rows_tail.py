@@ -1,0 +1,108 @@
+"""Distillation with the teacher's tail where the list holds (almost) all of a
+row's probability, or none, or where the temperature is low.
+
+Tolerances as in tests/test_gpu_rows.py: eps = 2^-24, log probabilities within
+SUM = 1e-5. A list's scores e^s that sum to 1 exactly do so only to some 46 eps
+in float32: with H = -sum q s <= ln 64 for 64 places, the scores are off by 4 H
+eps (quotient by the temperature, difference, product, subtraction), by 12 eps
+for the logarithm of the sum (1.5 units of its last place) and 3 eps for the sum;
+their exponentials by 1.5 H eps and 2 eps, and adding them up by 6 eps."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+SUM = 1e-5
+LEAST = 2.0 ** -18  # a rest below this is the scores' rounding
+NEG = -math.inf
+F32, BF16 = torch.float32, torch.bfloat16
+DTYPES = pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+
+
+def distill(z, ids, sc, tau=1.0, weight=None):
+    from paper_2608_21343_amd import capi
+    n = z.shape[0]
+    loss, grad = torch.full((n,), 77.0, device="cuda"), torch.full_like(z, 55.0)
+    only, alone = torch.full((n,), 77.0, device="cuda"), torch.full_like(z, 55.0)
+    args = (z, ids.to(torch.int32).cuda(), sc.to(F32).cuda())
+    w = None if weight is None else weight.cuda()
+    capi.tb_distill(*args, loss, grad, weight=w, temperature=tau, tail=True)
+    capi.tb_distill(*args, only, None, weight=w, temperature=tau, tail=True)
+    capi.tb_distill(*args, None, alone, weight=w, temperature=tau, tail=True)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(only.cpu().numpy(), loss.cpu().numpy())
+    np.testing.assert_array_equal(alone.float().cpu().numpy(), grad.float().cpu().numpy())
+    return loss.cpu().double(), grad.float().cpu().double()
+
+
+def scored(z, M, tau):
+    from paper_2608_21343_amd import capi
+    n = z.shape[0]
+    alt = torch.empty((n, M), dtype=torch.int32, device="cuda")
+    alt_lp = torch.empty((n, M), device="cuda")
+    capi.tb_token_logprobs(z, out_alt=alt, out_alt_logprob=alt_lp, temperature=tau)
+    return alt.cpu(), alt_lp.cpu()
+
+
+def masked_rows(g, n, C, visible, dtype, fill=NEG):
+    """n rows of which `visible` tokens each are not masked."""
+    at = torch.rand((n, C), generator=g).argsort(1)[:, :visible]
+    z = torch.full((n, C), fill)
+    z.scatter_(1, at, torch.randn((n, visible), generator=g) * 2)
+    return z.to(dtype), at
+
+
+@pytest.mark.parametrize("tau", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("C, visible", [(2, 2), (3, 3), (17, 17), (64, 64), (300, 2), (1025, 7),
+                                        (1025, 64), (9000, 33), (70001, 64), (140001, 20)])
+@DTYPES
+def test_a_list_of_all_that_is_visible(dtype, C, visible, tau):
+    """Scores of a whole vocabulary or of all tokens that a mask leaves: no mass
+    is left for a rest, for a student equal to the teacher (loss 0, no gradient)
+    and for another one of the same mask (the sum over the list alone)."""
+    g = torch.Generator().manual_seed(C + visible)
+    n = 200 if C < 5000 else 8
+    z, at = masked_rows(g, n, C, visible, dtype)
+    other = z.clone()
+    other.scatter_(1, at, (torch.randn((n, visible), generator=g) * 2).to(dtype))
+    alt, alt_lp = scored(z.cuda(), 64, tau)
+    plain = torch.log_softmax(torch.gather(z, 1, at).float() / tau, 1)
+    for ids, sc in ((alt, alt_lp), (at, plain)):
+        loss, grad = distill(z.cuda(), ids, sc, tau)
+        assert float(loss.abs().max()) < 3 * SUM
+        assert float(grad.abs().max()) < 3 * SUM / tau
+        loss, grad = distill(other.cuda(), ids, sc, tau)
+        logp = torch.log_softmax(other.double() / tau, 1)
+        q = torch.zeros(n, C).double().scatter_add_(
+            1, ids.clamp(min=0).long(), torch.where(ids >= 0, sc, NEG).double().exp())
+        lp = torch.gather(logp, 1, ids.clamp(min=0).long())
+        s = sc.double()
+        want = torch.where(ids >= 0, s.exp() * (s - lp), 0.0).sum(1)
+        # the terms of the sum are of size |s - lp| <= 40 / tau
+        assert float((loss - want).abs().max()) < SUM + 2e-6 * 40 / tau
+        d = (q.sum(1, keepdim=True) * logp.exp() - q) / tau
+        tol = 3 * SUM / tau + (2.0 ** -8 * d.abs() if dtype == BF16 else 0.0)
+        assert bool(((grad - d).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("shift", [-17, -19])
+def test_the_least_rest(shift):
+    """A rest of 2^-17 counts (an infinite loss where the student has no mass for
+    it, its own share of loss and gradient where it has), one of 2^-19 does not."""
+    rest = 2.0 ** shift
+    counts = rest >= LEAST
+    z = torch.tensor([[0.0, NEG, NEG, NEG], [0.0, -30.0, NEG, NEG]], device="cuda")
+    ids = torch.zeros((2, 1), dtype=torch.int32)
+    loss, grad = distill(z, ids, torch.full((2, 1), math.log1p(-rest)))
+    own = (1 - rest) * math.log1p(-rest)
+    assert math.isinf(loss[0]) if counts else abs(loss[0] - own) < 1e-6
+    # the exponential of the score, a number next to 1, is off by 2 eps at most
+    p = math.exp(-30.0)
+    want = own + (rest * (math.log(rest) - math.log(p)) if counts else 0.0)
+    assert abs(loss[1] - want) < 1e-6 + 2 * 21 * 2.0 ** -24
+    assert abs(grad[1, 1] + (rest if counts else 0.0)) < 4 * 2.0 ** -24
+    assert bool((grad[:, 2:] == 0).all())
