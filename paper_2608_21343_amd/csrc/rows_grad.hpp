@@ -165,6 +165,7 @@ constexpr float kLeastRest = 0x1p-18f;
 struct Teacher {
   int32_t id;
   bool ok, bad;      // bad: the row has a token out of range
+  bool none;         // no place is used
   float q, logq;
   float mass, rest;  // of the list and (with the tail) of all else
 };
@@ -186,6 +187,7 @@ __device__ __forceinline__ Teacher teacher(const DistillIO& io, const Places& p,
   t.id = p.id;
   t.ok = (uint32_t)t.id < (uint32_t)C;
   t.bad = __ballot(!t.ok && t.id != -1) != 0;
+  t.none = __ballot(t.ok) == 0;
   const float sc = t.ok ? p.score : kNegInf;
   t.rest = 0.f;
   if (io.tail) {
@@ -206,6 +208,12 @@ __device__ __forceinline__ Teacher teacher(const DistillIO& io, const Places& p,
     if (sum != sum) t.mass = sum;
   }
   return t;
+}
+
+// The sum outside the list. Without a listed token it is that of the row, which was
+// added up in another order: loss and gradient are then 0, not their difference.
+__device__ __forceinline__ float sum_outside(const Teacher& t, const Stats& s) {
+  return t.none ? s.S : s.R;
 }
 
 __device__ __forceinline__ float distill_loss(const Teacher& t, float zk, const Stats& s,
@@ -268,6 +276,7 @@ __global__ __launch_bounds__(Place<NWR>::kWg, least_waves(Shape{NWR, NP})) void 
     if (at.q == 0 && at.lane == 0) a.part[at.row * a.n_seg + blockIdx.y] = to_part(s, b);
     return;
   }
+  if (TAIL) s.R = sum_outside(t, s);
   if (PASS == kWhole && io.loss && at.q == 0) {
     const float loss = distill_loss(t, Elem<LT>::widen(zk), s, b, a.inv_tau);
     if (at.lane == 0) io.loss[at.row] = w * loss;
@@ -319,7 +328,8 @@ __global__ __launch_bounds__(kThreads) void distill_loss_kernel(Rows a, DistillI
   float loss = 0.f;
   if (w != 0.f && (t.mass != 0.f || t.bad)) {
     Basis b;
-    const Stats s = join(a.part + row * a.n_seg, a.n_seg, a.c, lane, b);
+    Stats s = join(a.part + row * a.n_seg, a.n_seg, a.c, lane, b);
+    s.R = sum_outside(t, s);
     loss = w * distill_loss(t, t.ok ? Elem<LT>::widen(z[t.id]) : kNegInf, s, b, a.inv_tau);
   }
   if (lane == 0) io.loss[row] = loss;

@@ -106,3 +106,21 @@ def test_the_least_rest(shift):
     assert abs(loss[1] - want) < 1e-6 + 2 * 21 * 2.0 ** -24
     assert abs(grad[1, 1] + (rest if counts else 0.0)) < 4 * 2.0 ** -24
     assert bool((grad[:, 2:] == 0).all())
+
+
+@pytest.mark.parametrize("C", [2, 300, 1025, 4100, 8196, 20000, 70001, 140001])
+@DTYPES
+def test_an_empty_list_asks_for_nothing(dtype, C):
+    """Without a listed token everything is the one event outside the list, which
+    both have with probability 1: loss and gradient are 0, not rounding noise."""
+    g = torch.Generator().manual_seed(C)
+    z = (torch.randn((5, C), generator=g) * 3).to(dtype)
+    z[1, 1:] = NEG
+    z[2] = NEG
+    z[3, C - 1] = math.nan
+    ids = torch.full((5, 4), -1, dtype=torch.int32)
+    sc = torch.randn((5, 4), generator=g)
+    loss, grad = distill(z.cuda(), ids, sc, 0.7)
+    assert loss[[0, 1, 4]].tolist() == [0.0] * 3 and bool((grad[[0, 1, 4]] == 0).all())
+    assert math.isinf(loss[2]) and bool((grad[2] == 0).all())  # no token for the event
+    assert math.isnan(loss[3]) and bool(torch.isnan(grad[3]).all())
