@@ -124,3 +124,35 @@ def test_an_empty_list_asks_for_nothing(dtype, C):
     assert loss[[0, 1, 4]].tolist() == [0.0] * 3 and bool((grad[[0, 1, 4]] == 0).all())
     assert math.isinf(loss[2]) and bool((grad[2] == 0).all())  # no token for the event
     assert math.isnan(loss[3]) and bool(torch.isnan(grad[3]).all())
+
+
+@pytest.mark.parametrize("tau, weight", [(1e-4, 1.0), (0.01, 1.0), (1.0, 1e30), (1e4, 1e-30)])
+@pytest.mark.parametrize("below", [1.0, 60.0, 80.0, 87.0])
+@pytest.mark.parametrize("C", [300, 5000, 140001])
+@DTYPES
+def test_the_rest_goes_to_few_tokens_at_any_temperature(dtype, C, below, tau, weight):
+    """Two tokens outside the list, `below` units of z / tau under the listed
+    ones, take the teacher's rest between them, whatever factor of weight / tau
+    stands before it: -w / tau (rest p_v / p_rest - p_v)."""
+    z = torch.full((2, C), NEG)
+    z[:, :40] = 0.0
+    z[:, C - 50] = -below * tau
+    z[:, C - 7] = -below * tau
+    z = z.to(dtype)
+    z = z.cuda()
+    ids = torch.arange(40, dtype=torch.int32).repeat(2, 1)
+    sc = torch.full((2, 40), math.log(0.5 / 40))
+    loss, grad = distill(z, ids, sc, tau, torch.full((2,), weight))
+    out = torch.exp(z[0, C - 7].double().cpu() / tau)
+    total = 40 + 2 * out
+    wt = weight / tau
+    tol = wt * (1e-5 + (2.0 ** -8 if dtype == BF16 else 0.0))
+    for v in (C - 50, C - 7):
+        assert float((grad[:, v] + wt * (0.25 - out / total)).abs().max()) < tol
+    assert float((grad[:, :40] - wt * (1 / total - 0.5 / 40)).abs().max()) < tol
+    rest = torch.ones(C, dtype=torch.bool)
+    rest[:40] = rest[C - 50] = rest[C - 7] = False
+    assert bool((grad[:, rest] == 0).all())
+    want = 0.5 * (math.log(0.5 / 40) + math.log(total)) + 0.5 * (
+        math.log(0.5) - math.log(2 * out / total))
+    np.testing.assert_allclose(loss.numpy(), weight * want, rtol=1e-5, atol=weight * SUM)
