@@ -5,7 +5,8 @@ Marshalling only, as in ``decoder``: buffers come from torch, all work runs in
 libtbias.so (tb_token_logprobs, tb_distill and their gradients), and the losses
 are torch.autograd functions whose backward passes are those of the library. A
 backward pass reads the logits again instead of keeping the probabilities: one
-read and one write of their size, and no memory between the passes.
+read and one write of their size, and no memory between the passes. Gradients
+are not themselves differentiable: a second derivative raises an error.
 """
 
 from __future__ import annotations
@@ -36,6 +37,26 @@ def _even(logits: torch.Tensor) -> torch.Tensor:
         return logits
     except ValueError:
         return logits.contiguous()
+
+
+class _Once(torch.autograd.Function):
+    """Passes a gradient on whose own derivative is asked for and not there."""
+
+    @staticmethod
+    def forward(ctx, grad):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the row operators have no second derivative: their gradient with "
+                           "respect to the logits is a constant to autograd")
+
+
+def _once(grad: torch.Tensor) -> torch.Tensor:
+    """The result of a backward pass. Where a graph of that pass is built
+    (create_graph), differentiating it again raises an error: torch's
+    once_differentiable does not where only the logits require a gradient."""
+    return _Once.apply(grad.requires_grad_()) if torch.is_grad_enabled() else grad
 
 
 class _TokenScores(torch.autograd.Function):
@@ -84,7 +105,7 @@ class _TokenScores(torch.autograd.Function):
             more = torch.empty_like(grad)
             capi.tb_token_logprobs_grad(z, t1, row(d1), more, temperature=ctx.temperature)
             grad += more
-        return grad, None, None, None
+        return _once(grad), None, None, None
 
 
 def token_scores(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, n_alt: int = 0,
@@ -123,7 +144,7 @@ class _Distill(torch.autograd.Function):
         w = d_loss.contiguous() if weight is None else d_loss * weight
         grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
         capi.tb_distill(z, tok, score, None, grad, weight=w, temperature=temperature, tail=tail)
-        return grad, None, None, None, None, None
+        return _once(grad), None, None, None, None, None
 
 
 def distill_loss(logits: torch.Tensor, teacher_tok: torch.Tensor, teacher_score: torch.Tensor,

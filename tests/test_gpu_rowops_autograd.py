@@ -1,0 +1,33 @@
+"""The differentiable layer over the row operators where a gradient could be
+wrong without a word: second derivatives, logits overwritten before their
+backward pass, teachers and weights that ask for a gradient, lists of more
+places than a call takes."""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def inputs(n=6, C=301, K=5, dtype=F32, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    z = (torch.randn((n, C), generator=g) * 2).to(dtype).cuda()
+    ids = torch.stack([torch.randperm(C, generator=g)[:K] for _ in range(n)]).to(torch.int32)
+    return z, ids.cuda(), torch.randn((n, K), generator=g).cuda()
+
+
+@pytest.mark.parametrize("entry", ["token_scores", "distill_loss"])
+def test_second_derivatives_are_refused(entry):
+    from paper_2608_21343_amd import rowops
+    z, ids, sc = inputs()
+    x = z.clone().requires_grad_()
+    if entry == "token_scores":
+        loss = rowops.token_scores(x, ids).logprob.sum()
+    else:
+        loss = rowops.distill_loss(x, ids, sc).sum()
+    grad, = torch.autograd.grad(loss, x, create_graph=True)
+    assert grad.requires_grad  # a penalty on it is not lost on the way ...
+    with pytest.raises(RuntimeError, match="second derivative"):
+        grad.pow(2).sum().backward()  # ... but refused
