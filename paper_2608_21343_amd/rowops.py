@@ -166,11 +166,16 @@ def distill_step(logits: torch.Tensor, teacher_tok: torch.Tensor, teacher_score:
                  temperature: float = 1.0, tail: bool = False,
                  weight: Optional[torch.Tensor] = None, in_place: bool = False):
     """(loss [...], gradient [..., V+1] of its sum) in one pass over the logits;
-    ``in_place`` writes the gradient over the logits."""
+    ``in_place`` writes the gradient over the logits (a backward pass that needs
+    them afterwards raises an error)."""
     z = logits.detach() if in_place else _even(logits.detach())
     loss = torch.empty(z.shape[:-1], dtype=torch.float32, device=z.device)
     grad = z if in_place else torch.empty(z.shape, dtype=z.dtype, device=z.device)
     capi.tb_distill(z, teacher_tok.contiguous(), teacher_score.contiguous(), loss, grad,
                     weight=None if weight is None else weight.contiguous(),
                     temperature=float(temperature), tail=bool(tail))
+    if in_place and not z.is_inference():
+        # the library writes by address: a backward pass that still needs these
+        # logits finds out by their version
+        torch.autograd.graph.increment_version(z)
     return loss, grad

@@ -31,3 +31,35 @@ def test_second_derivatives_are_refused(entry):
     assert grad.requires_grad  # a penalty on it is not lost on the way ...
     with pytest.raises(RuntimeError, match="second derivative"):
         grad.pow(2).sum().backward()  # ... but refused
+
+
+@pytest.mark.parametrize("entry", ["token_scores", "distill_loss"])
+def test_overwritten_logits_are_noticed(entry):
+    from paper_2608_21343_amd import rowops
+    z, ids, sc = inputs()
+    x = z.clone().requires_grad_()
+    y = x * 1.0
+    if entry == "token_scores":
+        loss = rowops.token_scores(y, ids).logprob.sum()
+    else:
+        loss = rowops.distill_loss(y, ids, sc).sum()
+    rowops.distill_step(y, ids, sc, in_place=True)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+
+
+def test_steps_in_place():
+    """Without a graph that needs the logits a step in place is an ordinary one."""
+    from paper_2608_21343_amd import rowops
+    z, ids, sc = inputs()
+    loss, grad = rowops.distill_step(z, ids, sc)
+    for mode in (torch.enable_grad, torch.no_grad, torch.inference_mode):
+        with mode():
+            over = z.clone()
+            loss2, grad2 = rowops.distill_step(over, ids, sc, in_place=True)
+            assert grad2.data_ptr() == over.data_ptr()
+            assert bool((loss2 == loss).all()) and bool((over == grad).all())
+    over = z.clone()
+    with torch.inference_mode():
+        rowops.distill_step(over, ids, sc, in_place=True)
+    assert bool((over == grad).all())
