@@ -127,6 +127,11 @@ def token_scores(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, n_
     return TokenScores(lp.squeeze(-1) if single else lp, lse, ent, alt, alt_lp)
 
 
+def _constant(t: Optional[torch.Tensor], name: str) -> None:
+    if t is not None and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which this loss does not give: detach it")
+
+
 class _Distill(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tok, score, weight, temperature, tail):
@@ -156,7 +161,10 @@ def distill_loss(logits: torch.Tensor, teacher_tok: torch.Tensor, teacher_score:
     temperature over its list; with it the scores are log probabilities (a
     teacher's TokenScores at the same temperature) and all other tokens count as
     one event. ``weight`` [...] multiplies the rows. Differentiable with respect
-    to the logits; distill_step gives loss and gradient in one pass."""
+    to the logits alone: scores and weights that require a gradient are refused.
+    distill_step gives loss and gradient in one pass."""
+    _constant(teacher_score, "teacher_score")
+    _constant(weight, "weight")
     return _Distill.apply(logits, teacher_tok.contiguous(), teacher_score.contiguous(),
                           None if weight is None else weight.contiguous(), float(temperature),
                           bool(tail))

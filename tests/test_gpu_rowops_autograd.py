@@ -63,3 +63,24 @@ def test_steps_in_place():
     with torch.inference_mode():
         rowops.distill_step(over, ids, sc, in_place=True)
     assert bool((over == grad).all())
+
+
+def test_teachers_and_weights_that_ask_for_a_gradient():
+    from paper_2608_21343_amd import rowops
+    z, ids, sc = inputs()
+    x = z.clone().requires_grad_()
+    w = torch.ones(6, device="cuda")
+    for kw, word in (({"teacher_score": sc.clone().requires_grad_()}, "teacher_score"),
+                     ({"weight": w.clone().requires_grad_()}, "weight")):
+        args = {"teacher_score": sc, "weight": w, **kw}
+        with pytest.raises(ValueError, match=word):
+            rowops.distill_loss(x, ids, **args)
+        with pytest.raises(ValueError, match=word):
+            rowops.distill_loss(z, ids, **args)
+        with torch.no_grad():
+            want = rowops.distill_loss(z, ids, **args)
+        got = rowops.distill_loss(x, ids, **{k: v.detach() for k, v in args.items()})
+        assert bool((got == want).all())
+        got.sum().backward()
+    # the gradient that distill_step returns is that of the logits alone
+    rowops.distill_step(z, ids, sc.clone().requires_grad_(), weight=w.clone().requires_grad_())
