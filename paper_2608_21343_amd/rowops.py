@@ -132,6 +132,19 @@ def _constant(t: Optional[torch.Tensor], name: str) -> None:
         raise ValueError(f"{name} requires a gradient, which this loss does not give: detach it")
 
 
+def _teacher(logits: torch.Tensor, tok: torch.Tensor, score: torch.Tensor,
+             weight: Optional[torch.Tensor]):
+    """The teacher's tensors, contiguous; their rows have to be the logits' rows."""
+    lead = logits.shape[:-1]
+    if tok.dim() != len(lead) + 1 or tok.shape[:-1] != lead:
+        raise ValueError("teacher_tok must be [..., k] for logits [..., V+1]")
+    if score.shape != tok.shape:
+        raise ValueError("teacher_score must have teacher_tok's shape")
+    if weight is not None and weight.shape != lead:
+        raise ValueError("weight must be [...] for logits [..., V+1]")
+    return tok.contiguous(), score.contiguous(), None if weight is None else weight.contiguous()
+
+
 class _Distill(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tok, score, weight, temperature, tail):
@@ -165,9 +178,8 @@ def distill_loss(logits: torch.Tensor, teacher_tok: torch.Tensor, teacher_score:
     distill_step gives loss and gradient in one pass."""
     _constant(teacher_score, "teacher_score")
     _constant(weight, "weight")
-    return _Distill.apply(logits, teacher_tok.contiguous(), teacher_score.contiguous(),
-                          None if weight is None else weight.contiguous(), float(temperature),
-                          bool(tail))
+    return _Distill.apply(logits, *_teacher(logits, teacher_tok, teacher_score, weight),
+                          float(temperature), bool(tail))
 
 
 def distill_step(logits: torch.Tensor, teacher_tok: torch.Tensor, teacher_score: torch.Tensor,
@@ -176,12 +188,12 @@ def distill_step(logits: torch.Tensor, teacher_tok: torch.Tensor, teacher_score:
     """(loss [...], gradient [..., V+1] of its sum) in one pass over the logits;
     ``in_place`` writes the gradient over the logits (a backward pass that needs
     them afterwards raises an error)."""
+    tok, score, weight = _teacher(logits, teacher_tok, teacher_score, weight)
     z = logits.detach() if in_place else _even(logits.detach())
     loss = torch.empty(z.shape[:-1], dtype=torch.float32, device=z.device)
     grad = z if in_place else torch.empty(z.shape, dtype=z.dtype, device=z.device)
-    capi.tb_distill(z, teacher_tok.contiguous(), teacher_score.contiguous(), loss, grad,
-                    weight=None if weight is None else weight.contiguous(),
-                    temperature=float(temperature), tail=bool(tail))
+    capi.tb_distill(z, tok, score, loss, grad, weight=weight, temperature=float(temperature),
+                    tail=bool(tail))
     if in_place and not z.is_inference():
         # the library writes by address: a backward pass that still needs these
         # logits finds out by their version

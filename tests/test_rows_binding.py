@@ -106,3 +106,38 @@ def test_calls_without_rows_of_any_shape(lead):
     loss = rowops.distill_loss(z, tok, torch.zeros(*lead, 2, device="cuda"))
     (loss.sum() + got.logprob.sum()).backward()
     assert loss.shape == lead and z.grad.shape == z.shape
+
+
+LEAD = (4, 3)
+TEACHERS = {
+    "lists of transposed rows": dict(teacher_tok=(3, 4, 5), teacher_score=(3, 4, 5)),
+    "flat lists": dict(teacher_tok=(12, 5), teacher_score=(12, 5)),
+    "scores of another number": dict(teacher_score=(4, 3, 4)),
+    "scores of transposed rows": dict(teacher_score=(3, 4, 5)),
+    "transposed weights": dict(weight=(3, 4)),
+    "flat weights": dict(weight=(12,)),
+    "weights of one column": dict(weight=(4, 3, 1)),
+    "one weight": dict(weight=()),
+}
+
+
+@pytest.mark.parametrize("entry", [rowops.distill_loss, rowops.distill_step])
+@pytest.mark.parametrize("name", TEACHERS)
+def test_teachers_of_other_shapes_are_refused(entry, name):
+    """As many elements are not enough: they would be taken for other rows."""
+    shape = {"teacher_tok": (4, 3, 5), "teacher_score": (4, 3, 5), "weight": (4, 3),
+             **TEACHERS[name]}
+    args = {k: torch.zeros(s, dtype=torch.int32 if k == "teacher_tok" else torch.float32)
+            for k, s in shape.items()}
+    with pytest.raises(ValueError, match="|".join(TEACHERS[name]) + " must"):
+        entry(torch.zeros(*LEAD, V1), **args)
+
+
+@pytest.mark.parametrize("entry", [rowops.distill_loss, rowops.distill_step])
+def test_teachers_of_the_rows_shapes_are_taken(entry):
+    """Up to the library, which takes device tensors only."""
+    for lead in (LEAD, (6,), (), (2, 0)):
+        tok = torch.zeros(*lead, 5, dtype=torch.int32)
+        for weight in (None, torch.ones(lead)):
+            with pytest.raises(ValueError, match="device"):
+                entry(torch.zeros(*lead, V1), tok, torch.zeros(*lead, 5), weight=weight)
