@@ -159,7 +159,7 @@ class _Distill(torch.autograd.Function):
     def backward(ctx, d_loss):
         z, tok, score, weight = ctx.saved_tensors
         temperature, tail = ctx.how
-        w = d_loss.contiguous() if weight is None else d_loss * weight
+        w = (d_loss if weight is None else d_loss * weight).contiguous()
         grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
         capi.tb_distill(z, tok, score, None, grad, weight=w, temperature=temperature, tail=tail)
         return _once(grad), None, None, None, None, None

@@ -84,3 +84,25 @@ def test_teachers_and_weights_that_ask_for_a_gradient():
         got.sum().backward()
     # the gradient that distill_step returns is that of the logits alone
     rowops.distill_step(z, ids, sc.clone().requires_grad_(), weight=w.clone().requires_grad_())
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+def test_incoming_gradients_of_any_layout(weighted):
+    """Losses and scores that are used transposed, expanded or in part."""
+    from paper_2608_21343_amd import rowops
+    z, ids, sc = inputs(12)
+    x = z.view(4, 3, -1).clone().requires_grad_()
+    tok, score = ids.view(4, 3, 5), sc.view(4, 3, 5)
+    w = torch.rand(4, 3, device="cuda") if weighted else None
+    f = torch.rand(3, 4, device="cuda")
+    for use in (lambda y: (y.transpose(0, 1) * f.reshape(3, 4, *[1] * (y.dim() - 2))).sum(),
+                lambda y: y.sum(), lambda y: y[:, 1].sum(), lambda y: y[::2].transpose(0, 1).max()):
+        for get in (lambda v: rowops.distill_loss(v, tok, score, weight=w),
+                    lambda v: rowops.token_scores(v, tok).logprob,
+                    lambda v: rowops.token_scores(v, tok, 3).alt_logprob,
+                    lambda v: rowops.token_scores(v, tok[..., 0]).logprob,
+                    lambda v: rowops.token_scores(v).lse, lambda v: rowops.token_scores(v).entropy):
+            y = get(x)
+            got, d = torch.autograd.grad(use(y), [x, y])
+            want, = torch.autograd.grad(get(x), x, d.contiguous())
+            assert bool((got == want).all())
