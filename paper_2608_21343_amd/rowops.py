@@ -89,22 +89,25 @@ class _TokenScores(torch.autograd.Function):
         if places:
             tok = torch.cat([t for t, _ in places], -1) if len(places) > 1 else places[0][0]
             d_tok = torch.cat([d for _, d in places], -1) if len(places) > 1 else places[0][1]
-        grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
 
         def row(d):
             return None if d is None else d.contiguous()
 
         wide = 0 if tok is None else tok.shape[-1]
         if wide <= capi.TB_MAX_LIST:
+            grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
             capi.tb_token_logprobs_grad(z, tok, row(d_tok), grad, row(d_lse), row(d_ent),
                                         temperature=ctx.temperature)
-        else:  # two lists that make no single one
+        else:
+            # two lists that make no single one: a gradient each in float32, so that
+            # bfloat16 rounds their sum once
             (t0, d0), (t1, d1) = places
-            capi.tb_token_logprobs_grad(z, t0, row(d0), grad, row(d_lse), row(d_ent),
+            z32 = z.float()
+            grad, more = torch.empty_like(z32), z32 if z32 is not z else torch.empty_like(z32)
+            capi.tb_token_logprobs_grad(z32, t0, row(d0), grad, row(d_lse), row(d_ent),
                                         temperature=ctx.temperature)
-            more = torch.empty_like(grad)
-            capi.tb_token_logprobs_grad(z, t1, row(d1), more, temperature=ctx.temperature)
-            grad += more
+            capi.tb_token_logprobs_grad(z32, t1, row(d1), more, temperature=ctx.temperature)
+            grad = grad.add_(more).to(z.dtype)
         return _once(grad), None, None, None
 
 

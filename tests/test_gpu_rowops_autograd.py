@@ -3,6 +3,7 @@ wrong without a word: second derivatives, logits overwritten before their
 backward pass, teachers and weights that ask for a gradient, lists of more
 places than a call takes."""
 
+import numpy as np
 import pytest
 import torch
 
@@ -106,3 +107,48 @@ def test_incoming_gradients_of_any_layout(weighted):
             got, d = torch.autograd.grad(use(y), [x, y])
             want, = torch.autograd.grad(get(x), x, d.contiguous())
             assert bool((got == want).all())
+
+
+def close(got, want, size, dtype):
+    got, want = got.float().cpu().double().numpy(), want.numpy()
+    tol = 1e-5 * size.numpy() + 1e-37 + (2.0 ** -7.99 if dtype == BF16 else 3e-7) * np.abs(want)
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], want[bad][:3])
+
+
+@pytest.mark.parametrize("J, M", [(24, 40), (25, 40), (40, 40), (64, 64), (64, 1), (1, 64)])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_more_places_than_a_list_holds(dtype, J, M):
+    """Given tokens and alternatives of up to 64 and of more places together: one
+    rounding of the gradient in both, also where the two lists' gradients of a
+    token or of the whole row nearly cancel. The tolerance is 1e-5 of the
+    magnitudes in 32 bits, and the one rounding to bfloat16."""
+    from paper_2608_21343_amd.rowops import token_scores
+    z, _, _ = inputs(4, 301, 1, dtype, J)
+    g = torch.Generator().manual_seed(M)
+    alt = torch.topk(z.float(), M, dim=1, sorted=True).indices.cpu()
+    tok = torch.randint(0, 301, (4, J), generator=g)
+    same = min(J, M)
+    tok[:, :same] = alt[:, :same]
+    d_tok = torch.randn((4, J), generator=g)
+    d_alt = torch.randn((4, M), generator=g)
+    d_alt[:2, :same] = -d_tok[:2, :same] + 0.001  # nearly cancel
+    d_ent, d_lse = torch.randn(4, generator=g), torch.randn(4, generator=g)
+    x = z.clone().requires_grad_()
+    got = token_scores(x, tok.to(torch.int32).cuda(), M, 1.3)
+    at = got.alt.cpu().long()
+    d_tok[2, 0] = d_alt[2, 0] = 0.0
+    ((got.logprob * d_tok.cuda()).sum() + (got.alt_logprob * d_alt.cuda()).sum()
+     + (got.entropy * d_ent.cuda()).sum() + (got.lse * d_lse.cuda()).sum()).backward()
+    y = z.double().cpu().requires_grad_()
+    logp = torch.log_softmax(y / 1.3, 1)
+    p = logp.exp()
+    ent = -(p * logp).sum(1)
+    ((torch.gather(logp, 1, tok) * d_tok.double()).sum()
+     + (torch.gather(logp, 1, at) * d_alt.double()).sum() + (ent * d_ent.double()).sum()
+     + (torch.logsumexp(y / 1.3, 1) * d_lse.double()).sum()).backward()
+    p, logp, ent = p.detach(), logp.detach(), ent.detach()
+    size = p * ((d_tok.abs().sum(1) + d_alt.abs().sum(1) + d_lse.abs())[:, None]
+                + d_ent.abs()[:, None] * (logp.abs() + ent[:, None]))
+    size = size.scatter_add(1, tok, d_tok.abs().double()).scatter_add(1, at, d_alt.abs().double())
+    close(x.grad, y.grad, size / 1.3, dtype)
