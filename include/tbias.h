@@ -521,7 +521,7 @@ int tb_unregister_model_noalloc(tb_registry* r, int32_t id, void* hip_stream);
  *   v_plus_blank  V + 1, in [2, TB_MAX_ROW]: also wider than the step calls take
  *   temperature   in [1e-4, 1e4]
  *   workspace     device, 16-byte aligned, tb_rows_workspace_bytes(...) bytes
- *                 (TB_ENOMEM when smaller); that is 0, and workspace may be
+ *                 (TB_ENOMEM when too small); that is 0, and workspace may be
  *                 NULL, unless rows are cut into segments (never rows of up
  *                 to 16384 values). It is free again once the stream has passed
  *                 the call.
@@ -544,9 +544,9 @@ int tb_unregister_model_noalloc(tb_registry* r, int32_t id, void* hip_stream);
 enum { TB_MAX_LIST = 64, TB_MAX_ROW = 1 << 20 };
 
 /*
- * tb_rows_workspace_bytes — bytes a row operator needs for rows of this type,
- * count and width and n_alt alternatives (0 for the gradients and tb_distill);
- * -1 for arguments the operators reject.
+ * tb_rows_workspace_bytes — bytes that suffice for every row operator on up to
+ * n_rows rows of this type and width, with up to n_alt alternatives (0 for the
+ * gradients and tb_distill); -1 for arguments the operators reject.
  */
 int64_t tb_rows_workspace_bytes(int32_t dtype, int64_t n_rows, int32_t v_plus_blank,
                                 int32_t n_alt);

@@ -1,5 +1,4 @@
 // C ABI shim: synchronous argument checks, then asynchronous launches.
-#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -330,9 +329,7 @@ extern "C" int64_t tb_rows_workspace_bytes(int32_t dtype, int64_t n_rows, int32_
     fail(TB_EINVAL, "bad dtype, n_rows, v_plus_blank or n_alt");
     return -1;
   }
-  return std::max(
-      rows::workspace_bytes(rows::plan(dtype, n_rows, v_plus_blank, false), n_rows, n_alt),
-      rows::workspace_bytes(rows::plan(dtype, n_rows, v_plus_blank, true), n_rows, 0));
+  return rows::most_workspace(dtype, n_rows, v_plus_blank, n_alt);
 }
 
 extern "C" int tb_token_logprobs(const void* logits, int32_t dtype, int64_t n_rows,

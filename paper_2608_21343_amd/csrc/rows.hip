@@ -54,5 +54,19 @@ Plan plan(int32_t dtype, int64_t n_rows, int32_t C, bool grad) {
   return {-1, 0, 0};
 }
 
+int64_t most_workspace(int32_t dtype, int64_t n_rows, int32_t C, int32_t n_alt) {
+  // Fewer rows may be cut into more segments: the last counts before plan() decides
+  // otherwise.
+  int64_t most = 0;
+  for (int64_t n : {n_rows, (int64_t)64, (int64_t)127, (int64_t)511, (int64_t)512, (int64_t)1023}) {
+    n = n < n_rows ? n : n_rows;
+    for (bool grad : {false, true}) {
+      const int64_t b = workspace_bytes(plan(dtype, n, C, grad), n, grad ? 0 : n_alt);
+      most = b > most ? b : most;
+    }
+  }
+  return most;
+}
+
 }  // namespace rows
 }  // namespace tbias

@@ -492,6 +492,8 @@ Plan plan(int32_t dtype, int64_t n_rows, int32_t C, bool grad);
 inline int64_t workspace_bytes(const Plan& p, int64_t n_rows, int32_t n_alt) {
   return p.n_seg > 1 ? n_rows * p.n_seg * (16 + 8 * (int64_t)n_alt) : 0;
 }
+// What suffices for any operator on up to n_rows rows.
+int64_t most_workspace(int32_t dtype, int64_t n_rows, int32_t C, int32_t n_alt);
 
 // Calls f(Int<NWR>, Int<NP>) for an instance.
 template <int N>

@@ -141,3 +141,20 @@ def test_teachers_of_the_rows_shapes_are_taken(entry):
         for weight in (None, torch.ones(lead)):
             with pytest.raises(ValueError, match="device"):
                 entry(torch.zeros(*lead, V1), tok, torch.zeros(*lead, 5), weight=weight)
+
+
+@pytest.mark.parametrize("n_alt", [0, 8, 64])
+@pytest.mark.parametrize("dtype", [capi.TB_F32, capi.TB_BF16])
+@pytest.mark.parametrize("width", [1025, 16388, 20000, 33000, 65540, 131073, 131080, 400003, 1 << 20])
+def test_a_workspace_serves_fewer_rows(dtype, width, n_alt):
+    """Bytes for n rows suffice for any call of up to n rows."""
+    need = [capi.LIB.tb_rows_workspace_bytes(dtype, n, width, n_alt)
+            for n in [*range(0, 2600), 4096, 8192, 1 << 20]]
+    assert need == sorted(need)
+    # cut where there are many rows: those that take more than four waves
+    assert (need[-1] > 0) == (width > (16387 if dtype == capi.TB_F32 else 32775))
+    # and those of fewer alternatives for any call of fewer
+    if n_alt:
+        for n in (1, 64, 65, 512, 513, 600, 4096):
+            assert (capi.LIB.tb_rows_workspace_bytes(dtype, n, width, n_alt - 1)
+                    <= capi.LIB.tb_rows_workspace_bytes(dtype, n, width, n_alt))
