@@ -657,10 +657,12 @@ def _grad_args(grad, logits):
 
 
 def tb_rows_workspace_bytes(logits, n_alt: int = 0) -> int:
-    """Workspace bytes of a row operator on these logits (0: none)."""
+    """Workspace bytes of the row operators on these logits or fewer rows of
+    their width (0: none)."""
     n, V1, _ = _rows(logits)
-    dt, _ = _logits_args(logits) if logits.dim() > 1 else (
-        TB_F32 if logits.dtype == _F32 else TB_BF16, 0)
+    if logits.dtype != _F32 and logits.dtype != _BF16:
+        raise ValueError("logits must be float32 or bfloat16")
+    dt = TB_F32 if logits.dtype == _F32 else TB_BF16
     return int(LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt))
 
 

@@ -158,3 +158,16 @@ def test_a_workspace_serves_fewer_rows(dtype, width, n_alt):
         for n in (1, 64, 65, 512, 513, 600, 4096):
             assert (capi.LIB.tb_rows_workspace_bytes(dtype, n, width, n_alt - 1)
                     <= capi.LIB.tb_rows_workspace_bytes(dtype, n, width, n_alt))
+
+
+def test_workspace_of_a_tensor():
+    """One row as a vector, and types that the operators do not take."""
+    for dtype, code in ((torch.float32, capi.TB_F32), (torch.bfloat16, capi.TB_BF16)):
+        x = torch.zeros(3, 400003, dtype=dtype)
+        for t, n in ((x, 3), (x[0], 1), (x[:, None], 3)):
+            want = capi.LIB.tb_rows_workspace_bytes(code, n, 400003, 5)
+            assert capi.tb_rows_workspace_bytes(t, 5) == want > 0
+        for other in (torch.float16, torch.float64, torch.int32):
+            for t in (x.to(other), x[0].to(other)):
+                with pytest.raises(ValueError, match="float32 or bfloat16"):
+                    capi.tb_rows_workspace_bytes(t, 5)
