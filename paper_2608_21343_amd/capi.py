@@ -663,7 +663,10 @@ def tb_rows_workspace_bytes(logits, n_alt: int = 0) -> int:
     if logits.dtype != _F32 and logits.dtype != _BF16:
         raise ValueError("logits must be float32 or bfloat16")
     dt = TB_F32 if logits.dtype == _F32 else TB_BF16
-    return int(LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt))
+    need = int(LIB.tb_rows_workspace_bytes(dt, n, V1, n_alt))
+    if need < 0:
+        _check(TB_EINVAL)
+    return need
 
 
 def tb_token_logprobs(logits, tokens=None, out_logprob=None, out_lse=None, out_entropy=None,

@@ -171,3 +171,9 @@ def test_workspace_of_a_tensor():
             for t in (x.to(other), x[0].to(other)):
                 with pytest.raises(ValueError, match="float32 or bfloat16"):
                     capi.tb_rows_workspace_bytes(t, 5)
+
+
+def test_workspace_of_arguments_out_of_range():
+    for width, n_alt, word in ((9, 65, "n_alt"), (9, -1, "n_alt"), ((1 << 20) + 1, 0, "v_plus")):
+        with pytest.raises(capi.TbError, match=word):
+            capi.tb_rows_workspace_bytes(torch.zeros(1, width), n_alt)
