@@ -652,6 +652,16 @@ int tb_debug_set_spin_limit(uint32_t polls);
  */
 int tb_debug_launch_empty(int32_t grid, int32_t block, int32_t lds_bytes, void* hip_stream);
 
+/*
+ * tb_debug_rows_plan — the layout that the row operators choose for rows of this
+ * type, count and width, with a gradient (grad = 1) or without: out[0] waves a
+ * row or segment, out[1] pieces of 16 bytes a lane, out[2] segments a row (1:
+ * rows are kept whole). out is host memory. TB_EINVAL for arguments that the
+ * operators reject, and for 0 rows.
+ */
+int tb_debug_rows_plan(int32_t dtype, int64_t n_rows, int32_t v_plus_blank, int32_t grad,
+                       int32_t out[3]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -88,6 +88,7 @@ def _load() -> C.CDLL:
         "tb_debug_select_kernels": [I32, I32],
         "tb_debug_set_spin_limit": [C.c_uint32],
         "tb_debug_launch_empty": [I32, I32, I32, P],
+        "tb_debug_rows_plan": [I32, I64, I32, I32, C.POINTER(I32)],
         "tb_token_logprobs": [P, I32, I64, I32, I64, C.c_float, P, I32, P, P, P, I32, P, P, P, I64,
                               P],
         "tb_token_logprobs_grad": [P, I32, I64, I32, I64, C.c_float, P, I32, P, P, P, P, I64, P,
@@ -142,6 +143,7 @@ EXPORTED = ("tb_compile_graphs", "tb_graphs_layout", "tb_graphs_host_image", "tb
             "tb_graphs_free", "tb_validate_image", "tb_init_states", "tb_boost_step_greedy",
             "tb_boost_step_beam", "tb_reset_stream", "tb_last_error",
             "tb_debug_select_kernels", "tb_debug_set_spin_limit", "tb_debug_launch_empty",
+            "tb_debug_rows_plan",
             "tb_registry_layout", "tb_registry_create", "tb_registry_arena", "tb_registry_model",
             "tb_registry_used_states", "tb_register_models", "tb_unregister_workspace_bytes",
             "tb_unregister_model", "tb_registry_free", "tb_unregister_model_noalloc",
@@ -823,6 +825,14 @@ def tb_debug_select_kernels(greedy: int = GREEDY_AUTO, beam: int = BEAM_AUTO) ->
 def tb_debug_set_spin_limit(polls: int = 0) -> None:
     """Test hook: poll limit of the greedy hand-off wait (0 = default)."""
     _check(LIB.tb_debug_set_spin_limit(polls))
+
+
+def tb_debug_rows_plan(dtype: int, n_rows: int, v_plus_blank: int,
+                       grad: bool = False) -> Tuple[int, int, int]:
+    """(waves a row or segment, pieces a lane, segments a row)."""
+    out = (C.c_int32 * 3)()
+    _check(LIB.tb_debug_rows_plan(dtype, n_rows, v_plus_blank, 1 if grad else 0, out))
+    return tuple(out)
 
 
 def tb_debug_launch_empty(grid: int, block: int, lds_bytes: int = 0, stream=None) -> None:

@@ -332,6 +332,18 @@ extern "C" int64_t tb_rows_workspace_bytes(int32_t dtype, int64_t n_rows, int32_
   return rows::most_workspace(dtype, n_rows, v_plus_blank, n_alt);
 }
 
+extern "C" int tb_debug_rows_plan(int32_t dtype, int64_t n_rows, int32_t v_plus_blank,
+                                  int32_t grad, int32_t out[3]) {
+  if ((dtype != TB_F32 && dtype != TB_BF16) || n_rows < 1 || n_rows > kMaxRows ||
+      v_plus_blank < 2 || v_plus_blank > TB_MAX_ROW || (grad != 0 && grad != 1) || !out)
+    return fail(TB_EINVAL, "bad dtype, n_rows, v_plus_blank, grad or out");
+  const rows::Plan p = rows::plan(dtype, n_rows, v_plus_blank, grad != 0);
+  out[0] = rows::kShape[p.shape].nwr;
+  out[1] = rows::kShape[p.shape].np;
+  out[2] = p.n_seg;
+  return TB_OK;
+}
+
 extern "C" int tb_token_logprobs(const void* logits, int32_t dtype, int64_t n_rows,
                                  int32_t v_plus_blank, int64_t row_stride, float temperature,
                                  const int32_t* tokens, int32_t n_tok, float* out_logprob,
