@@ -1,6 +1,5 @@
 // C ABI shim: synchronous argument checks, then asynchronous launches.
 #include <atomic>
-#include <cmath>
 #include <cstring>
 #include <string>
 

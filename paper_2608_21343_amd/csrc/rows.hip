@@ -42,8 +42,8 @@ Plan plan(int32_t dtype, int64_t n_rows, int32_t C, bool grad) {
     // where they are few, for it reads cut rows twice (one row of 131,073 17 us
     // whole, 15 cut, 128 24 and 24, 2048 227 and more than 300).
     const Shape s = kShape[best];
-    const bool fills = s.nwr == 16 && s.np == 16 && pv == 8;
-    const bool whole = s.nwr < 16 || (grad ? !fills || n_rows > 64 : !fills && n_rows <= 512);
+    const bool all = fills(s, pv);
+    const bool whole = s.nwr < 16 || (grad ? !all || n_rows > 64 : !all && n_rows <= 512);
     if (whole) return {best, 1, C};
   }
   // few rows: short segments on many CUs; many: fewer lists and sums to join

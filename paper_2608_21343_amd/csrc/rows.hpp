@@ -480,6 +480,8 @@ constexpr Shape kShape[kShapes] = {{1, 1}, {1, 2},  {1, 4},  {1, 8},  {1, 16}, {
                                    {4, 8}, {4, 16}, {16, 4}, {16, 8}, {16, 16}};
 // Shapes that the segments of cut rows take.
 constexpr bool cuts(Shape s) { return s.nwr == 4 && s.np >= 8; }
+// bfloat16's largest shape, which plan() takes only where a gradient is written.
+constexpr bool fills(Shape s, int pv) { return s.nwr == 16 && s.np == 16 && pv == 8; }
 
 struct Plan {
   int shape;       // instance of the (whole or cut) rows

@@ -441,10 +441,11 @@ hipError_t score_t(const Rows& a0, const ScoreIO& io, const Plan& p, hipStream_t
           else
             score_kernel<LT, NWR, NP, false, true><<<grid, Pl::kWg, 0, st>>>(a, io);
         }
-      } else if (io.M > 0) {
-        score_kernel<LT, NWR, NP, true, false><<<grid, Pl::kWg, 0, st>>>(a, io);
-      } else {
-        score_kernel<LT, NWR, NP, false, false><<<grid, Pl::kWg, 0, st>>>(a, io);
+      } else if constexpr (!fills(Shape{NWR, NP}, Elem<LT>::PV)) {
+        if (io.M > 0)
+          score_kernel<LT, NWR, NP, true, false><<<grid, Pl::kWg, 0, st>>>(a, io);
+        else
+          score_kernel<LT, NWR, NP, false, false><<<grid, Pl::kWg, 0, st>>>(a, io);
       }
     });
   });
