@@ -177,3 +177,25 @@ def test_workspace_of_arguments_out_of_range():
     for width, n_alt, word in ((9, 65, "n_alt"), (9, -1, "n_alt"), ((1 << 20) + 1, 0, "v_plus")):
         with pytest.raises(capi.TbError, match=word):
             capi.tb_rows_workspace_bytes(torch.zeros(1, width), n_alt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype, width", [(torch.bfloat16, 131073), (torch.float32, 70001)])
+def test_one_workspace_for_several_numbers_of_rows(dtype, width):
+    """Made for the largest batch and used for smaller ones, whose cuts differ."""
+    g = torch.Generator(device="cuda").manual_seed(width)
+    z = torch.randn(600, width, generator=g, device="cuda").to(dtype)
+    work = torch.empty(capi.tb_rows_workspace_bytes(z, 8), dtype=torch.uint8, device="cuda")
+    alt = torch.empty(600, 8, dtype=torch.int32, device="cuda")
+    alt_lp = torch.empty(600, 8, device="cuda")
+    want = torch.topk(z[:512].float(), 8, dim=1).values
+    for n in (600, 513, 512, 64, 1):
+        grad, loss = torch.empty_like(z[:n]), torch.empty(n, device="cuda")
+        capi.tb_token_logprobs(z[:n], out_alt=alt[:n], out_alt_logprob=alt_lp[:n], workspace=work)
+        capi.tb_distill(z[:n], alt[:n], alt_lp[:n], loss, grad, tail=True, workspace=work)
+        m = min(n, 512)
+        # ids of the largest values; equal values in either order
+        got = torch.gather(z[:m].float(), 1, alt[:m].long())
+        assert bool((got == want[:m]).all())
+        assert float(loss.abs().max()) < 3e-5  # a student equal to its teacher
+        assert float(grad.float().abs().max()) < 3e-5
