@@ -608,7 +608,8 @@ int tb_token_logprobs_grad(const void* logits, int32_t dtype, int64_t n_rows,
  *             1 - sum q (0 where that is below 2^-18, the rounding of a list
  *             that sums to 1) and p_r = the sum of p outside the list;
  *             loss = sum_k q_k (log q_k - log p[token_k]) + q_r (log q_r - log p_r);
- *             a p_r of less than 2^-126 of the row's largest p counts as 0
+ *             a p_r of less than 2^-126 of the row's largest p counts as 0 (the
+ *             loss is +inf where q_r is not): a mask of -1e4 is one of -inf here
  *
  *   teacher_tok    device int32[n_rows * n_teacher], teacher_score device float
  *   weight         device float[n_rows], or NULL (1): multiplies the row's loss;
