@@ -19,6 +19,7 @@ import numpy as np  # noqa: E402
 import torch  # noqa: E402
 
 from paper_2608_21343_amd.decoder import BoostDecoder  # noqa: E402
+from paper_2608_21343_amd.optim import AdamW  # noqa: E402
 from paper_2608_21343_amd.rowops import distill_loss, token_scores  # noqa: E402
 
 
@@ -54,7 +55,7 @@ def main(steps: int = 30, B: int = 32, T: int = 64, V: int = 1024, width: int = 
 
     # learn from its alternatives and from what was decoded
     student = torch.zeros((V + 1, width), device="cuda", requires_grad=True)
-    optimizer = torch.optim.Adam([student], lr=0.02)
+    optimizer = AdamW([student], lr=0.02, weight_decay=0.0)
     losses = []
     for step in range(steps):
         z = (frames.reshape(-1, width) @ student.T).view(T, B, V + 1)

@@ -624,6 +624,150 @@ int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus
                float* out_loss, void* grad, int64_t grad_stride, void* workspace,
                int64_t workspace_bytes, void* hip_stream);
 
+/*
+ * Output layer: the cross entropy of a linear layer without its logits. Features
+ * x[n_rows, width], weights w[V+1, width] and a bias b[V+1] (or none) of one type
+ * dtype (TB_F32, TB_BF16) give z = x w^T + b; the logits and their gradients exist in
+ * pieces of the workspace only, never all at once.
+ *
+ *   lse_i  = log sum_c exp z_ic
+ *   loss_i = weight_i (lse_i - z_i,target_i)
+ *   b_i = weight_i d_loss_i, a_i = b_i + d_lse_i,
+ *   G_ic = a_i exp(z_ic - lse_i) - b_i [c = target_i],
+ *   dx = G w, dw = G^T x, db_c = sum_i G_ic
+ *
+ * Arguments shared by both calls
+ *
+ *   x, w          device, row i at i * stride elements (stride >= width), aligned to
+ *                 their type
+ *   bias          device[V+1], or NULL (0)
+ *   n_rows        in [0, 2^24]; width in [1, 2^16]; v_plus_blank in [2, TB_MAX_ROW]
+ *   target        device int32[n_rows]; -1: the row is left out
+ *   weight        device float[n_rows], or NULL (1); 0: the row is left out
+ *   dx, dw, db    device, of type dtype, or NULL; rows of dx and dw at their strides,
+ *                 the values between rows are not touched
+ *   workspace     device, 256-byte aligned, tb_linear_xent_workspace_bytes(...) bytes
+ *                 (TB_ENOMEM when too small). It is free again once the stream has
+ *                 passed the call.
+ *
+ * A row that is left out costs nothing and reaches nothing, whatever its x holds: loss
+ * and lse 0, gradient 0. A target outside [-1, V] is never dereferenced and makes the
+ * row's loss, its dx, and all of dw and db NaN. A token whose bias is -inf has
+ * probability 0; a row without any other has lse -inf, loss +inf and gradient 0. A row
+ * whose logits hold a NaN or +inf has NaN lse, loss and gradients.
+ *
+ * Rounding. Sums are float32. bfloat16 products are exact; the products of float32
+ * operands are those of three bfloat16 planes each, to 2^-25 of the product (values
+ * of 3.39e38 and more count as infinite). The gradients of the logits are rounded once
+ * to dtype's precision, as they would be if they were kept (db is the sum of the
+ * unrounded ones); the results are rounded once to dtype. Results are the same bits
+ * for the same arguments.
+ *
+ * tb_linear_xent_workspace_bytes - for a call with these arguments; grads: sum of 1
+ *   (dx), 2 (dw) and 4 (db), 0 for the loss alone; with_lse: 1 for
+ *   tb_linear_xent_grad, else 0. w is not read: its address and stride say whether its
+ *   rows can be used where they are (16-byte aligned, width a multiple of 64,
+ *   TB_BF16) or need a copy. -1 for arguments that the calls reject.
+ */
+int64_t tb_linear_xent_workspace_bytes(int32_t dtype, int64_t n_rows, int32_t width,
+                                       int32_t v_plus_blank, const void* w, int64_t w_stride,
+                                       int32_t grads, int32_t with_lse);
+
+/*
+ * tb_linear_xent - loss and log-sum-exp of every row, and with dx, dw or db the
+ * gradients of the sum of the losses in the same call (a training step).
+ *
+ *   out_loss, out_lse  device float[n_rows], or NULL
+ */
+int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype,
+                   int64_t n_rows, int32_t width, int32_t v_plus_blank, int64_t x_stride,
+                   int64_t w_stride, const int32_t* target, const float* weight,
+                   float* out_loss, float* out_lse, void* dx, int64_t dx_stride, void* dw,
+                   int64_t dw_stride, void* db, void* workspace, int64_t workspace_bytes,
+                   void* hip_stream);
+
+/*
+ * tb_linear_xent_grad - the gradients of a scalar from its gradients with respect to
+ * loss and lse (a backward pass). lse is what tb_linear_xent gave for the same x, w,
+ * bias, target and weight.
+ *
+ *   lse            device float[n_rows]
+ *   d_loss, d_lse  device float[n_rows], or NULL (1 and 0)
+ *
+ * A row to which no gradient comes is left out as well.
+ */
+int tb_linear_xent_grad(const void* x, const void* w, const void* bias, int32_t dtype,
+                        int64_t n_rows, int32_t width, int32_t v_plus_blank, int64_t x_stride,
+                        int64_t w_stride, const int32_t* target, const float* weight,
+                        const float* lse, const float* d_loss, const float* d_lse, void* dx,
+                        int64_t dx_stride, void* dw, int64_t dw_stride, void* db,
+                        void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * AdamW over many tensors in few launches. Per value, with float32 operations that are
+ * rounded one by one (the constants are float64 expressions, rounded once):
+ *
+ *   g = grad * grad_scale (where that is given)
+ *   m = m * beta1 + g * (1 - beta1)
+ *   v = v * beta2 + g * (1 - beta2) * g
+ *   p = p * (1 - lr * weight_decay)
+ *       - m * (lr / (1 - beta1^step)) / (sqrt(v) * (1 / sqrt(1 - beta2^step)) + eps)
+ *
+ * Parameters and gradients have type dtype. With master copies p is read from and
+ * written to them in float32, and the parameter is their rounding.
+ *
+ * State in 8 bits: 256 neighbouring values share a unit. A code stands for a size: with
+ * P places, code c < 2^P for c, and c = 2^P (r + 1) + i, 0 <= i < 2^P, for
+ * (2^P + i) 2^r. A first moment is sign * size * unit (sign in bit 7, P = 4, sizes up to
+ * 1984), a second one size^2 * unit (P = 5, sizes up to 4032). A step takes the unit from the
+ * block's largest value (times float32 1/1984 or 1/4032^2), multiplies by 1 / unit, and rounds
+ * every value to one of its two neighbours so that its mean is kept, never a second moment
+ * above 0 to 0: value i of tensor k (its index
+ * in the call) is rounded up when its fraction exceeds (r + 0.5) / 65536, r being the low
+ * (first moment) or high (second) 16 bits of
+ * mix(i + mix(mix(seed ^ mix(step)) + k)) modulo 2^32, where
+ * mix(h): h ^= h >> 16; h *= 0x7feb352d; h ^= h >> 15; h *= 0x846ca68b; h ^= h >> 16.
+ * A unit below 2^-100 becomes 0, and the block's moments with it; a block with a value that
+ * is not finite becomes NaN. All zeros are the state before the first step.
+ */
+typedef struct {
+  void* param;       /* device, dtype[n], in/out */
+  const void* grad;  /* device, dtype[n] */
+  void* m;           /* device, float[n] or uint8[n], in/out */
+  void* v;           /* device, as m */
+  float* m_unit;     /* device, float[(n + 255) / 256], in/out; NULL for 32 bits */
+  float* v_unit;     /* device, as m_unit */
+  float* master;     /* device, float[n], in/out; NULL: none */
+  int64_t n;         /* values, in [0, 2^36]; 0: nothing is touched */
+} tb_adamw_tensor;
+
+/*
+ * tb_adamw_step - one step.
+ *
+ *   tensors      host array; all of their buffers aligned to their types (16 bytes are
+ *                faster). None that is written may share memory with another.
+ *   dtype        TB_F32 or TB_BF16 (master copies: TB_BF16 only, for all tensors or none)
+ *   state_bits   32 or 8
+ *   lr, weight_decay, eps >= 0, beta1 and beta2 in [0, 1), step >= 1 (the first is 1)
+ *   lr_dev       device float, or NULL: read instead of lr when the kernels run
+ *   step_dev     device int64, or NULL: read instead of step. A captured graph holds the
+ *                host's values of its capture, so one that is replayed as a training
+ *                loop takes lr and step from the device.
+ *   grad_scale   device float, or NULL: factor of the gradients (clipping)
+ *   seed         of the roundings of 8-bit states
+ *
+ * tb_adamw_moments - the first and second moments that 8-bit states stand for, as
+ * float32: out_m, out_v host arrays of device float[n]. param, grad and master are not
+ * looked at.
+ */
+int tb_adamw_step(const tb_adamw_tensor* tensors, int32_t n_tensors, int32_t dtype,
+                  int32_t state_bits, double lr, double beta1, double beta2, double eps,
+                  double weight_decay, int64_t step, const float* lr_dev,
+                  const int64_t* step_dev, const float* grad_scale, uint32_t seed,
+                  void* hip_stream);
+int tb_adamw_moments(const tb_adamw_tensor* tensors, int32_t n_tensors, float* const* out_m,
+                     float* const* out_v, void* hip_stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* tb_last_error(void);
 

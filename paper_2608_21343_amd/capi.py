@@ -94,6 +94,13 @@ def _load() -> C.CDLL:
         "tb_token_logprobs_grad": [P, I32, I64, I32, I64, C.c_float, P, I32, P, P, P, P, I64, P,
                                    I64, P],
         "tb_distill": [P, I32, I64, I32, I64, C.c_float, P, P, I32, I32, P, P, P, I64, P, I64, P],
+        "tb_linear_xent": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, I64, P, I64, P, P,
+                           I64, P],
+        "tb_linear_xent_grad": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, I64, P,
+                                I64, P, P, I64, P],
+        "tb_adamw_step": [P, I32, I32, I32, C.c_double, C.c_double, C.c_double, C.c_double,
+                          C.c_double, I64, P, P, P, C.c_uint32, P],
+        "tb_adamw_moments": [P, I32, P, P, P],
         "tb_registry_layout": [I32, I64, I32, C.POINTER(tb_arena_layout)],
         "tb_registry_create": [I32, I64, P, I32, P, I64, P, C.POINTER(C.c_void_p)],
         "tb_registry_arena": [P, C.POINTER(tb_arena)],
@@ -124,6 +131,8 @@ def _load() -> C.CDLL:
     lib.tb_unregister_workspace_bytes.argtypes = [P, I32]
     lib.tb_rows_workspace_bytes.restype = C.c_int64
     lib.tb_rows_workspace_bytes.argtypes = [I32, I64, I32, I32]
+    lib.tb_linear_xent_workspace_bytes.restype = C.c_int64
+    lib.tb_linear_xent_workspace_bytes.argtypes = [I32, I64, I32, I32, P, I64, I32, I32]
     lib.tb_last_error.argtypes = []
     lib.tb_last_error.restype = C.c_char_p
     return lib
@@ -151,7 +160,8 @@ EXPORTED = ("tb_compile_graphs", "tb_graphs_layout", "tb_graphs_host_image", "tb
             "tb_graphs_cache_create", "tb_graphs_cache_compile", "tb_graphs_cache_stats",
             "tb_graphs_cache_free", "tb_graphs_save", "tb_graphs_load",
             "tb_rows_workspace_bytes", "tb_token_logprobs", "tb_token_logprobs_grad",
-            "tb_distill")
+            "tb_distill", "tb_linear_xent_workspace_bytes", "tb_linear_xent",
+            "tb_linear_xent_grad", "tb_adamw_step", "tb_adamw_moments")
 
 
 def _check(code: int) -> None:
@@ -566,11 +576,18 @@ _WHOLE_ROW = 1 << 14
 
 def _rows(x, name: str = "logits"):
     """(rows, V+1, row stride) of a tensor [..., V+1] whose rows are evenly spaced."""
+    if x.dim() < 1 or x.shape[-1] < 2:
+        raise ValueError(f"{name} must be [..., V+1] with V+1 >= 2")
+    return _matrix(x, name)
+
+
+def _matrix(x, name: str):
+    """(rows, width, row stride) of a tensor [..., width] whose rows are evenly spaced."""
     shape, strides = x.shape, x.stride()
     n = len(shape)
-    if n < 1 or shape[-1] < 2:
-        raise ValueError(f"{name} must be [..., V+1] with V+1 >= 2")
-    if strides[-1] != 1:
+    if n < 1 or shape[-1] < 1:
+        raise ValueError(f"{name} must be [..., width] with width >= 1")
+    if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name} rows must be contiguous")
     rows, step = 1, None  # (0 is the stride of an expanded dimension)
     if n == 2 and shape[0] > 1:
@@ -726,6 +743,225 @@ def tb_distill(logits, teacher_tok, teacher_score, out_loss=None, grad=None, wei
     _check(LIB.tb_distill(*rows, temperature, p_tok, p_score, K, 1 if tail else 0,
                           _one(weight, n, "weight"), _one(out_loss, n, "out_loss"),
                           *_grad_args(grad, logits), ws, ws_bytes, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# training an output layer
+
+
+class _device_of:
+    """The device of a call's tensors made the current one, where it is not."""
+
+    def __init__(self, t, stream=None):
+        torch = sys.modules["torch"]
+        if not t.is_cuda:
+            raise ValueError("device tensors are needed")
+        index = t.device.index
+        if stream is not None and stream.device.index != index:
+            raise ValueError("the stream is of another device than the tensors")
+        current = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+        self.guard = None if current == index else torch.cuda.device(index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+        return False
+
+
+def _same_device(first, **others) -> None:
+    for name, t in others.items():
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{name} is on {t.device}, x on {first.device}")
+
+
+def _layer(x, w, bias):
+    """(x, w, bias pointers, dtype, rows, width, V+1, strides) of an output layer."""
+    n, D, xs = _matrix(x, "x")
+    if w.dim() != 2 or w.shape[1] != D or w.shape[0] < 2:
+        raise ValueError("w must be [V+1, width] with V+1 >= 2, width that of x")
+    V1, _, ws = _matrix(w, "w")
+    if x.dtype is not _F32 and x.dtype is not _BF16:
+        raise ValueError("x must be float32 or bfloat16")
+    if w.dtype != x.dtype or (bias is not None and bias.dtype != x.dtype):
+        raise ValueError("x, w and bias must have one dtype")
+    if bias is not None and (bias.shape != (V1,) or not bias.is_contiguous()):
+        raise ValueError("bias must be contiguous [V+1]")
+    if not x.is_cuda:
+        raise ValueError("x must be a device tensor")
+    return (x.data_ptr() if n else None, w.data_ptr(),
+            None if bias is None else bias.data_ptr(),
+            TB_F32 if x.dtype is _F32 else TB_BF16, n, D, V1, xs, ws)
+
+
+def _like(t, like, name: str):
+    """(device pointer, row stride) of a gradient of `like` (None passes NULL)."""
+    if t is None:
+        return None, 0
+    if t.dtype != like.dtype or t.shape != like.shape:
+        raise ValueError(f"{name} must have the shape and dtype of what it is the gradient of")
+    n, _, step = _matrix(t, name)
+    return t.data_ptr() if n else None, step
+
+
+def tb_linear_xent_workspace_bytes(x, w, grads: int = 0, with_lse: bool = False) -> int:
+    """Workspace bytes of a call on x [..., width] and w [V+1, width]; grads: sum
+    of 1 (dx), 2 (dw) and 4 (db)."""
+    _, wp, _, dt, n, D, V1, _, ws = _layer(x, w, None)
+    need = int(LIB.tb_linear_xent_workspace_bytes(dt, n, D, V1, wp, ws, grads, int(with_lse)))
+    if need < 0:
+        _check(TB_EINVAL)
+    return need
+
+
+def _linear_workspace(x, layer, dx, dw, db, with_lse, workspace, stream):
+    """(pointer, bytes, tensor): allocated on the call's stream where the caller
+    passed none."""
+    _, wp, _, dt, n, D, V1, _, ws = layer
+    if workspace is None:
+        import torch
+        grads = (dx is not None) + 2 * (dw is not None) + 4 * (db is not None)
+        need = int(LIB.tb_linear_xent_workspace_bytes(dt, n, D, V1, wp, ws, grads, with_lse))
+        if need < 0:
+            _check(TB_EINVAL)
+        with torch.cuda.stream(stream):  # (None: the current one)
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    return (_dptr(workspace, name="workspace"),
+            workspace.numel() * workspace.element_size(), workspace)
+
+
+def _target(target, n: int):
+    if target is None:
+        raise ValueError("target is required")
+    _need(target, n, "target")
+    return _dptr(target, _I32, "target")
+
+
+def tb_linear_xent(x, w, target, out_loss=None, out_lse=None, dx=None, dw=None, db=None,
+                   bias=None, weight=None, workspace=None, stream=None) -> None:
+    """x: [..., width] with evenly spaced rows; w: [V+1, width]; bias [V+1] or None;
+    target, weight, out_loss, out_lse: one value a row; dx, dw, db: like x, w, bias,
+    the gradients of the sum of the losses."""
+    layer = _layer(x, w, bias)
+    n = layer[4]
+    _same_device(x, w=w, bias=bias, target=target, weight=weight, out_loss=out_loss,
+                 out_lse=out_lse, dx=dx, dw=dw, db=db, workspace=workspace)
+    p_db = None if db is None else _like_bias(db, w)
+    with _device_of(x, stream):
+        ws, ws_bytes, keep = _linear_workspace(x, layer, dx, dw, db, 0, workspace, stream)
+        _check(LIB.tb_linear_xent(*layer, _target(target, n), _one(weight, n, "weight"),
+                                  _one(out_loss, n, "out_loss"), _one(out_lse, n, "out_lse"),
+                                  *_like(dx, x, "dx"), *_like(dw, w, "dw"), p_db, ws, ws_bytes,
+                                  _stream(stream)))
+
+
+def _like_bias(db, w):
+    if db.shape != (w.shape[0],):
+        raise ValueError("db must be [V+1]")
+    return _dptr(db, w.dtype, "db")
+
+
+def tb_linear_xent_grad(x, w, target, lse, d_loss=None, d_lse=None, dx=None, dw=None, db=None,
+                        bias=None, weight=None, workspace=None, stream=None) -> None:
+    """Gradients from those of loss and lse; lse: out_lse of tb_linear_xent for the
+    same layer and rows."""
+    layer = _layer(x, w, bias)
+    n = layer[4]
+    _same_device(x, w=w, bias=bias, target=target, weight=weight, lse=lse, d_loss=d_loss,
+                 d_lse=d_lse, dx=dx, dw=dw, db=db, workspace=workspace)
+    if lse is None:
+        raise ValueError("lse is required")
+    p_db = None if db is None else _like_bias(db, w)
+    with _device_of(x, stream):
+        ws, ws_bytes, keep = _linear_workspace(x, layer, dx, dw, db, 1, workspace, stream)
+        _check(LIB.tb_linear_xent_grad(*layer, _target(target, n), _one(weight, n, "weight"),
+                                       _one(lse, n, "lse"), _one(d_loss, n, "d_loss"),
+                                       _one(d_lse, n, "d_lse"), *_like(dx, x, "dx"),
+                                       *_like(dw, w, "dw"), p_db, ws, ws_bytes, _stream(stream)))
+
+
+_ADAMW_FIELDS = ("param", "grad", "m", "v", "m_unit", "v_unit", "master")
+
+
+def _adamw_table(lists, count: int, device):
+    """tb_adamw_tensor records as an array of words, from lists of tensors by field
+    (None: NULL)."""
+    table = np.zeros((count, 8), dtype=np.int64)
+    for name, dtype, tensors, sizes in lists:
+        if tensors is None:
+            continue
+        if len(tensors) != count:
+            raise ValueError(f"{name} holds {len(tensors)} tensors, needs {count}")
+        for i, t in enumerate(tensors):
+            if (t.dtype is not dtype or t.device != device or not t.is_contiguous()
+                    or t.numel() != sizes[i]):  # the first fault
+                if t.device != device:
+                    raise ValueError(f"{name}[{i}] must be on {device}")
+                _need(t, sizes[i], f"{name}[{i}]")
+                _dptr(t, dtype, f"{name}[{i}]")
+        table[:, _ADAMW_FIELDS.index(name)] = [t.data_ptr() for t in tensors]
+    return table
+
+
+def tb_adamw_step(param, grad, m, v, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                  eps: float = 1e-8, weight_decay: float = 0.01, step: int = 1, master=None,
+                  m_unit=None, v_unit=None, seed: int = 0, lr_dev=None, step_dev=None,
+                  grad_scale=None, stream=None) -> None:
+    """One step of lists of contiguous tensors: param and grad float32 or bfloat16;
+    m and v float32, or uint8 with m_unit and v_unit (float32, one value per 256);
+    master: float32 copies of bfloat16 parameters. lr_dev (float32), step_dev
+    (int64) and grad_scale (float32): device tensors of one value or None."""
+    import torch
+    count = len(param)
+    if count == 0:
+        return
+    if (m_unit is None) != (v_unit is None):
+        raise ValueError("m_unit and v_unit belong together")
+    device, dtype = param[0].device, param[0].dtype
+    if dtype is not _F32 and dtype is not _BF16:
+        raise ValueError("parameters must be float32 or bfloat16")
+    bits = 32 if m_unit is None else 8
+    state = _F32 if bits == 32 else torch.uint8
+    sizes = [t.numel() for t in param]
+    units = None if bits == 32 else [(n + 255) // 256 for n in sizes]
+    table = _adamw_table((("param", dtype, param, sizes), ("grad", dtype, grad, sizes),
+                          ("m", state, m, sizes), ("v", state, v, sizes),
+                          ("m_unit", _F32, m_unit, units), ("v_unit", _F32, v_unit, units),
+                          ("master", _F32, master, sizes)), count, device)
+    table[:, 7] = sizes
+    for name, t in (("lr_dev", lr_dev), ("step_dev", step_dev), ("grad_scale", grad_scale)):
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} must be on {device}")
+    with _device_of(param[0], stream):
+        _check(LIB.tb_adamw_step(_np_ptr(table), count, TB_F32 if dtype is _F32 else TB_BF16, bits,
+                                 lr, beta1, beta2, eps, weight_decay, step,
+                                 _one(lr_dev, 1, "lr_dev"), _dptr(step_dev, torch.int64, "step_dev"),
+                                 _one(grad_scale, 1, "grad_scale"), seed & 0xffffffff,
+                                 _stream(stream)))
+
+
+def tb_adamw_moments(m, v, m_unit, v_unit, out_m, out_v, stream=None) -> None:
+    """The moments that 8-bit states stand for: lists of uint8 tensors, their units,
+    and float32 tensors of the same sizes."""
+    import torch
+    count = len(m)
+    if count == 0:
+        return
+    device = m[0].device
+    sizes = [t.numel() for t in m]
+    units = [(n + 255) // 256 for n in sizes]
+    table = _adamw_table((("m", torch.uint8, m, sizes), ("v", torch.uint8, v, sizes),
+                          ("m_unit", _F32, m_unit, units), ("v_unit", _F32, v_unit, units)),
+                         count, device)
+    table[:, 7] = sizes
+    outs = _adamw_table((("m", _F32, out_m, sizes), ("v", _F32, out_v, sizes)), count, device)
+    to_m, to_v = np.ascontiguousarray(outs[:, 2]), np.ascontiguousarray(outs[:, 3])
+    with _device_of(m[0], stream):
+        _check(LIB.tb_adamw_moments(_np_ptr(table), count, _np_ptr(to_m), _np_ptr(to_v),
+                                    _stream(stream)))
 
 
 def tb_reset_stream(arena: Arena, b: int, new_model_id: int, K: int, model_ids, states,

@@ -1,0 +1,448 @@
+// AdamW over many tensors. A value costs its bytes: parameter, gradient and moments
+// are read once and written once, with the arithmetic between in registers.
+//
+// Moments in 8 bits are sizes times a unit that 256 neighbouring values share (two
+// floats for 512 bytes of codes). A size has runs of 2^P codes whose step doubles from
+// the second run on, so its error is about even over three decades: P = 4 and a sign
+// for the first moment, sizes up to 1984; P = 5 for the root of the second, up to
+// 4032 (the second moment itself is size^2 times the unit). A step changes a second
+// moment by one part in a thousand, far less than half a code: rounded to the nearest
+// one it would never move. So a moment goes to either neighbour with the probability
+// that keeps its mean, from 16 bits that a hash makes of seed, step, tensor and place.
+// A second moment above 0 never becomes 0, which would make the next step a large one.
+//
+// The products and sums are rounded one by one, in float32, as the interface states them,
+// so the codes are the same wherever the same arithmetic runs.
+#include "adamw.hpp"
+
+#include <cmath>
+
+namespace tbias {
+namespace adamw {
+
+namespace {
+
+constexpr int kThreads = 256, kEach = 8;           // values of a lane at a time
+constexpr int kChunk = kThreads * kEach * 4;       // values of a workgroup
+constexpr float kTopM = 1.f / 1984.f, kTopV = 1.f / 16257024.f;  // 1 / largest size, 1 / its square
+
+struct Rec {
+  void* param;
+  const void* grad;
+  void *m, *v;
+  float *m_unit, *v_unit;
+  float* master;
+  int64_t n;
+};
+
+struct Args {
+  Rec rec[kMost];
+  int32_t end[kMost];    // chunks up to and with a tensor
+  int32_t index[kMost];  // of a tensor in the call
+  int32_t count;
+  float decay, size, root, b1, c1, b2, c2, eps;
+  uint32_t key;
+  double lr, beta1, beta2, weight_decay;
+  const float* lr_dev;
+  const int64_t* step_dev;
+  const float* grad_scale;
+  int64_t step;
+  uint32_t seed;
+};
+static_assert(sizeof(Args) <= 4096, "kernel arguments");
+
+__host__ __device__ inline uint32_t mix(uint32_t h) {
+  h ^= h >> 16;
+  h *= 0x7feb352du;
+  h ^= h >> 15;
+  h *= 0x846ca68bu;
+  return h ^ (h >> 16);
+}
+
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+__device__ __forceinline__ uint16_t to_bf16(float v) {
+  return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+__device__ __forceinline__ void load8(const float* p, bool vec, int left, float* v) {
+  if (vec && left >= 8) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? p[e] : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, bool vec, int left, float* v) {
+  if (vec && left >= 8) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __uint_as_float(w[e] << 16);
+      v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? __uint_as_float((uint32_t)p[e] << 16) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(float* p, bool vec, int left, const float* v) {
+  if (vec && left >= 8) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = v[e];
+  }
+}
+__device__ __forceinline__ void store8(uint16_t* p, bool vec, int left, const float* v) {
+  if (vec && left >= 8) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x2 x = {v[2 * e], v[2 * e + 1]};
+      w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = to_bf16(v[e]);
+  }
+}
+__device__ __forceinline__ void load8(const uint8_t* p, bool vec, int left, uint32_t* c) {
+  if (vec && left >= 8) {
+    const uint2 a = *reinterpret_cast<const uint2*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      c[e] = (a.x >> (8 * e)) & 255;
+      c[e + 4] = (a.y >> (8 * e)) & 255;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = e < left ? p[e] : 0;
+  }
+}
+__device__ __forceinline__ void store8(uint8_t* p, bool vec, int left, const uint32_t* c) {
+  if (vec && left >= 8) {
+    uint2 a = make_uint2(0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a.x |= c[e] << (8 * e);
+      a.y |= c[e + 4] << (8 * e);
+    }
+    *reinterpret_cast<uint2*>(p) = a;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = (uint8_t)c[e];
+  }
+}
+
+template <int P>
+__device__ __forceinline__ float size_of(uint32_t code) {
+  const int e = max((int)(code >> P) - 1, 0);
+  return (float)((code - ((uint32_t)e << P)) << e);
+}
+__device__ __forceinline__ float decode_m(uint32_t code, float unit) {
+  const float s = size_of<4>(code & 127) * unit;
+  return code >= 128 ? -s : s;
+}
+__device__ __forceinline__ float decode_v(uint32_t code, float unit) {
+  const float s = size_of<5>(code);
+  return s * s * unit;
+}
+
+// The run of a size: e with size * 2^-e below 2^(P + 1), and 2^-e.
+template <int P>
+__device__ __forceinline__ int run_of(float size, float* scale) {
+  const int e = max((int)(__float_as_uint(size) >> 23) - 127 - P, 0);
+  *scale = __uint_as_float((uint32_t)(127 - e) << 23);
+  return e;
+}
+
+__device__ __forceinline__ uint32_t encode_m(float m, float inverse, float rnd) {
+  const float y = fabsf(m) * inverse;
+  float scale;
+  const int e = run_of<4>(y, &scale);
+  const float q = y * scale, low = floorf(q);
+  const int code = (e << 4) + (int)low + (q - low > rnd ? 1 : 0);
+  return (uint32_t)min(code, 127) + (m < 0.f ? 128u : 0u);
+}
+__device__ __forceinline__ uint32_t encode_v(float v, float inverse, float rnd) {
+  const float y = v * inverse, root = sqrtf(y);
+  float scale;
+  const int e = run_of<5>(root, &scale);
+  const float low = floorf(root * scale);
+  const bool more = y * scale * scale - low * low > (2.f * low + 1.f) * rnd;
+  const int code = (e << 5) + (int)low + (more ? 1 : 0);
+  return v > 0.f ? (uint32_t)min(max(code, 1), 255) : 0u;
+}
+
+// Largest of the 32 lanes that hold a block.
+__device__ __forceinline__ float block_max(float v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+// The unit of a block; NaN where it holds a value that is not finite.
+__device__ __forceinline__ float unit_of(float most, float top, bool bad) {
+  const float unit = most * top;
+  return bad ? __builtin_nanf("") : unit >= 0x1p-100f ? unit : 0.f;
+}
+
+// The tensor of a chunk: the first whose end is behind it.
+template <class A>
+__device__ __forceinline__ int find(const A& a, int chunk) {
+  const int lane = threadIdx.x & 63;
+  const bool before = lane < a.count && a.end[min(lane, kMost - 1)] <= chunk;
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(before)));
+}
+
+__device__ __forceinline__ bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+struct Consts {
+  float decay, size, root;
+  uint32_t key;
+};
+
+__host__ __device__ inline Consts consts(double lr, double beta1, double beta2, double wd,
+                                         int64_t step, uint32_t seed) {
+  Consts c;
+  c.decay = (float)(1.0 - lr * wd);
+  c.size = (float)(lr / (1.0 - pow(beta1, (double)step)));
+  c.root = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
+  c.key = mix(seed ^ mix((uint32_t)step));
+  return c;
+}
+
+template <class T, int BITS, bool MASTER>
+__global__ void __launch_bounds__(kThreads) step_kernel(const Args a) {
+  const int chunk = blockIdx.x;
+  const int k = find(a, chunk);
+  const Rec r = a.rec[k];
+  const int begin = k ? a.end[k - 1] : 0;
+
+  Consts c = {a.decay, a.size, a.root, a.key};
+  if (a.lr_dev || a.step_dev) {
+    __shared__ Consts shared;
+    if (threadIdx.x == 0)
+      shared = consts(a.lr_dev ? (double)*a.lr_dev : a.lr, a.beta1, a.beta2, a.weight_decay,
+                      a.step_dev ? *a.step_dev : a.step, a.seed);
+    __syncthreads();
+    c = shared;
+  }
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
+  const uint32_t key = mix(c.key + (uint32_t)a.index[k]);
+  const bool vec = on16(r.param) && on16(r.grad) && on16(r.m) && on16(r.v) &&
+                   (!MASTER || on16(r.master));
+
+#pragma unroll 1
+  for (int it = 0; it < kChunk / (kThreads * kEach); ++it) {
+    const int64_t i = (int64_t)(chunk - begin) * kChunk + it * (kThreads * kEach) +
+                      (int64_t)threadIdx.x * kEach;
+    const int left = (int)min((int64_t)kEach, max((int64_t)0, r.n - i));
+    const int64_t at = left > 0 ? i : 0;  // (no address behind the end)
+    float p[8], g[8], m[8], v[8];
+    if (MASTER) load8(r.master + at, vec, left, p);
+    else load8(static_cast<const T*>(r.param) + at, vec, left, p);
+    load8(static_cast<const T*>(r.grad) + at, vec, left, g);
+    if constexpr (BITS == 32) {
+      load8(static_cast<const float*>(r.m) + at, vec, left, m);
+      load8(static_cast<const float*>(r.v) + at, vec, left, v);
+    } else {
+      uint32_t cm[8], cv[8];
+      load8(static_cast<const uint8_t*>(r.m) + at, vec, left, cm);
+      load8(static_cast<const uint8_t*>(r.v) + at, vec, left, cv);
+      const float um = r.m_unit[at / kBlock], uv = r.v_unit[at / kBlock];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        m[e] = decode_m(cm[e], um);
+        v[e] = decode_v(cv[e], uv);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float ge = a.grad_scale ? g[e] * gs : g[e];
+      m[e] = m[e] * a.b1 + ge * a.c1;
+      v[e] = v[e] * a.b2 + ge * a.c2 * ge;
+      p[e] = p[e] * c.decay - m[e] * c.size / (sqrtf(v[e]) * c.root + a.eps);
+    }
+    store8(static_cast<T*>(r.param) + at, vec, left, p);
+    if (MASTER) store8(r.master + at, vec, left, p);
+    if constexpr (BITS == 32) {
+      store8(static_cast<float*>(r.m) + at, vec, left, m);
+      store8(static_cast<float*>(r.v) + at, vec, left, v);
+    } else {
+      float top_m = 0.f, top_v = 0.f;
+      bool bad_m = false, bad_v = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (e >= left) m[e] = v[e] = 0.f;
+        top_m = fmaxf(top_m, fabsf(m[e]));
+        top_v = fmaxf(top_v, v[e]);
+        bad_m |= !(fabsf(m[e]) < __builtin_huge_valf());
+        bad_v |= !(v[e] < __builtin_huge_valf());
+      }
+      const int half = threadIdx.x & 32;
+      const bool any_m = (uint32_t)(__ballot(bad_m) >> half) != 0;
+      const bool any_v = (uint32_t)(__ballot(bad_v) >> half) != 0;
+      const float um = unit_of(block_max(top_m), kTopM, any_m);
+      const float uv = unit_of(block_max(top_v), kTopV, any_v);
+      const float im = um > 0.f ? 1.f / um : 0.f, iv = uv > 0.f ? 1.f / uv : 0.f;
+      uint32_t cm[8], cv[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = mix((uint32_t)(at + e) + key);
+        cm[e] = encode_m(m[e], im, ((float)(bits & 0xffff) + 0.5f) * 0x1p-16f);
+        cv[e] = encode_v(v[e], iv, ((float)(bits >> 16) + 0.5f) * 0x1p-16f);
+      }
+      store8(static_cast<uint8_t*>(r.m) + at, vec, left, cm);
+      store8(static_cast<uint8_t*>(r.v) + at, vec, left, cv);
+      if ((threadIdx.x & 31) == 0 && left > 0) {
+        r.m_unit[at / kBlock] = um;
+        r.v_unit[at / kBlock] = uv;
+      }
+    }
+  }
+}
+
+struct ReadRec {
+  const uint8_t *m, *v;
+  const float *m_unit, *v_unit;
+  float *out_m, *out_v;
+  int64_t n;
+};
+struct ReadArgs {
+  ReadRec rec[kMost];
+  int32_t end[kMost];
+  int32_t count;
+};
+static_assert(sizeof(ReadArgs) <= 4096, "kernel arguments");
+
+__global__ void __launch_bounds__(kThreads) moments_kernel(const ReadArgs a) {
+  const int chunk = blockIdx.x;
+  const int k = find(a, chunk);
+  const ReadRec r = a.rec[k];
+  const int begin = k ? a.end[k - 1] : 0;
+  const bool vec = on16(r.m) && on16(r.v) && on16(r.out_m) && on16(r.out_v);
+#pragma unroll 1
+  for (int it = 0; it < kChunk / (kThreads * kEach); ++it) {
+    const int64_t i = (int64_t)(chunk - begin) * kChunk + it * (kThreads * kEach) +
+                      (int64_t)threadIdx.x * kEach;
+    if (i >= r.n) return;
+    const int left = (int)min((int64_t)kEach, r.n - i);
+    uint32_t cm[8], cv[8];
+    load8(r.m + i, vec, left, cm);
+    load8(r.v + i, vec, left, cv);
+    const float um = r.m_unit[i / kBlock], uv = r.v_unit[i / kBlock];
+    float m[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      m[e] = decode_m(cm[e], um);
+      v[e] = decode_v(cv[e], uv);
+    }
+    store8(r.out_m + i, vec, left, m);
+    store8(r.out_v + i, vec, left, v);
+  }
+}
+
+template <class T, int BITS, bool MASTER>
+void launch(const Args& a, int64_t chunks, hipStream_t st) {
+  step_kernel<T, BITS, MASTER><<<dim3((unsigned)chunks), dim3(kThreads), 0, st>>>(a);
+}
+
+// Groups of up to kMost tensors whose chunks make a launch: put(k, i) takes tensor i as
+// the k-th of a group, go(k, chunks) launches it.
+template <class Put, class Go>
+hipError_t groups(const tb_adamw_tensor* t, int32_t n, Put put, Go go) {
+  const int64_t most = most_groups(kThreads);
+  int32_t k = 0;
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (t[i].n == 0) continue;
+    const int64_t c = (t[i].n + kChunk - 1) / kChunk;
+    if (k == kMost || chunks + c > most) {
+      if (k > 0) go(k, chunks);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      k = 0;
+      chunks = 0;
+    }
+    chunks += c;
+    put(k++, i, (int32_t)chunks);
+  }
+  if (k > 0) go(k, chunks);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t step(const tb_adamw_tensor* t, int32_t n, const Step& s, hipStream_t st) {
+  Args a = {};
+  const Consts c = consts(s.lr, s.beta1, s.beta2, s.weight_decay, s.step, s.seed);
+  a.decay = c.decay;
+  a.size = c.size;
+  a.root = c.root;
+  a.key = c.key;
+  a.b1 = (float)s.beta1;
+  a.c1 = (float)(1.0 - s.beta1);
+  a.b2 = (float)s.beta2;
+  a.c2 = (float)(1.0 - s.beta2);
+  a.eps = (float)s.eps;
+  a.lr = s.lr;
+  a.beta1 = s.beta1;
+  a.beta2 = s.beta2;
+  a.weight_decay = s.weight_decay;
+  a.lr_dev = s.lr_dev;
+  a.step_dev = s.step_dev;
+  a.grad_scale = s.grad_scale;
+  a.step = s.step;
+  a.seed = s.seed;
+  return groups(
+      t, n,
+      [&](int32_t k, int32_t i, int32_t end) {
+        a.rec[k] = {t[i].param, t[i].grad, t[i].m, t[i].v, t[i].m_unit, t[i].v_unit,
+                    t[i].master, t[i].n};
+        a.end[k] = end;
+        a.index[k] = i;
+      },
+      [&](int32_t k, int64_t chunks) {
+        a.count = k;
+        if (s.dtype == TB_F32) {
+          if (s.bits == 32) launch<float, 32, false>(a, chunks, st);
+          else launch<float, 8, false>(a, chunks, st);
+        } else if (s.master) {
+          if (s.bits == 32) launch<uint16_t, 32, true>(a, chunks, st);
+          else launch<uint16_t, 8, true>(a, chunks, st);
+        } else {
+          if (s.bits == 32) launch<uint16_t, 32, false>(a, chunks, st);
+          else launch<uint16_t, 8, false>(a, chunks, st);
+        }
+      });
+}
+
+hipError_t moments(const tb_adamw_tensor* t, int32_t n, float* const* out_m, float* const* out_v,
+                   hipStream_t st) {
+  ReadArgs a = {};
+  return groups(
+      t, n,
+      [&](int32_t k, int32_t i, int32_t end) {
+        a.rec[k] = {static_cast<const uint8_t*>(t[i].m), static_cast<const uint8_t*>(t[i].v),
+                    t[i].m_unit, t[i].v_unit, out_m[i], out_v[i], t[i].n};
+        a.end[k] = end;
+      },
+      [&](int32_t k, int64_t chunks) {
+        a.count = k;
+        moments_kernel<<<dim3((unsigned)chunks), dim3(kThreads), 0, st>>>(a);
+      });
+}
+
+}  // namespace adamw
+}  // namespace tbias

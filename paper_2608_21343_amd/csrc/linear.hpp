@@ -1,0 +1,113 @@
+// Cross entropy of a linear layer without its logits: what the kernels share.
+//
+//   z = x w^T + b, lse_i = log sum_c exp z_ic, loss_i = weight_i (lse_i - z_i,t(i)),
+//   G_ic = a_i exp(z_ic - lse_i) - b_i [c = t(i)], dx = G w, dw = G^T x, db = sum_i G_i
+//
+// with b_i = weight_i d_loss_i and a_i = b_i + d_lse_i. All four products run on the
+// matrix cores as 16-bit operands with float32 sums (linear_gemm.hpp). bfloat16
+// operands are taken as they are. A float32 operand is the sum of three bfloat16
+// planes (each the rounding of what the ones before leave: 3 x 8 bits and their
+// signs hold the 24 of a float32), and a product of two of them is the sum of six
+// products of planes; the three left out are below 2^-26 of it.
+//
+// Rows that take part (target not -1, weight not 0) are gathered first, so that the
+// others cost nothing and whatever they hold reaches no sum. Rows of the gathered
+// matrix end at a multiple of 64 values, and its rows at one of 256, with zeros.
+#pragma once
+
+#include "device.hpp"
+#include "launch.hpp"
+
+namespace tbias {
+namespace linear {
+
+constexpr int kStep = 64;    // values of the summed axis that a tile takes at a time
+constexpr int kTile = 256;   // rows and columns of a tile
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__host__ __device__ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// Left by the gathering of the rows, read by every later kernel.
+struct Meta {
+  int32_t n;       // gathered rows
+  // G is kept divided by the largest finite |a_i|, |b_i|: with equal weights, as the mean
+  // over a batch has, the target's entry p - 1 is then rounded near 1 and not every
+  // row's by the same part of the weight (up to 2^-8, which no sum averages out)
+  float scale;
+  float inverse;
+};
+
+// A matrix as 16-bit planes. Element (i, k) of a plane, k the summed axis, lies at
+// i * ld + k, or (transposed) at k * ld + i. i < n and k < kn are in memory; a row
+// ends at a multiple of 8 elements, 16-byte aligned.
+struct Operand {
+  const uint16_t* p;
+  int64_t plane, ld;
+  int32_t n, kn;
+};
+
+// Per gathered row.
+struct RowArgs {
+  const int32_t* target;  // -1: none in range
+  const float *a, *b, *lse;
+};
+
+struct Gemm {
+  Operand P, Q;  // result element (p, q): sum over k of P(p, k) Q(q, k)
+  const Meta* meta;
+  int32_t tp, tq, splits;
+  int32_t k;       // length of the summed axis, a multiple of kStep
+  int32_t n_q;     // columns of the result that are kept
+  // statistics and gradients of the logits
+  const void* bias;
+  int32_t C, c0;   // tokens, and the first of P
+  RowArgs row;
+  float2* part;    // [gathered row, n_part]: maximum, sum
+  int32_t n_part;
+  float* hit;      // logit of the row's target
+  uint16_t* G;     // planes of [row, ldg]
+  int64_t g_plane;
+  int32_t ldg;
+  float* col;      // [row groups of 64, ldg], or NULL
+  // products with the gradients
+  float* acc;      // [split, n_q, lda]
+  int64_t acc_split;
+  int32_t lda, add;
+  void* out;       // or the result itself: [q, ldo], D values
+  int64_t ldo;
+  int32_t D;
+};
+
+enum { kStats, kLogitGrad, kDx, kDw };
+
+// One launch of tp * tq * splits tiles.
+hipError_t stats_bf16(const Gemm& g, hipStream_t st);
+hipError_t stats_f32(const Gemm& g, hipStream_t st);
+hipError_t logit_grad_bf16(const Gemm& g, hipStream_t st);
+hipError_t logit_grad_f32(const Gemm& g, hipStream_t st);
+hipError_t dx_bf16(const Gemm& g, hipStream_t st);
+hipError_t dx_f32(const Gemm& g, hipStream_t st);
+hipError_t dw_bf16(const Gemm& g, hipStream_t st);
+hipError_t dw_f32(const Gemm& g, hipStream_t st);
+
+// A call, after its checks.
+struct Call {
+  const void *x, *w, *bias;
+  int32_t dtype;
+  int64_t n;
+  int32_t D, C;
+  int64_t x_stride, w_stride;
+  const int32_t* target;
+  const float *weight, *d_loss, *d_lse;
+  const float* lse;  // of an earlier call, or NULL: computed here
+  float *out_loss, *out_lse;
+  void *dx, *dw, *db;
+  int64_t dx_stride, dw_stride;
+};
+
+// Bytes of workspace, and the launches of a call.
+int64_t workspace_bytes(const Call& c);
+hipError_t run(const Call& c, void* workspace, hipStream_t st);
+
+}  // namespace linear
+}  // namespace tbias

@@ -1,0 +1,474 @@
+"""AdamW over many tensors: every bit against the interface's formulas in numpy
+float32, and the optimizer against torch's own in float64."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+f = np.float32
+
+
+def mix(h):
+    h = np.asarray(h, dtype=np.uint32)
+    with np.errstate(over="ignore"):
+        h = h ^ (h >> np.uint32(16))
+        h = h * np.uint32(0x7feb352d)
+        h = h ^ (h >> np.uint32(15))
+        h = h * np.uint32(0x846ca68b)
+        return h ^ (h >> np.uint32(16))
+
+
+def size(code, places):
+    code = np.asarray(code, dtype=np.int64)
+    run = 1 << places
+    low = code % run
+    at = code // run
+    return np.where(at == 0, low, (run + low) * 2.0 ** (at - 1)).astype(f)
+
+
+def blocks(unit, n):
+    return np.repeat(unit, 256)[:n]
+
+
+def decode(m, v, um, uv):
+    s = size(m & 127, 4) * blocks(um, len(m))
+    r = size(v, 5)
+    return np.where(m >= 128, -s, s).astype(f), (r * r * blocks(uv, len(v))).astype(f)
+
+
+def unit(x, top):
+    n = len(x)
+    x = np.concatenate([x, np.zeros(-n % 256, f)]).reshape(-1, 256)
+    u = x.max(1) * (f(1) / f(top))
+    u = np.where(u >= f(2.0 ** -100), u, f(0))
+    return np.where(np.isfinite(x).all(1), u, f(math.nan)).astype(f)
+
+
+def encode(x, top, places, rnd):
+    """Codes of sizes (places 4) or of squares of sizes (places 5)."""
+    u = unit(np.abs(x), top)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        inv = np.where(u > 0, f(1) / u, f(0)).astype(f)
+    y = np.abs(x) * blocks(inv, len(x))
+    root = y if places == 4 else np.sqrt(y)
+    e = np.maximum(np.frexp(root)[1] - 1 - places, 0)
+    e = np.where(root > 0, e, 0)
+    scale = (f(2) ** -e.astype(f)).astype(f)
+    low = np.floor(root * scale)
+    if places == 4:
+        more = y * scale - low > rnd
+    else:
+        more = y * scale * scale - low * low > (f(2) * low + f(1)) * rnd
+    return (e << places) + low.astype(np.int64) + more, u
+
+
+def formula(p, g, m, v, lr, beta1, beta2, eps, weight_decay, step, k=0, seed=0, units=None):
+    """One step of one tensor, float32 operation by operation."""
+    n = len(p)
+    if units is not None:
+        m, v = decode(m, v, *units)
+    m = m * f(beta1) + g * f(1 - beta1)
+    v = v * f(beta2) + g * f(1 - beta2) * g
+    p = p * f(1 - lr * weight_decay) - m * f(lr / (1 - beta1 ** step)) / (
+        np.sqrt(v) * f(1 / math.sqrt(1 - beta2 ** step)) + f(eps))
+    if units is None:
+        return p, m, v, None, None
+    with np.errstate(over="ignore"):
+        key = mix(mix(np.uint32(seed) ^ mix(step)) + np.uint32(k))
+        bits = mix(np.arange(n, dtype=np.uint32) + key)
+    low = ((bits & np.uint32(0xffff)).astype(f) + f(0.5)) * f(2.0 ** -16)
+    high = ((bits >> np.uint32(16)).astype(f) + f(0.5)) * f(2.0 ** -16)
+    cm, um = encode(m, 1984, 4, low)
+    cv, uv = encode(v, 16257024, 5, high)
+    cm = np.minimum(cm, 127) + np.where(m < 0, 128, 0)
+    cv = np.where(v > 0, np.clip(cv, 1, 255), 0)
+    return p, cm.astype(np.uint8), cv.astype(np.uint8), um, uv
+
+
+HOW = dict(lr=2e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.02)
+
+
+def tensors(sizes, dtype, bits, master, seed=0, pad=0):
+    """Lists of tensors, `pad` values behind an aligned address."""
+    g = torch.Generator().manual_seed(seed)
+
+    def place(t, dtype):
+        at = torch.zeros(t.numel() + pad + 8, dtype=dtype, device="cuda")
+        at[:] = 99
+        view = at[pad:pad + t.numel()]
+        view.copy_(t)
+        return view
+
+    s = dict(param=[], grad=[], m=[], v=[], master=[] if master else None, m_unit=None, v_unit=None)
+    if bits == 8:
+        s.update(m_unit=[], v_unit=[])
+    for n in sizes:
+        p = torch.randn(n, generator=g)
+        spread = torch.exp(2 * torch.randn(n, generator=g)) * 1e-3
+        spread[torch.rand(n, generator=g) < 0.05] = 0
+        s["param"].append(place(p, dtype))
+        s["grad"].append(place(torch.randn(n, generator=g) * spread, dtype))
+        if master:
+            s["master"].append(place(p, F32))
+        if bits == 32:
+            s["m"].append(place(torch.randn(n, generator=g) * spread, F32))
+            s["v"].append(place(spread * spread, F32))
+        else:
+            s["m"].append(place(torch.randint(0, 256, (n,), generator=g), torch.uint8))
+            s["v"].append(place(torch.randint(0, 256, (n,), generator=g), torch.uint8))
+            units = (n + 255) // 256
+            s["m_unit"].append(torch.rand(units, generator=g).cuda() * 1e-5)
+            s["v_unit"].append(torch.rand(units, generator=g).cuda() * 1e-12)
+    return s
+
+
+def host(t):
+    return t.float().cpu().numpy() if t.dtype != torch.uint8 else t.cpu().numpy()
+
+
+def compare(before, s, step, seed=0, how=HOW, scale=None):
+    for k, p in enumerate(before["param"]):
+        units = None
+        if s["m_unit"] is not None:
+            units = host(before["m_unit"][k]), host(before["v_unit"][k])
+        start = before["master"][k] if s["master"] else p
+        g = host(before["grad"][k])
+        if scale is not None:
+            g = g * f(scale)
+        want, m, v, um, uv = formula(host(start), g, host(before["m"][k]), host(before["v"][k]),
+                                     **how, step=step, k=k, seed=seed, units=units)
+        rounded = torch.from_numpy(want).to(p.dtype)
+        same(host(s["param"][k]), rounded.float().numpy(), f"param {k}")
+        if s["master"]:
+            same(host(s["master"][k]), want, f"master {k}")
+        same(host(s["m"][k]), m, f"m {k}")
+        same(host(s["v"][k]), v, f"v {k}")
+        if units is not None:
+            same(host(s["m_unit"][k]), um, f"m_unit {k}")
+            same(host(s["v_unit"][k]), uv, f"v_unit {k}")
+
+
+def same(a, b, name):
+    assert np.array_equal(a, b, equal_nan=a.dtype != np.uint8), (
+        name, int((a != b).sum()), a[a != b][:4], b[a != b][:4])
+
+
+def copies(s):
+    return {k: None if v is None else [t.clone() for t in v] for k, v in s.items()}
+
+
+KINDS = [(F32, 32, False), (F32, 8, False), (BF16, 32, False), (BF16, 8, False),
+         (BF16, 32, True), (BF16, 8, True)]
+SIZES = [1, 7, 8, 9, 255, 256, 257, 300, 2047, 2048, 2049, 8191, 8192, 8193, 70001, 0, 3]
+
+
+@pytest.mark.parametrize("pad", [0, 1, 4])
+@pytest.mark.parametrize("dtype, bits, master", KINDS)
+def test_every_bit(dtype, bits, master, pad):
+    from paper_2608_21343_amd import capi
+    s = tensors(SIZES, dtype, bits, master, pad=pad)
+    for step in (1, 2, 1000):
+        before = copies(s)
+        capi.tb_adamw_step(**s, **HOW, step=step, seed=step * 77)
+        compare(before, s, step, step * 77)
+    # nothing behind or before a tensor is written
+    for kind in ("param", "m", "v"):
+        for t in s[kind]:
+            whole = torch.as_strided(t, (t.numel() + pad + 8,), (1,), 0) if t.numel() else None
+            if whole is not None:
+                assert bool((whole[:pad] == 99).all()) and bool((whole[pad + t.numel():] == 99).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_many_tensors(bits):
+    """More tensors than a launch takes; their index makes the roundings."""
+    from paper_2608_21343_amd import capi
+    s = tensors([(37 * k) % 700 for k in range(230)], F32, bits, False)
+    before = copies(s)
+    capi.tb_adamw_step(**s, **HOW, step=5, seed=3)
+    compare(before, s, 5, 3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_values_from_the_device(bits):
+    """Learning rate, step and factor of the gradients on the device, in a graph
+    that is replayed."""
+    from paper_2608_21343_amd import capi
+    s = tensors([1000, 5000], F32, bits, False)
+    lr = torch.tensor([1e-3], device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    scale = torch.tensor([0.25], device="cuda")
+
+    def run():
+        step.add_(1)
+        capi.tb_adamw_step(**s, **dict(HOW, lr=7.0), seed=9, lr_dev=lr, step_dev=step,
+                           grad_scale=scale)
+
+    side = torch.cuda.Stream()
+    start = copies(s)
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for kind, list_ in start.items():
+        for k, t in enumerate(list_ or []):
+            s[kind][k].copy_(t)
+    step.zero_()
+    for turn in range(1, 5):
+        before = copies(s)
+        lr.fill_(1e-3 * turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        rate = float(np.float32(1e-3 * turn))
+        compare(before, s, turn, 9, dict(HOW, lr=rate), 0.25)
+
+
+def test_bad_gradients():
+    """NaN and infinities reach their own values, and in 8 bits their block."""
+    from paper_2608_21343_amd import capi
+    for bits in (32, 8):
+        s = tensors([1000], F32, bits, False)
+        s["grad"][0][300], s["grad"][0][700] = math.nan, math.inf
+        before = copies(s)
+        capi.tb_adamw_step(**s, **HOW, step=2)
+        bad = torch.zeros(1000, dtype=torch.bool, device="cuda")
+        bad[[300, 700]] = True
+        assert bool((torch.isnan(s["param"][0]) == bad).all())
+        if bits == 8:
+            assert bool((torch.isnan(s["m_unit"][0]) == torch.tensor([0, 1, 1, 0], device="cuda")
+                         .bool()).all())
+            m, v = torch.empty((2, 1000), device="cuda")
+            capi.tb_adamw_moments(s["m"], s["v"], s["m_unit"], s["v_unit"], [m], [v])
+            block = torch.arange(1000, device="cuda") // 256
+            assert bool((torch.isnan(v) == ((block == 1) | (block == 2))).all())
+        else:
+            compare(before, s, 2)
+
+
+def test_zero_and_tiny_gradients():
+    from paper_2608_21343_amd import capi
+    s = tensors([600], F32, 8, False)
+    for kind in ("m", "v", "m_unit", "v_unit"):
+        s[kind][0].zero_()
+    s["grad"][0].zero_()
+    s["grad"][0][300:600] = 1e-30  # their squares are below any unit
+    p = s["param"][0].clone()
+    capi.tb_adamw_step(**s, **dict(HOW, weight_decay=0.0), step=1)
+    assert bool((s["param"][0][:300] == p[:300]).all())
+    assert bool(torch.isfinite(s["param"][0]).all())
+    assert not s["v"][0][:256].any() and not s["v_unit"][0].any()
+    # a second moment above 0 stays above 0 next to one that is 10^16 times as large
+    s["grad"][0][:2] = torch.tensor([1.0, 1e-8])
+    capi.tb_adamw_step(**s, **HOW, step=2)
+    assert s["v"][0][1] == 1
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+def test_moments(pad):
+    from paper_2608_21343_amd import capi
+    s = tensors([0, 1, 256, 257, 9000], F32, 8, False, pad=pad)
+    out = [[torch.empty(t.numel() + pad, device="cuda")[pad:] for t in s["m"]] for _ in range(2)]
+    capi.tb_adamw_moments(s["m"], s["v"], s["m_unit"], s["v_unit"], *out)
+    for k, code in enumerate(s["m"]):
+        m, v = decode(host(code), host(s["v"][k]), host(s["m_unit"][k]), host(s["v_unit"][k]))
+        same(host(out[0][k]), m, "m")
+        same(host(out[1][k]), v, "v")
+
+
+def test_roundings_keep_the_mean():
+    """The mean of the moments over many seeds: 400 roundings of a step of at most
+    a 16th (first) and a 8th (second) are off by 5 / sqrt(400) / 2 of a step with a
+    probability below 1e-6 a value."""
+    from paper_2608_21343_amd import capi
+    n, turns = 256, 400
+    s = tensors([n], F32, 8, False, seed=4)
+    s["grad"][0].copy_(torch.exp(torch.linspace(-3, 3, n)) * 1e-3)
+    for kind in ("m", "v", "m_unit", "v_unit"):
+        s[kind][0].zero_()
+    total = torch.zeros((2, n), dtype=torch.float64, device="cuda")
+    start = copies(s)
+    m, v = torch.empty((2, n), device="cuda")
+    for seed in range(turns):
+        for kind in start:
+            if start[kind]:
+                s[kind][0].copy_(start[kind][0])
+        capi.tb_adamw_step(**s, **HOW, step=1, seed=seed)
+        capi.tb_adamw_moments(s["m"], s["v"], s["m_unit"], s["v_unit"], [m], [v])
+        total += torch.stack([m, v]).double()
+    g = s["grad"][0].double()
+    for mean, right, width in zip(total / turns, (0.1 * g, 0.001 * g * g), (16, 8)):
+        off = ((mean - right) / right).abs()
+        assert float(off.max()) <= 5 * 0.5 / math.sqrt(turns) / width + 1e-4
+
+
+# ---- the optimizer
+
+
+def layers(dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.nn.Parameter(torch.randn(s, generator=g).to(dtype).cuda())
+            for s in ((33, 17), (33,), (1,), (300, 5))]
+
+
+def set_grads(params, turn):
+    g = torch.Generator().manual_seed(1000 + turn)
+    for p in params:
+        p.grad = (torch.randn(p.shape, generator=g) * 1e-2).to(p.dtype).cuda()
+
+
+def test_optimizer_is_adamw():
+    """Twenty steps beside torch's AdamW in float64. A step's relative error is a few
+    roundings; over t steps an error of at most t * 2^-20 of a step's size is left."""
+    from paper_2608_21343_amd.optim import AdamW
+    ours = layers(F32)
+    theirs = [torch.nn.Parameter(p.detach().double()) for p in ours]
+    groups = [dict(params=ours[:2], weight_decay=0.1), dict(params=ours[2:], lr=1e-2)]
+    a = AdamW(groups, lr=1e-3)
+    b = torch.optim.AdamW([dict(params=theirs[:2], weight_decay=0.1),
+                           dict(params=theirs[2:], lr=1e-2)], lr=1e-3)
+    for turn in range(20):
+        set_grads(ours, turn)
+        if turn % 3 == 0:
+            ours[1].grad = None  # steps of its own count
+        for p, q in zip(ours, theirs):
+            q.grad = None if p.grad is None else p.grad.double()
+        a.step()
+        b.step()
+    for p, q in zip(ours, theirs):
+        tol = 20 * 2.0 ** -24 * q.abs() + 20 * 1e-2 * 2.0 ** -16
+        assert bool(((p.double() - q).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype, bits, master", KINDS)
+def test_optimizer_resumes(dtype, bits, master):
+    """A run continued from its state dict goes on bit for bit."""
+    from paper_2608_21343_amd.optim import AdamW
+
+    def make(params):
+        return AdamW(params, lr=1e-2, state_bits=bits, master=master, seed=5)
+
+    one = layers(dtype)
+    a = make(one)
+    for turn in range(3):
+        set_grads(one, turn)
+        a.step()
+    two = [torch.nn.Parameter(p.detach().clone()) for p in one]
+    b = make(two)
+    b.load_state_dict(a.state_dict())
+    for params, opt in ((one, a), (two, b)):
+        for turn in range(3, 6):
+            set_grads(params, turn)
+            opt.step()
+    for p, q in zip(one, two):
+        assert bool((p == q).all())
+        for name, t in a.state[p].items():
+            if isinstance(t, torch.Tensor):
+                assert b.state[q][name].dtype == t.dtype and bool((b.state[q][name] == t).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_capturable(bits):
+    from paper_2608_21343_amd.optim import AdamW
+    one, two = layers(F32), layers(F32)
+    lr = torch.tensor(1e-3, device="cuda")
+    a = AdamW(one, lr=float(torch.tensor(1e-3)), state_bits=bits)
+    b = AdamW([dict(params=two)], lr=lr, state_bits=bits, capturable=True)
+    set_grads(one, 0)
+    set_grads(two, 0)
+    a.step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.step()
+    for turn in range(1, 4):
+        set_grads(one, turn)
+        for p, q in zip(one, two):
+            q.grad.copy_(p.grad)
+        a.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(one, two):
+            assert bool((p == q).all()), turn
+    two[0].grad = None
+    with pytest.raises(RuntimeError, match="every gradient"):
+        b.step()
+
+
+def test_optimizer_refusals():
+    from paper_2608_21343_amd import capi
+    from paper_2608_21343_amd.optim import AdamW
+    p = torch.nn.Parameter(torch.zeros((4, 6), device="cuda").t())
+    with pytest.raises(ValueError, match="contiguous"):
+        AdamW([p])
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        AdamW([torch.nn.Parameter(torch.zeros(4, dtype=torch.float16, device="cuda"))])
+    with pytest.raises(ValueError, match="state_bits"):
+        AdamW([torch.nn.Parameter(torch.zeros(4, device="cuda"))], state_bits=4)
+    s = tensors([100, 200], F32, 32, False)
+    for kind, k, t, error, message in (
+            ("grad", 1, s["grad"][1][:199], ValueError, "grad"),
+            ("grad", 0, s["grad"][0].bfloat16(), ValueError, "dtype"),
+            ("m", 0, s["m"][0].cpu(), ValueError, "must be on"),
+            ("v", 1, torch.zeros((200, 2), device="cuda")[:, 0], ValueError, "contiguous"),
+            ("param", 1, s["param"][0].repeat(2).clone(), None, ""),
+            ("grad", 1, s["param"][1], capi.TbError, "shares memory")):
+        other = {n: None if v is None else list(v) for n, v in s.items()}
+        other[kind][k] = t
+        if error is None:
+            capi.tb_adamw_step(**other, **HOW)
+            continue
+        with pytest.raises(error, match=message):
+            capi.tb_adamw_step(**other, **HOW)
+    with pytest.raises(ValueError, match="holds 1 tensors"):
+        capi.tb_adamw_step(**dict(s, grad=s["grad"][:1]), **HOW)
+    with pytest.raises(ValueError, match="belong together"):
+        capi.tb_adamw_step(**dict(s, m_unit=s["m"]), **HOW)
+    capi.tb_adamw_step([], [], [], [], lr=1e-3)
+
+
+def test_stale_graphs_notice_a_step():
+    from paper_2608_21343_amd.optim import AdamW
+    p = torch.nn.Parameter(torch.ones(100, device="cuda"))
+    opt = AdamW([p])
+    loss = (p * p).sum()
+    p.grad = torch.ones_like(p)
+    opt.step()
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+
+
+def test_training_an_output_layer():
+    """Loss, gradients and steps together: forty steps from random weights, and each
+    one's loss is that of the layer in float64 before it."""
+    from paper_2608_21343_amd.linearops import linear_xent, linear_xent_step
+    from paper_2608_21343_amd.optim import AdamW
+    from tests import linear_reference as R
+    c = R.case(200, 96, 400, F32, 21, device="cuda", gaps=True)
+    for bits in (32, 8):
+        w = torch.nn.Parameter(torch.zeros_like(c["w"]))
+        b = torch.nn.Parameter(torch.zeros_like(c["bias"]))
+        opt = AdamW([w, b], lr=1e-2, state_bits=bits)
+        for turn in range(40):
+            opt.zero_grad()
+            if turn % 2:
+                loss = linear_xent(c["x"], w, c["target"], b).loss
+                loss.sum().backward()
+            else:
+                loss, _, w.grad, b.grad = linear_xent_step(c["x"], w, c["target"], b)
+            if turn % 13 == 0:
+                want = R.expected(dict(c, w=w.detach(), bias=b.detach()))
+                R.check(loss.detach(), want["loss"], "loss")
+                R.check(w.grad, want["dw"], "dw")
+                R.check(b.grad, want["db"], "db")
+            opt.step()
