@@ -14,149 +14,331 @@ struct Gather {
   int32_t C;
   const int32_t* target;
   const float *weight, *d_loss, *d_lse, *lse;
-  int32_t grads, rows_up;  // rows_up: gathered rows there is room for
+  bool grads;
   Meta* meta;
+  int32_t* counts;  // per group of kGroup rows: rows that take part ...
+  float* tops;      // ... and their largest finite |a|, |b|; NULL for a single group
   int32_t *idx, *inv, *tgt;
-  float *a, *b, *lse_c;
+  float *a, *b, *lse_c, *r, *m;
   float *out_loss, *out_lse;
+  // the features, and their planes
+  int64_t stride, plane;
+  int32_t D, dp;
+  uint16_t* out;
 };
 
-constexpr int kRowsEach = 8;  // rows of a thread at a time
+constexpr int kGroup = 2048, kEach = kGroup / 256;  // rows of a count, and of a thread of it
+constexpr int kRows = 16;                           // gathered by a workgroup
 
-// One workgroup: order and arguments of the rows that take part. 16 rows cost about as
-// much as one, so 16,384 rows take two rounds.
-__global__ void __launch_bounds__(1024) gather_kernel(const Gather g) {
-  __shared__ int32_t sums[16];
-  __shared__ float tops[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int32_t before = 0;
-  float top = 0.f;
-  for (int64_t r0 = 0; r0 < g.n; r0 += 1024 * kRowsEach) {
-    const int64_t first = r0 + (int64_t)threadIdx.x * kRowsEach;
-    int32_t t[kRowsEach];
-    float a[kRowsEach], b[kRowsEach], l[kRowsEach];
-    int32_t mine = 0;
-#pragma unroll
-    for (int e = 0; e < kRowsEach; ++e) {
-      const int64_t r = first + e;
-      const bool in = r < g.n;
-      t[e] = in ? g.target[r] : -1;
-      const float w = in && g.weight ? g.weight[r] : 1.f;
-      b[e] = w;
-      a[e] = w;
-      l[e] = 0.f;
-      bool keep = t[e] != -1 && w != 0.f;
-      if (g.grads) {
-        if (in && g.d_loss) b[e] = w * g.d_loss[r];
-        a[e] = b[e] + (in && g.d_lse ? g.d_lse[r] : 0.f);
-        if (in && g.lse) l[e] = g.lse[r];
-        // a row without a gradient is left out, unless its loss is asked for
-        if (g.lse) keep = keep && (a[e] != 0.f || b[e] != 0.f);
-      }
-      if (keep && (uint32_t)t[e] >= (uint32_t)g.C) {
-        t[e] = -2;
-        a[e] = b[e] = __builtin_nanf("");
-      }
-      if (!keep) t[e] = -1;
-      mine += t[e] != -1;
-    }
-    int32_t upto = mine;  // of this wave's lanes up to this one
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int32_t v = __shfl_up(upto, d);
-      if (lane >= d) upto += v;
-    }
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    int32_t at = before + upto - mine, all = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) at += sums[w];
-      all += sums[w];
-    }
-    before += all;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kRowsEach; ++e) {
-      const int64_t r = first + e;
-      if (r >= g.n) break;
-      if (t[e] == -1) {
-        g.inv[r] = -1;
-        if (g.out_loss) g.out_loss[r] = 0.f;
-        if (g.out_lse) g.out_lse[r] = 0.f;
-        continue;
-      }
-      // an empty row (no token above -inf) has no gradient
-      if (l[e] == -__builtin_huge_valf()) a[e] = b[e] = l[e] = 0.f;
-      g.inv[r] = at;
-      g.idx[at] = (int32_t)r;
-      g.tgt[at] = t[e];
-      g.a[at] = a[e];
-      g.b[at] = b[e];
-      g.lse_c[at] = l[e];
-      if (fabsf(a[e]) < __builtin_huge_valf()) top = fmaxf(top, fabsf(a[e]));
-      if (fabsf(b[e]) < __builtin_huge_valf()) top = fmaxf(top, fabsf(b[e]));
-      ++at;
-    }
+struct Row {
+  int32_t target;  // -1: left out, -2: out of range
+  float a, b;
+};
+
+__device__ __forceinline__ Row row_of(const Gather& g, int64_t r) {
+  Row o = {-1, 0.f, 0.f};
+  if (r >= g.n) return o;
+  o.target = g.target[r];
+  const float w = g.weight ? g.weight[r] : 1.f;
+  o.a = o.b = w;
+  bool keep = o.target != -1 && w != 0.f;
+  if (g.grads) {
+    if (g.d_loss) o.b = w * g.d_loss[r];
+    o.a = o.b + (g.d_lse ? g.d_lse[r] : 0.f);
+    // a row without a gradient is left out, unless its loss is asked for
+    if (g.lse) keep = keep && (o.a != 0.f || o.b != 0.f);
   }
+  if (!keep) {
+    o.target = -1;
+  } else if ((uint32_t)o.target >= (uint32_t)g.C) {
+    o.target = -2;
+    o.a = o.b = __builtin_nanf("");
+  }
+  return o;
+}
+
+__device__ __forceinline__ float finite_top(const Row& o) {
+  const float a = fabsf(o.a), b = fabsf(o.b), inf = __builtin_huge_valf();
+  return o.target == -1 ? 0.f : fmaxf(a < inf ? a : 0.f, b < inf ? b : 0.f);
+}
+
+// Sums of two counts and the maximum of a float over a workgroup of 256.
+__device__ __forceinline__ void join256(int32_t* x, int32_t* y, float* top) {
+  __shared__ int32_t xs[4], ys[4];
+  __shared__ float ts[4];
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if (lane == 0) tops[wave] = top;
+  for (int d = 32; d > 0; d >>= 1) {
+    *x += __shfl_xor(*x, d);
+    *y += __shfl_xor(*y, d);
+    *top = fmaxf(*top, __shfl_xor(*top, d));
+  }
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    xs[wave] = *x;
+    ys[wave] = *y;
+    ts[wave] = *top;
+  }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  *x = xs[0] + xs[1] + xs[2] + xs[3];
+  *y = ys[0] + ys[1] + ys[2] + ys[3];
+  *top = fmaxf(fmaxf(ts[0], ts[1]), fmaxf(ts[2], ts[3]));
+}
+
+__global__ void __launch_bounds__(256) count_kernel(const Gather g) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) g.meta->S = g.meta->T = 0;
+  int32_t count = 0, none = 0;
+  float top = 0.f;
+  const int64_t first = (int64_t)blockIdx.x * kGroup;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) top = fmaxf(top, tops[w]);
-    // (no further, so that rows of far smaller weights keep their place in float32)
-    top = fminf(fmaxf(top, 0x1p-24f), 0x1p24f);
-    *g.meta = {before, top, 1.f / top};
+  for (int e = 0; e < kEach; ++e) {
+    const Row o = row_of(g, first + e * 256 + threadIdx.x);
+    count += o.target != -1;
+    top = fmaxf(top, finite_top(o));
+  }
+  join256(&count, &none, &top);
+  if (threadIdx.x == 0 && g.counts) {
+    g.counts[blockIdx.x] = count;
+    g.tops[blockIdx.x] = top;
   }
 }
 
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
-// Rows of a matrix as planes, padded with zeros to dp values: the gathered rows idx
-// and zeros up to a multiple of kTile, or (idx NULL) all n of them.
-template <class T>
-__global__ void __launch_bounds__(256)
-    planes_kernel(const T* x, int64_t stride, int32_t D, int32_t dp, const int32_t* idx,
-                  const Meta* meta, int64_t n, uint16_t* out, int64_t plane) {
-  constexpr int PLANES = sizeof(T) == 4 ? 3 : 1;
-  const int64_t each = dp / 4;
-  const int64_t have = idx ? meta->n : n, rows = idx ? up(have, kTile) : n;
-  const bool whole = (stride * sizeof(T)) % 16 == 0 && (uintptr_t)x % 16 == 0;
-  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows * each;
-       at += (int64_t)gridDim.x * 256) {
-    const int64_t row = at / each;
-    const int d = (int)(at - row * each) * 4;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (row < have) {
-      const T* from = x + (idx ? (int64_t)idx[row] : row) * stride + d;
-      if (whole && d + 4 <= D) {
-        if constexpr (sizeof(T) == 4) {
-          const float4 q = *reinterpret_cast<const float4*>(from);
-          v[0] = q.x;
-          v[1] = q.y;
-          v[2] = q.z;
-          v[3] = q.w;
-        } else {
-          const uint2 q = *reinterpret_cast<const uint2*>(from);
-          v[0] = low16(q.x);
-          v[1] = high16(q.x);
-          v[2] = low16(q.y);
-          v[3] = high16(q.y);
-        }
-      } else {
+// Four values of a row from d on, 0 behind its end. `wide`: aligned to 16 bytes.
+__device__ __forceinline__ void load4(const float* x, int d, int D, bool wide, float* v) {
+  if (wide && d + 4 <= D) {
+    const float4 q = *reinterpret_cast<const float4*>(x + d);
+    v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+  } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (d + e < D) v[e] = widen(from[e]);
+    for (int e = 0; e < 4; ++e) v[e] = d + e < D ? x[d + e] : 0.f;
+  }
+}
+__device__ __forceinline__ void load4(const uint16_t* x, int d, int D, bool wide, float* v) {
+  if (wide && d + 4 <= D) {
+    const uint2 q = *reinterpret_cast<const uint2*>(x + d);
+    v[0] = low16(q.x), v[1] = high16(q.x), v[2] = low16(q.y), v[3] = high16(q.y);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = d + e < D ? widen(x[d + e]) : 0.f;
+  }
+}
+
+// Raises *to to the largest of a workgroup's values (not negative, of the waves' first
+// lanes), whatever the order; one atomic a workgroup, and none where it changes nothing.
+__device__ __forceinline__ void raise(uint32_t* to, float v) {
+  __shared__ float tops[4];
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const uint32_t top = __float_as_uint(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+    if (top > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, top);
+  }
+}
+
+// One wave: a row as planes of dp values, and (float32) the unit it is divided by.
+// `most`: its largest value. Up to 2048 values stay in registers; longer rows are read
+// twice, the second time from the caches.
+template <class T>
+__device__ __forceinline__ float row_planes(const T* x, int D, int dp, bool wide, uint16_t* out,
+                                            int64_t plane, float* most) {
+  constexpr int kKept = 8;
+  const int lane = threadIdx.x & 63;
+  float kept[kKept][4];
+  float unit = 1.f, inverse = 1.f, top = 0.f;
+  const bool keep = D <= kKept * 256;
+  auto size = [&](const float* v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (fabsf(v[e]) < __builtin_huge_valf()) top = fmaxf(top, fabsf(v[e]));
+  };
+  auto store = [&](int d, const float* v) {
+    const float w[4] = {v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse};
+    uint2 p[Elem<T>::PLANES];
+    Elem<T>::planes4(w, p);
+#pragma unroll
+    for (int s = 0; s < Elem<T>::PLANES; ++s)
+      *reinterpret_cast<uint2*>(out + s * plane + d) = p[s];
+  };
+  if (keep) {
+#pragma unroll
+    for (int k = 0; k < kKept; ++k)
+      if (256 * k < dp) load4(x, 256 * k + 4 * lane, D, wide, kept[k]);
+  }
+  if (Elem<T>::kScaled) {
+    if (keep) {
+#pragma unroll
+      for (int k = 0; k < kKept; ++k)
+        if (256 * k < dp) size(kept[k]);
+    } else {
+      for (int d = 4 * lane; d < D; d += 256) {
+        float v[4];
+        load4(x, d, D, wide, v);
+        size(v);
       }
     }
-    uint2 p[PLANES];
-    planes4<PLANES>(v, p);
 #pragma unroll
-    for (int s = 0; s < PLANES; ++s)
-      *reinterpret_cast<uint2*>(out + s * plane + row * dp + d) = p[s];
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    unit = unit_of(top);
+    inverse = 1.f / unit;
+  }
+  *most = top;
+  if (keep) {
+#pragma unroll
+    for (int k = 0; k < kKept; ++k)
+      if (256 * k + 4 * lane < dp) store(256 * k + 4 * lane, kept[k]);
+  } else {
+    for (int d = 4 * lane; d < dp; d += 256) {
+      float v[4];
+      load4(x, d, D, wide, v);
+      store(d, v);
+    }
+  }
+  return unit;
+}
+
+template <class T>
+__device__ __forceinline__ bool rows_wide(const T* x, int64_t stride) {
+  return stride * sizeof(T) % 16 == 0 && (uintptr_t)x % 16 == 0;
+}
+
+// kRows rows: their place among those that take part, their arguments and planes.
+// The rows before them are counted again up to the group's start, and groups by
+// their counts, so that no launch has to wait for a sum over all of them.
+template <class T>
+__global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row0 = (int64_t)blockIdx.x * kRows;
+  const int64_t group = row0 / kGroup, groups = (g.n + kGroup - 1) / kGroup;
+  int32_t before = 0, all = 0;
+  float top = 0.f;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int64_t r = group * kGroup + e * 256 + threadIdx.x;
+    const Row o = row_of(g, r);
+    before += o.target != -1 && r < row0;
+    all += o.target != -1;
+    top = fmaxf(top, finite_top(o));
+  }
+  if (groups > 1) {
+    all = 0;
+    for (int64_t i = threadIdx.x; i < groups; i += 256) {
+      const int32_t count = g.counts[i];
+      all += count;
+      if (i < group) before += count;
+      top = fmaxf(top, g.tops[i]);
+    }
+  }
+  join256(&before, &all, &top);
+
+  __shared__ int32_t places[kRows];
+  if (wave == 0) {
+    const int64_t r = row0 + lane;
+    Row o = {-1, 0.f, 0.f};
+    if (lane < kRows) o = row_of(g, r);
+    const uint64_t keep = __ballot(o.target != -1);
+    const int32_t at = before + __popcll(keep & ((1ull << lane) - 1));
+    if (lane < kRows) places[lane] = o.target != -1 ? at : -1;
+    if (lane < kRows && r < g.n) {
+      if (o.target == -1) {
+        g.inv[r] = -1;
+        if (g.out_loss) g.out_loss[r] = 0.f;
+        if (g.out_lse) g.out_lse[r] = 0.f;
+      } else {
+        float lse = g.lse ? g.lse[r] : 0.f;
+        // an empty row (no token above -inf) has no gradient
+        if (lse == -__builtin_huge_valf()) o.a = o.b = lse = 0.f;
+        if (Elem<T>::kScaled) {
+          float m = fmaxf(fabsf(o.a), fabsf(o.b));
+          if (!(m > 0.f)) m = 1.f;  // (0 or NaN)
+          o.a /= m;
+          o.b /= m;
+          g.m[at] = m;
+        }
+        g.inv[r] = at;
+        g.idx[at] = (int32_t)r;
+        g.tgt[at] = o.target;
+        g.a[at] = o.a;
+        g.b[at] = o.b;
+        g.lse_c[at] = lse;
+      }
+    }
+  }
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
+    // (no further, so that rows of far smaller weights keep their place in float32)
+    top = fminf(fmaxf(top, 0x1p-24f), 0x1p24f);
+    g.meta->n = all;
+    g.meta->scale = top;
+    g.meta->inverse = 1.f / top;
+  }
+  __syncthreads();
+  const bool wide = rows_wide(x, g.stride);
+  float weighty = 0.f;
+  for (int i = wave; i < kRows; i += 4) {
+    const int32_t at = places[i];
+    if (at < 0) continue;
+    float most;
+    const float unit = row_planes<T>(x + (row0 + i) * g.stride, g.D, g.dp, wide,
+                                     g.out + (int64_t)at * g.dp, g.plane, &most);
+    if (Elem<T>::kScaled && lane == 0) {
+      g.r[at] = unit;
+      const float with = most * g.m[at];  // (written by this workgroup)
+      if (with < __builtin_huge_valf()) weighty = fmaxf(weighty, with);
+    }
+  }
+  if (Elem<T>::kScaled && g.grads) raise(&g.meta->T, weighty);
+  if (blockIdx.x == gridDim.x - 1) {
+    // the zeros behind the last row
+    const int64_t end = up(all, kStep) * g.dp;
+    for (int64_t i = (int64_t)all * g.dp + 4 * threadIdx.x; i < end; i += 1024)
+#pragma unroll
+      for (int s = 0; s < Elem<T>::PLANES; ++s)
+        *reinterpret_cast<uint2*>(g.out + s * g.plane + i) = make_uint2(0, 0);
+  }
+}
+
+// The weights' planes, one wave a row.
+template <class T>
+__global__ void __launch_bounds__(256)
+    weights_kernel(const T* w, int64_t stride, int32_t D, int32_t dp, int32_t C, uint16_t* out,
+                   int64_t plane, float* units, Meta* meta) {
+  const bool wide = rows_wide(w, stride);
+  float top = 0.f;
+  for (int64_t c = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); c < C; c += (int64_t)gridDim.x * 4) {
+    float most;
+    const float unit = row_planes<T>(w + c * stride, D, dp, wide, out + c * dp, plane, &most);
+    // (a token without weights says nothing of the others' scale)
+    if (Elem<T>::kScaled && (threadIdx.x & 63) == 0) units[c] = most > 0.f ? unit : 0.f;
+    if (most > 0.f) top = fmaxf(top, unit);
+  }
+  if (Elem<T>::kScaled) raise(&meta->S, top);
+}
+
+// float32: the planes of x_i m_i / T of the gathered rows.
+__global__ void __launch_bounds__(256)
+    weighted_kernel(const float* x, int64_t stride, int32_t D, int32_t dp, const int32_t* idx,
+                    const float* m, const Meta* meta, uint16_t* out, int64_t plane) {
+  const int lane = threadIdx.x & 63;
+  const bool wide = rows_wide(x, stride);
+  const int64_t have = meta->n, rows = up(have, kStep);
+  const float inverse = 1.f / unit_of(__uint_as_float(meta->T));
+  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows;
+       i += (int64_t)gridDim.x * 4) {
+    const float* from = i < have ? x + (int64_t)idx[i] * stride : nullptr;
+    const float scale = i < have ? m[i] : 0.f;
+    for (int d = 4 * lane; d < dp; d += 256) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (from && d < D) {
+        load4(from, d, D, wide, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = v[e] * scale * inverse;
+      }
+      uint2 p[2];
+      Elem<float>::planes4(v, p);
+      *reinterpret_cast<uint2*>(out + i * dp + d) = p[0];
+      *reinterpret_cast<uint2*>(out + plane + i * dp + d) = p[1];
+    }
   }
 }
 
@@ -209,45 +391,53 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   }
 }
 
-template <class T>
-__device__ __forceinline__ void store_row4(T* o, const float* v, int left) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < left) store_out(o + e, v[e]);
-}
-
-// out[r] = scale * the sum of the splits' rows inv[r] (or r); 0 for the rows left out.
+// out[r] = the sum of the splits' rows inv[r] (dx; 0 for the rows left out) or r (dw).
 template <class T>
 __global__ void __launch_bounds__(256)
-    join_kernel(const float* acc, int64_t split, int32_t splits, int32_t lda, const int32_t* inv,
-                const Meta* meta, T* out, int64_t ldo, int64_t n, int32_t D) {
-  const int64_t each = (D + 3) / 4;
-  const float scale = meta->scale;
+    join_kernel(const Gemm g, const int32_t* inv, T* out, int64_t ldo, int64_t n) {
+  const int64_t each = (g.D + 3) / 4;
+  const Meta meta = *g.meta;
+  const bool wide = ldo % 4 == 0 && (uintptr_t)out % (4 * sizeof(T)) == 0;
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n * each;
        at += (int64_t)gridDim.x * 256) {
     const int64_t row = at / each;
     const int d = (int)(at - row * each) * 4;
     const int64_t from = inv ? inv[row] : row;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    float scale = 0.f;
     if (from >= 0) {
-      const float* p = acc + from * lda + d;
-      for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * split);
+      const float* p = g.acc + from * g.lda + d;
+      for (int s = 0; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * g.acc_split);
+      if (!inv) scale = dw_scale<T>(g, meta, (int)row);
+      else if (!Elem<T>::kScaled) scale = meta.scale;
+      else scale = g.row.m[from] * top_unit(meta) * 0x1p-14f;
     }
-    const float w[4] = {v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale};
-    store_row4(out + row * ldo + d, w, D - d);
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    if (from >= 0)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = v[e] * scale;
+    store4(out + row * ldo + d, w, wide, g.D - d);
   }
 }
 
-// db[c] = scale * the sum of the row groups' columns.
+// db[c] = the sum of the row tiles' columns: 64 tokens a workgroup, a quarter of the
+// tiles each wave.
 template <class T>
 __global__ void __launch_bounds__(256)
     columns_kernel(const float* col, int32_t ldg, const Meta* meta, T* db, int32_t n) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= n) return;
-  const int groups = (int)up(meta->n, kTile) / 64;
+  __shared__ float sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + lane;
+  const int tiles = (meta->n + kTile - 1) / kTile;
   float sum = 0.f;
-  for (int q = 0; q < groups; ++q) sum += col[(int64_t)q * ldg + c];
-  store_out(db + c, sum * meta->scale);
+  if (c < n)
+    for (int q = wave; q < tiles; q += 4) sum += col[(int64_t)q * ldg + c];
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && c < n) {
+    sum = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    store_out(db + c, Elem<T>::kScaled ? sum : sum * meta->scale);
+  }
 }
 
 // ---- workspace
@@ -260,20 +450,32 @@ struct Layout {
   int32_t n_part;
   int32_t piece, pieces;       // tokens of a piece of the vocabulary
   int32_t split_x, split_w;
-  int64_t meta, idx, inv, tgt, a, b, lse, hit, part, x, w, G, acc_x, acc_w, col, total;
+  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, s, hit, part, x, xm, w, G, acc_x;
+  int64_t acc_w, col, total;
 };
 
+// In how many parts the summed axis is cut: the rounds of 256 workgroups that the tiles
+// take, against what a part costs by itself (its first loads, and its sums' way through
+// memory: about three steps).
 int splits(int64_t tiles, int64_t steps) {
-  // enough workgroups for every CU, each with a few steps
-  int64_t s = tiles < 1 || tiles >= 160 ? 1 : (256 + tiles - 1) / tiles;
-  s = s > steps / 4 ? steps / 4 : s;
-  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 64 && s <= (steps + 3) / 4; ++s) {
+    const double cost =
+        (double)((tiles * s + 255) / 256) * ((double)((steps + s - 1) / s) + (s > 1 ? 6 : 3));
+    if (s == 1 || cost < least * 0.97) {
+      best = s;
+      least = cost;
+    }
+  }
+  return best;
 }
 
 Layout plan(const Call& c) {
   Layout L = {};
   const bool f32 = c.dtype == TB_F32;
-  L.planes = f32 ? 3 : 1;
+  L.planes = f32 ? 2 : 1;
+  const bool grads = c.dx || c.dw || c.db;
   L.np = up(c.n, kTile);
   L.dp = up(c.D, kStep);
   L.copy_w = f32 || c.D % kStep != 0 || c.w_stride % 8 != 0 || (uintptr_t)c.w % 16 != 0;
@@ -285,17 +487,24 @@ Layout plan(const Call& c) {
     return here;
   };
   L.meta = take(sizeof(Meta));
+  const int64_t groups = (c.n + kGroup - 1) / kGroup;
+  L.counts = take((groups + 1) * 4);  // (without rows one is written all the same)
+  L.tops = take((groups + 1) * 4);
   L.idx = take(c.n * 4);
   L.inv = take(c.n * 4);
   L.tgt = take(L.np * 4);
   L.a = take(L.np * 4);
   L.b = take(L.np * 4);
   L.lse = take(L.np * 4);
+  if (f32) L.r = take(L.np * 4);
+  if (f32) L.m = take(L.np * 4);
+  if (f32) L.s = take((int64_t)c.C * 4);
   L.hit = take(L.np * 4);
   if (!c.lse) L.part = take(L.np * L.n_part * 8);
   L.x = take(L.planes * L.np * L.dp * 2);
+  if (f32 && c.dw) L.xm = take(L.planes * L.np * L.dp * 2);
   if (L.copy_w) L.w = take(L.planes * c.C * L.dp * 2);
-  if (c.dx || c.dw || c.db) {
+  if (grads) {
     // pieces of the vocabulary of about kGradBytes of gradients, of equal sizes
     const int64_t all = L.planes * L.np * 2 * c.C;
     int64_t pieces = (all + kGradBytes / 2) / kGradBytes;
@@ -312,7 +521,7 @@ Layout plan(const Call& c) {
       L.split_w = splits(td * (L.piece / kTile), L.np / kStep);
       if (L.split_w > 1) L.acc_w = take(L.split_w * (int64_t)L.piece * L.dp * 4);
     }
-    if (c.db) L.col = take(L.np / 64 * L.piece * 4);
+    if (c.db) L.col = take(L.np / kTile * L.piece * 4);
   }
   L.total = at;
   return L;
@@ -325,7 +534,7 @@ unsigned blocks(int64_t work) {
 
 template <class T>
 hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
-  const bool f32 = sizeof(T) == 4;
+  constexpr bool f32 = sizeof(T) == 4;
   const Layout L = plan(c);
   const bool grads = c.dx || c.dw || c.db;
   Meta* meta = reinterpret_cast<Meta*>(ws + L.meta);
@@ -334,16 +543,21 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   auto u16 = [&](int64_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
   int32_t *idx = i32(L.idx), *inv = i32(L.inv), *tgt = i32(L.tgt);
   float *a = flt(L.a), *b = flt(L.b), *lse = flt(L.lse);
-  const Gather ga = {c.n, c.C, c.target, c.weight, c.d_loss, c.d_lse, c.lse, grads, (int32_t)L.np,
-                     meta, idx, inv, tgt, a, b, lse, c.out_loss, c.out_lse};
-  gather_kernel<<<dim3(1), dim3(1024), 0, st>>>(ga);
-  planes_kernel<T><<<dim3(blocks(L.np * (L.dp / 4))), dim3(256), 0, st>>>(
-      static_cast<const T*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, meta, c.n, u16(L.x),
-      L.np * L.dp);
+  float *r = f32 ? flt(L.r) : nullptr, *m = f32 ? flt(L.m) : nullptr;
+  const int64_t groups = (c.n + kGroup - 1) / kGroup;
+  const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse,
+                     grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
+                     a,      b,    lse, r, m, c.out_loss, c.out_lse,
+                     c.x_stride, L.np * L.dp, c.D, (int32_t)L.dp, u16(L.x)};
+  // (float32 gradients: it also clears what the others take maxima into)
+  if (groups != 1 || f32)
+    count_kernel<<<dim3((unsigned)(groups < 1 ? 1 : groups)), dim3(256), 0, st>>>(ga);
+  gather_kernel<T><<<dim3((unsigned)(c.n < 1 ? 1 : (c.n + kRows - 1) / kRows)), dim3(256), 0, st>>>(
+      ga, static_cast<const T*>(c.x));
   if (L.copy_w && c.n > 0)
-    planes_kernel<T><<<dim3(blocks(c.C * (L.dp / 4))), dim3(256), 0, st>>>(
-        static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, nullptr, nullptr, c.C, u16(L.w),
-        c.C * L.dp);
+    weights_kernel<T><<<dim3(c.C < 8192 ? (c.C + 3) / 4 : 2048), dim3(256), 0, st>>>(
+        static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, c.C, u16(L.w), c.C * L.dp,
+        f32 ? flt(L.s) : nullptr, meta);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
 
@@ -354,7 +568,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   g.meta = meta;
   g.bias = c.bias;
   g.C = c.C;
-  g.row = {tgt, a, b, lse};
+  g.row = {tgt, a, b, lse, r, m};
+  g.s = f32 ? flt(L.s) : nullptr;
   g.k = (int32_t)L.dp;
   g.splits = 1;
   g.Q = X;
@@ -376,6 +591,17 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   }
   if (!grads) return hipSuccess;
 
+  Operand XM = X;  // of dw
+  if constexpr (f32) {
+    if (c.dw && c.n > 0) {
+      XM.p = u16(L.xm);
+      weighted_kernel<<<dim3(c.n < 8192 ? (c.n + 3) / 4 : 2048), dim3(256), 0, st>>>(
+          static_cast<const T*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, meta, u16(L.xm),
+          L.np * L.dp);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
   const int32_t td = (int32_t)((L.dp + kTile - 1) / kTile);
   for (int32_t piece = 0; piece < L.pieces; ++piece) {
     const int32_t c0 = piece * L.piece, n = c.C - c0 < L.piece ? c.C - c0 : L.piece;
@@ -394,7 +620,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (e != hipSuccess) return e;
     const Operand G = {z.G, z.g_plane, L.piece, (int32_t)L.np, n};
     if (c.db) {
-      columns_kernel<T><<<dim3((n + 255) / 256), dim3(256), 0, st>>>(
+      columns_kernel<T><<<dim3((n + 63) / 64), dim3(256), 0, st>>>(
           flt(L.col), L.piece, meta, static_cast<T*>(c.db) + c0, n);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
@@ -416,7 +642,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     }
     if (c.dw) {
       Gemm w = g;
-      w.P = {X.p, X.plane, X.ld, (int32_t)L.dp, (int32_t)L.np};
+      w.P = {XM.p, XM.plane, XM.ld, (int32_t)L.dp, (int32_t)L.np};
+      w.c0 = c0;
       w.Q = {G.p, G.plane, G.ld, L.piece, (int32_t)L.np};
       w.tp = td;
       w.tq = cols / kTile;
@@ -436,16 +663,21 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       if (e != hipSuccess) return e;
       if (L.split_w > 1) {
         join_kernel<T><<<dim3(blocks((int64_t)n * ((c.D + 3) / 4))), dim3(256), 0, st>>>(
-            w.acc, w.acc_split, L.split_w, w.lda, nullptr, meta, out, c.dw_stride, n, c.D);
+            w, nullptr, out, c.dw_stride, n);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
       }
     }
   }
-  if (c.dx)
+  if (c.dx && c.n > 0) {
+    Gemm x = g;
+    x.splits = L.split_x;
+    x.acc = flt(L.acc_x);
+    x.acc_split = L.np * L.dp;
+    x.lda = (int32_t)L.dp;
     join_kernel<T><<<dim3(blocks(c.n * ((c.D + 3) / 4))), dim3(256), 0, st>>>(
-        flt(L.acc_x), L.np * L.dp, L.split_x, (int32_t)L.dp, inv, meta, static_cast<T*>(c.dx),
-        c.dx_stride, c.n, c.D);
+        x, inv, static_cast<T*>(c.dx), c.dx_stride, c.n);
+  }
   return hipGetLastError();
 }
 

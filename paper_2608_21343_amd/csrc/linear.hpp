@@ -4,15 +4,30 @@
 //   G_ic = a_i exp(z_ic - lse_i) - b_i [c = t(i)], dx = G w, dw = G^T x, db = sum_i G_i
 //
 // with b_i = weight_i d_loss_i and a_i = b_i + d_lse_i. All four products run on the
-// matrix cores as 16-bit operands with float32 sums (linear_gemm.hpp). bfloat16
-// operands are taken as they are. A float32 operand is the sum of three bfloat16
-// planes (each the rounding of what the ones before leave: 3 x 8 bits and their
-// signs hold the 24 of a float32), and a product of two of them is the sum of six
-// products of planes; the three left out are below 2^-26 of it.
+// matrix cores as 16-bit operands with float32 sums (linear_gemm.hpp).
+//
+// bfloat16 operands are taken as they are, and G is rounded to bfloat16.
+//
+// A float32 operand is the sum of two float16 planes, the second the rounding of what
+// the first leaves: 22 bits and two signs, so what they leave is below 2^-24 of the
+// value. A product of two such operands is the sum of three products of planes; the
+// fourth is below 2^-24 of it. (Three bfloat16 planes hold as much but take six
+// products: a step of 2048 x 1024 features against 32,769 tokens took 3.4 ms with them.)
+// What float16 lacks is range: 2^-14 to 2^16, and absolute steps of 2^-24 below. So rows of x
+// and of w are divided by powers of two, r_i and s_c, that bring their largest value to
+// 2^14..2^15 (a value below 2^-16 of its row's largest loses precision, at most 2^-40 of
+// that; an entry of G below 2^-16 of its row's weight at most 2^-39 of that weight), and
+//
+//   z_ic  = (x_i / r_i) (w_c / s_c) r_i s_c
+//   G'_ic = G_ic / m_i * s_c / S * 2^14,  m_i = max(|a_i|, |b_i|), S = max s_c
+//   dx_i  = G'_i (w / s) * m_i S 2^-14
+//   dw_c  = G'_c^T (x_i m_i / T) * T S / s_c 2^-14,  T a power of two for all rows
+//
+// so that a row's gradient is as exact as if it were alone, whatever the others weigh.
 //
 // Rows that take part (target not -1, weight not 0) are gathered first, so that the
 // others cost nothing and whatever they hold reaches no sum. Rows of the gathered
-// matrix end at a multiple of 64 values, and its rows at one of 256, with zeros.
+// matrix end at a multiple of 64 values, and its rows at one of 64, with zeros.
 #pragma once
 
 #include "device.hpp"
@@ -29,12 +44,12 @@ __host__ __device__ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1)
 
 // Left by the gathering of the rows, read by every later kernel.
 struct Meta {
-  int32_t n;       // gathered rows
-  // G is kept divided by the largest finite |a_i|, |b_i|: with equal weights, as the mean
-  // over a batch has, the target's entry p - 1 is then rounded near 1 and not every
-  // row's by the same part of the weight (up to 2^-8, which no sum averages out)
-  float scale;
-  float inverse;
+  int32_t n;  // gathered rows
+  // bfloat16: G is kept divided by the largest finite |a_i|, |b_i|. With equal weights, as
+  // the mean over a batch has, the target's entry p - 1 is then rounded near 1 and not
+  // every row's by the same part of the weight (up to 2^-8, which no sum averages out).
+  float scale, inverse;
+  uint32_t S, T;  // float32: bits of max s_c, and of the largest |x_i m_i|
 };
 
 // A matrix as 16-bit planes. Element (i, k) of a plane, k the summed axis, lies at
@@ -49,7 +64,8 @@ struct Operand {
 // Per gathered row.
 struct RowArgs {
   const int32_t* target;  // -1: none in range
-  const float *a, *b, *lse;
+  const float *a, *b, *lse;  // float32: a and b divided by m
+  const float *r, *m;        // float32 only
 };
 
 struct Gemm {
@@ -61,6 +77,7 @@ struct Gemm {
   // statistics and gradients of the logits
   const void* bias;
   int32_t C, c0;   // tokens, and the first of P
+  const float* s;  // [C], float32 only
   RowArgs row;
   float2* part;    // [gathered row, n_part]: maximum, sum
   int32_t n_part;
@@ -68,7 +85,7 @@ struct Gemm {
   uint16_t* G;     // planes of [row, ldg]
   int64_t g_plane;
   int32_t ldg;
-  float* col;      // [row groups of 64, ldg], or NULL
+  float* col;      // [row tiles, ldg], or NULL
   // products with the gradients
   float* acc;      // [split, n_q, lda]
   int64_t acc_split;
