@@ -9,6 +9,8 @@
 // pieces exchanged, and is read through the transposing LDS read.
 #pragma once
 
+#include <cstddef>
+
 #include "linear.hpp"
 
 namespace tbias {
@@ -21,6 +23,7 @@ typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((address_space(3))) char lds_char;
 
@@ -73,26 +76,33 @@ struct Elem<float> {
   }
 };
 
-// Where a lane's 16-byte loads of a stage come from, in bytes from the operand's
-// tile (i0, k0).
+// A lane's first 16-byte load of a stage: the row of the operand's memory that it comes
+// from (its own rows, or transposed the summed values), counted from the tile's, and the
+// bytes in that row. The next ones come from kNextRows rows further on.
 template <bool TR>
-__device__ __forceinline__ void lane_offsets(const Operand& o, int32_t i0, int32_t k_left,
-                                             uint32_t (&off)[kLoads]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int it = 0; it < kLoads; ++it) {
-    const int at = (it * kWaves + wave) * 64 + lane;
-    if (!TR) {
-      const int row = at >> 3, piece = (at & 7) ^ ((row >> 1) & 7);
-      const int r = min(row, o.n - 1 - i0);
-      off[it] = (uint32_t)r * (uint32_t)(o.ld * 2) + piece * 16;
-    } else {
-      const int k = at / (kTile / 8), piece = at % (kTile / 8);
-      const int f = (k & 3) | ((k >> 1) & 4);
-      const int col = (((piece >> 1) ^ f) * 2 + (piece & 1)) * 8;
-      off[it] = (uint32_t)min(k, k_left - 1) * (uint32_t)(o.ld * 2) + min(col, o.n - 8 - i0) * 2;
-    }
+struct Lane {
+  static constexpr int kNextRows = TR ? kWaves * 512 / kTile : kWaves * 8;
+  int row;
+  uint32_t bytes;
+};
+template <bool TR>
+__device__ __forceinline__ Lane<TR> lane_of(const Operand& o, int32_t i0) {
+  const int at = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 + (threadIdx.x & 63);
+  if (!TR) {
+    const int row = at >> 3;
+    return {row, (uint32_t)((at & 7) ^ ((row >> 1) & 7)) * 16};
   }
+  const int k = at / (kTile / 8), piece = at % (kTile / 8), f = (k & 3) | ((k >> 1) & 4);
+  const int col = (((piece >> 1) ^ f) * 2 + (piece & 1)) * 8;
+  return {k, (uint32_t)min(col, o.n - 8 - i0) * 2};
+}
+
+// An address that is the same in every lane, in scalar registers.
+__device__ __forceinline__ const char* uniform(const void* p) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+  return (const char*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
 // One 16-byte load of every lane, straight into LDS: lane l's piece goes to `to` + 16 l.
@@ -101,6 +111,20 @@ __device__ __forceinline__ void lane_offsets(const Operand& o, int32_t i0, int32
 // %DW%. It has no result register; land() waits for it.
 __device__ __forceinline__ void load_lds(uint32_t to, const char* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(to), "v"(off), "s"(base)
+               : "memory");
+}
+
+// The same of one float, or one bfloat16 in the low half of a word, a lane.
+__device__ __forceinline__ void load_lds4(uint32_t to, const char* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(to), "v"(off), "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void load_lds2(uint32_t to, const char* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2"
                :
                : "s"(to), "v"(off), "s"(base)
                : "memory");
@@ -124,11 +148,25 @@ __device__ __forceinline__ void interleave() {
   __builtin_amdgcn_sched_group_barrier(0x008, 32 - READS * kEach, 0);
 }
 
-__device__ __forceinline__ void load_stage(uint32_t to, const char* base,
-                                           const uint32_t (&off)[kLoads]) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// A stage of an operand from `base`, off: of the lane's first load. `rows` of it are in
+// memory; the others are read as the last of them.
+template <bool TR>
+__device__ __forceinline__ void load_stage(uint32_t to, const uint16_t* base, uint32_t off,
+                                           const Operand& o, int32_t i0, int32_t rows) {
+  constexpr int kNext = Lane<TR>::kNextRows;
+  to += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+  if (rows >= kNext * kLoads) {
+    const char* from = uniform(base);
+    const int64_t step = kNext * 2 * o.ld;
 #pragma unroll
-  for (int it = 0; it < kLoads; ++it) load_lds(to + (it * kWaves + wave) * 1024, base, off[it]);
+    for (int it = 0; it < kLoads; ++it, from += step) load_lds(to + it * kWaves * 1024, from, off);
+  } else {
+    const Lane<TR> l = lane_of<TR>(o, i0);
+#pragma unroll
+    for (int it = 0; it < kLoads; ++it)
+      load_lds(to + it * kWaves * 1024, uniform(base),
+               (uint32_t)min(l.row + it * kNext, rows - 1) * (uint32_t)(o.ld * 2) + l.bytes);
+  }
 }
 
 // Fragment of 16 rows from i (a multiple of 16) and 32 summed values from 32 * ks:
@@ -151,10 +189,6 @@ __device__ __forceinline__ s16x8 fragment(const lds_char* tile, int i, int ks) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-__device__ __forceinline__ float load_bias(const float* b, int64_t i) { return b[i]; }
-__device__ __forceinline__ float load_bias(const uint16_t* b, int64_t i) {
-  return __uint_as_float((uint32_t)b[i] << 16);
-}
 __device__ __forceinline__ void store_out(float* o, float v) { *o = v; }
 __device__ __forceinline__ void store_out(uint16_t* o, float v) { *o = (uint16_t)pack2(v, 0.f); }
 // Up to four values; `wide`: the place is aligned to four.
@@ -184,6 +218,25 @@ __device__ __forceinline__ float unit_of(float top) {
   return e == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)max(e - 14, 17) << 23);
 }
 
+// Of four blocks of 16 values, of which a lane holds a quarter each (four values: lanes
+// l, l + 16, l + 32, l + 48 hold the first to the last), the lane's own block whole: the
+// l / 16-th. Stores of 32 bytes a lane fill whole lines; of 8 bytes, as the products
+// leave them, they took half as long again as the products of a piece.
+__device__ __forceinline__ void gather16(uint2 a, uint2 b, uint2 c, uint2 d, uint4* lo, uint4* hi) {
+  auto transpose = [](uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, uint32_t* t) {
+    const u32x2 x = __builtin_amdgcn_permlane32_swap(r0, r2, false, false);
+    const u32x2 y = __builtin_amdgcn_permlane32_swap(r1, r3, false, false);
+    const u32x2 v = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
+    const u32x2 w = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+    t[0] = v[0], t[1] = v[1], t[2] = w[0], t[3] = w[1];
+  };
+  uint32_t x[4], y[4];
+  transpose(a.x, b.x, c.x, d.x, x);
+  transpose(a.y, b.y, c.y, d.y, y);
+  *lo = make_uint4(x[0], y[0], x[1], y[1]);
+  *hi = make_uint4(x[2], y[2], x[3], y[3]);
+}
+
 // S; a token without weights has s_c = 0, which counts as S for its gradient.
 __device__ __forceinline__ float top_unit(const Meta& meta) {
   return meta.S ? __uint_as_float(meta.S) : 1.f;
@@ -197,91 +250,136 @@ __device__ __forceinline__ float dw_scale(const Gemm& g, const Meta& meta, int q
   return (s > 0.f ? top / s : 1.f) * 0x1p-14f * unit_of(__uint_as_float(meta.T));
 }
 
+// Per token and row of a tile, kept in LDS for the epilogue.
+struct Params {
+  uint32_t bias[kTile];  // float32, or bfloat16 in the low half
+  float s[kTile];
+  int32_t target[kTile];
+  float lse[kTile], a[kTile], b[kTile], r[kTile], m[kTile];
+};
+constexpr int kSets = 3;
+constexpr int kColBytes = 4 * kTile * 4;  // column sums of the four waves along Q
+constexpr int kLdsBytes = 2 * kStageBytes + kSets * (int)sizeof(Params) + kColBytes;
+constexpr int kGroupP = 4;                // tiles of P that a run takes by all of Q
+
+// A workgroup per CU works through tiles. The stages of its tiles are one sequence: the
+// first two of the next tile are loaded while the present one's last products and its
+// epilogue run, so only the epilogue's own arithmetic is left between two tiles (a
+// workgroup per tile spent 8 us on a tile beside its products, 22 us in all at a width
+// of 640).
 template <int KIND, class T>
 __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   typedef Elem<T> El;
   constexpr bool TP = KIND == kDx || KIND == kDw, TQ = KIND == kDw;
+  constexpr bool kLogits = KIND == kStats || KIND == kLogitGrad;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char* lds = (lds_char*)smem;
   const uint32_t lds_at = (uint32_t)(uintptr_t)lds;
-  lds_poison(smem, 2 * kStageBytes);
+  Params* params = reinterpret_cast<Params*>(smem + 2 * kStageBytes);
+  lds_poison(smem, kLdsBytes);
 
   const Meta meta = *g.meta;
-  // Workgroups go round the eight dies: each gets a run of neighbouring tiles, four
-  // of P by all of Q at a time, so that what a die's tiles read meets in its L2.
-  const int total = g.tp * g.tq * g.splits, each = (total + 7) / 8;
-  int id = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= each || id >= total) return;
-  const int split = id / (g.tp * g.tq);
-  id -= split * (g.tp * g.tq);
-  const int group = id / (4 * g.tq), in = id - group * 4 * g.tq;
-  const int wide = min(4, g.tp - group * 4);
-  const int tq = in / wide, tp = group * 4 + in % wide;
-  const int p0 = tp * kTile, q0 = tq * kTile;
-  int k_all = g.k;
-  if (KIND == kDw) k_all = min(k_all, (meta.n + kStep - 1) / kStep * kStep);
-  else if (q0 >= meta.n) return;
-  const int steps_all = k_all / kStep, each_split = (steps_all + g.splits - 1) / g.splits;
-  const int first = min(split * each_split, steps_all);
-  const int steps = min(each_split, steps_all - first);
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = (wave >> 2) * 128, wq = (wave & 3) * 64;
-  // lane l holds q = l % 16 and p = 4 (l / 16) ... of each 16 x 16
-  const int lq = lane & 15, lp = 4 * (lane >> 4);
-  const int c_wave = g.c0 + p0 + wp + lp;  // first token of the lane, of 4 in every 16
-  constexpr bool kLogits = KIND == kStats || KIND == kLogitGrad;
-  const T* bias = static_cast<const T*>(g.bias);
-  f32x4 acc[8][4];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (kLogits && !El::kScaled) {
-    // sums begin at the bias, and at -inf behind the last token
-    if (bias) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          acc[i][0][e] = load_bias(bias, min(c_wave + 16 * i + e, g.C - 1));
-    }
-    if (g.c0 + p0 + kTile > g.C) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c_wave + 16 * i + e >= g.C) acc[i][0][e] = -__builtin_huge_valf();
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int j = 1; j < 4; ++j) acc[i][j] = acc[i][0];
-  }
 
-  uint32_t off_p[kLoads], off_q[kLoads];
-  lane_offsets<TP>(g.P, p0, kStep, off_p);
-  lane_offsets<TQ>(g.Q, q0, kStep, off_q);
-  const char* base_p = (const char*)(g.P.p + (TP ? p0 : p0 * g.P.ld));
-  const char* base_q = (const char*)(g.Q.p + (TQ ? q0 : q0 * g.Q.ld));
-  const int64_t step_p = TP ? g.P.ld * (kStep * 2) : kStep * 2;
-  const int64_t step_q = TQ ? g.Q.ld * (kStep * 2) : kStep * 2;
-  auto issue = [&](int s, int buf) {
-    const int k = first + s / El::PAIRS, pair = s % El::PAIRS;
-    const char* bp = base_p + k * step_p + El::p(pair) * g.P.plane * 2;
-    const char* bq = base_q + k * step_q + El::q(pair) * g.Q.plane * 2;
-    if (TP && KIND == kDx) {
-      // the last tokens: rows of w behind them are not read
-      const int left = g.P.kn - k * kStep;
-      if (left < kStep) lane_offsets<TP>(g.P, p0, left, off_p);
-    }
-    load_stage(lds_at + buf * kStageBytes, bp, off_p);
-    load_stage(lds_at + buf * kStageBytes + kOperandBytes, bq, off_q);
+  // Workgroups go round the eight dies: each die has a run of neighbouring tiles, four of P
+  // by all of Q at a time, so that what its workgroups read meets in its L2.
+  const int tiles_q = KIND == kDw ? g.tq : min(g.tq, (meta.n + kTile - 1) / kTile);
+  const int tiles = g.tp * tiles_q, total = tiles * g.splits, each = (total + 7) / 8;
+  const int stride = gridDim.x >> 3, end = min(((int)(blockIdx.x & 7) + 1) * each, total);
+  const int begin = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  int steps_all = g.k / kStep;
+  if (KIND == kDw) steps_all = min(steps_all, (meta.n + kStep - 1) / kStep);
+  const int steps_each =
+      __builtin_amdgcn_readfirstlane((steps_all + g.splits - 1) / g.splits);
+  struct Tile {
+    int p, q, split, first, steps;
   };
+  auto tile_of = [&](int id) {
+    Tile t;
+    // (quotients come from vector instructions)
+    t.split = __builtin_amdgcn_readfirstlane(id / tiles);
+    id -= t.split * tiles;
+    const int group = __builtin_amdgcn_readfirstlane(id / (kGroupP * tiles_q));
+    const int in = id - group * kGroupP * tiles_q, wide = min(kGroupP, g.tp - group * kGroupP);
+    t.q = __builtin_amdgcn_readfirstlane(in / wide);
+    t.p = group * kGroupP + in - t.q * wide;
+    t.first = min(t.split * steps_each, steps_all);
+    t.steps = min(steps_each, steps_all - t.first);
+    return t;
+  };
+
+  // the sequence of stages that are loaded
+  int load_id = begin - stride, load_s = 0, load_n = 0;
+  Tile load_tile = {};
+  uint32_t off_p = 0, off_q = 0;
+  int load_turn = 0;
+  // What the epilogue needs, one token or row a lane. A tile's are loaded with its first
+  // stage: up to two tiles ahead (tiles of one stage), when every wave has left the
+  // epilogue before the present tile. So three sets are enough.
+  auto load_params = [&](const Tile& t, int turn) {
+    const uint32_t to = lds_at + 2 * kStageBytes + turn * sizeof(Params);
+    auto four = [&](const void* from, uint32_t index, uint32_t at) {
+      load_lds4(to + at, (const char*)from, 4 * index);
+    };
+    if (wave < 4) {
+      const uint32_t c = min(g.c0 + t.p * kTile + 64 * wave + lane, g.C - 1), at = 256 * wave;
+      if (El::kScaled) four(g.s, c, offsetof(Params, s) + at);
+      if (g.bias && sizeof(T) == 4) four(g.bias, c, offsetof(Params, bias) + at);
+      if (g.bias && sizeof(T) == 2)
+        load_lds2(to + offsetof(Params, bias) + at, (const char*)g.bias, 2 * c);
+    } else {
+      const uint32_t row = min(t.q * kTile + 64 * (wave - 4) + lane, meta.n - 1);
+      const uint32_t at = 256 * (wave - 4);
+      four(g.row.target, row, offsetof(Params, target) + at);
+      if (KIND == kLogitGrad) {
+        four(g.row.lse, row, offsetof(Params, lse) + at);
+        four(g.row.a, row, offsetof(Params, a) + at);
+        four(g.row.b, row, offsetof(Params, b) + at);
+        if (El::kScaled) four(g.row.m, row, offsetof(Params, m) + at);
+      }
+      if (El::kScaled) four(g.row.r, row, offsetof(Params, r) + at);
+    }
+  };
+  auto issue = [&](int buf) {
+    while (load_s == load_n) {  // (a part may have no steps)
+      load_id += stride;
+      if (load_id >= end) {
+        load_n = load_s + 1;  // (and stays so)
+        load_id = end;
+        break;
+      }
+      load_tile = tile_of(load_id);
+      load_s = 0;
+      load_n = load_tile.steps * El::PAIRS;
+      if (load_n > 0) {
+        if (kLogits) load_params(load_tile, load_turn);
+        load_turn = load_turn == kSets - 1 ? 0 : load_turn + 1;
+        const Lane<TP> lp = lane_of<TP>(g.P, load_tile.p * kTile);
+        const Lane<TQ> lq = lane_of<TQ>(g.Q, load_tile.q * kTile);
+        off_p = lp.row * (uint32_t)(g.P.ld * 2) + lp.bytes;
+        off_q = lq.row * (uint32_t)(g.Q.ld * 2) + lq.bytes;
+      }
+    }
+    if (load_id >= end) return;
+    const int k = load_tile.first + load_s / El::PAIRS, pair = load_s % El::PAIRS;
+    const int64_t p0 = load_tile.p * kTile, q0 = load_tile.q * kTile, k0 = (int64_t)k * kStep;
+    const uint16_t* bp = g.P.p + El::p(pair) * g.P.plane + (TP ? k0 * g.P.ld + p0 : p0 * g.P.ld + k0);
+    const uint16_t* bq = g.Q.p + El::q(pair) * g.Q.plane + (TQ ? k0 * g.Q.ld + q0 : q0 * g.Q.ld + k0);
+    // (a transposed operand has all of a stage's rows, but for w behind the last token)
+    const int rows_p = TP ? (KIND == kDx ? g.P.kn - (int)k0 : kStep) : g.P.n - (int)p0;
+    const int rows_q = TQ ? kStep : g.Q.n - (int)q0;
+    const uint32_t to = lds_at + buf * kStageBytes;
+    load_stage<TP>(to, bp, off_p, g.P, (int)p0, rows_p);
+    load_stage<TQ>(to + kOperandBytes, bq, off_q, g.Q, (int)q0, rows_q);
+    ++load_s;
+  };
+
   // Fragments of one half of a stage are read while the products of the other half run.
   // A stage's second half is in registers before the barrier in its middle, so behind
   // that its place takes the stage after next, whose loads then have a whole stage's
   // time; and no wave waits for LDS right after a barrier.
+  f32x4 acc[8][4];
   s16x8 pa[2][8], qb[2][4];
   auto read = [&](int buf, int half) {
     const lds_char* P = lds + buf * kStageBytes;
@@ -298,208 +396,280 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       for (int j = 0; j < 4; ++j) acc[i][j] = El::mfma(pa[half][i], qb[half][j], acc[i][j]);
     interleave<(TP ? 16 : 8) + (TQ ? 8 : 4)>();
   };
-  const int n_stage = steps * El::PAIRS;
-  if (n_stage > 0) {
-    issue(0, 0);
-    if (n_stage > 1) {
-      issue(1, 1);
-      land<2 * kLoads>();
-    } else {
-      land<0>();
-    }
-    __syncthreads();
-    read(0, 0);
+
+  issue(0);
+  issue(1);
+  land<0>();
+  __syncthreads();
+  int buf = 0, turn = 0;
+  for (int id = begin; id < end; id += stride) {
+    const Tile tile = tile_of(id);
+    const int p0 = tile.p * kTile, q0 = tile.q * kTile, n_stage = tile.steps * El::PAIRS;
+    const Params& par = params[turn];
+    turn = turn == kSets - 1 ? 0 : turn + 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    read(buf, 0);
     for (int s = 0; s < n_stage; ++s) {
-      read(s & 1, 1);
+      read(buf, 1);
       multiply(0);
       land<0>();  // the next stage
       __syncthreads();
-      if (s + 2 < n_stage) issue(s + 2, s & 1);
-      read((s + 1) & 1, 0);  // (behind the last stage nothing uses it)
+      issue(buf);
+      buf ^= 1;
+      read(buf, 0);  // (behind the last stage nothing uses it)
       multiply(1);
     }
-  }
 
-  if (kLogits && El::kScaled) {
-    float r[4];
+    // (the epilogue's addresses are made here: kept over the loop above they would not
+    // leave enough registers for it)
+    int of_lane = lane;
+    asm volatile("" : "+v"(of_lane));
+    // lane l holds q = l % 16 and p = 4 (l / 16) ... of each 16 x 16
+    const int lq = of_lane & 15, lp = 4 * (of_lane >> 4);
+    const int c_lane = wp + lp;  // first token of the lane in the tile, of 4 in every 16
+    if (kLogits) {
+      if (El::kScaled) {
+        float r[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r[j] = g.row.r[min(q0 + wq + 16 * j + lq, meta.n - 1)];
+        for (int j = 0; j < 4; ++j) r[j] = par.r[wq + 16 * j + lq];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i) {
+          const f32x4 s = *reinterpret_cast<const f32x4*>(&par.s[c_lane + 16 * i]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = c_wave + 16 * i + e, at = min(c, g.C - 1);
-        const float s = g.s[at];
-        float add = bias ? load_bias(bias, at) : 0.f;
-        if (c >= g.C) add = -__builtin_huge_valf();
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j][e] = acc[i][j][e] * s * r[j] + add;
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * s[e] * r[j];
+        }
       }
-  }
-  if (KIND == kStats) {
+      if (g.bias) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = q0 + wq + 16 * j + lq;
-      // the row's target among the lane's tokens
-      const int t = (row < meta.n ? g.row.target[row] : -1) - c_wave;
-      const bool mine = t >= 0 && t < 128 && (t & 12) == 0;
-      if (__ballot(mine)) {
-        float hit = 0.f;
+        for (int i = 0; i < 8; ++i) {
+          const uint4 b = *reinterpret_cast<const uint4*>(&par.bias[c_lane + 16 * i]);
+          const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float add = __uint_as_float(sizeof(T) == 4 ? w[e] : w[e] << 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j][e] += add;
+          }
+        }
+      }
+      if (g.c0 + p0 + kTile > g.C) {
+        // nothing behind the last token
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (t == 16 * i + e) hit = acc[i][j][e];
-        if (mine) g.hit[row] = hit;
+            if (g.c0 + p0 + c_lane + 16 * i + e >= g.C) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) acc[i][j][e] = -__builtin_huge_valf();
+            }
       }
-      float m = -__builtin_huge_valf();
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
-      m = fmaxf(m, __shfl_xor(m, 16));
-      m = fmaxf(m, __shfl_xor(m, 32));
-      // (a NaN among the logits is no maximum, but it is in the sum)
-      const float base = m == -__builtin_huge_valf() ? 0.f : m;
-      // one rounding for all terms: it moves the log-sum-exp by half a step of m
-      const float shift = -base * kLog2e;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, shift));
-      float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      all += __shfl_xor(all, 16);
-      all += __shfl_xor(all, 32);
-      if (row < meta.n && lane < 16)
-        g.part[(int64_t)row * g.n_part + 2 * tp + (wave >> 2)] = make_float2(m, all);
     }
-  }
-  if (KIND == kLogitGrad) {
-    float cs[8][4];
+    if (KIND == kStats) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+      for (int j = 0; j < 4; ++j) {
+        const int row = q0 + wq + 16 * j + lq;
+        // the row's target among the lane's tokens
+        const int t =
+            row < meta.n ? par.target[wq + 16 * j + lq] - (g.c0 + p0 + c_lane) : -1;
+        const bool here = t >= 0 && t < 128 && (t & 12) == 0;
+        if (__ballot(here)) {
+          float hit = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) cs[i][e] = 0.f;
-    float to_f16[8][4];
-    if (El::kScaled) {
-      const float top = 0x1p14f / top_unit(meta);
+          for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float s = g.s[min(c_wave + 16 * i + e, g.C - 1)];
-          to_f16[i][e] = s > 0.f ? s * top : 0x1p14f;
+            for (int e = 0; e < 4; ++e)
+              if (t == 16 * i + e) hit = acc[i][j][e];
+          if (here) g.hit[row] = hit;
         }
-    }
+        float m = -__builtin_huge_valf();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = q0 + wq + 16 * j + lq;
-      const bool in = row < meta.n;
-      const float norm = El::kScaled ? 1.f : meta.inverse;
-      const float lse = in ? g.row.lse[row] : 0.f, shift = -lse * kLog2e;
-      const float a = in ? g.row.a[row] * norm : 0.f;
-      const float m = El::kScaled && in ? g.row.m[row] : 0.f;
-      const int t = (in ? g.row.target[row] : -1) - c_wave;
-      const bool mine = t >= 0 && t < 128 && (t & 12) == 0;
-      // G over the logits
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // float32: the difference first, whose rounding is small where p is not
-          const float z = acc[i][j][e];
-          const float p = __builtin_amdgcn_exp2f(El::kScaled ? (z - lse) * kLog2e
-                                                             : __builtin_fmaf(z, kLog2e, shift));
-          acc[i][j][e] = in ? a * p : 0.f;
-        }
-      if (__ballot(mine)) {
-        const float b = in ? g.row.b[row] * norm : 0.f;
+          for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        // (a NaN among the logits is no maximum, but it is in the sum)
+        const float base = m == -__builtin_huge_valf() ? 0.f : m;
+        // one rounding for all terms: it moves the log-sum-exp by half a step of m
+        const float shift = -base * kLog2e;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (t == 16 * i + e) acc[i][j][e] -= b;
+            sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, shift));
+        float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        all += __shfl_xor(all, 16);
+        all += __shfl_xor(all, 32);
+        if (row < meta.n && of_lane < 16)
+          g.part[(int64_t)row * g.n_part + 2 * tile.p + (wave >> 2)] = make_float2(m, all);
+      }
+    }
+    if (KIND == kLogitGrad) {
+      const float top = 0x1p14f / top_unit(meta), norm = El::kScaled ? 1.f : meta.inverse;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = wq + 16 * j + lq, row = q0 + at;
+        const bool in = row < meta.n;
+        const float lse = par.lse[at], shift = -lse * kLog2e, a = par.a[at] * norm;
+        const int t = in ? par.target[at] - (g.c0 + p0 + c_lane) : -1;
+        // G over the logits
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            // float32: the difference first, whose rounding is small where p is not
+            const float z = acc[i][j][e];
+            const float p = __builtin_amdgcn_exp2f(El::kScaled ? (z - lse) * kLog2e
+                                                               : __builtin_fmaf(z, kLog2e, shift));
+            acc[i][j][e] = in ? a * p : 0.f;
+          }
+        if (__ballot(t >= 0 && t < 128 && (t & 12) == 0)) {
+          const float b = par.b[at] * norm;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (t == 16 * i + e) acc[i][j][e] -= b;
+        }
       }
       if (g.col) {
+        // the tile's columns: over the lane's rows, 16 lanes, and the four waves through LDS
+        float* sums = reinterpret_cast<float*>(smem + 2 * kStageBytes + kSets * sizeof(Params));
+        float m[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int j = 0; j < 4; ++j) m[j] = El::kScaled ? par.m[wq + 16 * j + lq] : 1.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) cs[i][e] += El::kScaled ? acc[i][j][e] * m : acc[i][j][e];
-      }
-      uint16_t* to = g.G + (int64_t)row * g.ldg + p0 + wp + lp;
+        for (int i = 0; i < 8; ++i) {
+          float cs[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = El::kScaled ? acc[i][j][e] * to_f16[i][e] : acc[i][j][e];
-        uint2 out[El::PLANES];
-        El::planes4(v, out);
-#pragma unroll
-        for (int s = 0; s < El::PLANES; ++s)
-          *reinterpret_cast<uint2*>(to + s * g.g_plane + 16 * i) = out[s];
-      }
-    }
-    if (g.col) {
-      // the tile's columns: over 16 lanes, then over the four waves through LDS
-      float* sums = reinterpret_cast<float*>(smem);  // [4, kTile]
-      __syncthreads();  // (the last stage is read)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = cs[i][e];
-          v += __shfl_xor(v, 1);
-          v += __shfl_xor(v, 2);
-          v += __shfl_xor(v, 4);
-          v += __shfl_xor(v, 8);
-          cs[i][e] = v;
+          for (int e = 0; e < 4; ++e) {
+            float v = El::kScaled ? (acc[i][0][e] * m[0] + acc[i][1][e] * m[1]) +
+                                        (acc[i][2][e] * m[2] + acc[i][3][e] * m[3])
+                                  : (acc[i][0][e] + acc[i][1][e]) + (acc[i][2][e] + acc[i][3][e]);
+            v += __shfl_xor(v, 1);
+            v += __shfl_xor(v, 2);
+            v += __shfl_xor(v, 4);
+            v += __shfl_xor(v, 8);
+            cs[e] = v;
+          }
+          if (lq == 0)
+            *reinterpret_cast<float4*>(sums + (wave & 3) * kTile + c_lane + 16 * i) =
+                make_float4(cs[0], cs[1], cs[2], cs[3]);
         }
-        if (lq == 0)
-          *reinterpret_cast<float4*>(sums + (wave & 3) * kTile + wp + lp + 16 * i) =
-              make_float4(cs[i][0], cs[i][1], cs[i][2], cs[i][3]);
+        __syncthreads();
+        const int c = threadIdx.x;
+        if (c < kTile)
+          g.col[(int64_t)tile.q * g.ldg + p0 + c] =
+              (sums[c] + sums[kTile + c]) + (sums[2 * kTile + c] + sums[3 * kTile + c]);
+        // (the next tile's sums come behind its own barriers)
       }
-      __syncthreads();
-      const int c = threadIdx.x;
-      if (c < kTile)
-        g.col[(int64_t)tq * g.ldg + p0 + c] =
-            (sums[c] + sums[kTile + c]) + (sums[2 * kTile + c] + sums[3 * kTile + c]);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float to_f16[4][4];
+        if (El::kScaled) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 s =
+                *reinterpret_cast<const f32x4*>(&par.s[c_lane + 64 * half + 16 * i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to_f16[i][e] = s[e] > 0.f ? s[e] * top : 0x1p14f;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint2 out[4][El::PLANES];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = acc[4 * half + i][j][e];
+              v[e] = El::kScaled ? x * to_f16[i][e] : x;
+            }
+            El::planes4(v, out[i]);
+          }
+          const int64_t row = q0 + wq + 16 * j + lq;
+          uint16_t* to = g.G + row * g.ldg + p0 + wp + 64 * half + 4 * lp;
+#pragma unroll
+          for (int s = 0; s < El::PLANES; ++s) {
+            uint4 lo, hi;
+            gather16(out[0][s], out[1][s], out[2][s], out[3][s], &lo, &hi);
+            reinterpret_cast<uint4*>(to + s * g.g_plane)[0] = lo;
+            reinterpret_cast<uint4*>(to + s * g.g_plane)[1] = hi;
+          }
+        }
+      }
     }
-  }
-  if (KIND == kDx || KIND == kDw) {
-    const bool wide = g.ldo % 4 == 0 && (uintptr_t)g.out % (4 * sizeof(T)) == 0;
+    if (KIND == kDx || KIND == kDw) {
+      // rows that can be stored by 16 bytes (bfloat16: and end at one)
+      const bool wide = g.ldo % 8 == 0 && (uintptr_t)g.out % 16 == 0 &&
+                        (sizeof(T) == 4 || g.D % 8 == 0);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int q = q0 + wq + 16 * j + lq;
-      if (q >= (KIND == kDx ? meta.n : g.n_q)) continue;
-      float scale = 1.f;
-      if (KIND == kDw && g.out) scale = dw_scale<T>(g, meta, q);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int d = p0 + wp + 16 * i + lp;
+      for (int j = 0; j < 4; ++j) {
+        const int q = q0 + wq + 16 * j + lq;
+        float scale = 1.f;
+        if (KIND == kDw && g.out && q < g.n_q) scale = dw_scale<T>(g, meta, q);
         if (KIND == kDw && g.out) {
-          const float v[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale, acc[i][j][2] * scale,
-                              acc[i][j][3] * scale};
-          store4(static_cast<T*>(g.out) + q * g.ldo + d, v, wide, g.D - d);
-        } else if (d < g.lda) {
-          f32x4* o = reinterpret_cast<f32x4*>(g.acc + split * g.acc_split + (int64_t)q * g.lda + d);
-          *o = g.add ? *o + acc[i][j] : acc[i][j];
+          T* o = static_cast<T*>(g.out) + q * g.ldo;
+          if constexpr (sizeof(T) == 2) {
+            if (wide) {
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                uint2 out[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const f32x4 v = acc[4 * half + i][j] * scale;
+                  out[i] = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+                }
+                uint4 lo, hi;
+                gather16(out[0], out[1], out[2], out[3], &lo, &hi);
+                const int d = p0 + wp + 64 * half + 4 * lp;
+                if (q < g.n_q && d < g.D) reinterpret_cast<uint4*>(o + d)[0] = lo;
+                if (q < g.n_q && d + 8 < g.D) reinterpret_cast<uint4*>(o + d)[1] = hi;
+              }
+              continue;
+            }
+          }
+          if (q < g.n_q) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int d = p0 + c_lane + 16 * i;
+              const float v[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale,
+                                  acc[i][j][2] * scale, acc[i][j][3] * scale};
+              store4(o + d, v, wide, g.D - d);
+            }
+          }
+        } else if (q < (KIND == kDx ? meta.n : g.n_q)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int d = p0 + c_lane + 16 * i;
+            if (d >= g.lda) break;
+            f32x4* o =
+                reinterpret_cast<f32x4*>(g.acc + tile.split * g.acc_split + (int64_t)q * g.lda + d);
+            *o = g.add ? *o + acc[i][j] : acc[i][j];
+          }
         }
       }
     }
   }
+  land<0>();  // (nothing is left in flight into LDS that another workgroup may get)
 }
 
 template <int KIND, class T>
 hipError_t launch(const Gemm& g, hipStream_t st) {
   const int64_t total = (int64_t)g.tp * g.tq * g.splits;
   if (total <= 0) return hipSuccess;
-  const int64_t grid = up(total, 8);
-  if (grid > most_groups(kThreads)) return hipErrorInvalidValue;
+  if (total > INT32_MAX / 2) return hipErrorInvalidValue;
+  const int64_t grid = total < 256 ? up(total, 8) : 256;
   (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_kernel<KIND, T>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kStageBytes);
-  gemm_kernel<KIND, T><<<dim3((unsigned)grid), dim3(kThreads), 2 * kStageBytes, st>>>(g);
+                            hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+  gemm_kernel<KIND, T><<<dim3((unsigned)grid), dim3(kThreads), kLdsBytes, st>>>(g);
   return hipGetLastError();
 }
 
