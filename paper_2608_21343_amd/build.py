@@ -25,7 +25,7 @@ HIP_SOURCES = ["capi.hip", "greedy.hip", "greedy_seg.hip",
                "rows.hip", "rows_score_f32.hip", "rows_score_bf16.hip", "rows_grad_f32.hip",
                "rows_grad_bf16.hip", "rows_distill_f32.hip", "rows_distill_bf16.hip",
                "capi_train.hip", "linear.hip", "linear_fwd_f32.hip", "linear_fwd_bf16.hip",
-               "linear_bwd_f32.hip", "linear_bwd_bf16.hip", "adamw.hip"]
+               "linear_bwd_f32.hip", "linear_bwd_bf16.hip", "linear_few.hip", "adamw.hip"]
 CXX_SOURCES = ["compiler.cpp", "variative.cpp", "cache.cpp", "errors.cpp"]
 
 HIPCC_FLAGS = [

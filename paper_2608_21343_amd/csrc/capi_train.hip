@@ -139,7 +139,7 @@ extern "C" int64_t tb_linear_xent_workspace_bytes(int32_t dtype, int64_t n_rows,
   c.dx = grads & 1 ? &some : nullptr;
   c.dw = grads & 2 ? &some : nullptr;
   c.db = grads & 4 ? &some : nullptr;
-  return linear::workspace_bytes(c);
+  return linear::most_workspace(c);
 }
 
 extern "C" int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype,

@@ -1,5 +1,7 @@
 // Cross entropy of a linear layer without its logits (linear.hpp): gathering of the
 // rows, what joins the tiles' results, and the launches of a call.
+#include <algorithm>
+
 #include "linear_gemm.hpp"
 
 namespace tbias {
@@ -344,13 +346,16 @@ __global__ void __launch_bounds__(256)
 
 // ---- what joins the tiles
 
-// One wave a gathered row: log-sum-exp and loss.
+// One wave a row: log-sum-exp and loss. Gathered rows, whose parts lie by their place
+// or (by_row) by their row; or (idx NULL) all rows, and 0 for those left out.
 struct Finish {
   const Meta* meta;
   const float2* part;
   int32_t n_part;
   const float* hit;
-  const int32_t *idx, *tgt;
+  const int32_t *idx, *target;  // target of every row of x
+  bool by_row;
+  int32_t n, C;
   const float* weight;
   float *lse_c, *a, *b;
   float *out_loss, *out_lse;
@@ -358,9 +363,17 @@ struct Finish {
 
 __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= f.meta->n) return;
-  const float2* part = f.part + row * f.n_part;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= (f.idx ? f.meta->n : f.n)) return;
+  const int64_t row = f.idx ? f.idx[at] : at, from = f.by_row ? row : at;
+  const int32_t t = f.target[row];
+  const float weight = f.weight ? f.weight[row] : 1.f;
+  if (!f.idx && (t == -1 || weight == 0.f)) {
+    if (lane == 0 && f.out_loss) f.out_loss[row] = 0.f;
+    if (lane == 0 && f.out_lse) f.out_lse[row] = 0.f;
+    return;
+  }
+  const float2* part = f.part + from * f.n_part;
   float m = -__builtin_huge_valf();
   for (int i = lane; i < f.n_part; i += 64) m = fmaxf(m, part[i].x);
 #pragma unroll
@@ -376,18 +389,91 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   if (lane != 0) return;
   const float lse = base + logf(sum);
-  const int64_t r = f.idx[row];
-  if (f.out_lse) f.out_lse[r] = lse;
+  if (f.out_lse) f.out_lse[row] = lse;
   if (f.out_loss) {
-    const float hit = f.tgt[row] < 0 ? __builtin_nanf("") : f.hit[row];
+    const float hit = (uint32_t)t < (uint32_t)f.C ? f.hit[from] : __builtin_nanf("");
     const float nll = lse == -__builtin_huge_valf() && hit == lse ? __builtin_huge_valf() : lse - hit;
-    f.out_loss[r] = f.weight ? f.weight[r] * nll : nll;
+    f.out_loss[row] = f.weight ? weight * nll : nll;
   }
+  if (!f.idx) return;
   if (lse == -__builtin_huge_valf()) {
-    f.lse_c[row] = 0.f;
-    f.a[row] = f.b[row] = 0.f;
+    f.lse_c[at] = 0.f;
+    f.a[at] = f.b[at] = 0.f;
   } else {
-    f.lse_c[row] = lse;
+    f.lse_c[at] = lse;
+  }
+}
+
+// The gradients of logits that are kept: 64 gathered rows by 256 tokens a workgroup, 16
+// rows a wave. The rows behind the last one, up to a multiple of kStep, get zeros, and so
+// do the tokens.
+struct Kept {
+  const Meta* meta;
+  const float* z;
+  int32_t ldz;
+  const int32_t* idx;  // rows of z, or NULL: gathered ones
+  RowArgs row;
+  const float* s;
+  int32_t C, cols;
+  uint16_t* G;
+  int64_t plane;
+  float* col;
+};
+
+template <class T>
+__global__ void __launch_bounds__(256) kept_kernel(const Kept k) {
+  typedef Elem<T> El;
+  const Meta meta = *k.meta;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row0 = (int64_t)blockIdx.y * 64 + 16 * wave;
+  const int c0 = blockIdx.x * 256 + 4 * lane;
+  if ((int64_t)blockIdx.y * 64 >= up(meta.n, kStep)) return;
+  float scale[4] = {1.f, 1.f, 1.f, 1.f};
+  if (El::kScaled) {
+    const float top = 0x1p14f / top_unit(meta);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float s = k.s[min(c0 + e, k.C - 1)];
+      scale[e] = s > 0.f ? s * top : 0x1p14f;
+    }
+  }
+  const float norm = El::kScaled ? 1.f : meta.inverse;
+  float cs[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c0 < k.cols) {
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+      const int64_t at = row0 + i;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (at < meta.n) {
+        const float* z = k.z + (k.idx ? (int64_t)k.idx[at] : at) * k.ldz + c0;
+        const float lse = k.row.lse[at], a = k.row.a[at] * norm, b = k.row.b[at] * norm;
+        const int t = k.row.target[at] - c0;
+        const f32x4 l = *reinterpret_cast<const f32x4*>(z);
+        const float m = El::kScaled ? k.row.m[at] : 1.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (c0 + e >= k.C) continue;
+          v[e] = a * __builtin_amdgcn_exp2f((l[e] - lse) * kLog2e) - (t == e ? b : 0.f);
+          cs[e] += v[e] * m;
+          if (El::kScaled) v[e] *= scale[e];
+        }
+      }
+      uint2 p[El::PLANES];
+      El::planes4(v, p);
+#pragma unroll
+      for (int s = 0; s < El::PLANES; ++s)
+        *reinterpret_cast<uint2*>(k.G + s * k.plane + at * k.ldz + c0) = p[s];
+    }
+  }
+  if (!k.col) return;
+  __shared__ float4 sums[4][64];
+  sums[wave][lane] = make_float4(cs[0], cs[1], cs[2], cs[3]);
+  __syncthreads();
+  if (wave == 0 && c0 < k.cols) {
+    const float4 a = sums[0][lane], b = sums[1][lane], c = sums[2][lane], d = sums[3][lane];
+    *reinterpret_cast<float4*>(k.col + (int64_t)blockIdx.y * k.ldz + c0) =
+        make_float4((a.x + b.x) + (c.x + d.x), (a.y + b.y) + (c.y + d.y),
+                    (a.z + b.z) + (c.z + d.z), (a.w + b.w) + (c.w + d.w));
   }
 }
 
@@ -420,15 +506,16 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// db[c] = the sum of the row tiles' columns: 64 tokens a workgroup, a quarter of the
-// tiles each wave.
+// db[c] = the sum of the columns over the blocks of `rows` rows: 64 tokens a workgroup,
+// a quarter of the blocks each wave.
 template <class T>
 __global__ void __launch_bounds__(256)
-    columns_kernel(const float* col, int32_t ldg, const Meta* meta, T* db, int32_t n) {
+    columns_kernel(const float* col, int32_t ldg, const Meta* meta, int32_t rows, T* db,
+                   int32_t n) {
   __shared__ float sums[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = blockIdx.x * 64 + lane;
-  const int tiles = (meta->n + kTile - 1) / kTile;
+  const int tiles = (meta->n + rows - 1) / rows;
   float sum = 0.f;
   if (c < n)
     for (int q = wave; q < tiles; q += 4) sum += col[(int64_t)q * ldg + c];
@@ -443,14 +530,15 @@ __global__ void __launch_bounds__(256)
 // ---- workspace
 
 constexpr int64_t kGradBytes = 256ll << 20;  // of the gradients of a piece's logits
+constexpr int32_t kFewRows = 64;             // that linear_few.hip takes
 
 struct Layout {
   int64_t np, dp, planes;      // gathered rows and values a row, rounded up
-  bool copy_w;
+  bool copy_w, few, gather, kept;      // kept: the logits, from the statistics to their gradients
   int32_t n_part;
   int32_t piece, pieces;       // tokens of a piece of the vocabulary
   int32_t split_x, split_w;
-  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, s, hit, part, x, xm, w, G, acc_x;
+  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, s, hit, part, x, xm, w, z, G, acc_x;
   int64_t acc_w, col, total;
 };
 
@@ -479,7 +567,16 @@ Layout plan(const Call& c) {
   L.np = up(c.n, kTile);
   L.dp = up(c.D, kStep);
   L.copy_w = f32 || c.D % kStep != 0 || c.w_stride % 8 != 0 || (uintptr_t)c.w % 16 != 0;
-  L.n_part = 2 * (int32_t)(up(c.C, kTile) / kTile);
+  // few rows are read where they are (16-byte aligned, of whole pieces of 16 bytes)
+  const int64_t size = f32 ? 4 : 2;
+  const bool read = c.D * size % 16 == 0 && c.w_stride * size % 16 == 0 &&
+                    (uintptr_t)c.w % 16 == 0 && c.x_stride * size % 16 == 0 &&
+                    (uintptr_t)c.x % 16 == 0;
+  L.few = !c.lse && read && c.n <= kFewRows;
+  // (the loss of few rows needs no copies)
+  L.gather = grads || !L.few;
+  L.copy_w = L.copy_w && L.gather;
+  L.n_part = L.few ? few_parts(c.C) : 2 * (int32_t)(up(c.C, kTile) / kTile);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -501,7 +598,7 @@ Layout plan(const Call& c) {
   if (f32) L.s = take((int64_t)c.C * 4);
   L.hit = take(L.np * 4);
   if (!c.lse) L.part = take(L.np * L.n_part * 8);
-  L.x = take(L.planes * L.np * L.dp * 2);
+  if (L.gather) L.x = take(L.planes * L.np * L.dp * 2);
   if (f32 && c.dw) L.xm = take(L.planes * L.np * L.dp * 2);
   if (L.copy_w) L.w = take(L.planes * c.C * L.dp * 2);
   if (grads) {
@@ -511,7 +608,9 @@ Layout plan(const Call& c) {
     pieces = pieces < 1 ? 1 : pieces;
     L.piece = (int32_t)up((c.C + pieces - 1) / pieces, kTile);
     L.pieces = (c.C + L.piece - 1) / L.piece;
+    L.kept = !c.lse && L.pieces == 1 && c.n * L.piece * 4 <= kGradBytes;
     L.G = take(L.planes * L.np * L.piece * 2);
+    if (L.kept) L.z = take(L.np * L.piece * 4);
     const int64_t td = (L.dp + kTile - 1) / kTile;
     if (c.dx) {
       L.split_x = splits(td * (L.np / kTile), L.piece / kStep);
@@ -521,7 +620,7 @@ Layout plan(const Call& c) {
       L.split_w = splits(td * (L.piece / kTile), L.np / kStep);
       if (L.split_w > 1) L.acc_w = take(L.split_w * (int64_t)L.piece * L.dp * 4);
     }
-    if (c.db) L.col = take(L.np / kTile * L.piece * 4);
+    if (c.db) L.col = take(L.np / (L.kept ? 64 : kTile) * L.piece * 4);
   }
   L.total = at;
   return L;
@@ -550,9 +649,10 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
                      a,      b,    lse, r, m, c.out_loss, c.out_lse,
                      c.x_stride, L.np * L.dp, c.D, (int32_t)L.dp, u16(L.x)};
   // (float32 gradients: it also clears what the others take maxima into)
-  if (groups != 1 || f32)
+  if (L.gather && (groups != 1 || f32))
     count_kernel<<<dim3((unsigned)(groups < 1 ? 1 : groups)), dim3(256), 0, st>>>(ga);
-  gather_kernel<T><<<dim3((unsigned)(c.n < 1 ? 1 : (c.n + kRows - 1) / kRows)), dim3(256), 0, st>>>(
+  if (L.gather)
+    gather_kernel<T><<<dim3((unsigned)(c.n < 1 ? 1 : (c.n + kRows - 1) / kRows)), dim3(256), 0, st>>>(
       ga, static_cast<const T*>(c.x));
   if (L.copy_w && c.n > 0)
     weights_kernel<T><<<dim3(c.C < 8192 ? (c.C + 3) / 4 : 2048), dim3(256), 0, st>>>(
@@ -576,15 +676,26 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   g.tq = (int32_t)(L.np / kTile);
   g.D = c.D;
   if (!c.lse && c.n > 0) {
-    g.P = W;
-    g.tp = (c.C + kTile - 1) / kTile;
-    g.part = reinterpret_cast<float2*>(ws + L.part);
-    g.n_part = L.n_part;
-    g.hit = flt(L.hit);
-    e = f32 ? stats_f32(g, st) : stats_bf16(g, st);
+    float2* part = reinterpret_cast<float2*>(ws + L.part);
+    float *hit = flt(L.hit), *z = L.kept ? flt(L.z) : nullptr;
+    if (L.few) {
+      const Few f = {c.x,      c.w,      c.bias,   c.x_stride, c.w_stride, (int32_t)c.n, c.D, c.C,
+                     c.target, L.n_part, part, hit, z, L.piece};
+      e = few(f, c.dtype, st);
+    } else {
+      Gemm s = g;
+      s.P = W;
+      s.tp = (c.C + kTile - 1) / kTile;
+      s.part = part;
+      s.n_part = L.n_part;
+      s.hit = hit;
+      s.z = z;
+      s.ldg = L.piece;
+      e = f32 ? stats_f32(s, st) : stats_bf16(s, st);
+    }
     if (e != hipSuccess) return e;
-    const Finish f = {meta, g.part, L.n_part, g.hit, idx, tgt, c.weight, lse, a, b, c.out_loss,
-                      c.out_lse};
+    const Finish f = {meta,  part, L.n_part, hit,     L.gather ? idx : nullptr, c.target,
+                      L.few, (int32_t)c.n, c.C, c.weight, lse, a, b, c.out_loss, c.out_lse};
     finish_kernel<<<dim3((unsigned)((c.n + 3) / 4)), dim3(256), 0, st>>>(f);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -616,12 +727,19 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     z.g_plane = L.np * L.piece;
     z.ldg = L.piece;
     z.col = c.db ? flt(L.col) : nullptr;
-    e = f32 ? logit_grad_f32(z, st) : logit_grad_bf16(z, st);
+    if (L.kept && c.n > 0) {
+      const Kept k = {meta, flt(L.z), L.piece, L.few ? idx : nullptr, z.row, z.s, c.C,
+                      (int32_t)up(c.C, kStep), z.G, z.g_plane, z.col};
+      kept_kernel<T><<<dim3((c.C + 255) / 256, (unsigned)(L.np / 64)), dim3(256), 0, st>>>(k);
+      e = hipGetLastError();
+    } else {
+      e = f32 ? logit_grad_f32(z, st) : logit_grad_bf16(z, st);
+    }
     if (e != hipSuccess) return e;
     const Operand G = {z.G, z.g_plane, L.piece, (int32_t)L.np, n};
     if (c.db) {
       columns_kernel<T><<<dim3((n + 63) / 64), dim3(256), 0, st>>>(
-          flt(L.col), L.piece, meta, static_cast<T*>(c.db) + c0, n);
+          flt(L.col), L.piece, meta, L.kept ? 64 : kTile, static_cast<T*>(c.db) + c0, n);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -684,6 +802,15 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
 }  // namespace
 
 int64_t workspace_bytes(const Call& c) { return plan(c).total; }
+
+int64_t most_workspace(Call c) {
+  // wherever x lies
+  c.x_stride = c.w_stride;
+  c.x = nullptr;
+  const int64_t aligned = plan(c).total;
+  c.x = reinterpret_cast<const void*>(1);
+  return std::max(aligned, plan(c).total);
+}
 
 hipError_t run(const Call& c, void* workspace, hipStream_t st) {
   char* ws = static_cast<char*>(workspace);

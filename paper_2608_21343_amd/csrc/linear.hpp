@@ -82,6 +82,7 @@ struct Gemm {
   float2* part;    // [gathered row, n_part]: maximum, sum
   int32_t n_part;
   float* hit;      // logit of the row's target
+  float* z;        // [gathered row, ldg] the logits, where they are kept
   uint16_t* G;     // planes of [row, ldg]
   int64_t g_plane;
   int32_t ldg;
@@ -96,6 +97,22 @@ struct Gemm {
 };
 
 enum { kStats, kLogitGrad, kDx, kDw };
+
+// Statistics of the logits of few rows (linear_few.hip), by their place in x.
+struct Few {
+  const void *x, *w, *bias;
+  int64_t x_stride, w_stride;
+  int32_t n, D, C;
+  const int32_t* target;
+  int32_t parts;  // waves that share the tokens
+  float2* part;   // [n, parts]
+  float* hit;     // [n]
+  float* z;       // [n, ldz] the logits, -inf up to a multiple of 16 tokens; or NULL
+  int32_t ldz;
+};
+constexpr int32_t kFewWaves = 2048;  // eight a CU
+int32_t few_parts(int32_t C);
+hipError_t few(const Few& f, int32_t dtype, hipStream_t st);
 
 // One launch of tp * tq * splits tiles.
 hipError_t stats_bf16(const Gemm& g, hipStream_t st);
@@ -122,8 +139,10 @@ struct Call {
   int64_t dx_stride, dw_stride;
 };
 
-// Bytes of workspace, and the launches of a call.
+// Bytes of workspace that a call needs, and that suffice for every x of its sizes; the
+// launches of a call.
 int64_t workspace_bytes(const Call& c);
+int64_t most_workspace(Call c);
 hipError_t run(const Call& c, void* workspace, hipStream_t st);
 
 }  // namespace linear

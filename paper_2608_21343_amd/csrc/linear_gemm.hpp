@@ -470,6 +470,15 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       }
     }
     if (KIND == kStats) {
+      if (g.z) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int64_t row = q0 + wq + 16 * j + lq;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<f32x4*>(g.z + row * g.ldg + p0 + c_lane + 16 * i) = acc[i][j];
+        }
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int row = q0 + wq + 16 * j + lq;
