@@ -827,8 +827,11 @@ def _linear_workspace(x, layer, dx, dw, db, with_lse, workspace, stream):
         need = int(LIB.tb_linear_xent_workspace_bytes(dt, n, D, V1, wp, ws, grads, with_lse))
         if need < 0:
             _check(TB_EINVAL)
-        with torch.cuda.stream(stream):  # (None: the current one)
+        if stream is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        else:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
     return (_dptr(workspace, name="workspace"),
             workspace.numel() * workspace.element_size(), workspace)
 
@@ -889,20 +892,24 @@ _ADAMW_FIELDS = ("param", "grad", "m", "v", "m_unit", "v_unit", "master")
 def _adamw_table(lists, count: int, device):
     """tb_adamw_tensor records as an array of words, from lists of tensors by field
     (None: NULL)."""
+    import torch
+    T, index = torch.Tensor, device.index
     table = np.zeros((count, 8), dtype=np.int64)
     for name, dtype, tensors, sizes in lists:
         if tensors is None:
             continue
         if len(tensors) != count:
             raise ValueError(f"{name} holds {len(tensors)} tensors, needs {count}")
-        for i, t in enumerate(tensors):
-            if (t.dtype is not dtype or t.device != device or not t.is_contiguous()
-                    or t.numel() != sizes[i]):  # the first fault
+        # (a few passes in C: a step of a model's tensors is otherwise bound by this)
+        if (list(map(T.numel, tensors)) != sizes or False in map(T.is_contiguous, tensors)
+                or [t.dtype for t in tensors].count(dtype) != count
+                or list(map(T.get_device, tensors)).count(index) != count):  # the first fault
+            for i, t in enumerate(tensors):
                 if t.device != device:
                     raise ValueError(f"{name}[{i}] must be on {device}")
                 _need(t, sizes[i], f"{name}[{i}]")
                 _dptr(t, dtype, f"{name}[{i}]")
-        table[:, _ADAMW_FIELDS.index(name)] = [t.data_ptr() for t in tensors]
+        table[:, _ADAMW_FIELDS.index(name)] = list(map(T.data_ptr, tensors))
     return table
 
 
@@ -921,11 +928,13 @@ def tb_adamw_step(param, grad, m, v, lr: float, beta1: float = 0.9, beta2: float
     if (m_unit is None) != (v_unit is None):
         raise ValueError("m_unit and v_unit belong together")
     device, dtype = param[0].device, param[0].dtype
+    if device.type != "cuda":
+        raise ValueError("param[0] must be a device tensor")
     if dtype is not _F32 and dtype is not _BF16:
         raise ValueError("parameters must be float32 or bfloat16")
     bits = 32 if m_unit is None else 8
     state = _F32 if bits == 32 else torch.uint8
-    sizes = [t.numel() for t in param]
+    sizes = list(map(torch.Tensor.numel, param))
     units = None if bits == 32 else [(n + 255) // 256 for n in sizes]
     table = _adamw_table((("param", dtype, param, sizes), ("grad", dtype, grad, sizes),
                           ("m", state, m, sizes), ("v", state, v, sizes),
@@ -951,7 +960,9 @@ def tb_adamw_moments(m, v, m_unit, v_unit, out_m, out_v, stream=None) -> None:
     if count == 0:
         return
     device = m[0].device
-    sizes = [t.numel() for t in m]
+    if device.type != "cuda":
+        raise ValueError("m[0] must be a device tensor")
+    sizes = list(map(torch.Tensor.numel, m))
     units = [(n + 255) // 256 for n in sizes]
     table = _adamw_table((("m", torch.uint8, m, sizes), ("v", torch.uint8, v, sizes),
                           ("m_unit", _F32, m_unit, units), ("v_unit", _F32, v_unit, units)),

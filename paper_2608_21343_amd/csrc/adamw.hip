@@ -144,57 +144,65 @@ __device__ __forceinline__ void store8(uint8_t* p, bool vec, int left, const uin
   }
 }
 
+// A code as bits of a float: its run in the exponent, its place in the run in the mantissa,
+// and the first run among the denormals, so that one product (a denormal operand is exact)
+// gives its size times 2^-P.
 template <int P>
 __device__ __forceinline__ float size_of(uint32_t code) {
-  const int e = max((int)(code >> P) - 1, 0);
-  return (float)((code - ((uint32_t)e << P)) << e);
+  return __uint_as_float(code << (23 - P)) * 0x1p126f;
 }
+// `unit` is the block's times 2^4 and 2^10, which undoes the 2^-P: exact powers of two.
 __device__ __forceinline__ float decode_m(uint32_t code, float unit) {
   const float s = size_of<4>(code & 127) * unit;
-  return code >= 128 ? -s : s;
+  return __uint_as_float(__float_as_uint(s) | (code << 24 & 0x80000000u));
 }
 __device__ __forceinline__ float decode_v(uint32_t code, float unit) {
   const float s = size_of<5>(code);
   return s * s * unit;
 }
 
-// The run of a size: e with size * 2^-e below 2^(P + 1), and 2^-e.
+// The run of a size below 2^(P + 7): e with size * 2^-e below 2^(P + 1).
 template <int P>
-__device__ __forceinline__ int run_of(float size, float* scale) {
-  const int e = max((int)(__float_as_uint(size) >> 23) - 127 - P, 0);
-  *scale = __uint_as_float((uint32_t)(127 - e) << 23);
-  return e;
+__device__ __forceinline__ int run_of(float size) {
+  return max(__builtin_amdgcn_frexp_expf(size) - (P + 1), 0);
 }
 
 __device__ __forceinline__ uint32_t encode_m(float m, float inverse, float rnd) {
   const float y = fabsf(m) * inverse;
-  float scale;
-  const int e = run_of<4>(y, &scale);
-  const float q = y * scale, low = floorf(q);
-  const int code = (e << 4) + (int)low + (q - low > rnd ? 1 : 0);
-  return (uint32_t)min(code, 127) + (m < 0.f ? 128u : 0u);
+  const int e = run_of<4>(y);
+  const float q = __builtin_amdgcn_ldexpf(y, -e);
+  const uint32_t code = (e << 4) + (uint32_t)q + (__builtin_amdgcn_fractf(q) > rnd ? 1 : 0);
+  return min(code, 127u) | (m < 0.f ? 128u : 0u);
 }
+// The square root may be off by some steps: where that moves it over a whole number i, the
+// value lies within i^2 2^-22 of i^2, and the comparison takes it to i from either
+// side (its right side is at least (2 i - 1) 2^-17 from both ends, and i is below 64).
 __device__ __forceinline__ uint32_t encode_v(float v, float inverse, float rnd) {
-  const float y = v * inverse, root = sqrtf(y);
-  float scale;
-  const int e = run_of<5>(root, &scale);
-  const float low = floorf(root * scale);
-  const bool more = y * scale * scale - low * low > (2.f * low + 1.f) * rnd;
-  const int code = (e << 5) + (int)low + (more ? 1 : 0);
-  return v > 0.f ? (uint32_t)min(max(code, 1), 255) : 0u;
+  const float y = v * inverse, root = __builtin_amdgcn_sqrtf(y);
+  const int e = run_of<5>(root);
+  const float low = floorf(__builtin_amdgcn_ldexpf(root, -e));
+  const float over = __builtin_fmaf(-low, low, __builtin_amdgcn_ldexpf(y, -2 * e));
+  const uint32_t code = (e << 5) + (uint32_t)low + (over > __builtin_fmaf(2.f, low, 1.f) * rnd ? 1 : 0);
+  return v > 0.f ? min(max(code, 1u), 255u) : 0u;
 }
 
-// Largest of the 32 lanes that hold a block.
-__device__ __forceinline__ float block_max(float v) {
+// 2^-16 (r + 1 / 2)
+__device__ __forceinline__ float fraction(uint32_t r) {
+  return __builtin_fmaf((float)r, 0x1p-16f, 0x1p-17f);
+}
+
+// Largest of the 32 lanes that hold a block, of bits of floats without their signs: those
+// of infinity and NaN lie above all others.
+__device__ __forceinline__ uint32_t block_max(uint32_t v) {
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  for (int d = 16; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
   return v;
 }
 
 // The unit of a block; NaN where it holds a value that is not finite.
-__device__ __forceinline__ float unit_of(float most, float top, bool bad) {
-  const float unit = most * top;
-  return bad ? __builtin_nanf("") : unit >= 0x1p-100f ? unit : 0.f;
+__device__ __forceinline__ float unit_of(uint32_t most, float top) {
+  const float unit = __uint_as_float(most) * top;
+  return most >= 0x7f800000u ? __builtin_nanf("") : unit >= 0x1p-100f ? unit : 0.f;
 }
 
 // The tensor of a chunk: the first whose end is behind it.
@@ -260,7 +268,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const Args a) {
       uint32_t cm[8], cv[8];
       load8(static_cast<const uint8_t*>(r.m) + at, vec, left, cm);
       load8(static_cast<const uint8_t*>(r.v) + at, vec, left, cv);
-      const float um = r.m_unit[at / kBlock], uv = r.v_unit[at / kBlock];
+      const float um = r.m_unit[at / kBlock] * 0x1p4f, uv = r.v_unit[at / kBlock] * 0x1p10f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         m[e] = decode_m(cm[e], um);
@@ -280,28 +288,21 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const Args a) {
       store8(static_cast<float*>(r.m) + at, vec, left, m);
       store8(static_cast<float*>(r.v) + at, vec, left, v);
     } else {
-      float top_m = 0.f, top_v = 0.f;
-      bool bad_m = false, bad_v = false;
+      uint32_t top_m = 0, top_v = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (e >= left) m[e] = v[e] = 0.f;
-        top_m = fmaxf(top_m, fabsf(m[e]));
-        top_v = fmaxf(top_v, v[e]);
-        bad_m |= !(fabsf(m[e]) < __builtin_huge_valf());
-        bad_v |= !(v[e] < __builtin_huge_valf());
+        top_m = max(top_m, __float_as_uint(m[e]) & 0x7fffffffu);
+        top_v = max(top_v, __float_as_uint(v[e]) & 0x7fffffffu);
       }
-      const int half = threadIdx.x & 32;
-      const bool any_m = (uint32_t)(__ballot(bad_m) >> half) != 0;
-      const bool any_v = (uint32_t)(__ballot(bad_v) >> half) != 0;
-      const float um = unit_of(block_max(top_m), kTopM, any_m);
-      const float uv = unit_of(block_max(top_v), kTopV, any_v);
+      const float um = unit_of(block_max(top_m), kTopM), uv = unit_of(block_max(top_v), kTopV);
       const float im = um > 0.f ? 1.f / um : 0.f, iv = uv > 0.f ? 1.f / uv : 0.f;
       uint32_t cm[8], cv[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t bits = mix((uint32_t)(at + e) + key);
-        cm[e] = encode_m(m[e], im, ((float)(bits & 0xffff) + 0.5f) * 0x1p-16f);
-        cv[e] = encode_v(v[e], iv, ((float)(bits >> 16) + 0.5f) * 0x1p-16f);
+        cm[e] = encode_m(m[e], im, fraction(bits & 0xffff));
+        cv[e] = encode_v(v[e], iv, fraction(bits >> 16));
       }
       store8(static_cast<uint8_t*>(r.m) + at, vec, left, cm);
       store8(static_cast<uint8_t*>(r.v) + at, vec, left, cv);
@@ -326,30 +327,33 @@ struct ReadArgs {
 };
 static_assert(sizeof(ReadArgs) <= 4096, "kernel arguments");
 
+// Four values a lane, so that the stores fill whole lines.
 __global__ void __launch_bounds__(kThreads) moments_kernel(const ReadArgs a) {
   const int chunk = blockIdx.x;
   const int k = find(a, chunk);
   const ReadRec r = a.rec[k];
-  const int begin = k ? a.end[k - 1] : 0;
+  const int64_t begin = (int64_t)(chunk - (k ? a.end[k - 1] : 0)) * kChunk;
   const bool vec = on16(r.m) && on16(r.v) && on16(r.out_m) && on16(r.out_v);
-#pragma unroll 1
-  for (int it = 0; it < kChunk / (kThreads * kEach); ++it) {
-    const int64_t i = (int64_t)(chunk - begin) * kChunk + it * (kThreads * kEach) +
-                      (int64_t)threadIdx.x * kEach;
+#pragma unroll 2
+  for (int it = 0; it < kChunk / (kThreads * 4); ++it) {
+    const int64_t i = begin + it * (kThreads * 4) + threadIdx.x * 4;
     if (i >= r.n) return;
-    const int left = (int)min((int64_t)kEach, r.n - i);
-    uint32_t cm[8], cv[8];
-    load8(r.m + i, vec, left, cm);
-    load8(r.v + i, vec, left, cv);
-    const float um = r.m_unit[i / kBlock], uv = r.v_unit[i / kBlock];
-    float m[8], v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      m[e] = decode_m(cm[e], um);
-      v[e] = decode_v(cv[e], uv);
+    const float um = r.m_unit[i / kBlock] * 0x1p4f, uv = r.v_unit[i / kBlock] * 0x1p10f;
+    if (vec && i + 4 <= r.n) {
+      const uint32_t cm = *reinterpret_cast<const uint32_t*>(r.m + i);
+      const uint32_t cv = *reinterpret_cast<const uint32_t*>(r.v + i);
+      *reinterpret_cast<float4*>(r.out_m + i) =
+          make_float4(decode_m(cm & 255, um), decode_m(cm >> 8 & 255, um),
+                      decode_m(cm >> 16 & 255, um), decode_m(cm >> 24, um));
+      *reinterpret_cast<float4*>(r.out_v + i) =
+          make_float4(decode_v(cv & 255, uv), decode_v(cv >> 8 & 255, uv),
+                      decode_v(cv >> 16 & 255, uv), decode_v(cv >> 24, uv));
+    } else {
+      for (int64_t j = i; j < i + 4 && j < r.n; ++j) {
+        r.out_m[j] = decode_m(r.m[j], um);
+        r.out_v[j] = decode_v(r.v[j], uv);
+      }
     }
-    store8(r.out_m + i, vec, left, m);
-    store8(r.out_v + i, vec, left, v);
   }
 }
 

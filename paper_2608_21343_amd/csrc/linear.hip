@@ -27,6 +27,8 @@ struct Gather {
   int64_t stride, plane;
   int32_t D, dp;
   uint16_t* out;
+  void* dx;  // rows that are left out get 0 here; or NULL
+  int64_t dx_stride;
 };
 
 constexpr int kGroup = 2048, kEach = kGroup / 256;  // rows of a count, and of a thread of it
@@ -279,7 +281,12 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
   float weighty = 0.f;
   for (int i = wave; i < kRows; i += 4) {
     const int32_t at = places[i];
-    if (at < 0) continue;
+    if (at < 0) {
+      if (g.dx && row0 + i < g.n)
+        for (int d = lane; d < g.D; d += 64)
+          static_cast<T*>(g.dx)[(row0 + i) * g.dx_stride + d] = T(0);
+      continue;
+    }
     float most;
     const float unit = row_planes<T>(x + (row0 + i) * g.stride, g.D, g.dp, wide,
                                      g.out + (int64_t)at * g.dp, g.plane, &most);
@@ -346,7 +353,8 @@ __global__ void __launch_bounds__(256)
 
 // ---- what joins the tiles
 
-// One wave a row: log-sum-exp and loss. Gathered rows, whose parts lie by their place
+// One wave a row (or, few rows with many parts, a workgroup): log-sum-exp and loss.
+// Gathered rows, whose parts lie by their place
 // or (by_row) by their row; or (idx NULL) all rows, and 0 for those left out.
 struct Finish {
   const Meta* meta;
@@ -361,9 +369,24 @@ struct Finish {
   float *out_loss, *out_lse;
 };
 
+// Maximum (or sum) over the first W waves of a workgroup.
+template <int W, bool MAX>
+__device__ __forceinline__ float over(float v, float* lds) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = MAX ? fmaxf(v, __shfl_xor(v, d)) : v + __shfl_xor(v, d);
+  if (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return MAX ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]))
+             : (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+template <int W>
 __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  static_assert(W == 1 || W == 4, "waves of a row");
+  __shared__ float lds[2][4];
+  const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t at = W == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (at >= (f.idx ? f.meta->n : f.n)) return;
   const int64_t row = f.idx ? f.idx[at] : at, from = f.by_row ? row : at;
   const int32_t t = f.target[row];
@@ -375,18 +398,16 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   }
   const float2* part = f.part + from * f.n_part;
   float m = -__builtin_huge_valf();
-  for (int i = lane; i < f.n_part; i += 64) m = fmaxf(m, part[i].x);
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  for (int i = lane; i < f.n_part; i += 64 * W) m = fmaxf(m, part[i].x);
+  m = over<W, true>(m, lds[0]);
   const float base = m == -__builtin_huge_valf() ? 0.f : m;
   float sum = 0.f;
-  for (int i = lane; i < f.n_part; i += 64) {
+  for (int i = lane; i < f.n_part; i += 64 * W) {
     const float2 v = part[i];
     // (a part without a value has maximum -inf and sum 0; a NaN in either stays)
     sum += v.y * __builtin_amdgcn_exp2f((v.x - base) * kLog2e);
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  sum = over<W, false>(sum, lds[1]);
   if (lane != 0) return;
   const float lse = base + logf(sum);
   if (f.out_lse) f.out_lse[row] = lse;
@@ -494,9 +515,7 @@ __global__ void __launch_bounds__(256)
     if (from >= 0) {
       const float* p = g.acc + from * g.lda + d;
       for (int s = 0; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * g.acc_split);
-      if (!inv) scale = dw_scale<T>(g, meta, (int)row);
-      else if (!Elem<T>::kScaled) scale = meta.scale;
-      else scale = g.row.m[from] * top_unit(meta) * 0x1p-14f;
+      scale = inv ? dx_scale<T>(g, meta, from) : dw_scale<T>(g, meta, (int)row);
     }
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     if (from >= 0)
@@ -507,22 +526,23 @@ __global__ void __launch_bounds__(256)
 }
 
 // db[c] = the sum of the columns over the blocks of `rows` rows: 64 tokens a workgroup,
-// a quarter of the blocks each wave.
+// a sixteenth of the blocks each wave.
 template <class T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
     columns_kernel(const float* col, int32_t ldg, const Meta* meta, int32_t rows, T* db,
                    int32_t n) {
-  __shared__ float sums[4][64];
+  __shared__ float sums[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = blockIdx.x * 64 + lane;
   const int tiles = (meta->n + rows - 1) / rows;
   float sum = 0.f;
   if (c < n)
-    for (int q = wave; q < tiles; q += 4) sum += col[(int64_t)q * ldg + c];
+    for (int q = wave; q < tiles; q += 16) sum += col[(int64_t)q * ldg + c];
   sums[wave][lane] = sum;
   __syncthreads();
   if (wave == 0 && c < n) {
-    sum = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+#pragma unroll
+    for (int w = 1; w < 16; ++w) sum += sums[w][lane];
     store_out(db + c, Elem<T>::kScaled ? sum : sum * meta->scale);
   }
 }
@@ -532,32 +552,49 @@ __global__ void __launch_bounds__(256)
 constexpr int64_t kGradBytes = 256ll << 20;  // of the gradients of a piece's logits
 constexpr int32_t kFewRows = 64;             // that linear_few.hip takes
 
+// How a product is cut: tiles of 256 x 256, or smaller ones where those would leave CUs
+// idle, and parts of the summed axis where that still leaves them idle. The costs are in
+// stages of a tile of 256 (1.3 us in bfloat16, measured at full load); a smaller tile's
+// takes longer for its size, since its operands are read from LDS more often, and every
+// tile costs some besides (first loads, epilogue), parts a way through memory.
+struct Cut {
+  int32_t tile, parts;
+};
+Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
+  Cut best = {256, 1};
+  double least = 0;
+  const struct {
+    int32_t tile;
+    double step, fixed;
+  } sizes[] = {{256, 1.0, 4.0}, {128, 0.36, 2.5}, {64, 0.15, 1.5}};
+  // parts are written and read once more, 7 MB in the time of a stage
+  const double way = 8.0 * (double)p * (double)q / 7e6;
+  for (const auto& s : sizes) {
+    const int64_t tiles = ((p + s.tile - 1) / s.tile) * ((q + s.tile - 1) / s.tile);
+    for (int n = 1; n <= (parts ? 64 : 1) && n <= (steps + 3) / 4; ++n) {
+      const double rounds = (double)((tiles * n + 255) / 256);
+      const double cost = rounds * ((double)((steps + n - 1) / n) * stages * s.step + s.fixed) +
+                          (n > 1 ? 4.0 + n * way : 0.0);
+      if (least == 0 || cost < least * 0.97) {
+        best = {s.tile, n};
+        least = cost;
+      }
+    }
+  }
+  return best;
+}
+
 struct Layout {
   int64_t np, dp, planes;      // gathered rows and values a row, rounded up
   bool copy_w, few, gather, kept;      // kept: the logits, from the statistics to their gradients
   int32_t n_part;
   int32_t piece, pieces;       // tokens of a piece of the vocabulary
-  int32_t split_x, split_w;
-  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, s, hit, part, x, xm, w, z, G, acc_x;
+  Cut stats, grad, x, w;       // of the four products
+  int32_t col_rows;            // rows of a partial sum of columns
+  bool direct;                 // dx leaves its product's sums as it is
+  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, s, hit, part, px, pxm, pw, z, G, acc_x;
   int64_t acc_w, col, total;
 };
-
-// In how many parts the summed axis is cut: the rounds of 256 workgroups that the tiles
-// take, against what a part costs by itself (its first loads, and its sums' way through
-// memory: about three steps).
-int splits(int64_t tiles, int64_t steps) {
-  int best = 1;
-  double least = 0;
-  for (int s = 1; s <= 64 && s <= (steps + 3) / 4; ++s) {
-    const double cost =
-        (double)((tiles * s + 255) / 256) * ((double)((steps + s - 1) / s) + (s > 1 ? 6 : 3));
-    if (s == 1 || cost < least * 0.97) {
-      best = s;
-      least = cost;
-    }
-  }
-  return best;
-}
 
 Layout plan(const Call& c) {
   Layout L = {};
@@ -576,7 +613,10 @@ Layout plan(const Call& c) {
   // (the loss of few rows needs no copies)
   L.gather = grads || !L.few;
   L.copy_w = L.copy_w && L.gather;
-  L.n_part = L.few ? few_parts(c.C) : 2 * (int32_t)(up(c.C, kTile) / kTile);
+  // products of planes that a step takes
+  const int64_t stages = f32 ? 3 : 1;
+  L.stats = cut(c.C, c.n, L.dp / kStep, stages, false);
+  L.n_part = L.few ? few_parts(c.C) : 2 * ((c.C + L.stats.tile - 1) / L.stats.tile);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -598,9 +638,9 @@ Layout plan(const Call& c) {
   if (f32) L.s = take((int64_t)c.C * 4);
   L.hit = take(L.np * 4);
   if (!c.lse) L.part = take(L.np * L.n_part * 8);
-  if (L.gather) L.x = take(L.planes * L.np * L.dp * 2);
-  if (f32 && c.dw) L.xm = take(L.planes * L.np * L.dp * 2);
-  if (L.copy_w) L.w = take(L.planes * c.C * L.dp * 2);
+  if (L.gather) L.px = take(L.planes * L.np * L.dp * 2);
+  if (f32 && c.dw) L.pxm = take(L.planes * L.np * L.dp * 2);
+  if (L.copy_w) L.pw = take(L.planes * c.C * L.dp * 2);
   if (grads) {
     // pieces of the vocabulary of about kGradBytes of gradients, of equal sizes
     const int64_t all = L.planes * L.np * 2 * c.C;
@@ -611,16 +651,19 @@ Layout plan(const Call& c) {
     L.kept = !c.lse && L.pieces == 1 && c.n * L.piece * 4 <= kGradBytes;
     L.G = take(L.planes * L.np * L.piece * 2);
     if (L.kept) L.z = take(L.np * L.piece * 4);
-    const int64_t td = (L.dp + kTile - 1) / kTile;
+    const int64_t n = c.C < L.piece ? c.C : L.piece;
+    L.grad = cut(n, c.n, L.dp / kStep, stages, false);
     if (c.dx) {
-      L.split_x = splits(td * (L.np / kTile), L.piece / kStep);
-      L.acc_x = take(L.split_x * L.np * L.dp * 4);
+      L.x = cut(L.dp, c.n, up(n, kStep) / kStep, stages, true);
+      L.direct = L.x.parts == 1;
+      if (!L.direct || L.pieces > 1) L.acc_x = take(L.x.parts * L.np * L.dp * 4);
     }
     if (c.dw) {
-      L.split_w = splits(td * (L.piece / kTile), L.np / kStep);
-      if (L.split_w > 1) L.acc_w = take(L.split_w * (int64_t)L.piece * L.dp * 4);
+      L.w = cut(L.dp, n, L.np / kStep, stages, true);
+      if (L.w.parts > 1) L.acc_w = take(L.w.parts * (int64_t)L.piece * L.dp * 4);
     }
-    if (c.db) L.col = take(L.np / (L.kept ? 64 : kTile) * L.piece * 4);
+    L.col_rows = L.kept ? 64 : L.grad.tile;
+    if (c.db) L.col = take(L.np / L.col_rows * L.piece * 4);
   }
   L.total = at;
   return L;
@@ -647,7 +690,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse,
                      grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
                      a,      b,    lse, r, m, c.out_loss, c.out_lse,
-                     c.x_stride, L.np * L.dp, c.D, (int32_t)L.dp, u16(L.x)};
+                     c.x_stride, L.np * L.dp, c.D, (int32_t)L.dp, u16(L.px),
+                     L.direct ? c.dx : nullptr, c.dx_stride};
   // (float32 gradients: it also clears what the others take maxima into)
   if (L.gather && (groups != 1 || f32))
     count_kernel<<<dim3((unsigned)(groups < 1 ? 1 : groups)), dim3(256), 0, st>>>(ga);
@@ -656,13 +700,13 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       ga, static_cast<const T*>(c.x));
   if (L.copy_w && c.n > 0)
     weights_kernel<T><<<dim3(c.C < 8192 ? (c.C + 3) / 4 : 2048), dim3(256), 0, st>>>(
-        static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, c.C, u16(L.w), c.C * L.dp,
+        static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, c.C, u16(L.pw), c.C * L.dp,
         f32 ? flt(L.s) : nullptr, meta);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
 
-  const Operand X = {u16(L.x), L.np * L.dp, L.dp, (int32_t)L.np, (int32_t)L.np};
-  const Operand W = {L.copy_w ? u16(L.w) : static_cast<const uint16_t*>(c.w), c.C * L.dp,
+  const Operand X = {u16(L.px), L.np * L.dp, L.dp, (int32_t)L.np, (int32_t)L.np};
+  const Operand W = {L.copy_w ? u16(L.pw) : static_cast<const uint16_t*>(c.w), c.C * L.dp,
                      L.copy_w ? L.dp : c.w_stride, c.C, c.C};
   Gemm g = {};
   g.meta = meta;
@@ -673,8 +717,9 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   g.k = (int32_t)L.dp;
   g.splits = 1;
   g.Q = X;
-  g.tq = (int32_t)(L.np / kTile);
   g.D = c.D;
+  g.idx = idx;
+  auto tiles = [](int64_t n, const Cut& cut) { return (int32_t)((n + cut.tile - 1) / cut.tile); };
   if (!c.lse && c.n > 0) {
     float2* part = reinterpret_cast<float2*>(ws + L.part);
     float *hit = flt(L.hit), *z = L.kept ? flt(L.z) : nullptr;
@@ -685,7 +730,9 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     } else {
       Gemm s = g;
       s.P = W;
-      s.tp = (c.C + kTile - 1) / kTile;
+      s.tile = L.stats.tile;
+      s.tp = tiles(c.C, L.stats);
+      s.tq = tiles(c.n, L.stats);
       s.part = part;
       s.n_part = L.n_part;
       s.hit = hit;
@@ -696,7 +743,10 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (e != hipSuccess) return e;
     const Finish f = {meta,  part, L.n_part, hit,     L.gather ? idx : nullptr, c.target,
                       L.few, (int32_t)c.n, c.C, c.weight, lse, a, b, c.out_loss, c.out_lse};
-    finish_kernel<<<dim3((unsigned)((c.n + 3) / 4)), dim3(256), 0, st>>>(f);
+    if (c.n <= 1024 && L.n_part >= 256)
+      finish_kernel<4><<<dim3((unsigned)c.n), dim3(256), 0, st>>>(f);
+    else
+      finish_kernel<1><<<dim3((unsigned)((c.n + 3) / 4)), dim3(256), 0, st>>>(f);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -705,23 +755,23 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   Operand XM = X;  // of dw
   if constexpr (f32) {
     if (c.dw && c.n > 0) {
-      XM.p = u16(L.xm);
+      XM.p = u16(L.pxm);
       weighted_kernel<<<dim3(c.n < 8192 ? (c.n + 3) / 4 : 2048), dim3(256), 0, st>>>(
-          static_cast<const T*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, meta, u16(L.xm),
+          static_cast<const T*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, meta, u16(L.pxm),
           L.np * L.dp);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
   }
-  const int32_t td = (int32_t)((L.dp + kTile - 1) / kTile);
   for (int32_t piece = 0; piece < L.pieces; ++piece) {
     const int32_t c0 = piece * L.piece, n = c.C - c0 < L.piece ? c.C - c0 : L.piece;
-    const int32_t cols = (int32_t)up(n, kTile);
     Gemm z = g;
     z.P = W;
     z.P.p += c0 * W.ld;
     z.P.n = n;
-    z.tp = cols / kTile;
+    z.tile = L.grad.tile;
+    z.tp = tiles(n, L.grad);
+    z.tq = tiles(c.n, L.grad);
     z.c0 = c0;
     z.G = u16(L.G);
     z.g_plane = L.np * L.piece;
@@ -738,8 +788,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (e != hipSuccess) return e;
     const Operand G = {z.G, z.g_plane, L.piece, (int32_t)L.np, n};
     if (c.db) {
-      columns_kernel<T><<<dim3((n + 63) / 64), dim3(256), 0, st>>>(
-          flt(L.col), L.piece, meta, L.kept ? 64 : kTile, static_cast<T*>(c.db) + c0, n);
+      columns_kernel<T><<<dim3((n + 63) / 64), dim3(1024), 0, st>>>(
+          flt(L.col), L.piece, meta, L.col_rows, static_cast<T*>(c.db) + c0, n);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -748,10 +798,16 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       Gemm x = g;
       x.P = {W.p + c0 * W.ld, W.plane, W.ld, (int32_t)L.dp, n};
       x.Q = G;
-      x.tp = td;
-      x.splits = L.split_x;
+      x.tile = L.x.tile;
+      x.tp = tiles(L.dp, L.x);
+      x.tq = tiles(c.n, L.x);
+      x.splits = L.x.parts;
       x.k = (int32_t)up(n, kStep);
       x.acc = flt(L.acc_x);
+      if (L.direct && piece + 1 == L.pieces) {
+        x.out = c.dx;
+        x.ldo = c.dx_stride;
+      }
       x.acc_split = L.np * L.dp;
       x.lda = (int32_t)L.dp;
       x.add = piece > 0;
@@ -763,13 +819,14 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       w.P = {XM.p, XM.plane, XM.ld, (int32_t)L.dp, (int32_t)L.np};
       w.c0 = c0;
       w.Q = {G.p, G.plane, G.ld, L.piece, (int32_t)L.np};
-      w.tp = td;
-      w.tq = cols / kTile;
+      w.tile = L.w.tile;
+      w.tp = tiles(L.dp, L.w);
+      w.tq = tiles(n, L.w);
       w.n_q = n;
-      w.splits = L.split_w;
+      w.splits = L.w.parts;
       w.k = (int32_t)L.np;
       T* out = static_cast<T*>(c.dw) + c0 * c.dw_stride;
-      if (L.split_w > 1) {
+      if (L.w.parts > 1) {
         w.acc = flt(L.acc_w);
         w.acc_split = (int64_t)L.piece * L.dp;
         w.lda = (int32_t)L.dp;
@@ -779,7 +836,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       }
       e = f32 ? dw_f32(w, st) : dw_bf16(w, st);
       if (e != hipSuccess) return e;
-      if (L.split_w > 1) {
+      if (L.w.parts > 1) {
         join_kernel<T><<<dim3(blocks((int64_t)n * ((c.D + 3) / 4))), dim3(256), 0, st>>>(
             w, nullptr, out, c.dw_stride, n);
         e = hipGetLastError();
@@ -787,9 +844,9 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       }
     }
   }
-  if (c.dx && c.n > 0) {
+  if (c.dx && c.n > 0 && !L.direct) {
     Gemm x = g;
-    x.splits = L.split_x;
+    x.splits = L.x.parts;
     x.acc = flt(L.acc_x);
     x.acc_split = L.np * L.dp;
     x.lda = (int32_t)L.dp;

@@ -37,7 +37,7 @@ namespace tbias {
 namespace linear {
 
 constexpr int kStep = 64;    // values of the summed axis that a tile takes at a time
-constexpr int kTile = 256;   // rows and columns of a tile
+constexpr int kTile = 256;   // rows and columns of the largest tile
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __host__ __device__ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -71,7 +71,7 @@ struct RowArgs {
 struct Gemm {
   Operand P, Q;  // result element (p, q): sum over k of P(p, k) Q(q, k)
   const Meta* meta;
-  int32_t tp, tq, splits;
+  int32_t tile, tp, tq, splits;  // size of a tile (256, 128, 64), and their numbers
   int32_t k;       // length of the summed axis, a multiple of kStep
   int32_t n_q;     // columns of the result that are kept
   // statistics and gradients of the logits
@@ -90,8 +90,9 @@ struct Gemm {
   // products with the gradients
   float* acc;      // [split, n_q, lda]
   int64_t acc_split;
-  int32_t lda, add;
-  void* out;       // or the result itself: [q, ldo], D values
+  int32_t lda, add;  // add: to what is there
+  void* out;         // or the result itself: [q, ldo] (dx: [idx[q], ldo]), D values
+  const int32_t* idx;
   int64_t ldo;
   int32_t D;
 };
@@ -114,7 +115,7 @@ constexpr int32_t kFewWaves = 2048;  // eight a CU
 int32_t few_parts(int32_t C);
 hipError_t few(const Few& f, int32_t dtype, hipStream_t st);
 
-// One launch of tp * tq * splits tiles.
+// One launch over tp * tq * splits tiles.
 hipError_t stats_bf16(const Gemm& g, hipStream_t st);
 hipError_t stats_f32(const Gemm& g, hipStream_t st);
 hipError_t logit_grad_bf16(const Gemm& g, hipStream_t st);

@@ -28,9 +28,18 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kLoads = kTile * kStep * 2 / (16 * kThreads);  // of a lane, for a stage of an operand
-constexpr int kOperandBytes = kTile * kStep * 2;
-constexpr int kStageBytes = 2 * kOperandBytes;
+
+// A tile of N x N, by waves of N / 2 x N / 4, and its stages in LDS.
+template <int N>
+struct Tiling {
+  static constexpr int FP = N / 32, FQ = N / 64;             // fragments of 16 of a wave
+  static constexpr int kLoads = N / 64;                      // of a lane, for a stage of an operand
+  static constexpr int kOperandBytes = N * kStep * 2, kStageBytes = 2 * kOperandBytes;
+  static constexpr int kStages = 512 / N;                    // 128 KB of them
+  static constexpr int kSets = kStages + 1;                  // of Params
+  static constexpr int kParamBytes = 8 * N * 4, kColBytes = 4 * N * 4;
+  static constexpr int kLdsBytes = kStages * kStageBytes + kSets * kParamBytes + kColBytes;
+};
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const f32x2 v = {a, b};
@@ -79,21 +88,30 @@ struct Elem<float> {
 // A lane's first 16-byte load of a stage: the row of the operand's memory that it comes
 // from (its own rows, or transposed the summed values), counted from the tile's, and the
 // bytes in that row. The next ones come from kNextRows rows further on.
-template <bool TR>
+template <int N, bool TR>
 struct Lane {
-  static constexpr int kNextRows = TR ? kWaves * 512 / kTile : kWaves * 8;
+  static constexpr int kNextRows = TR ? kWaves * 512 / N : kWaves * 8;
   int row;
   uint32_t bytes;
 };
-template <bool TR>
-__device__ __forceinline__ Lane<TR> lane_of(const Operand& o, int32_t i0) {
+
+// By how much the 32-byte pieces of row k of a transposed operand's stage are exchanged:
+// the eight rows that half a wave reads at once then lie in different banks (rows of 64
+// values fill half of the banks, two of them all).
+template <int N>
+__device__ __forceinline__ int turn_of(int k) {
+  return N >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);
+}
+
+template <int N, bool TR>
+__device__ __forceinline__ Lane<N, TR> lane_of(const Operand& o, int32_t i0) {
   const int at = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 + (threadIdx.x & 63);
   if (!TR) {
     const int row = at >> 3;
     return {row, (uint32_t)((at & 7) ^ ((row >> 1) & 7)) * 16};
   }
-  const int k = at / (kTile / 8), piece = at % (kTile / 8), f = (k & 3) | ((k >> 1) & 4);
-  const int col = (((piece >> 1) ^ f) * 2 + (piece & 1)) * 8;
+  const int k = at / (N / 8), piece = at % (N / 8);
+  const int col = (((piece >> 1) ^ turn_of<N>(k)) * 2 + (piece & 1)) * 8;
   return {k, (uint32_t)min(col, o.n - 8 - i0) * 2};
 }
 
@@ -136,24 +154,24 @@ __device__ __forceinline__ void land() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory");
 }
 
-// The order of a block with READS LDS reads and 32 products: a read every product or two.
-template <int READS>
+// The order of a block with READS LDS reads and MUL products: a read every product or two.
+template <int READS, int MUL>
 __device__ __forceinline__ void interleave() {
-  constexpr int kEach = READS > 16 ? 1 : 2;
+  constexpr int kEach = 2 * READS <= MUL ? 2 : 1;
 #pragma unroll
   for (int r = 0; r < READS; ++r) {
     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
     __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);  // product
   }
-  __builtin_amdgcn_sched_group_barrier(0x008, 32 - READS * kEach, 0);
+  if (MUL > READS * kEach) __builtin_amdgcn_sched_group_barrier(0x008, MUL - READS * kEach, 0);
 }
 
 // A stage of an operand from `base`, off: of the lane's first load. `rows` of it are in
 // memory; the others are read as the last of them.
-template <bool TR>
+template <int N, bool TR>
 __device__ __forceinline__ void load_stage(uint32_t to, const uint16_t* base, uint32_t off,
                                            const Operand& o, int32_t i0, int32_t rows) {
-  constexpr int kNext = Lane<TR>::kNextRows;
+  constexpr int kNext = Lane<N, TR>::kNextRows, kLoads = Tiling<N>::kLoads;
   to += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
   if (rows >= kNext * kLoads) {
     const char* from = uniform(base);
@@ -161,7 +179,7 @@ __device__ __forceinline__ void load_stage(uint32_t to, const uint16_t* base, ui
 #pragma unroll
     for (int it = 0; it < kLoads; ++it, from += step) load_lds(to + it * kWaves * 1024, from, off);
   } else {
-    const Lane<TR> l = lane_of<TR>(o, i0);
+    const Lane<N, TR> l = lane_of<N, TR>(o, i0);
 #pragma unroll
     for (int it = 0; it < kLoads; ++it)
       load_lds(to + it * kWaves * 1024, uniform(base),
@@ -171,7 +189,7 @@ __device__ __forceinline__ void load_stage(uint32_t to, const uint16_t* base, ui
 
 // Fragment of 16 rows from i (a multiple of 16) and 32 summed values from 32 * ks:
 // lane l holds row l % 16, values 8 (l / 16) ...
-template <bool TR>
+template <int N, bool TR>
 __device__ __forceinline__ s16x8 fragment(const lds_char* tile, int i, int ks) {
   const int lane = threadIdx.x & 63;
   if (!TR) {
@@ -180,12 +198,12 @@ __device__ __forceinline__ s16x8 fragment(const lds_char* tile, int i, int ks) {
         tile + (i + r) * (kStep * 2) + piece * 16);
   }
   const int k = 8 * (lane >> 4) + ((lane & 15) >> 2);
-  const int f = (k & 3) | ((k >> 1) & 4);
-  const lds_char* at = tile + (k + 32 * ks) * (kTile * 2) + (((i >> 4) ^ f) * 32) + (lane & 3) * 8;
+  const lds_char* at =
+      tile + (k + 32 * ks) * (N * 2) + (((i >> 4) ^ turn_of<N>(k)) * 32) + (lane & 3) * 8;
   const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
       (__attribute__((address_space(3))) s16x4*)at);
   const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) s16x4*)(at + 4 * kTile * 2));
+      (__attribute__((address_space(3))) s16x4*)(at + 4 * N * 2));
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -250,24 +268,26 @@ __device__ __forceinline__ float dw_scale(const Gemm& g, const Meta& meta, int q
   return (s > 0.f ? top / s : 1.f) * 0x1p-14f * unit_of(__uint_as_float(meta.T));
 }
 
-// Per token and row of a tile, kept in LDS for the epilogue.
-struct Params {
-  uint32_t bias[kTile];  // float32, or bfloat16 in the low half
-  float s[kTile];
-  int32_t target[kTile];
-  float lse[kTile], a[kTile], b[kTile], r[kTile], m[kTile];
-};
-constexpr int kSets = 3;
-constexpr int kColBytes = 4 * kTile * 4;  // column sums of the four waves along Q
-constexpr int kLdsBytes = 2 * kStageBytes + kSets * (int)sizeof(Params) + kColBytes;
-constexpr int kGroupP = 4;                // tiles of P that a run takes by all of Q
+// What gathered row q of dx is multiplied with.
+template <class T>
+__device__ __forceinline__ float dx_scale(const Gemm& g, const Meta& meta, int64_t q) {
+  return Elem<T>::kScaled ? g.row.m[q] * top_unit(meta) * 0x1p-14f : meta.scale;
+}
 
-// A workgroup per CU works through tiles. The stages of its tiles are one sequence: the
-// first two of the next tile are loaded while the present one's last products and its
-// epilogue run, so only the epilogue's own arithmetic is left between two tiles (a
-// workgroup per tile spent 8 us on a tile beside its products, 22 us in all at a width
-// of 640).
-template <int KIND, class T>
+// Per token and row of a tile, kept in LDS for the epilogue.
+template <int N>
+struct Params {
+  uint32_t bias[N];  // float32, or bfloat16 in the low half
+  float s[N];
+  int32_t target[N];
+  float lse[N], a[N], b[N], r[N], m[N];
+};
+constexpr int kGroupP = 4;  // tiles of P that a run takes by all of Q
+
+// A workgroup per CU works through tiles of N x N. The stages of its tiles are one
+// sequence: the first ones of the next tile are loaded while the present one's last
+// products and its epilogue run.
+template <int KIND, class T, int N>
 __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   typedef Elem<T> El;
   constexpr bool TP = KIND == kDx || KIND == kDw, TQ = KIND == kDw;
@@ -275,16 +295,19 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char* lds = (lds_char*)smem;
   const uint32_t lds_at = (uint32_t)(uintptr_t)lds;
-  Params* params = reinterpret_cast<Params*>(smem + 2 * kStageBytes);
-  lds_poison(smem, kLdsBytes);
+  typedef Tiling<N> Ti;
+  constexpr int FP = Ti::FP, FQ = Ti::FQ, kStages = Ti::kStages, kSets = Ti::kSets;
+  static_assert(sizeof(Params<N>) == Ti::kParamBytes, "parameters in LDS");
+  Params<N>* params = reinterpret_cast<Params<N>*>(smem + kStages * Ti::kStageBytes);
+  lds_poison(smem, Ti::kLdsBytes);
 
   const Meta meta = *g.meta;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wp = (wave >> 2) * 128, wq = (wave & 3) * 64;
+  const int wp = (wave >> 2) * (N / 2), wq = (wave & 3) * (N / 4);
 
   // Workgroups go round the eight dies: each die has a run of neighbouring tiles, four of P
   // by all of Q at a time, so that what its workgroups read meets in its L2.
-  const int tiles_q = KIND == kDw ? g.tq : min(g.tq, (meta.n + kTile - 1) / kTile);
+  const int tiles_q = KIND == kDw ? g.tq : min(g.tq, (meta.n + N - 1) / N);
   const int tiles = g.tp * tiles_q, total = tiles * g.splits, each = (total + 7) / 8;
   const int stride = gridDim.x >> 3, end = min(((int)(blockIdx.x & 7) + 1) * each, total);
   const int begin = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
@@ -315,30 +338,31 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   uint32_t off_p = 0, off_q = 0;
   int load_turn = 0;
   // What the epilogue needs, one token or row a lane. A tile's are loaded with its first
-  // stage: up to two tiles ahead (tiles of one stage), when every wave has left the
-  // epilogue before the present tile. So three sets are enough.
+  // stage: up to kStages tiles ahead (tiles of one stage), when every wave has left the
+  // epilogue before the present tile. So kStages + 1 sets are enough.
   auto load_params = [&](const Tile& t, int turn) {
-    const uint32_t to = lds_at + 2 * kStageBytes + turn * sizeof(Params);
+    const uint32_t to = lds_at + kStages * Ti::kStageBytes + turn * sizeof(Params<N>);
     auto four = [&](const void* from, uint32_t index, uint32_t at) {
       load_lds4(to + at, (const char*)from, 4 * index);
     };
-    if (wave < 4) {
-      const uint32_t c = min(g.c0 + t.p * kTile + 64 * wave + lane, g.C - 1), at = 256 * wave;
-      if (El::kScaled) four(g.s, c, offsetof(Params, s) + at);
-      if (g.bias && sizeof(T) == 4) four(g.bias, c, offsetof(Params, bias) + at);
+    constexpr int kPer = N / 64;
+    if (wave < kPer) {
+      const uint32_t c = min(g.c0 + t.p * N + 64 * wave + lane, g.C - 1), at = 256 * wave;
+      if (El::kScaled) four(g.s, c, offsetof(Params<N>, s) + at);
+      if (g.bias && sizeof(T) == 4) four(g.bias, c, offsetof(Params<N>, bias) + at);
       if (g.bias && sizeof(T) == 2)
-        load_lds2(to + offsetof(Params, bias) + at, (const char*)g.bias, 2 * c);
-    } else {
-      const uint32_t row = min(t.q * kTile + 64 * (wave - 4) + lane, meta.n - 1);
+        load_lds2(to + offsetof(Params<N>, bias) + at, (const char*)g.bias, 2 * c);
+    } else if (wave >= 4 && wave < 4 + kPer) {
+      const uint32_t row = min(t.q * N + 64 * (wave - 4) + lane, meta.n - 1);
       const uint32_t at = 256 * (wave - 4);
-      four(g.row.target, row, offsetof(Params, target) + at);
+      four(g.row.target, row, offsetof(Params<N>, target) + at);
       if (KIND == kLogitGrad) {
-        four(g.row.lse, row, offsetof(Params, lse) + at);
-        four(g.row.a, row, offsetof(Params, a) + at);
-        four(g.row.b, row, offsetof(Params, b) + at);
-        if (El::kScaled) four(g.row.m, row, offsetof(Params, m) + at);
+        four(g.row.lse, row, offsetof(Params<N>, lse) + at);
+        four(g.row.a, row, offsetof(Params<N>, a) + at);
+        four(g.row.b, row, offsetof(Params<N>, b) + at);
+        if (El::kScaled) four(g.row.m, row, offsetof(Params<N>, m) + at);
       }
-      if (El::kScaled) four(g.row.r, row, offsetof(Params, r) + at);
+      if (El::kScaled) four(g.row.r, row, offsetof(Params<N>, r) + at);
     }
   };
   auto issue = [&](int buf) {
@@ -355,23 +379,23 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       if (load_n > 0) {
         if (kLogits) load_params(load_tile, load_turn);
         load_turn = load_turn == kSets - 1 ? 0 : load_turn + 1;
-        const Lane<TP> lp = lane_of<TP>(g.P, load_tile.p * kTile);
-        const Lane<TQ> lq = lane_of<TQ>(g.Q, load_tile.q * kTile);
+        const Lane<N, TP> lp = lane_of<N, TP>(g.P, load_tile.p * N);
+        const Lane<N, TQ> lq = lane_of<N, TQ>(g.Q, load_tile.q * N);
         off_p = lp.row * (uint32_t)(g.P.ld * 2) + lp.bytes;
         off_q = lq.row * (uint32_t)(g.Q.ld * 2) + lq.bytes;
       }
     }
     if (load_id >= end) return;
     const int k = load_tile.first + load_s / El::PAIRS, pair = load_s % El::PAIRS;
-    const int64_t p0 = load_tile.p * kTile, q0 = load_tile.q * kTile, k0 = (int64_t)k * kStep;
+    const int64_t p0 = load_tile.p * N, q0 = load_tile.q * N, k0 = (int64_t)k * kStep;
     const uint16_t* bp = g.P.p + El::p(pair) * g.P.plane + (TP ? k0 * g.P.ld + p0 : p0 * g.P.ld + k0);
     const uint16_t* bq = g.Q.p + El::q(pair) * g.Q.plane + (TQ ? k0 * g.Q.ld + q0 : q0 * g.Q.ld + k0);
     // (a transposed operand has all of a stage's rows, but for w behind the last token)
     const int rows_p = TP ? (KIND == kDx ? g.P.kn - (int)k0 : kStep) : g.P.n - (int)p0;
     const int rows_q = TQ ? kStep : g.Q.n - (int)q0;
-    const uint32_t to = lds_at + buf * kStageBytes;
-    load_stage<TP>(to, bp, off_p, g.P, (int)p0, rows_p);
-    load_stage<TQ>(to + kOperandBytes, bq, off_q, g.Q, (int)q0, rows_q);
+    const uint32_t to = lds_at + buf * Ti::kStageBytes;
+    load_stage<N, TP>(to, bp, off_p, g.P, (int)p0, rows_p);
+    load_stage<N, TQ>(to + Ti::kOperandBytes, bq, off_q, g.Q, (int)q0, rows_q);
     ++load_s;
   };
 
@@ -379,46 +403,53 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   // A stage's second half is in registers before the barrier in its middle, so behind
   // that its place takes the stage after next, whose loads then have a whole stage's
   // time; and no wave waits for LDS right after a barrier.
-  f32x4 acc[8][4];
-  s16x8 pa[2][8], qb[2][4];
+  f32x4 acc[FP][FQ];
+  s16x8 pa[2][FP], qb[2][FQ];
   auto read = [&](int buf, int half) {
-    const lds_char* P = lds + buf * kStageBytes;
-    const lds_char* Q = P + kOperandBytes;
+    const lds_char* P = lds + buf * Ti::kStageBytes;
+    const lds_char* Q = P + Ti::kOperandBytes;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) qb[half][j] = fragment<TQ>(Q, wq + 16 * j, half);
+    for (int j = 0; j < FQ; ++j) qb[half][j] = fragment<N, TQ>(Q, wq + 16 * j, half);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pa[half][i] = fragment<TP>(P, wp + 16 * i, half);
+    for (int i = 0; i < FP; ++i) pa[half][i] = fragment<N, TP>(P, wp + 16 * i, half);
   };
   auto multiply = [&](int half) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < FP; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = El::mfma(pa[half][i], qb[half][j], acc[i][j]);
-    interleave<(TP ? 16 : 8) + (TQ ? 8 : 4)>();
+      for (int j = 0; j < FQ; ++j) acc[i][j] = El::mfma(pa[half][i], qb[half][j], acc[i][j]);
+    interleave<(TP ? 2 : 1) * FP + (TQ ? 2 : 1) * FQ, FP * FQ>();
   };
 
-  issue(0);
-  issue(1);
-  land<0>();
+  // Waits for the stage after the present one: those behind it may be in flight, as long
+  // as there are any.
+  auto land_next = [&]() {
+    if (kStages > 2 && load_id < end) land<2 * (kStages - 2) * Ti::kLoads>();
+    else land<0>();
+  };
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) issue(s);
+  if (kStages > 2 && load_id < end) land<2 * (kStages - 1) * Ti::kLoads>();
+  else land<0>();
   __syncthreads();
   int buf = 0, turn = 0;
   for (int id = begin; id < end; id += stride) {
     const Tile tile = tile_of(id);
-    const int p0 = tile.p * kTile, q0 = tile.q * kTile, n_stage = tile.steps * El::PAIRS;
-    const Params& par = params[turn];
+    const int p0 = tile.p * N, q0 = tile.q * N, n_stage = tile.steps * El::PAIRS;
+    const Params<N>& par = params[turn];
     turn = turn == kSets - 1 ? 0 : turn + 1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < FP; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     read(buf, 0);
     for (int s = 0; s < n_stage; ++s) {
       read(buf, 1);
       multiply(0);
-      land<0>();  // the next stage
+      land_next();
       __syncthreads();
       issue(buf);
-      buf ^= 1;
+      buf = buf == kStages - 1 ? 0 : buf + 1;
       read(buf, 0);  // (behind the last stage nothing uses it)
       multiply(1);
     }
@@ -432,64 +463,64 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
     const int c_lane = wp + lp;  // first token of the lane in the tile, of 4 in every 16
     if (kLogits) {
       if (El::kScaled) {
-        float r[4];
+        float r[FQ];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = par.r[wq + 16 * j + lq];
+        for (int j = 0; j < FQ; ++j) r[j] = par.r[wq + 16 * j + lq];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < FP; ++i) {
           const f32x4 s = *reinterpret_cast<const f32x4*>(&par.s[c_lane + 16 * i]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < FQ; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * s[e] * r[j];
         }
       }
       if (g.bias) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < FP; ++i) {
           const uint4 b = *reinterpret_cast<const uint4*>(&par.bias[c_lane + 16 * i]);
           const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float add = __uint_as_float(sizeof(T) == 4 ? w[e] : w[e] << 16);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j][e] += add;
+            for (int j = 0; j < FQ; ++j) acc[i][j][e] += add;
           }
         }
       }
-      if (g.c0 + p0 + kTile > g.C) {
+      if (g.c0 + p0 + N > g.C) {
         // nothing behind the last token
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (g.c0 + p0 + c_lane + 16 * i + e >= g.C) {
 #pragma unroll
-              for (int j = 0; j < 4; ++j) acc[i][j][e] = -__builtin_huge_valf();
+              for (int j = 0; j < FQ; ++j) acc[i][j][e] = -__builtin_huge_valf();
             }
       }
     }
     if (KIND == kStats) {
       if (g.z) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < FQ; ++j) {
           const int64_t row = q0 + wq + 16 * j + lq;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < FP; ++i)
             *reinterpret_cast<f32x4*>(g.z + row * g.ldg + p0 + c_lane + 16 * i) = acc[i][j];
         }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < FQ; ++j) {
         const int row = q0 + wq + 16 * j + lq;
         // the row's target among the lane's tokens
         const int t =
             row < meta.n ? par.target[wq + 16 * j + lq] - (g.c0 + p0 + c_lane) : -1;
-        const bool here = t >= 0 && t < 128 && (t & 12) == 0;
+        const bool here = t >= 0 && t < N / 2 && (t & 12) == 0;
         if (__ballot(here)) {
           float hit = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < FP; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (t == 16 * i + e) hit = acc[i][j][e];
@@ -497,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
         }
         float m = -__builtin_huge_valf();
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
         m = fmaxf(m, __shfl_xor(m, 16));
@@ -508,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
         const float shift = -base * kLog2e;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, shift));
@@ -522,14 +553,14 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
     if (KIND == kLogitGrad) {
       const float top = 0x1p14f / top_unit(meta), norm = El::kScaled ? 1.f : meta.inverse;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < FQ; ++j) {
         const int at = wq + 16 * j + lq, row = q0 + at;
         const bool in = row < meta.n;
         const float lse = par.lse[at], shift = -lse * kLog2e, a = par.a[at] * norm;
         const int t = in ? par.target[at] - (g.c0 + p0 + c_lane) : -1;
         // G over the logits
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             // float32: the difference first, whose rounding is small where p is not
@@ -538,10 +569,10 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
                                                                : __builtin_fmaf(z, kLog2e, shift));
             acc[i][j][e] = in ? a * p : 0.f;
           }
-        if (__ballot(t >= 0 && t < 128 && (t & 12) == 0)) {
+        if (__ballot(t >= 0 && t < N / 2 && (t & 12) == 0)) {
           const float b = par.b[at] * norm;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < FP; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (t == 16 * i + e) acc[i][j][e] -= b;
@@ -549,18 +580,18 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       }
       if (g.col) {
         // the tile's columns: over the lane's rows, 16 lanes, and the four waves through LDS
-        float* sums = reinterpret_cast<float*>(smem + 2 * kStageBytes + kSets * sizeof(Params));
-        float m[4];
+        float* sums = reinterpret_cast<float*>(smem + kStages * Ti::kStageBytes + kSets * sizeof(Params<N>));
+        float m[FQ];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) m[j] = El::kScaled ? par.m[wq + 16 * j + lq] : 1.f;
+        for (int j = 0; j < FQ; ++j) m[j] = El::kScaled ? par.m[wq + 16 * j + lq] : 1.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < FP; ++i) {
           float cs[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            float v = El::kScaled ? (acc[i][0][e] * m[0] + acc[i][1][e] * m[1]) +
-                                        (acc[i][2][e] * m[2] + acc[i][3][e] * m[3])
-                                  : (acc[i][0][e] + acc[i][1][e]) + (acc[i][2][e] + acc[i][3][e]);
+            float v = 0.f;
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) v += El::kScaled ? acc[i][j][e] * m[j] : acc[i][j][e];
             v += __shfl_xor(v, 1);
             v += __shfl_xor(v, 2);
             v += __shfl_xor(v, 4);
@@ -568,49 +599,57 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
             cs[e] = v;
           }
           if (lq == 0)
-            *reinterpret_cast<float4*>(sums + (wave & 3) * kTile + c_lane + 16 * i) =
+            *reinterpret_cast<float4*>(sums + (wave & 3) * N + c_lane + 16 * i) =
                 make_float4(cs[0], cs[1], cs[2], cs[3]);
         }
         __syncthreads();
         const int c = threadIdx.x;
-        if (c < kTile)
+        if (c < N)
           g.col[(int64_t)tile.q * g.ldg + p0 + c] =
-              (sums[c] + sums[kTile + c]) + (sums[2 * kTile + c] + sums[3 * kTile + c]);
+              (sums[c] + sums[N + c]) + (sums[2 * N + c] + sums[3 * N + c]);
         // (the next tile's sums come behind its own barriers)
       }
+      // four fragments of tokens at a time (two in tiles of 64, each lane its own four)
+      constexpr int kF = FP < 4 ? FP : 4;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        float to_f16[4][4];
+      for (int part = 0; part < FP / kF; ++part) {
+        float to_f16[kF][4];
         if (El::kScaled) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < kF; ++i) {
             const f32x4 s =
-                *reinterpret_cast<const f32x4*>(&par.s[c_lane + 64 * half + 16 * i]);
+                *reinterpret_cast<const f32x4*>(&par.s[c_lane + 64 * part + 16 * i]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) to_f16[i][e] = s[e] > 0.f ? s[e] * top : 0x1p14f;
           }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint2 out[4][El::PLANES];
+        for (int j = 0; j < FQ; ++j) {
+          uint2 out[kF][El::PLANES];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < kF; ++i) {
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float x = acc[4 * half + i][j][e];
+              const float x = acc[kF * part + i][j][e];
               v[e] = El::kScaled ? x * to_f16[i][e] : x;
             }
             El::planes4(v, out[i]);
           }
           const int64_t row = q0 + wq + 16 * j + lq;
-          uint16_t* to = g.G + row * g.ldg + p0 + wp + 64 * half + 4 * lp;
+          uint16_t* to = g.G + row * g.ldg + p0 + wp + 64 * part;
 #pragma unroll
           for (int s = 0; s < El::PLANES; ++s) {
-            uint4 lo, hi;
-            gather16(out[0][s], out[1][s], out[2][s], out[3][s], &lo, &hi);
-            reinterpret_cast<uint4*>(to + s * g.g_plane)[0] = lo;
-            reinterpret_cast<uint4*>(to + s * g.g_plane)[1] = hi;
+            if constexpr (kF == 4) {
+              uint4 lo, hi;
+              gather16(out[0][s], out[1][s], out[2][s], out[3][s], &lo, &hi);
+              reinterpret_cast<uint4*>(to + s * g.g_plane + 4 * lp)[0] = lo;
+              reinterpret_cast<uint4*>(to + s * g.g_plane + 4 * lp)[1] = hi;
+            } else {
+#pragma unroll
+              for (int i = 0; i < kF; ++i)
+                *reinterpret_cast<uint2*>(to + s * g.g_plane + 16 * i + lp) = out[i][s];
+            }
           }
         }
       }
@@ -620,48 +659,50 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       const bool wide = g.ldo % 8 == 0 && (uintptr_t)g.out % 16 == 0 &&
                         (sizeof(T) == 4 || g.D % 8 == 0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < FQ; ++j) {
         const int q = q0 + wq + 16 * j + lq;
-        float scale = 1.f;
-        if (KIND == kDw && g.out && q < g.n_q) scale = dw_scale<T>(g, meta, q);
-        if (KIND == kDw && g.out) {
-          T* o = static_cast<T*>(g.out) + q * g.ldo;
-          if constexpr (sizeof(T) == 2) {
-            if (wide) {
+        const bool in = q < (KIND == kDx ? meta.n : g.n_q);
+        f32x4* sums = reinterpret_cast<f32x4*>(g.acc + tile.split * g.acc_split +
+                                               (int64_t)q * g.lda + p0 + c_lane);
+        if (g.add && in) {
 #pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                uint2 out[4];
+          for (int i = 0; i < FP; ++i)
+            if (p0 + c_lane + 16 * i < g.lda) acc[i][j] += sums[4 * i];
+        }
+        if (!g.out) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const f32x4 v = acc[4 * half + i][j] * scale;
-                  out[i] = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
-                }
-                uint4 lo, hi;
-                gather16(out[0], out[1], out[2], out[3], &lo, &hi);
-                const int d = p0 + wp + 64 * half + 4 * lp;
-                if (q < g.n_q && d < g.D) reinterpret_cast<uint4*>(o + d)[0] = lo;
-                if (q < g.n_q && d + 8 < g.D) reinterpret_cast<uint4*>(o + d)[1] = hi;
+          for (int i = 0; i < FP; ++i)
+            if (in && p0 + c_lane + 16 * i < g.lda) sums[4 * i] = acc[i][j];
+          continue;
+        }
+        const float scale = !in ? 0.f : KIND == kDx ? dx_scale<T>(g, meta, q) : dw_scale<T>(g, meta, q);
+        T* o = static_cast<T*>(g.out) + (KIND == kDx && in ? (int64_t)g.idx[q] : q) * g.ldo;
+        if constexpr (sizeof(T) == 2 && FP >= 4) {
+          if (wide) {
+#pragma unroll
+            for (int part = 0; part < FP / 4; ++part) {
+              uint2 out[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const f32x4 v = acc[4 * part + i][j] * scale;
+                out[i] = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
               }
-              continue;
+              uint4 lo, hi;
+              gather16(out[0], out[1], out[2], out[3], &lo, &hi);
+              const int d = p0 + wp + 64 * part + 4 * lp;
+              if (in && d < g.D) reinterpret_cast<uint4*>(o + d)[0] = lo;
+              if (in && d + 8 < g.D) reinterpret_cast<uint4*>(o + d)[1] = hi;
             }
+            continue;
           }
-          if (q < g.n_q) {
+        }
+        if (in) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int d = p0 + c_lane + 16 * i;
-              const float v[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale,
-                                  acc[i][j][2] * scale, acc[i][j][3] * scale};
-              store4(o + d, v, wide, g.D - d);
-            }
-          }
-        } else if (q < (KIND == kDx ? meta.n : g.n_q)) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < FP; ++i) {
             const int d = p0 + c_lane + 16 * i;
-            if (d >= g.lda) break;
-            f32x4* o =
-                reinterpret_cast<f32x4*>(g.acc + tile.split * g.acc_split + (int64_t)q * g.lda + d);
-            *o = g.add ? *o + acc[i][j] : acc[i][j];
+            const float v[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale, acc[i][j][2] * scale,
+                                acc[i][j][3] * scale};
+            store4(o + d, v, wide, g.D - d);
           }
         }
       }
@@ -670,16 +711,24 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   land<0>();  // (nothing is left in flight into LDS that another workgroup may get)
 }
 
-template <int KIND, class T>
-hipError_t launch(const Gemm& g, hipStream_t st) {
+template <int KIND, class T, int N>
+hipError_t launch_n(const Gemm& g, hipStream_t st) {
+  constexpr int kLds = Tiling<N>::kLdsBytes;
   const int64_t total = (int64_t)g.tp * g.tq * g.splits;
   if (total <= 0) return hipSuccess;
   if (total > INT32_MAX / 2) return hipErrorInvalidValue;
   const int64_t grid = total < 256 ? up(total, 8) : 256;
-  (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_kernel<KIND, T>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
-  gemm_kernel<KIND, T><<<dim3((unsigned)grid), dim3(kThreads), kLdsBytes, st>>>(g);
+  (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_kernel<KIND, T, N>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  gemm_kernel<KIND, T, N><<<dim3((unsigned)grid), dim3(kThreads), kLds, st>>>(g);
   return hipGetLastError();
+}
+
+template <int KIND, class T>
+hipError_t launch(const Gemm& g, hipStream_t st) {
+  return g.tile == 256   ? launch_n<KIND, T, 256>(g, st)
+         : g.tile == 128 ? launch_n<KIND, T, 128>(g, st)
+                         : launch_n<KIND, T, 64>(g, st);
 }
 
 }  // namespace linear
