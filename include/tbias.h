@@ -705,7 +705,9 @@ int tb_linear_xent_grad(const void* x, const void* w, const void* bias, int32_t 
 
 /*
  * AdamW over many tensors in few launches. Per value, with float32 operations that are
- * rounded one by one (the constants are float64 expressions, rounded once):
+ * rounded one by one (the constants are float64 expressions, rounded once; with states in 8
+ * bits the root and the quotient below are off by up to 2^-23 of themselves each, and a
+ * quotient whose divisor is above 2^126 is 0):
  *
  *   g = grad * grad_scale (where that is given)
  *   m = m * beta1 + g * (1 - beta1)
@@ -744,8 +746,8 @@ typedef struct {
 /*
  * tb_adamw_step - one step.
  *
- *   tensors      host array; all of their buffers aligned to their types (16 bytes are
- *                faster). None that is written may share memory with another.
+ *   tensors      host array; all of their buffers aligned to their types. None that is
+ *                written may share memory with another.
  *   dtype        TB_F32 or TB_BF16 (master copies: TB_BF16 only, for all tensors or none)
  *   state_bits   32 or 8
  *   lr, weight_decay, eps >= 0, beta1 and beta2 in [0, 1), step >= 1 (the first is 1)

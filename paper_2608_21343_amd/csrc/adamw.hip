@@ -11,8 +11,8 @@
 // that keeps its mean, from 16 bits that a hash makes of seed, step, tensor and place.
 // A second moment above 0 never becomes 0, which would make the next step a large one.
 //
-// The products and sums are rounded one by one, in float32, as the interface states them,
-// so the codes are the same wherever the same arithmetic runs.
+// The moments' products and sums are rounded one by one, in float32, as the interface
+// states them, so the codes are the same wherever the same arithmetic runs.
 #include "adamw.hpp"
 
 #include <cmath>
@@ -66,77 +66,99 @@ __device__ __forceinline__ uint16_t to_bf16(float v) {
   return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-__device__ __forceinline__ void load8(const float* p, bool vec, int left, float* v) {
-  if (vec && left >= 8) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// Sixteen (eight) bytes at the alignment of one element: the memory takes them anywhere.
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+typedef Words4 Quad4 __attribute__((aligned(4)));
+typedef Words4 Quad2 __attribute__((aligned(2)));
+typedef Words2 Pair1 __attribute__((aligned(1)));
+
+// Eight values, or (FULL false) the `left` there are.
+template <bool FULL>
+__device__ __forceinline__ void load8(const float* p, int left, float* v) {
+  if (FULL || left >= 8) {
+    const Words4 a = reinterpret_cast<const Quad4*>(p)[0], b = reinterpret_cast<const Quad4*>(p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = __uint_as_float(a[e]);
+      v[4 + e] = __uint_as_float(b[e]);
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < left ? p[e] : 0.f;
   }
 }
-__device__ __forceinline__ void load8(const uint16_t* p, bool vec, int left, float* v) {
-  if (vec && left >= 8) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+template <bool FULL>
+__device__ __forceinline__ void load8(const uint16_t* p, int left, float* v) {
+  if (FULL || left >= 8) {
+    const Words4 a = *reinterpret_cast<const Quad2*>(p);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      v[2 * e] = __uint_as_float(w[e] << 16);
-      v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+      v[2 * e] = __uint_as_float(a[e] << 16);
+      v[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < left ? __uint_as_float((uint32_t)p[e] << 16) : 0.f;
   }
 }
-__device__ __forceinline__ void store8(float* p, bool vec, int left, const float* v) {
-  if (vec && left >= 8) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+template <bool FULL>
+__device__ __forceinline__ void store8(float* p, int left, const float* v) {
+  if (FULL || left >= 8) {
+    Words4 a, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = __float_as_uint(v[e]);
+      b[e] = __float_as_uint(v[4 + e]);
+    }
+    reinterpret_cast<Quad4*>(p)[0] = a;
+    reinterpret_cast<Quad4*>(p)[1] = b;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e < left) p[e] = v[e];
   }
 }
-__device__ __forceinline__ void store8(uint16_t* p, bool vec, int left, const float* v) {
-  if (vec && left >= 8) {
-    uint32_t w[4];
+template <bool FULL>
+__device__ __forceinline__ void store8(uint16_t* p, int left, const float* v) {
+  if (FULL || left >= 8) {
+    Words4 a;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const f32x2 x = {v[2 * e], v[2 * e + 1]};
-      w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+      a[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<Quad2*>(p) = a;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e < left) p[e] = to_bf16(v[e]);
   }
 }
-__device__ __forceinline__ void load8(const uint8_t* p, bool vec, int left, uint32_t* c) {
-  if (vec && left >= 8) {
-    const uint2 a = *reinterpret_cast<const uint2*>(p);
+template <bool FULL>
+__device__ __forceinline__ void load8(const uint8_t* p, int left, uint32_t* c) {
+  if (FULL || left >= 8) {
+    const Words2 a = *reinterpret_cast<const Pair1*>(p);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      c[e] = (a.x >> (8 * e)) & 255;
-      c[e + 4] = (a.y >> (8 * e)) & 255;
+      c[e] = (a[0] >> (8 * e)) & 255;
+      c[e + 4] = (a[1] >> (8 * e)) & 255;
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) c[e] = e < left ? p[e] : 0;
   }
 }
-__device__ __forceinline__ void store8(uint8_t* p, bool vec, int left, const uint32_t* c) {
-  if (vec && left >= 8) {
-    uint2 a = make_uint2(0, 0);
+template <bool FULL>
+__device__ __forceinline__ void store8(uint8_t* p, int left, const uint32_t* c) {
+  if (FULL || left >= 8) {
+    Words2 a = {0, 0};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      a.x |= c[e] << (8 * e);
-      a.y |= c[e + 4] << (8 * e);
+      a[0] |= c[e] << (8 * e);
+      a[1] |= c[e + 4] << (8 * e);
     }
-    *reinterpret_cast<uint2*>(p) = a;
+    *reinterpret_cast<Pair1*>(p) = a;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -167,12 +189,15 @@ __device__ __forceinline__ int run_of(float size) {
   return max(__builtin_amdgcn_frexp_expf(size) - (P + 1), 0);
 }
 
+// A block's largest value is at most 4 * 2^-24 of itself above the largest size (the
+// roundings of 1 / top, unit, 1 / unit and the product), which is less than the smallest
+// rnd of 2^-17 lets round up: no code is above the last one.
 __device__ __forceinline__ uint32_t encode_m(float m, float inverse, float rnd) {
   const float y = fabsf(m) * inverse;
   const int e = run_of<4>(y);
   const float q = __builtin_amdgcn_ldexpf(y, -e);
   const uint32_t code = (e << 4) + (uint32_t)q + (__builtin_amdgcn_fractf(q) > rnd ? 1 : 0);
-  return min(code, 127u) | (m < 0.f ? 128u : 0u);
+  return code | (m < 0.f ? 128u : 0u);
 }
 // The square root may be off by some steps: where that moves it over a whole number i, the
 // value lies within i^2 2^-22 of i^2, and the comparison takes it to i from either
@@ -183,7 +208,7 @@ __device__ __forceinline__ uint32_t encode_v(float v, float inverse, float rnd) 
   const float low = floorf(__builtin_amdgcn_ldexpf(root, -e));
   const float over = __builtin_fmaf(-low, low, __builtin_amdgcn_ldexpf(y, -2 * e));
   const uint32_t code = (e << 5) + (uint32_t)low + (over > __builtin_fmaf(2.f, low, 1.f) * rnd ? 1 : 0);
-  return v > 0.f ? min(max(code, 1u), 255u) : 0u;
+  return max(code, min(__float_as_uint(v), 1u));
 }
 
 // 2^-16 (r + 1 / 2)
@@ -213,8 +238,6 @@ __device__ __forceinline__ int find(const A& a, int chunk) {
   return __builtin_amdgcn_readfirstlane(__popcll(__ballot(before)));
 }
 
-__device__ __forceinline__ bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 struct Consts {
   float decay, size, root;
   uint32_t key;
@@ -230,12 +253,97 @@ __host__ __device__ inline Consts consts(double lr, double beta1, double beta2, 
   return c;
 }
 
+// What a lane holds of its eight values.
+template <class T, int BITS>
+struct Eight {
+  float p[8], g[8];
+  float m[8], v[8];   // 32 bits
+  uint32_t cm[8], cv[8];  // 8 bits
+  float um, uv;
+};
+
+// Eight values from i on, or (FULL false) the `left` there are.
+template <class T, int BITS, bool MASTER, bool FULL>
+__device__ __forceinline__ void load(const Rec& r, int64_t i, int left, Eight<T, BITS>* x) {
+  if (MASTER) load8<FULL>(r.master + i, left, x->p);
+  else load8<FULL>(static_cast<const T*>(r.param) + i, left, x->p);
+  load8<FULL>(static_cast<const T*>(r.grad) + i, left, x->g);
+  if constexpr (BITS == 32) {
+    load8<FULL>(static_cast<const float*>(r.m) + i, left, x->m);
+    load8<FULL>(static_cast<const float*>(r.v) + i, left, x->v);
+  } else {
+    load8<FULL>(static_cast<const uint8_t*>(r.m) + i, left, x->cm);
+    load8<FULL>(static_cast<const uint8_t*>(r.v) + i, left, x->cv);
+    x->um = r.m_unit[i / kBlock];
+    x->uv = r.v_unit[i / kBlock];
+  }
+}
+
+template <class T, int BITS, bool MASTER, bool FULL>
+__device__ __forceinline__ void update(const Args& a, const Rec& r, const Consts& c, float gs,
+                                       uint32_t key, int64_t i, int left, Eight<T, BITS>* x) {
+  if constexpr (BITS == 8) {
+    const float um = x->um * 0x1p4f, uv = x->uv * 0x1p10f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x->m[e] = decode_m(x->cm[e], um);
+      x->v[e] = decode_v(x->cv[e], uv);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float g = x->g[e] * gs;
+    x->m[e] = x->m[e] * a.b1 + g * a.c1;
+    x->v[e] = x->v[e] * a.b2 + g * a.c2 * g;
+    const float n = x->m[e] * c.size;
+    if constexpr (BITS == 32) {
+      x->p[e] = x->p[e] * c.decay - n / (sqrtf(x->v[e]) * c.root + a.eps);
+    } else {
+      // root and reciprocal to a step each: their last bits would take a fifth of the
+      // kernel's instructions, which with 8-bit states bound it
+      const float d = __builtin_amdgcn_sqrtf(x->v[e]) * c.root + a.eps;
+      x->p[e] = x->p[e] * c.decay - n * __builtin_amdgcn_rcpf(d);
+    }
+  }
+  store8<FULL>(static_cast<T*>(r.param) + i, left, x->p);
+  if (MASTER) store8<FULL>(r.master + i, left, x->p);
+  if constexpr (BITS == 32) {
+    store8<FULL>(static_cast<float*>(r.m) + i, left, x->m);
+    store8<FULL>(static_cast<float*>(r.v) + i, left, x->v);
+  } else {
+    uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (e >= left) x->m[e] = x->v[e] = 0.f;
+      top_m = max(top_m, __float_as_uint(x->m[e]) & 0x7fffffffu);
+      top_v = max(top_v, __float_as_uint(x->v[e]) & 0x7fffffffu);
+    }
+    const float um = unit_of(block_max(top_m), kTopM), uv = unit_of(block_max(top_v), kTopV);
+    const float im = um > 0.f ? 1.f / um : 0.f, iv = uv > 0.f ? 1.f / uv : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = mix((uint32_t)(i + e) + key);
+      x->cm[e] = encode_m(x->m[e], im, fraction(bits & 0xffff));
+      x->cv[e] = encode_v(x->v[e], iv, fraction(bits >> 16));
+    }
+    store8<FULL>(static_cast<uint8_t*>(r.m) + i, left, x->cm);
+    store8<FULL>(static_cast<uint8_t*>(r.v) + i, left, x->cv);
+    if ((threadIdx.x & 31) == 0 && left > 0) {
+      r.m_unit[i / kBlock] = um;
+      r.v_unit[i / kBlock] = uv;
+    }
+  }
+}
+
+// A whole chunk takes no checks, and its next values are loaded before the present ones
+// are worked on.
 template <class T, int BITS, bool MASTER>
 __global__ void __launch_bounds__(kThreads) step_kernel(const Args a) {
+  constexpr int kStep = kThreads * kEach;
   const int chunk = blockIdx.x;
   const int k = find(a, chunk);
   const Rec r = a.rec[k];
-  const int begin = k ? a.end[k - 1] : 0;
+  const int64_t begin = (int64_t)(chunk - (k ? a.end[k - 1] : 0)) * kChunk;
 
   Consts c = {a.decay, a.size, a.root, a.key};
   if (a.lr_dev || a.step_dev) {
@@ -248,69 +356,26 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const Args a) {
   }
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const uint32_t key = mix(c.key + (uint32_t)a.index[k]);
-  const bool vec = on16(r.param) && on16(r.grad) && on16(r.m) && on16(r.v) &&
-                   (!MASTER || on16(r.master));
-
+  const int64_t first = begin + (int64_t)threadIdx.x * kEach;
+  if (begin + kChunk <= r.n) {
+    Eight<T, BITS> x[2];
+    load<T, BITS, MASTER, true>(r, first, 8, &x[0]);
+#pragma unroll
+    for (int it = 0; it < kChunk / kStep; ++it) {
+      if (it + 1 < kChunk / kStep)
+        load<T, BITS, MASTER, true>(r, first + (it + 1) * kStep, 8, &x[(it + 1) & 1]);
+      update<T, BITS, MASTER, true>(a, r, c, gs, key, first + it * kStep, 8, &x[it & 1]);
+    }
+    return;
+  }
 #pragma unroll 1
-  for (int it = 0; it < kChunk / (kThreads * kEach); ++it) {
-    const int64_t i = (int64_t)(chunk - begin) * kChunk + it * (kThreads * kEach) +
-                      (int64_t)threadIdx.x * kEach;
+  for (int it = 0; it < kChunk / kStep; ++it) {
+    const int64_t i = first + it * kStep;
     const int left = (int)min((int64_t)kEach, max((int64_t)0, r.n - i));
     const int64_t at = left > 0 ? i : 0;  // (no address behind the end)
-    float p[8], g[8], m[8], v[8];
-    if (MASTER) load8(r.master + at, vec, left, p);
-    else load8(static_cast<const T*>(r.param) + at, vec, left, p);
-    load8(static_cast<const T*>(r.grad) + at, vec, left, g);
-    if constexpr (BITS == 32) {
-      load8(static_cast<const float*>(r.m) + at, vec, left, m);
-      load8(static_cast<const float*>(r.v) + at, vec, left, v);
-    } else {
-      uint32_t cm[8], cv[8];
-      load8(static_cast<const uint8_t*>(r.m) + at, vec, left, cm);
-      load8(static_cast<const uint8_t*>(r.v) + at, vec, left, cv);
-      const float um = r.m_unit[at / kBlock] * 0x1p4f, uv = r.v_unit[at / kBlock] * 0x1p10f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        m[e] = decode_m(cm[e], um);
-        v[e] = decode_v(cv[e], uv);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float ge = a.grad_scale ? g[e] * gs : g[e];
-      m[e] = m[e] * a.b1 + ge * a.c1;
-      v[e] = v[e] * a.b2 + ge * a.c2 * ge;
-      p[e] = p[e] * c.decay - m[e] * c.size / (sqrtf(v[e]) * c.root + a.eps);
-    }
-    store8(static_cast<T*>(r.param) + at, vec, left, p);
-    if (MASTER) store8(r.master + at, vec, left, p);
-    if constexpr (BITS == 32) {
-      store8(static_cast<float*>(r.m) + at, vec, left, m);
-      store8(static_cast<float*>(r.v) + at, vec, left, v);
-    } else {
-      uint32_t top_m = 0, top_v = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (e >= left) m[e] = v[e] = 0.f;
-        top_m = max(top_m, __float_as_uint(m[e]) & 0x7fffffffu);
-        top_v = max(top_v, __float_as_uint(v[e]) & 0x7fffffffu);
-      }
-      const float um = unit_of(block_max(top_m), kTopM), uv = unit_of(block_max(top_v), kTopV);
-      const float im = um > 0.f ? 1.f / um : 0.f, iv = uv > 0.f ? 1.f / uv : 0.f;
-      uint32_t cm[8], cv[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t bits = mix((uint32_t)(at + e) + key);
-        cm[e] = encode_m(m[e], im, fraction(bits & 0xffff));
-        cv[e] = encode_v(v[e], iv, fraction(bits >> 16));
-      }
-      store8(static_cast<uint8_t*>(r.m) + at, vec, left, cm);
-      store8(static_cast<uint8_t*>(r.v) + at, vec, left, cv);
-      if ((threadIdx.x & 31) == 0 && left > 0) {
-        r.m_unit[at / kBlock] = um;
-        r.v_unit[at / kBlock] = uv;
-      }
-    }
+    Eight<T, BITS> x;
+    load<T, BITS, MASTER, false>(r, at, left, &x);
+    update<T, BITS, MASTER, false>(a, r, c, gs, key, at, left, &x);
   }
 }
 
@@ -327,27 +392,30 @@ struct ReadArgs {
 };
 static_assert(sizeof(ReadArgs) <= 4096, "kernel arguments");
 
+typedef uint32_t __attribute__((aligned(1))) Four;  // codes, at any address
+
 // Four values a lane, so that the stores fill whole lines.
 __global__ void __launch_bounds__(kThreads) moments_kernel(const ReadArgs a) {
   const int chunk = blockIdx.x;
   const int k = find(a, chunk);
   const ReadRec r = a.rec[k];
   const int64_t begin = (int64_t)(chunk - (k ? a.end[k - 1] : 0)) * kChunk;
-  const bool vec = on16(r.m) && on16(r.v) && on16(r.out_m) && on16(r.out_v);
 #pragma unroll 2
   for (int it = 0; it < kChunk / (kThreads * 4); ++it) {
     const int64_t i = begin + it * (kThreads * 4) + threadIdx.x * 4;
     if (i >= r.n) return;
     const float um = r.m_unit[i / kBlock] * 0x1p4f, uv = r.v_unit[i / kBlock] * 0x1p10f;
-    if (vec && i + 4 <= r.n) {
-      const uint32_t cm = *reinterpret_cast<const uint32_t*>(r.m + i);
-      const uint32_t cv = *reinterpret_cast<const uint32_t*>(r.v + i);
-      *reinterpret_cast<float4*>(r.out_m + i) =
-          make_float4(decode_m(cm & 255, um), decode_m(cm >> 8 & 255, um),
-                      decode_m(cm >> 16 & 255, um), decode_m(cm >> 24, um));
-      *reinterpret_cast<float4*>(r.out_v + i) =
-          make_float4(decode_v(cv & 255, uv), decode_v(cv >> 8 & 255, uv),
-                      decode_v(cv >> 16 & 255, uv), decode_v(cv >> 24, uv));
+    if (i + 4 <= r.n) {
+      const uint32_t cm = *reinterpret_cast<const Four*>(r.m + i);
+      const uint32_t cv = *reinterpret_cast<const Four*>(r.v + i);
+      Words4 m, v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        m[e] = __float_as_uint(decode_m(cm >> (8 * e) & 255, um));
+        v[e] = __float_as_uint(decode_v(cv >> (8 * e) & 255, uv));
+      }
+      *reinterpret_cast<Quad4*>(r.out_m + i) = m;
+      *reinterpret_cast<Quad4*>(r.out_v + i) = v;
     } else {
       for (int64_t j = i; j < i + 4 && j < r.n; ++j) {
         r.out_m[j] = decode_m(r.m[j], um);

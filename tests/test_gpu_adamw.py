@@ -142,10 +142,20 @@ def compare(before, s, step, seed=0, how=HOW, scale=None):
             g = g * f(scale)
         want, m, v, um, uv = formula(host(start), g, host(before["m"][k]), host(before["v"][k]),
                                      **how, step=step, k=k, seed=seed, units=units)
-        rounded = torch.from_numpy(want).to(p.dtype)
-        same(host(s["param"][k]), rounded.float().numpy(), f"param {k}")
-        if s["master"]:
-            same(host(s["master"][k]), want, f"master {k}")
+        rounded = torch.from_numpy(want).to(p.dtype).float().numpy()
+        if units is None:
+            same(host(s["param"][k]), rounded, f"param {k}")
+            if s["master"]:
+                same(host(s["master"][k]), want, f"master {k}")
+        else:
+            # root, quotient, and the roundings of a product and a sum of them: within
+            # 2^-23 + 2^-23 + 2 * 2^-24 of the move, and half a step more of the result
+            move = np.abs(host(start) * f(1 - how["lr"] * how["weight_decay"]) - want)
+            tol = 2.0 ** -21 * move + 2.0 ** -23 * np.abs(want)
+            if s["master"]:
+                near(host(s["master"][k]), want, tol, f"master {k}")
+            step_of = 2.0 ** -7 if p.dtype == BF16 else 2.0 ** -23
+            near(host(s["param"][k]), rounded, tol + step_of * np.abs(rounded), f"param {k}")
         same(host(s["m"][k]), m, f"m {k}")
         same(host(s["v"][k]), v, f"v {k}")
         if units is not None:
@@ -156,6 +166,11 @@ def compare(before, s, step, seed=0, how=HOW, scale=None):
 def same(a, b, name):
     assert np.array_equal(a, b, equal_nan=a.dtype != np.uint8), (
         name, int((a != b).sum()), a[a != b][:4], b[a != b][:4])
+
+
+def near(a, b, tol, name):
+    off = np.abs(a.astype(np.float64) - b)
+    assert bool((off <= tol).all()), (name, float((off / np.maximum(tol, 1e-300)).max()))
 
 
 def copies(s):
