@@ -400,28 +400,44 @@ __global__ void __launch_bounds__(kThreads) moments_kernel(const ReadArgs a) {
   const int k = find(a, chunk);
   const ReadRec r = a.rec[k];
   const int64_t begin = (int64_t)(chunk - (k ? a.end[k - 1] : 0)) * kChunk;
-#pragma unroll 2
-  for (int it = 0; it < kChunk / (kThreads * 4); ++it) {
-    const int64_t i = begin + it * (kThreads * 4) + threadIdx.x * 4;
-    if (i >= r.n) return;
-    const float um = r.m_unit[i / kBlock] * 0x1p4f, uv = r.v_unit[i / kBlock] * 0x1p10f;
-    if (i + 4 <= r.n) {
-      const uint32_t cm = *reinterpret_cast<const Four*>(r.m + i);
-      const uint32_t cv = *reinterpret_cast<const Four*>(r.v + i);
-      Words4 m, v;
+  if (begin + kChunk <= r.n) {
+    // a whole chunk: the loads of four rounds before their stores
+    constexpr int kRounds = 4, kEach = kThreads * 4;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        m[e] = __float_as_uint(decode_m(cm >> (8 * e) & 255, um));
-        v[e] = __float_as_uint(decode_v(cv >> (8 * e) & 255, uv));
+    for (int half = 0; half < kChunk / (kRounds * kEach); ++half) {
+      const int64_t first = begin + half * (kRounds * kEach) + threadIdx.x * 4;
+      uint32_t cm[kRounds], cv[kRounds];
+      float um[kRounds], uv[kRounds];
+#pragma unroll
+      for (int it = 0; it < kRounds; ++it) {
+        const int64_t i = first + it * kEach;
+        cm[it] = *reinterpret_cast<const Four*>(r.m + i);
+        cv[it] = *reinterpret_cast<const Four*>(r.v + i);
+        um[it] = r.m_unit[i / kBlock] * 0x1p4f;
+        uv[it] = r.v_unit[i / kBlock] * 0x1p10f;
       }
-      *reinterpret_cast<Quad4*>(r.out_m + i) = m;
-      *reinterpret_cast<Quad4*>(r.out_v + i) = v;
-    } else {
-      for (int64_t j = i; j < i + 4 && j < r.n; ++j) {
-        r.out_m[j] = decode_m(r.m[j], um);
-        r.out_v[j] = decode_v(r.v[j], uv);
+#pragma unroll
+      for (int it = 0; it < kRounds; ++it) {
+        Words4 m, v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          m[e] = __float_as_uint(decode_m(cm[it] >> (8 * e) & 255, um[it]));
+          v[e] = __float_as_uint(decode_v(cv[it] >> (8 * e) & 255, uv[it]));
+        }
+        *reinterpret_cast<Quad4*>(r.out_m + first + it * kEach) = m;
+        *reinterpret_cast<Quad4*>(r.out_v + first + it * kEach) = v;
       }
     }
+    return;
+  }
+  for (int64_t i = begin + threadIdx.x * 4; i < r.n; i += kThreads * 4) {
+    const float um = r.m_unit[i / kBlock] * 0x1p4f, uv = r.v_unit[i / kBlock] * 0x1p10f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < r.n) {
+        r.out_m[i + e] = decode_m(r.m[i + e], um);
+        r.out_v[i + e] = decode_v(r.v[i + e], uv);
+      }
   }
 }
 
