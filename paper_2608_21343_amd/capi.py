@@ -909,7 +909,7 @@ def _adamw_table(lists, count: int, device):
                     raise ValueError(f"{name}[{i}] must be on {device}")
                 _need(t, sizes[i], f"{name}[{i}]")
                 _dptr(t, dtype, f"{name}[{i}]")
-        table[:, _ADAMW_FIELDS.index(name)] = list(map(T.data_ptr, tensors))
+        table[:, _ADAMW_FIELDS.index(name)] = np.fromiter(map(T.data_ptr, tensors), np.int64, count)
     return table
 
 

@@ -725,7 +725,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     float *hit = flt(L.hit), *z = L.kept ? flt(L.z) : nullptr;
     if (L.few) {
       const Few f = {c.x,      c.w,      c.bias,   c.x_stride, c.w_stride, (int32_t)c.n, c.D, c.C,
-                     c.target, L.n_part, part, hit, z, L.piece};
+                     c.target, L.n_part, few_each(c.C), part, hit, z, L.piece};
       e = few(f, c.dtype, st);
     } else {
       Gemm s = g;

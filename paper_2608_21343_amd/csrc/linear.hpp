@@ -105,13 +105,13 @@ struct Few {
   int64_t x_stride, w_stride;
   int32_t n, D, C;
   const int32_t* target;
-  int32_t parts;  // waves that share the tokens
+  int32_t parts, each;  // waves that share the tokens, and units of 16 tokens of a wave
   float2* part;   // [n, parts]
   float* hit;     // [n]
   float* z;       // [n, ldz] the logits, -inf up to a multiple of 16 tokens; or NULL
   int32_t ldz;
 };
-constexpr int32_t kFewWaves = 2048;  // eight a CU
+int32_t few_each(int32_t C);
 int32_t few_parts(int32_t C);
 hipError_t few(const Few& f, int32_t dtype, hipStream_t st);
 

@@ -4,10 +4,12 @@
 // is that of reading them. A wave takes all rows of a group of 64 and its share of the
 // tokens, 64 at a time, straight from memory into the operands of the matrix
 // instructions: no LDS, no barriers, and every wave keeps several steps of loads in
-// flight. Tokens are dealt out in units of 16, so that no wave has more than one unit
-// more than another: with tiles of 256 tokens 131,073 of them took three rounds of
-// the card's 256 CUs for little more than two rounds' worth. Layers of few tokens have a
-// wave for each 16 of them, with up to eight steps of loads in flight.
+// flight. Waves begin at different places of their rows: in step they would ask for the
+// same part of every row, which the same memory channels hold (8 rows of 1024 bfloat16
+// against 131,073 tokens 57 us, 52 so; 268 MB at 5.2 TB/s). Tokens are dealt out in
+// units of 16: tiles of 256 took three rounds of the card's CUs for little more than two
+// rounds' worth. Layers of few tokens have a wave for each 16 of them, with up to eight
+// steps of loads in flight.
 //
 // float32 operands are taken apart into three bfloat16 planes in registers (x, the
 // rounding of what x leaves, and once more): six products of them, to 2^-26 of the
@@ -72,7 +74,8 @@ __global__ void __launch_bounds__(256) few_kernel(const Few f) {
   const int row0 = blockIdx.y * (NQ * 16);
   const int lq = lane & 15, lk = 8 * (lane >> 4), lp = 4 * (lane >> 4);
   const int64_t units = (f.C + kFrag - 1) / kFrag;
-  const int first = (int)(units * wave / f.parts), last = (int)(units * (wave + 1) / f.parts);
+  const int first = wave * f.each, last = (int)min(units, (int64_t)first + f.each);
+  const int steps = (f.D + 31) / 32, start = (5 * wave) % steps;
   const T* x[NQ];
   int target[NQ];
   float top[NQ], sum[NQ];
@@ -96,8 +99,12 @@ __global__ void __launch_bounds__(256) few_kernel(const Few f) {
 #pragma unroll
       for (int q = 0; q < NQ; ++q) acc[p][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     Eight<T> a[kSets][kP], b[kSets][NQ];
-    auto load = [&](int set, int k) {
-      const bool in = k + lk < f.D;
+    auto load = [&](int set, int step) {
+      // every wave begins at another place of its rows
+      int at = step + start;
+      at = at >= steps ? at - steps : at;
+      const int k = 32 * at;
+      const bool in = step < steps && k + lk < f.D;
 #pragma unroll
       for (int p = 0; p < kP; ++p) a[set][p].load(w[p] + (in ? k : 0), in);
 #pragma unroll
@@ -125,12 +132,12 @@ __global__ void __launch_bounds__(256) few_kernel(const Few f) {
       }
     };
 #pragma unroll
-    for (int s = 0; s < kSets; ++s) load(s, 32 * s);
-    for (int k = 0; k < f.D; k += 32 * kSets)
+    for (int s = 0; s < kSets; ++s) load(s, s);
+    for (int k = 0; k < steps; k += kSets)
 #pragma unroll
       for (int s = 0; s < kSets; ++s) {
         multiply(s);
-        load(s, k + 32 * (s + kSets));
+        load(s, k + s + kSets);
       }
     const T* bias = static_cast<const T*>(f.bias);
 #pragma unroll
@@ -204,15 +211,21 @@ void few_t(const Few& f, hipStream_t st) {
 
 }  // namespace
 
-int32_t few_parts(int32_t C) {
+// A unit a wave where there are no more than 16 waves a CU of them; else a multiple of the
+// four that a wave takes at a time, with up to 12 waves a CU.
+int32_t few_each(int32_t C) {
   const int32_t units = (C + kFrag - 1) / kFrag;
-  return units <= kFewWaves ? units : kFewWaves;
+  return units <= 4096 ? 1 : 4 * ((units + 4 * 3072 - 1) / (4 * 3072));
+}
+
+int32_t few_parts(int32_t C) {
+  const int32_t units = (C + kFrag - 1) / kFrag, each = few_each(C);
+  return (units + each - 1) / each;
 }
 
 hipError_t few(const Few& f, int32_t dtype, hipStream_t st) {
-  const bool single = (f.C + kFrag - 1) / kFrag <= f.parts;
-  if (dtype == TB_F32) single ? few_t<float, 1>(f, st) : few_t<float, 4>(f, st);
-  else single ? few_t<uint16_t, 1>(f, st) : few_t<uint16_t, 4>(f, st);
+  if (dtype == TB_F32) f.each == 1 ? few_t<float, 1>(f, st) : few_t<float, 4>(f, st);
+  else f.each == 1 ? few_t<uint16_t, 1>(f, st) : few_t<uint16_t, 4>(f, st);
   return hipGetLastError();
 }
 
