@@ -412,8 +412,9 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   const float lse = base + logf(sum);
   if (f.out_lse) f.out_lse[row] = lse;
   if (f.out_loss) {
-    const float hit = (uint32_t)t < (uint32_t)f.C ? f.hit[from] : __builtin_nanf("");
-    const float nll = lse == -__builtin_huge_valf() && hit == lse ? __builtin_huge_valf() : lse - hit;
+    // (the maximum first: a small loss keeps its digits; an empty row's is +inf)
+    float nll = lse == -__builtin_huge_valf() ? -lse : (base - f.hit[from]) + logf(sum);
+    if ((uint32_t)t >= (uint32_t)f.C) nll = __builtin_nanf("");
     f.out_loss[row] = f.weight ? weight * nll : nll;
   }
   if (!f.idx) return;
@@ -525,15 +526,16 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// db[c] = the sum of the columns over the blocks of `rows` rows: 64 tokens a workgroup,
-// a sixteenth of the blocks each wave.
+// db[c] = the sum of the columns over the blocks of `rows` rows (rows_rest from token `main`
+// on): 64 tokens a workgroup, a sixteenth of the blocks each wave.
 template <class T>
 __global__ void __launch_bounds__(1024)
-    columns_kernel(const float* col, int32_t ldg, const Meta* meta, int32_t rows, T* db,
-                   int32_t n) {
+    columns_kernel(const float* col, int32_t ldg, const Meta* meta, int32_t rows, int32_t main,
+                   int32_t rows_rest, T* db, int32_t n) {
   __shared__ float sums[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = blockIdx.x * 64 + lane;
+  if (c >= main) rows = rows_rest;
   const int tiles = (meta->n + rows - 1) / rows;
   float sum = 0.f;
   if (c < n)
@@ -559,10 +561,10 @@ constexpr int32_t kFewRows = 64;             // that linear_few.hip takes
 // tile costs some besides (first loads, epilogue), parts a way through memory.
 struct Cut {
   int32_t tile, parts;
+  double cost;
 };
 Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
-  Cut best = {256, 1};
-  double least = 0;
+  Cut best = {256, 1, 0};
   const struct {
     int32_t tile;
     double step, fixed;
@@ -575,22 +577,39 @@ Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
       const double rounds = (double)((tiles * n + 255) / 256);
       const double cost = rounds * ((double)((steps + n - 1) / n) * stages * s.step + s.fixed) +
                           (n > 1 ? 4.0 + n * way : 0.0);
-      if (least == 0 || cost < least * 0.97) {
-        best = {s.tile, n};
-        least = cost;
-      }
+      if (best.cost == 0 || cost < best.cost * 0.97) best = {s.tile, n, cost};
     }
   }
   return best;
+}
+
+// The tokens of a product: those in whole tiles of 256, and where it pays the few behind
+// them on their own. A vocabulary and its blank are often one more than a multiple of 256,
+// and a row of tiles for that one token may be a round of the whole card.
+constexpr int64_t kRest = 64;  // tokens that may be on their own
+struct Strips {
+  int32_t main;  // tokens of the first
+  Cut cut[2];
+};
+Strips strips(int64_t tokens, int64_t others, int64_t steps, int64_t stages, bool parts) {
+  Strips s = {(int32_t)tokens, {cut(tokens, others, steps, stages, parts), {64, 1, 0}}};
+  const int64_t rest = tokens % 256, main = tokens - rest;
+  if (rest == 0 || rest > kRest || main == 0) return s;
+  const Cut a = cut(main, others, steps, stages, parts), b = cut(rest, others, steps, stages, parts);
+  // (a launch of its own: 4 us)
+  if (a.cost + b.cost + 3.0 < s.cut[0].cost) s = {(int32_t)main, {a, b}};
+  return s;
 }
 
 struct Layout {
   int64_t np, dp, planes;      // gathered rows and values a row, rounded up
   bool copy_w, few, gather, kept;      // kept: the logits, from the statistics to their gradients
   int32_t n_part;
-  int32_t piece, pieces;       // tokens of a piece of the vocabulary
-  Cut stats, grad, x, w;       // of the four products
-  int32_t col_rows;            // rows of a partial sum of columns
+  // tokens of a piece of the vocabulary (of all but the last), and of a row of gradients
+  int32_t piece, pieces, ldg;
+  Strips stats, grad, w;       // of the products with tokens of their own ...
+  Cut grad_all, w_all;         // (pieces but the last)
+  Cut x;                       // ... and that which sums over them
   bool direct;                 // dx leaves its product's sums as it is
   int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, s, hit, part, px, pxm, pw, z, G, acc_x;
   int64_t acc_w, col, total;
@@ -615,8 +634,13 @@ Layout plan(const Call& c) {
   L.copy_w = L.copy_w && L.gather;
   // products of planes that a step takes
   const int64_t stages = f32 ? 3 : 1;
-  L.stats = cut(c.C, c.n, L.dp / kStep, stages, false);
-  L.n_part = L.few ? few_parts(c.C) : 2 * ((c.C + L.stats.tile - 1) / L.stats.tile);
+  L.stats = strips(c.C, c.n, L.dp / kStep, stages, false);
+  L.n_part = few_parts(c.C);
+  if (!L.few) {
+    const int32_t main = L.stats.main, rest = c.C - main;
+    const int32_t a = L.stats.cut[0].tile, b = L.stats.cut[1].tile;
+    L.n_part = 2 * ((main + a - 1) / a + (rest + b - 1) / b);
+  }
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -646,24 +670,29 @@ Layout plan(const Call& c) {
     const int64_t all = L.planes * L.np * 2 * c.C;
     int64_t pieces = (all + kGradBytes / 2) / kGradBytes;
     pieces = pieces < 1 ? 1 : pieces;
-    L.piece = (int32_t)up((c.C + pieces - 1) / pieces, kTile);
-    L.pieces = (c.C + L.piece - 1) / L.piece;
-    L.kept = !c.lse && L.pieces == 1 && c.n * L.piece * 4 <= kGradBytes;
-    L.G = take(L.planes * L.np * L.piece * 2);
-    if (L.kept) L.z = take(L.np * L.piece * 4);
-    const int64_t n = c.C < L.piece ? c.C : L.piece;
-    L.grad = cut(n, c.n, L.dp / kStep, stages, false);
+    // (a few tokens more than whole tiles go with the last piece)
+    L.piece = (int32_t)up(pieces == 1 ? c.C : (c.C - kRest + pieces - 1) / pieces, kTile);
+    L.pieces = pieces == 1 ? 1 : (int32_t)((c.C - kRest + L.piece - 1) / L.piece);
+    const int32_t last = c.C - (L.pieces - 1) * L.piece, most = std::max(last, std::min(c.C, L.piece));
+    L.ldg = (int32_t)up(most, kTile);
+    L.kept = !c.lse && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
+    L.G = take(L.planes * L.np * L.ldg * 2);
+    if (L.kept) L.z = take(L.np * L.ldg * 4);
     if (c.dx) {
-      L.x = cut(L.dp, c.n, up(n, kStep) / kStep, stages, true);
+      L.x = cut(L.dp, c.n, up(most, kStep) / kStep, stages, true);
       L.direct = L.x.parts == 1;
       if (!L.direct || L.pieces > 1) L.acc_x = take(L.x.parts * L.np * L.dp * 4);
     }
     if (c.dw) {
-      L.w = cut(L.dp, n, L.np / kStep, stages, true);
-      if (L.w.parts > 1) L.acc_w = take(L.w.parts * (int64_t)L.piece * L.dp * 4);
+      // (the last piece's cut: all others have whole tiles)
+      L.w = strips(last, L.dp, L.np / kStep, stages, true);
+      L.w_all = cut(L.piece, L.dp, L.np / kStep, stages, true);
+      const int32_t parts = std::max({L.w.cut[0].parts, L.w.cut[1].parts, L.w_all.parts});
+      if (parts > 1) L.acc_w = take(parts * (int64_t)L.ldg * L.dp * 4);
     }
-    L.col_rows = L.kept ? 64 : L.grad.tile;
-    if (c.db) L.col = take(L.np / L.col_rows * L.piece * 4);
+    L.grad = strips(last, c.n, L.dp / kStep, stages, false);
+    L.grad_all = cut(L.piece, c.n, L.dp / kStep, stages, false);
+    if (c.db) L.col = take(L.np / 64 * L.ldg * 4);
   }
   L.total = at;
   return L;
@@ -720,25 +749,34 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   g.D = c.D;
   g.idx = idx;
   auto tiles = [](int64_t n, const Cut& cut) { return (int32_t)((n + cut.tile - 1) / cut.tile); };
+  // The launches over the tokens of a product, strip by strip: at(g, first token of the
+  // strip, its tokens, its cut) completes and launches one.
+  auto over = [&](const Strips& s, int32_t tokens, auto at) {
+    hipError_t r = at(0, std::min(s.main, tokens), s.cut[0]);
+    return r != hipSuccess || s.main >= tokens ? r : at(s.main, tokens - s.main, s.cut[1]);
+  };
   if (!c.lse && c.n > 0) {
     float2* part = reinterpret_cast<float2*>(ws + L.part);
     float *hit = flt(L.hit), *z = L.kept ? flt(L.z) : nullptr;
     if (L.few) {
       const Few f = {c.x,      c.w,      c.bias,   c.x_stride, c.w_stride, (int32_t)c.n, c.D, c.C,
-                     c.target, L.n_part, few_each(c.C), part, hit, z, L.piece};
+                     c.target, L.n_part, few_each(c.C), part, hit, z, L.ldg};
       e = few(f, c.dtype, st);
     } else {
-      Gemm s = g;
-      s.P = W;
-      s.tile = L.stats.tile;
-      s.tp = tiles(c.C, L.stats);
-      s.tq = tiles(c.n, L.stats);
-      s.part = part;
-      s.n_part = L.n_part;
-      s.hit = hit;
-      s.z = z;
-      s.ldg = L.piece;
-      e = f32 ? stats_f32(s, st) : stats_bf16(s, st);
+      e = over(L.stats, c.C, [&](int32_t first, int32_t n, const Cut& cut) {
+        Gemm s = g;
+        s.P = {W.p + first * W.ld, W.plane, W.ld, n, n};
+        s.tile = cut.tile;
+        s.tp = tiles(n, cut);
+        s.tq = tiles(c.n, cut);
+        s.c0 = first;
+        s.part = part + (first ? 2 * tiles(first, L.stats.cut[0]) : 0);
+        s.n_part = L.n_part;
+        s.hit = hit;
+        s.z = z ? z + first : nullptr;
+        s.ldg = L.ldg;
+        return f32 ? stats_f32(s, st) : stats_bf16(s, st);
+      });
     }
     if (e != hipSuccess) return e;
     const Finish f = {meta,  part, L.n_part, hit,     L.gather ? idx : nullptr, c.target,
@@ -764,32 +802,36 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     }
   }
   for (int32_t piece = 0; piece < L.pieces; ++piece) {
-    const int32_t c0 = piece * L.piece, n = c.C - c0 < L.piece ? c.C - c0 : L.piece;
-    Gemm z = g;
-    z.P = W;
-    z.P.p += c0 * W.ld;
-    z.P.n = n;
-    z.tile = L.grad.tile;
-    z.tp = tiles(n, L.grad);
-    z.tq = tiles(c.n, L.grad);
-    z.c0 = c0;
-    z.G = u16(L.G);
-    z.g_plane = L.np * L.piece;
-    z.ldg = L.piece;
-    z.col = c.db ? flt(L.col) : nullptr;
+    const bool last = piece + 1 == L.pieces;
+    const int32_t c0 = piece * L.piece, n = last ? c.C - c0 : L.piece;
+    const Strips grad = last ? L.grad : Strips{n, {L.grad_all, L.grad_all}};
+    const Operand G = {u16(L.G), L.np * L.ldg, L.ldg, (int32_t)L.np, n};
+    float* col = c.db ? flt(L.col) : nullptr;
     if (L.kept && c.n > 0) {
-      const Kept k = {meta, flt(L.z), L.piece, L.few ? idx : nullptr, z.row, z.s, c.C,
-                      (int32_t)up(c.C, kStep), z.G, z.g_plane, z.col};
+      const Kept k = {meta, flt(L.z), L.ldg, L.few ? idx : nullptr, g.row, g.s, c.C,
+                      (int32_t)up(c.C, kStep), u16(L.G), G.plane, col};
       kept_kernel<T><<<dim3((c.C + 255) / 256, (unsigned)(L.np / 64)), dim3(256), 0, st>>>(k);
       e = hipGetLastError();
     } else {
-      e = f32 ? logit_grad_f32(z, st) : logit_grad_bf16(z, st);
+      e = over(grad, n, [&](int32_t first, int32_t n, const Cut& cut) {
+        Gemm z = g;
+        z.P = {W.p + (c0 + first) * W.ld, W.plane, W.ld, n, n};
+        z.tile = cut.tile;
+        z.tp = tiles(n, cut);
+        z.tq = tiles(c.n, cut);
+        z.c0 = c0 + first;
+        z.G = u16(L.G) + first;
+        z.g_plane = G.plane;
+        z.ldg = L.ldg;
+        z.col = col ? col + first : nullptr;
+        return f32 ? logit_grad_f32(z, st) : logit_grad_bf16(z, st);
+      });
     }
     if (e != hipSuccess) return e;
-    const Operand G = {z.G, z.g_plane, L.piece, (int32_t)L.np, n};
     if (c.db) {
       columns_kernel<T><<<dim3((n + 63) / 64), dim3(1024), 0, st>>>(
-          flt(L.col), L.piece, meta, L.col_rows, static_cast<T*>(c.db) + c0, n);
+          col, L.ldg, meta, L.kept ? 64 : grad.cut[0].tile, grad.main,
+          L.kept ? 64 : grad.cut[1].tile, static_cast<T*>(c.db) + c0, n);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -804,7 +846,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       x.splits = L.x.parts;
       x.k = (int32_t)up(n, kStep);
       x.acc = flt(L.acc_x);
-      if (L.direct && piece + 1 == L.pieces) {
+      if (L.direct && last) {
         x.out = c.dx;
         x.ldo = c.dx_stride;
       }
@@ -815,33 +857,34 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       if (e != hipSuccess) return e;
     }
     if (c.dw) {
-      Gemm w = g;
-      w.P = {XM.p, XM.plane, XM.ld, (int32_t)L.dp, (int32_t)L.np};
-      w.c0 = c0;
-      w.Q = {G.p, G.plane, G.ld, L.piece, (int32_t)L.np};
-      w.tile = L.w.tile;
-      w.tp = tiles(L.dp, L.w);
-      w.tq = tiles(n, L.w);
-      w.n_q = n;
-      w.splits = L.w.parts;
-      w.k = (int32_t)L.np;
-      T* out = static_cast<T*>(c.dw) + c0 * c.dw_stride;
-      if (L.w.parts > 1) {
+      const Strips all = last ? L.w : Strips{n, {L.w_all, L.w_all}};
+      e = over(all, n, [&](int32_t first, int32_t n, const Cut& cut) {
+        Gemm w = g;
+        w.P = {XM.p, XM.plane, XM.ld, (int32_t)L.dp, (int32_t)L.np};
+        w.c0 = c0 + first;
+        w.Q = {G.p + first, G.plane, G.ld, L.ldg - first, (int32_t)L.np};
+        w.tile = cut.tile;
+        w.tp = tiles(L.dp, cut);
+        w.tq = tiles(n, cut);
+        w.n_q = n;
+        w.splits = cut.parts;
+        w.k = (int32_t)L.np;
+        T* out = static_cast<T*>(c.dw) + (c0 + first) * c.dw_stride;
+        if (cut.parts == 1) {
+          w.out = out;
+          w.ldo = c.dw_stride;
+          return f32 ? dw_f32(w, st) : dw_bf16(w, st);
+        }
         w.acc = flt(L.acc_w);
-        w.acc_split = (int64_t)L.piece * L.dp;
+        w.acc_split = (int64_t)L.ldg * L.dp;
         w.lda = (int32_t)L.dp;
-      } else {
-        w.out = out;
-        w.ldo = c.dw_stride;
-      }
-      e = f32 ? dw_f32(w, st) : dw_bf16(w, st);
-      if (e != hipSuccess) return e;
-      if (L.w.parts > 1) {
+        const hipError_t r = f32 ? dw_f32(w, st) : dw_bf16(w, st);
+        if (r != hipSuccess) return r;
         join_kernel<T><<<dim3(blocks((int64_t)n * ((c.D + 3) / 4))), dim3(256), 0, st>>>(
             w, nullptr, out, c.dw_stride, n);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-      }
+        return hipGetLastError();
+      });
+      if (e != hipSuccess) return e;
     }
   }
   if (c.dx && c.n > 0 && !L.direct) {

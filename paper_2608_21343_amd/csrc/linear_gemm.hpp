@@ -535,14 +535,12 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
         m = fmaxf(m, __shfl_xor(m, 32));
         // (a NaN among the logits is no maximum, but it is in the sum)
         const float base = m == -__builtin_huge_valf() ? 0.f : m;
-        // one rounding for all terms: it moves the log-sum-exp by half a step of m
-        const float shift = -base * kLog2e;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, shift));
+            sum[e] += __builtin_amdgcn_exp2f((acc[i][j][e] - base) * kLog2e);
         float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
         all += __shfl_xor(all, 16);
         all += __shfl_xor(all, 32);
