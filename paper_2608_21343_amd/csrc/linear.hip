@@ -24,7 +24,7 @@ struct Gather {
   float *a, *b, *lse_c, *r, *m;
   float *out_loss, *out_lse;
   // the features, and their planes
-  int64_t stride, plane;
+  int64_t stride;
   int32_t D, dp;
   uint16_t* out;
   void* dx;  // rows that are left out get 0 here; or NULL
@@ -146,7 +146,7 @@ __device__ __forceinline__ void raise(uint32_t* to, float v) {
 // twice, the second time from the caches.
 template <class T>
 __device__ __forceinline__ float row_planes(const T* x, int D, int dp, bool wide, uint16_t* out,
-                                            int64_t plane, float* most) {
+                                            float* most) {
   constexpr int kKept = 8;
   const int lane = threadIdx.x & 63;
   float kept[kKept][4];
@@ -163,7 +163,7 @@ __device__ __forceinline__ float row_planes(const T* x, int D, int dp, bool wide
     Elem<T>::planes4(w, p);
 #pragma unroll
     for (int s = 0; s < Elem<T>::PLANES; ++s)
-      *reinterpret_cast<uint2*>(out + s * plane + d) = p[s];
+      *reinterpret_cast<uint2*>(out + place<Elem<T>::PLANES>(d) + s * kTurn) = p[s];
   };
   if (keep) {
 #pragma unroll
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
     }
     float most;
     const float unit = row_planes<T>(x + (row0 + i) * g.stride, g.D, g.dp, wide,
-                                     g.out + (int64_t)at * g.dp, g.plane, &most);
+                                     g.out + (int64_t)at * Elem<T>::PLANES * g.dp, &most);
     if (Elem<T>::kScaled && lane == 0) {
       g.r[at] = unit;
       const float with = most * g.m[at];  // (written by this workgroup)
@@ -299,11 +299,9 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
   if (Elem<T>::kScaled && g.grads) raise(&g.meta->T, weighty);
   if (blockIdx.x == gridDim.x - 1) {
     // the zeros behind the last row
-    const int64_t end = up(all, kStep) * g.dp;
-    for (int64_t i = (int64_t)all * g.dp + 4 * threadIdx.x; i < end; i += 1024)
-#pragma unroll
-      for (int s = 0; s < Elem<T>::PLANES; ++s)
-        *reinterpret_cast<uint2*>(g.out + s * g.plane + i) = make_uint2(0, 0);
+    const int64_t row = Elem<T>::PLANES * g.dp, end = up(all, kStep) * row;
+    for (int64_t i = all * row + 4 * threadIdx.x; i < end; i += 1024)
+      *reinterpret_cast<uint2*>(g.out + i) = make_uint2(0, 0);
   }
 }
 
@@ -311,12 +309,12 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
 template <class T>
 __global__ void __launch_bounds__(256)
     weights_kernel(const T* w, int64_t stride, int32_t D, int32_t dp, int32_t C, uint16_t* out,
-                   int64_t plane, float* units, Meta* meta) {
+                   float* units, Meta* meta) {
   const bool wide = rows_wide(w, stride);
   float top = 0.f;
   for (int64_t c = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); c < C; c += (int64_t)gridDim.x * 4) {
     float most;
-    const float unit = row_planes<T>(w + c * stride, D, dp, wide, out + c * dp, plane, &most);
+    const float unit = row_planes<T>(w + c * stride, D, dp, wide, out + c * Elem<T>::PLANES * dp, &most);
     // (a token without weights says nothing of the others' scale)
     if (Elem<T>::kScaled && (threadIdx.x & 63) == 0) units[c] = most > 0.f ? unit : 0.f;
     if (most > 0.f) top = fmaxf(top, unit);
@@ -327,7 +325,7 @@ __global__ void __launch_bounds__(256)
 // float32: the planes of x_i m_i / T of the gathered rows.
 __global__ void __launch_bounds__(256)
     weighted_kernel(const float* x, int64_t stride, int32_t D, int32_t dp, const int32_t* idx,
-                    const float* m, const Meta* meta, uint16_t* out, int64_t plane) {
+                    const float* m, const Meta* meta, uint16_t* out) {
   const int lane = threadIdx.x & 63;
   const bool wide = rows_wide(x, stride);
   const int64_t have = meta->n, rows = up(have, kStep);
@@ -345,8 +343,9 @@ __global__ void __launch_bounds__(256)
       }
       uint2 p[2];
       Elem<float>::planes4(v, p);
-      *reinterpret_cast<uint2*>(out + i * dp + d) = p[0];
-      *reinterpret_cast<uint2*>(out + plane + i * dp + d) = p[1];
+      uint16_t* to = out + i * 2 * dp + place<2>(d);
+      *reinterpret_cast<uint2*>(to) = p[0];
+      *reinterpret_cast<uint2*>(to + kTurn) = p[1];
     }
   }
 }
@@ -438,7 +437,6 @@ struct Kept {
   const float* s;
   int32_t C, cols;
   uint16_t* G;
-  int64_t plane;
   float* col;
 };
 
@@ -484,7 +482,8 @@ __global__ void __launch_bounds__(256) kept_kernel(const Kept k) {
       El::planes4(v, p);
 #pragma unroll
       for (int s = 0; s < El::PLANES; ++s)
-        *reinterpret_cast<uint2*>(k.G + s * k.plane + at * k.ldz + c0) = p[s];
+        *reinterpret_cast<uint2*>(k.G + at * El::PLANES * k.ldz + place<El::PLANES>(c0) +
+                                  s * kTurn) = p[s];
     }
   }
   if (!k.col) return;
@@ -719,7 +718,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse,
                      grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
                      a,      b,    lse, r, m, c.out_loss, c.out_lse,
-                     c.x_stride, L.np * L.dp, c.D, (int32_t)L.dp, u16(L.px),
+                     c.x_stride, c.D, (int32_t)L.dp, u16(L.px),
                      L.direct ? c.dx : nullptr, c.dx_stride};
   // (float32 gradients: it also clears what the others take maxima into)
   if (L.gather && (groups != 1 || f32))
@@ -729,14 +728,15 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       ga, static_cast<const T*>(c.x));
   if (L.copy_w && c.n > 0)
     weights_kernel<T><<<dim3(c.C < 8192 ? (c.C + 3) / 4 : 2048), dim3(256), 0, st>>>(
-        static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, c.C, u16(L.pw), c.C * L.dp,
+        static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, c.C, u16(L.pw),
         f32 ? flt(L.s) : nullptr, meta);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
 
-  const Operand X = {u16(L.px), L.np * L.dp, L.dp, (int32_t)L.np, (int32_t)L.np};
-  const Operand W = {L.copy_w ? u16(L.pw) : static_cast<const uint16_t*>(c.w), c.C * L.dp,
-                     L.copy_w ? L.dp : c.w_stride, c.C, c.C};
+  constexpr int PL = Elem<T>::PLANES;
+  const Operand X = {u16(L.px), PL * L.dp, (int32_t)L.np, (int32_t)L.np};
+  const Operand W = {L.copy_w ? u16(L.pw) : static_cast<const uint16_t*>(c.w),
+                     L.copy_w ? PL * L.dp : c.w_stride, c.C, c.C};
   Gemm g = {};
   g.meta = meta;
   g.bias = c.bias;
@@ -765,7 +765,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     } else {
       e = over(L.stats, c.C, [&](int32_t first, int32_t n, const Cut& cut) {
         Gemm s = g;
-        s.P = {W.p + first * W.ld, W.plane, W.ld, n, n};
+        s.P = {W.p + first * W.ld, W.ld, n, n};
         s.tile = cut.tile;
         s.tp = tiles(n, cut);
         s.tq = tiles(c.n, cut);
@@ -795,8 +795,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (c.dw && c.n > 0) {
       XM.p = u16(L.pxm);
       weighted_kernel<<<dim3(c.n < 8192 ? (c.n + 3) / 4 : 2048), dim3(256), 0, st>>>(
-          static_cast<const T*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, meta, u16(L.pxm),
-          L.np * L.dp);
+          static_cast<const T*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, meta, u16(L.pxm));
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -805,23 +804,22 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     const bool last = piece + 1 == L.pieces;
     const int32_t c0 = piece * L.piece, n = last ? c.C - c0 : L.piece;
     const Strips grad = last ? L.grad : Strips{n, {L.grad_all, L.grad_all}};
-    const Operand G = {u16(L.G), L.np * L.ldg, L.ldg, (int32_t)L.np, n};
+    const Operand G = {u16(L.G), PL * L.ldg, (int32_t)L.np, n};
     float* col = c.db ? flt(L.col) : nullptr;
     if (L.kept && c.n > 0) {
       const Kept k = {meta, flt(L.z), L.ldg, L.few ? idx : nullptr, g.row, g.s, c.C,
-                      (int32_t)up(c.C, kStep), u16(L.G), G.plane, col};
+                      (int32_t)up(c.C, kStep), u16(L.G), col};
       kept_kernel<T><<<dim3((c.C + 255) / 256, (unsigned)(L.np / 64)), dim3(256), 0, st>>>(k);
       e = hipGetLastError();
     } else {
       e = over(grad, n, [&](int32_t first, int32_t n, const Cut& cut) {
         Gemm z = g;
-        z.P = {W.p + (c0 + first) * W.ld, W.plane, W.ld, n, n};
+        z.P = {W.p + (c0 + first) * W.ld, W.ld, n, n};
         z.tile = cut.tile;
         z.tp = tiles(n, cut);
         z.tq = tiles(c.n, cut);
         z.c0 = c0 + first;
-        z.G = u16(L.G) + first;
-        z.g_plane = G.plane;
+        z.G = u16(L.G) + PL * first;
         z.ldg = L.ldg;
         z.col = col ? col + first : nullptr;
         return f32 ? logit_grad_f32(z, st) : logit_grad_bf16(z, st);
@@ -838,13 +836,13 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (c.dx) {
       // sum over the piece's tokens; a transposed operand's columns are the layer's width
       Gemm x = g;
-      x.P = {W.p + c0 * W.ld, W.plane, W.ld, (int32_t)L.dp, n};
+      x.P = {W.p + c0 * W.ld, W.ld, (int32_t)L.dp, n};
       x.Q = G;
       x.tile = L.x.tile;
       x.tp = tiles(L.dp, L.x);
       x.tq = tiles(c.n, L.x);
       x.splits = L.x.parts;
-      x.k = (int32_t)up(n, kStep);
+      x.k = (int32_t)up(n, kStep / PL);  // (a stage has a token at least)
       x.acc = flt(L.acc_x);
       if (L.direct && last) {
         x.out = c.dx;
@@ -860,9 +858,9 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       const Strips all = last ? L.w : Strips{n, {L.w_all, L.w_all}};
       e = over(all, n, [&](int32_t first, int32_t n, const Cut& cut) {
         Gemm w = g;
-        w.P = {XM.p, XM.plane, XM.ld, (int32_t)L.dp, (int32_t)L.np};
+        w.P = {XM.p, XM.ld, (int32_t)L.dp, (int32_t)L.np};
         w.c0 = c0 + first;
-        w.Q = {G.p + first, G.plane, G.ld, L.ldg - first, (int32_t)L.np};
+        w.Q = {G.p + PL * first, G.ld, L.ldg - first, (int32_t)L.np};
         w.tile = cut.tile;
         w.tp = tiles(L.dp, cut);
         w.tq = tiles(n, cut);

@@ -52,14 +52,22 @@ struct Meta {
   uint32_t S, T;  // float32: bits of max s_c, and of the largest |x_i m_i|
 };
 
-// A matrix as 16-bit planes. Element (i, k) of a plane, k the summed axis, lies at
-// i * ld + k, or (transposed) at k * ld + i. i < n and k < kn are in memory; a row
-// ends at a multiple of 8 elements, 16-byte aligned.
+// A matrix as 16-bit planes. Element (i, k), k the summed axis, lies in row i at value k,
+// or (transposed) in row k at value i; ld: 16-bit values from row to row. i < n and
+// k < kn are in memory; a row ends at a multiple of 8 values, 16-byte aligned. Two planes
+// lie in turns of 32 values, so that 64 of a row's are 32 of the matrix's, whole.
 struct Operand {
   const uint16_t* p;
-  int64_t plane, ld;
+  int64_t ld;
   int32_t n, kn;
 };
+
+// Where value c of a row's first plane lies, and how much further on the next plane's.
+constexpr int kTurn = 32;
+template <int PLANES>
+__host__ __device__ inline int64_t place(int64_t c) {
+  return PLANES == 1 ? c : 2 * c - (c & (kTurn - 1));
+}
 
 // Per gathered row.
 struct RowArgs {
@@ -84,7 +92,6 @@ struct Gemm {
   float* hit;      // logit of the row's target
   float* z;        // [gathered row, ldg] the logits, where they are kept
   uint16_t* G;     // planes of [row, ldg]
-  int64_t g_plane;
   int32_t ldg;
   float* col;      // [row tiles, ldg], or NULL
   // products with the gradients

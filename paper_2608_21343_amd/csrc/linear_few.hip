@@ -213,9 +213,10 @@ void few_t(const Few& f, hipStream_t st) {
 
 // A unit a wave where there are no more than 16 waves a CU of them; else a multiple of the
 // four that a wave takes at a time, with up to 12 waves a CU.
+constexpr int32_t kMost = 12 * 256;
 int32_t few_each(int32_t C) {
   const int32_t units = (C + kFrag - 1) / kFrag;
-  return units <= 4096 ? 1 : 4 * ((units + 4 * 3072 - 1) / (4 * 3072));
+  return units <= 4096 ? 1 : 4 * ((units + 4 * kMost - 1) / (4 * kMost));
 }
 
 int32_t few_parts(int32_t C) {

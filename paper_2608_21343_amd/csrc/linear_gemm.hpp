@@ -48,16 +48,13 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 __device__ __forceinline__ float low16(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float high16(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
-// An operand of one type: its planes, the products of them that are summed (the
-// largest last), and the matrix instruction.
+// An operand of one type: its planes, and the matrix instruction.
 template <class T>
 struct Elem;
 template <>
 struct Elem<uint16_t> {
-  static constexpr int PLANES = 1, PAIRS = 1;
+  static constexpr int PLANES = 1;
   static constexpr bool kScaled = false;
-  __device__ static inline int p(int) { return 0; }
-  __device__ static inline int q(int) { return 0; }
   __device__ static inline void planes4(const float* v, uint2* out) {
     out[0] = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
   }
@@ -68,10 +65,8 @@ struct Elem<uint16_t> {
 };
 template <>
 struct Elem<float> {
-  static constexpr int PLANES = 2, PAIRS = 3;  // (1, 0) (0, 1) (0, 0)
+  static constexpr int PLANES = 2;
   static constexpr bool kScaled = true;
-  __device__ static inline int p(int s) { return s == 0 ? 1 : 0; }
-  __device__ static inline int q(int s) { return s == 1 ? 1 : 0; }
   __device__ static inline void planes4(const float* v, uint2* out) {
     const f16x2 a = {(_Float16)v[0], (_Float16)v[1]}, b = {(_Float16)v[2], (_Float16)v[3]};
     const f16x2 c = {(_Float16)(v[0] - (float)a[0]), (_Float16)(v[1] - (float)a[1])};
@@ -85,14 +80,21 @@ struct Elem<float> {
   }
 };
 
-// A lane's first 16-byte load of a stage: the row of the operand's memory that it comes
-// from (its own rows, or transposed the summed values), counted from the tile's, and the
-// bytes in that row. The next ones come from kNextRows rows further on.
-template <int N, bool TR>
+// A lane's first 16-byte load of a stage: the stage's row that it fills and where in a row
+// of the operand's memory it comes from, in bytes. The next ones fill rows kNextRows further
+// on. Stage rows are the operand's own rows, or (transposed) the summed values: 64, or 32
+// of the first plane and the same 32 of the second.
+template <int N, bool TR, int PLANES>
 struct Lane {
   static constexpr int kNextRows = TR ? kWaves * 512 / N : kWaves * 8;
+  static constexpr int kK = TR ? kStep / PLANES : N;  // rows of the operand of a stage
   int row;
   uint32_t bytes;
+  // of load `it`, `rows` rows being in memory
+  __device__ inline uint32_t at(int it, uint32_t row_bytes, int rows) const {
+    return (uint32_t)min((row + it * kNextRows) & (kK - 1), rows - 1) * row_bytes + bytes +
+           it * kNextRows / kK * (kTurn * 2);
+  }
 };
 
 // By how much the 32-byte pieces of row k of a transposed operand's stage are exchanged:
@@ -103,16 +105,16 @@ __device__ __forceinline__ int turn_of(int k) {
   return N >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);
 }
 
-template <int N, bool TR>
-__device__ __forceinline__ Lane<N, TR> lane_of(const Operand& o, int32_t i0) {
+template <int N, bool TR, int PLANES>
+__device__ __forceinline__ Lane<N, TR, PLANES> lane_of(const Operand& o, int32_t i0) {
   const int at = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 + (threadIdx.x & 63);
   if (!TR) {
     const int row = at >> 3;
     return {row, (uint32_t)((at & 7) ^ ((row >> 1) & 7)) * 16};
   }
   const int k = at / (N / 8), piece = at % (N / 8);
-  const int col = (((piece >> 1) ^ turn_of<N>(k)) * 2 + (piece & 1)) * 8;
-  return {k, (uint32_t)min(col, o.n - 8 - i0) * 2};
+  const int col = min((((piece >> 1) ^ turn_of<N>(k)) * 2 + (piece & 1)) * 8, o.n - 8 - i0);
+  return {k, (uint32_t)(place<PLANES>(col) + k / (kStep / PLANES) * kTurn) * 2};
 }
 
 // An address that is the same in every lane, in scalar registers.
@@ -166,32 +168,51 @@ __device__ __forceinline__ void interleave() {
   if (MUL > READS * kEach) __builtin_amdgcn_sched_group_barrier(0x008, MUL - READS * kEach, 0);
 }
 
-// A stage of an operand from `base`, off: of the lane's first load. `rows` of it are in
-// memory; the others are read as the last of them.
-template <int N, bool TR>
-__device__ __forceinline__ void load_stage(uint32_t to, const uint16_t* base, uint32_t off,
-                                           const Operand& o, int32_t i0, int32_t rows) {
-  constexpr int kNext = Lane<N, TR>::kNextRows, kLoads = Tiling<N>::kLoads;
-  to += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
-  if (rows >= kNext * kLoads) {
-    const char* from = uniform(base);
-    const int64_t step = kNext * 2 * o.ld;
+// The same of FP x FQ products, column by column, while FP fragments of RP reads and FQ of
+// RQ are read, these each in the place of its column's.
+template <int FP, int RP, int FQ, int RQ>
+__device__ __forceinline__ void interleave_columns() {
+  static_assert(FP == 2 * FQ, "two fragments of P a column");
 #pragma unroll
-    for (int it = 0; it < kLoads; ++it, from += step) load_lds(to + it * kWaves * 1024, from, off);
-  } else {
-    const Lane<N, TR> l = lane_of<N, TR>(o, i0);
+  for (int j = 0; j < FQ; ++j) {
 #pragma unroll
-    for (int it = 0; it < kLoads; ++it)
-      load_lds(to + it * kWaves * 1024, uniform(base),
-               (uint32_t)min(l.row + it * kNext, rows - 1) * (uint32_t)(o.ld * 2) + l.bytes);
+    for (int i = 0; i < 2; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, FP / 2, 0);  // products
+      __builtin_amdgcn_sched_group_barrier(0x100, RP, 0);      // LDS reads
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, RQ, 0);
   }
 }
 
-// Fragment of 16 rows from i (a multiple of 16) and 32 summed values from 32 * ks:
-// lane l holds row l % 16, values 8 (l / 16) ...
+// A stage of an operand from `base`, off: of the lane's first load. `rows` of it are in
+// memory; the others are read as the last of them.
+template <int N, bool TR, int PLANES>
+__device__ __forceinline__ void load_stage(uint32_t to, const uint16_t* base, uint32_t off,
+                                           const Operand& o, int32_t i0, int32_t rows) {
+  typedef Lane<N, TR, PLANES> La;
+  constexpr int kLoads = Tiling<N>::kLoads;
+  to += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+  if (rows >= La::kK) {
+    const char* from = uniform(base);
+#pragma unroll
+    for (int it = 0; it < kLoads; ++it) {
+      constexpr int kNext = La::kNextRows;
+      load_lds(to + it * kWaves * 1024,
+               from + (int64_t)(it * kNext % La::kK) * 2 * o.ld + it * kNext / La::kK * (kTurn * 2),
+               off);
+    }
+  } else {
+    const La l = lane_of<N, TR, PLANES>(o, i0);
+#pragma unroll
+    for (int it = 0; it < kLoads; ++it)
+      load_lds(to + it * kWaves * 1024, uniform(base), l.at(it, (uint32_t)(o.ld * 2), rows));
+  }
+}
+
+// Fragment of 16 rows from i (a multiple of 16) and the ks-th 32 values of a stage (two
+// planes: the ks-th plane): lane l holds row l % 16, values 8 (l / 16) ...
 template <int N, bool TR>
-__device__ __forceinline__ s16x8 fragment(const lds_char* tile, int i, int ks) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ s16x8 fragment(const lds_char* tile, int i, int ks, int lane) {
   if (!TR) {
     const int r = lane & 15, piece = ((lane >> 4) + 4 * ks) ^ (r >> 1);
     return *reinterpret_cast<const __attribute__((address_space(3))) s16x8*>(
@@ -290,6 +311,7 @@ constexpr int kGroupP = 4;  // tiles of P that a run takes by all of Q
 template <int KIND, class T, int N>
 __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   typedef Elem<T> El;
+  constexpr int PL = El::PLANES, kK = kStep / PL;  // summed values of a stage
   constexpr bool TP = KIND == kDx || KIND == kDw, TQ = KIND == kDw;
   constexpr bool kLogits = KIND == kStats || KIND == kLogitGrad;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -311,8 +333,8 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   const int tiles = g.tp * tiles_q, total = tiles * g.splits, each = (total + 7) / 8;
   const int stride = gridDim.x >> 3, end = min(((int)(blockIdx.x & 7) + 1) * each, total);
   const int begin = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-  int steps_all = g.k / kStep;
-  if (KIND == kDw) steps_all = min(steps_all, (meta.n + kStep - 1) / kStep);
+  int steps_all = g.k / kK;
+  if (KIND == kDw) steps_all = min(steps_all, (meta.n + kK - 1) / kK);
   const int steps_each =
       __builtin_amdgcn_readfirstlane((steps_all + g.splits - 1) / g.splits);
   struct Tile {
@@ -375,50 +397,57 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       }
       load_tile = tile_of(load_id);
       load_s = 0;
-      load_n = load_tile.steps * El::PAIRS;
+      load_n = load_tile.steps;
       if (load_n > 0) {
         if (kLogits) load_params(load_tile, load_turn);
         load_turn = load_turn == kSets - 1 ? 0 : load_turn + 1;
-        const Lane<N, TP> lp = lane_of<N, TP>(g.P, load_tile.p * N);
-        const Lane<N, TQ> lq = lane_of<N, TQ>(g.Q, load_tile.q * N);
-        off_p = lp.row * (uint32_t)(g.P.ld * 2) + lp.bytes;
-        off_q = lq.row * (uint32_t)(g.Q.ld * 2) + lq.bytes;
+        off_p = lane_of<N, TP, PL>(g.P, load_tile.p * N).at(0, (uint32_t)(g.P.ld * 2), N);
+        off_q = lane_of<N, TQ, PL>(g.Q, load_tile.q * N).at(0, (uint32_t)(g.Q.ld * 2), N);
       }
     }
     if (load_id >= end) return;
-    const int k = load_tile.first + load_s / El::PAIRS, pair = load_s % El::PAIRS;
-    const int64_t p0 = load_tile.p * N, q0 = load_tile.q * N, k0 = (int64_t)k * kStep;
-    const uint16_t* bp = g.P.p + El::p(pair) * g.P.plane + (TP ? k0 * g.P.ld + p0 : p0 * g.P.ld + k0);
-    const uint16_t* bq = g.Q.p + El::q(pair) * g.Q.plane + (TQ ? k0 * g.Q.ld + q0 : q0 * g.Q.ld + k0);
+    const int64_t p0 = load_tile.p * N, q0 = load_tile.q * N, k = load_tile.first + load_s;
+    const uint16_t* bp = g.P.p + (TP ? k * kK * g.P.ld + p0 * PL : p0 * g.P.ld + k * kStep);
+    const uint16_t* bq = g.Q.p + (TQ ? k * kK * g.Q.ld + q0 * PL : q0 * g.Q.ld + k * kStep);
     // (a transposed operand has all of a stage's rows, but for w behind the last token)
-    const int rows_p = TP ? (KIND == kDx ? g.P.kn - (int)k0 : kStep) : g.P.n - (int)p0;
-    const int rows_q = TQ ? kStep : g.Q.n - (int)q0;
+    const int rows_p = TP ? (KIND == kDx ? g.P.kn - (int)k * kK : kK) : g.P.n - (int)p0;
+    const int rows_q = TQ ? kK : g.Q.n - (int)q0;
     const uint32_t to = lds_at + buf * Ti::kStageBytes;
-    load_stage<N, TP>(to, bp, off_p, g.P, (int)p0, rows_p);
-    load_stage<N, TQ>(to + Ti::kOperandBytes, bq, off_q, g.Q, (int)q0, rows_q);
+    load_stage<N, TP, PL>(to, bp, off_p, g.P, (int)p0, rows_p);
+    load_stage<N, TQ, PL>(to + Ti::kOperandBytes, bq, off_q, g.Q, (int)q0, rows_q);
     ++load_s;
   };
 
-  // Fragments of one half of a stage are read while the products of the other half run.
-  // A stage's second half is in registers before the barrier in its middle, so behind
-  // that its place takes the stage after next, whose loads then have a whole stage's
-  // time; and no wave waits for LDS right after a barrier.
+  // A stage's second half (its second plane) is in registers before the barrier in its
+  // middle, so behind that its place takes another stage, whose loads then have all the
+  // time that the stages before it take; and no wave waits for LDS right after a barrier.
   f32x4 acc[FP][FQ];
   s16x8 pa[2][FP], qb[2][FQ];
-  auto read = [&](int buf, int half) {
-    const lds_char* P = lds + buf * Ti::kStageBytes;
-    const lds_char* Q = P + Ti::kOperandBytes;
+  constexpr int kReadP = (TP ? 2 : 1) * FP, kReadQ = (TQ ? 2 : 1) * FQ;  // LDS reads
+  int frag_lane = lane;
+  auto read_p = [&](int buf, int half) {
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) qb[half][j] = fragment<N, TQ>(Q, wq + 16 * j, half);
-#pragma unroll
-    for (int i = 0; i < FP; ++i) pa[half][i] = fragment<N, TP>(P, wp + 16 * i, half);
+    for (int i = 0; i < FP; ++i)
+      pa[half][i] = fragment<N, TP>(lds + buf * Ti::kStageBytes, wp + 16 * i, half, frag_lane);
   };
-  auto multiply = [&](int half) {
+  auto read_q = [&](int buf, int half) {
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+      qb[half][j] = fragment<N, TQ>(lds + buf * Ti::kStageBytes + Ti::kOperandBytes, wq + 16 * j,
+                                    half, frag_lane);
+  };
+  auto multiply = [&](int p, int q) {
 #pragma unroll
     for (int i = 0; i < FP; ++i)
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) acc[i][j] = El::mfma(pa[half][i], qb[half][j], acc[i][j]);
-    interleave<(TP ? 2 : 1) * FP + (TQ ? 2 : 1) * FQ, FP * FQ>();
+      for (int j = 0; j < FQ; ++j) acc[i][j] = El::mfma(pa[p][i], qb[q][j], acc[i][j]);
+  };
+  // (by columns, so that each of Q's fragments is free after its FP products)
+  auto multiply_by_q = [&](int p, int q) {
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+#pragma unroll
+      for (int i = 0; i < FP; ++i) acc[i][j] = El::mfma(pa[p][i], qb[q][j], acc[i][j]);
   };
 
   // Waits for the stage after the present one: those behind it may be in flight, as long
@@ -435,23 +464,44 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   int buf = 0, turn = 0;
   for (int id = begin; id < end; id += stride) {
     const Tile tile = tile_of(id);
-    const int p0 = tile.p * N, q0 = tile.q * N, n_stage = tile.steps * El::PAIRS;
+    const int p0 = tile.p * N, q0 = tile.q * N, n_stage = tile.steps;
     const Params<N>& par = params[turn];
     turn = turn == kSets - 1 ? 0 : turn + 1;
 #pragma unroll
     for (int i = 0; i < FP; ++i)
 #pragma unroll
       for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    read(buf, 0);
+    read_q(buf, 0);
+    read_p(buf, 0);
     for (int s = 0; s < n_stage; ++s) {
-      read(buf, 1);
-      multiply(0);
+      // (made again in every stage: kept, the places of fragments left too few registers for
+      // two planes' products)
+      if (KIND == kStats && PL == 2 && N == 256) asm volatile("" : "+v"(frag_lane));
+      // the first half's products while the second half is read ...
+      read_q(buf, 1);
+      read_p(buf, 1);
+      PL == 1 ? multiply(0, 0) : multiply_by_q(0, 0);
+      interleave<kReadP + kReadQ, FP * FQ>();
       land_next();
       __syncthreads();
       issue(buf);
       buf = buf == kStages - 1 ? 0 : buf + 1;
-      read(buf, 0);  // (behind the last stage nothing uses it)
-      multiply(1);
+      // ... and the others while the next stage's is (behind the last nothing uses it)
+      if constexpr (PL == 1) {
+        read_q(buf, 0);
+        read_p(buf, 0);
+        multiply(1, 1);
+        interleave<kReadP + kReadQ, FP * FQ>();
+      } else {
+        // (the next stage's first half takes the first one's registers, when its products
+        // have begun)
+        multiply(0, 1);
+        __builtin_amdgcn_sched_group_barrier(0x008, FP * FQ, 0);
+        read_p(buf, 0);
+        multiply_by_q(1, 0);
+        read_q(buf, 0);
+        interleave_columns<FP, kReadP / FP, FQ, kReadQ / FQ>();
+      }
     }
 
     // (the epilogue's addresses are made here: kept over the loop above they would not
@@ -635,18 +685,19 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
             El::planes4(v, out[i]);
           }
           const int64_t row = q0 + wq + 16 * j + lq;
-          uint16_t* to = g.G + row * g.ldg + p0 + wp + 64 * part;
+          uint16_t* to = g.G + row * PL * g.ldg + PL * (p0 + wp + 64 * part);
 #pragma unroll
           for (int s = 0; s < El::PLANES; ++s) {
             if constexpr (kF == 4) {
               uint4 lo, hi;
               gather16(out[0][s], out[1][s], out[2][s], out[3][s], &lo, &hi);
-              reinterpret_cast<uint4*>(to + s * g.g_plane + 4 * lp)[0] = lo;
-              reinterpret_cast<uint4*>(to + s * g.g_plane + 4 * lp)[1] = hi;
+              uint4* at = reinterpret_cast<uint4*>(to + place<PL>(4 * lp) + s * kTurn);
+              at[0] = lo;
+              at[1] = hi;
             } else {
 #pragma unroll
               for (int i = 0; i < kF; ++i)
-                *reinterpret_cast<uint2*>(to + s * g.g_plane + 16 * i + lp) = out[i][s];
+                *reinterpret_cast<uint2*>(to + place<PL>(16 * i + lp) + s * kTurn) = out[i][s];
             }
           }
         }
