@@ -18,7 +18,7 @@ struct Gather {
   const float *weight, *d_loss, *d_lse, *lse;
   bool grads;
   Meta* meta;
-  int32_t* counts;  // per group of kGroup rows: rows that take part ...
+  int32_t* counts;  // per group: rows that take part ...
   float* tops;      // ... and their largest finite |a|, |b|; NULL for a single group
   int32_t *idx, *inv, *tgt;
   float *a, *b, *lse_c, *r, *m;
@@ -31,8 +31,16 @@ struct Gather {
   int64_t dx_stride;
 };
 
-constexpr int kGroup = 2048, kEach = kGroup / 256;  // rows of a count, and of a thread of it
-constexpr int kRows = 16;                           // gathered by a workgroup
+// Rows of a count, in 256s, and rows that a workgroup gathers. Up to 2048 rows are one
+// group, which every workgroup counts, so that no launch counts before it, and take many
+// workgroups, for their latency (2048 rows of 1024 float32: 21 us with 16 rows each, 13
+// with 4). More rows are counted in groups of 256, since a workgroup counts its own group
+// once more; workgroups of 16 rows, since in float32 each raises one word of the whole
+// (16,000 rows of 512: 21 us, with groups of 2048 rows 25, with 4 rows each 34).
+constexpr int kOnly = 8, kRowsOnly = 4, kMany = 1, kRowsMany = 16;
+__host__ __device__ inline int64_t group_rows(int64_t n) {
+  return 256 * (n <= 256 * kOnly ? kOnly : kMany);
+}
 
 struct Row {
   int32_t target;  // -1: left out, -2: out of range
@@ -92,10 +100,9 @@ __global__ void __launch_bounds__(256) count_kernel(const Gather g) {
   if (blockIdx.x == 0 && threadIdx.x == 0) g.meta->S = g.meta->T = 0;
   int32_t count = 0, none = 0;
   float top = 0.f;
-  const int64_t first = (int64_t)blockIdx.x * kGroup;
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const Row o = row_of(g, first + e * 256 + threadIdx.x);
+  const int64_t first = blockIdx.x * group_rows(g.n);
+  for (int64_t r = first + threadIdx.x; r < first + group_rows(g.n); r += 256) {
+    const Row o = row_of(g, r);
     count += o.target != -1;
     top = fmaxf(top, finite_top(o));
   }
@@ -207,18 +214,19 @@ __device__ __forceinline__ bool rows_wide(const T* x, int64_t stride) {
   return stride * sizeof(T) % 16 == 0 && (uintptr_t)x % 16 == 0;
 }
 
-// kRows rows: their place among those that take part, their arguments and planes.
+// ROWS rows: their place among those that take part, their arguments and planes.
 // The rows before them are counted again up to the group's start, and groups by
 // their counts, so that no launch has to wait for a sum over all of them.
-template <class T>
+template <class T, int EACH, int ROWS>
 __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row0 = (int64_t)blockIdx.x * kRows;
+  const int64_t row0 = (int64_t)blockIdx.x * ROWS;
+  constexpr int64_t kGroup = 256 * EACH;
   const int64_t group = row0 / kGroup, groups = (g.n + kGroup - 1) / kGroup;
   int32_t before = 0, all = 0;
   float top = 0.f;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
+  for (int e = 0; e < EACH; ++e) {
     const int64_t r = group * kGroup + e * 256 + threadIdx.x;
     const Row o = row_of(g, r);
     before += o.target != -1 && r < row0;
@@ -236,15 +244,15 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
   }
   join256(&before, &all, &top);
 
-  __shared__ int32_t places[kRows];
+  __shared__ int32_t places[ROWS];
   if (wave == 0) {
     const int64_t r = row0 + lane;
     Row o = {-1, 0.f, 0.f};
-    if (lane < kRows) o = row_of(g, r);
+    if (lane < ROWS) o = row_of(g, r);
     const uint64_t keep = __ballot(o.target != -1);
     const int32_t at = before + __popcll(keep & ((1ull << lane) - 1));
-    if (lane < kRows) places[lane] = o.target != -1 ? at : -1;
-    if (lane < kRows && r < g.n) {
+    if (lane < ROWS) places[lane] = o.target != -1 ? at : -1;
+    if (lane < ROWS && r < g.n) {
       if (o.target == -1) {
         g.inv[r] = -1;
         if (g.out_loss) g.out_loss[r] = 0.f;
@@ -279,7 +287,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
   __syncthreads();
   const bool wide = rows_wide(x, g.stride);
   float weighty = 0.f;
-  for (int i = wave; i < kRows; i += 4) {
+  for (int i = wave; i < ROWS; i += 4) {
     const int32_t at = places[i];
     if (at < 0) {
       if (g.dx && row0 + i < g.n)
@@ -352,9 +360,8 @@ __global__ void __launch_bounds__(256)
 
 // ---- what joins the tiles
 
-// One wave a row (or, few rows with many parts, a workgroup): log-sum-exp and loss.
-// Gathered rows, whose parts lie by their place
-// or (by_row) by their row; or (idx NULL) all rows, and 0 for those left out.
+// Log-sum-exp and loss, of gathered rows, whose parts lie by their place or (by_row) by
+// their row; or (idx NULL) of all rows, and 0 for those left out.
 struct Finish {
   const Meta* meta;
   const float2* part;
@@ -368,24 +375,27 @@ struct Finish {
   float *out_loss, *out_lse;
 };
 
-// Maximum (or sum) over the first W waves of a workgroup.
-template <int W, bool MAX>
+// Maximum (or sum) over L lanes: part of a wave, or the four waves of a workgroup.
+template <int L, bool MAX>
 __device__ __forceinline__ float over(float v, float* lds) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v = MAX ? fmaxf(v, __shfl_xor(v, d)) : v + __shfl_xor(v, d);
-  if (W == 1) return v;
+  for (int d = L < 64 ? L / 2 : 32; d > 0; d >>= 1)
+    v = MAX ? fmaxf(v, __shfl_xor(v, d)) : v + __shfl_xor(v, d);
+  if (L <= 64) return v;
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
   return MAX ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]))
              : (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-template <int W>
+// L lanes a row: 16 for up to 128 parts (32,768 rows of 66: 7 us instead of 13 with a
+// wave each), or the workgroup for few rows with many parts.
+template <int L>
 __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
-  static_assert(W == 1 || W == 4, "waves of a row");
+  static_assert(L == 16 || L == 64 || L == 256, "lanes of a row");
   __shared__ float lds[2][4];
-  const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const int64_t at = W == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int lane = threadIdx.x % L;
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
   if (at >= (f.idx ? f.meta->n : f.n)) return;
   const int64_t row = f.idx ? f.idx[at] : at, from = f.by_row ? row : at;
   const int32_t t = f.target[row];
@@ -397,16 +407,16 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   }
   const float2* part = f.part + from * f.n_part;
   float m = -__builtin_huge_valf();
-  for (int i = lane; i < f.n_part; i += 64 * W) m = fmaxf(m, part[i].x);
-  m = over<W, true>(m, lds[0]);
+  for (int i = lane; i < f.n_part; i += L) m = fmaxf(m, part[i].x);
+  m = over<L, true>(m, lds[0]);
   const float base = m == -__builtin_huge_valf() ? 0.f : m;
   float sum = 0.f;
-  for (int i = lane; i < f.n_part; i += 64 * W) {
+  for (int i = lane; i < f.n_part; i += L) {
     const float2 v = part[i];
     // (a part without a value has maximum -inf and sum 0; a NaN in either stays)
     sum += v.y * __builtin_amdgcn_exp2f((v.x - base) * kLog2e);
   }
-  sum = over<W, false>(sum, lds[1]);
+  sum = over<L, false>(sum, lds[1]);
   if (lane != 0) return;
   const float lse = base + logf(sum);
   if (f.out_lse) f.out_lse[row] = lse;
@@ -647,7 +657,7 @@ Layout plan(const Call& c) {
     return here;
   };
   L.meta = take(sizeof(Meta));
-  const int64_t groups = (c.n + kGroup - 1) / kGroup;
+  const int64_t groups = (c.n + group_rows(c.n) - 1) / group_rows(c.n);
   L.counts = take((groups + 1) * 4);  // (without rows one is written all the same)
   L.tops = take((groups + 1) * 4);
   L.idx = take(c.n * 4);
@@ -714,7 +724,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   int32_t *idx = i32(L.idx), *inv = i32(L.inv), *tgt = i32(L.tgt);
   float *a = flt(L.a), *b = flt(L.b), *lse = flt(L.lse);
   float *r = f32 ? flt(L.r) : nullptr, *m = f32 ? flt(L.m) : nullptr;
-  const int64_t groups = (c.n + kGroup - 1) / kGroup;
+  const int64_t groups = (c.n + group_rows(c.n) - 1) / group_rows(c.n);
   const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse,
                      grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
                      a,      b,    lse, r, m, c.out_loss, c.out_lse,
@@ -723,9 +733,12 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   // (float32 gradients: it also clears what the others take maxima into)
   if (L.gather && (groups != 1 || f32))
     count_kernel<<<dim3((unsigned)(groups < 1 ? 1 : groups)), dim3(256), 0, st>>>(ga);
-  if (L.gather)
-    gather_kernel<T><<<dim3((unsigned)(c.n < 1 ? 1 : (c.n + kRows - 1) / kRows)), dim3(256), 0, st>>>(
-      ga, static_cast<const T*>(c.x));
+  if (L.gather) {
+    const int rows = groups > 1 ? kRowsMany : kRowsOnly;
+    const auto gather = groups > 1 ? &gather_kernel<T, kMany, kRowsMany> : &gather_kernel<T, kOnly, kRowsOnly>;
+    gather<<<dim3((unsigned)(c.n < 1 ? 1 : (c.n + rows - 1) / rows)), dim3(256), 0, st>>>(
+        ga, static_cast<const T*>(c.x));
+  }
   if (L.copy_w && c.n > 0)
     weights_kernel<T><<<dim3(c.C < 8192 ? (c.C + 3) / 4 : 2048), dim3(256), 0, st>>>(
         static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, c.C, u16(L.pw),
@@ -781,10 +794,10 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (e != hipSuccess) return e;
     const Finish f = {meta,  part, L.n_part, hit,     L.gather ? idx : nullptr, c.target,
                       L.few, (int32_t)c.n, c.C, c.weight, lse, a, b, c.out_loss, c.out_lse};
-    if (c.n <= 1024 && L.n_part >= 256)
-      finish_kernel<4><<<dim3((unsigned)c.n), dim3(256), 0, st>>>(f);
-    else
-      finish_kernel<1><<<dim3((unsigned)((c.n + 3) / 4)), dim3(256), 0, st>>>(f);
+    const int lanes = L.n_part <= 128 ? 16 : c.n <= 1024 && L.n_part >= 256 ? 256 : 64;
+    const auto finish =
+        lanes == 16 ? &finish_kernel<16> : lanes == 64 ? &finish_kernel<64> : &finish_kernel<256>;
+    finish<<<dim3((unsigned)((c.n * lanes + 255) / 256)), dim3(256), 0, st>>>(f);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
