@@ -96,23 +96,6 @@ __device__ __forceinline__ void join256(int32_t* x, int32_t* y, float* top) {
   *top = fmaxf(fmaxf(ts[0], ts[1]), fmaxf(ts[2], ts[3]));
 }
 
-__global__ void __launch_bounds__(256) count_kernel(const Gather g) {
-  if (blockIdx.x == 0 && threadIdx.x == 0) g.meta->S = g.meta->T = 0;
-  int32_t count = 0, none = 0;
-  float top = 0.f;
-  const int64_t first = blockIdx.x * group_rows(g.n);
-  for (int64_t r = first + threadIdx.x; r < first + group_rows(g.n); r += 256) {
-    const Row o = row_of(g, r);
-    count += o.target != -1;
-    top = fmaxf(top, finite_top(o));
-  }
-  join256(&count, &none, &top);
-  if (threadIdx.x == 0 && g.counts) {
-    g.counts[blockIdx.x] = count;
-    g.tops[blockIdx.x] = top;
-  }
-}
-
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
@@ -133,6 +116,65 @@ __device__ __forceinline__ void load4(const uint16_t* x, int d, int D, bool wide
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = d + e < D ? widen(x[d + e]) : 0.f;
+  }
+}
+
+// Of the weights' copy as planes.
+struct Weights {
+  int64_t stride;
+  int32_t D, dp, C;
+  const float* bias;  // float32 only
+  float* tops;        // [kTops] the largest finite value of some tokens each; float32 only
+  uint16_t* out;
+};
+constexpr int kTops = 1024;
+
+// A token that the bias takes out of every sum.
+__device__ __forceinline__ bool masked(const float* bias, int64_t c) {
+  return bias && bias[c] < -0x1p100f;
+}
+
+// One of kTops workgroups: the largest finite value of its rows' tokens.
+__device__ __forceinline__ void top_of(const Weights& g, const float* w, int at) {
+  const int lane = threadIdx.x & 63;
+  const bool wide = g.stride % 4 == 0 && (uintptr_t)w % 16 == 0;
+  int32_t none = 0;
+  float top = 0.f;
+  for (int64_t c = (int64_t)at * 4 + (threadIdx.x >> 6); c < g.C; c += 4 * kTops) {
+    if (masked(g.bias, c)) continue;
+#pragma unroll 4
+    for (int d = 4 * lane; d < g.D; d += 256) {
+      float v[4];
+      load4(w + c * g.stride, d, g.D, wide, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (fabsf(v[e]) < __builtin_huge_valf()) top = fmaxf(top, fabsf(v[e]));
+    }
+  }
+  join256(&none, &none, &top);
+  if (threadIdx.x == 0) g.tops[at] = top;
+}
+
+// Rows that take part; behind the groups of rows (float32) the weights' largest values.
+__global__ void __launch_bounds__(256) count_kernel(const Gather g, const Weights of, const float* w) {
+  const int groups = gridDim.x - (w ? kTops : 0);
+  if ((int)blockIdx.x >= groups) {
+    top_of(of, w, blockIdx.x - groups);
+    return;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) g.meta->T = 0;
+  int32_t count = 0, none = 0;
+  float top = 0.f;
+  const int64_t first = blockIdx.x * group_rows(g.n);
+  for (int64_t r = first + threadIdx.x; r < first + group_rows(g.n); r += 256) {
+    const Row o = row_of(g, r);
+    count += o.target != -1;
+    top = fmaxf(top, finite_top(o));
+  }
+  join256(&count, &none, &top);
+  if (threadIdx.x == 0 && g.counts) {
+    g.counts[blockIdx.x] = count;
+    g.tops[blockIdx.x] = top;
   }
 }
 
@@ -245,6 +287,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
   join256(&before, &all, &top);
 
   __shared__ int32_t places[ROWS];
+  lds_poison(places, sizeof(places));
   if (wave == 0) {
     const int64_t r = row0 + lane;
     Row o = {-1, 0.f, 0.f};
@@ -315,19 +358,40 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
 
 // The weights' planes, one wave a row.
 template <class T>
-__global__ void __launch_bounds__(256)
-    weights_kernel(const T* w, int64_t stride, int32_t D, int32_t dp, int32_t C, uint16_t* out,
-                   float* units, Meta* meta) {
-  const bool wide = rows_wide(w, stride);
-  float top = 0.f;
-  for (int64_t c = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); c < C; c += (int64_t)gridDim.x * 4) {
-    float most;
-    const float unit = row_planes<T>(w + c * stride, D, dp, wide, out + c * Elem<T>::PLANES * dp, &most);
-    // (a token without weights says nothing of the others' scale)
-    if (Elem<T>::kScaled && (threadIdx.x & 63) == 0) units[c] = most > 0.f ? unit : 0.f;
-    if (most > 0.f) top = fmaxf(top, unit);
+__global__ void __launch_bounds__(256) weights_kernel(const Weights g, const T* w, Meta* meta) {
+  const int lane = threadIdx.x & 63;
+  const bool wide = rows_wide(w, g.stride);
+  float inverse = 1.f;
+  if (Elem<T>::kScaled) {
+    int32_t none = 0;
+    float top = 0.f;
+    for (int i = threadIdx.x; i < kTops; i += 256) top = fmaxf(top, g.tops[i]);
+    join256(&none, &none, &top);
+    const float unit = unit_of(top);
+    if (blockIdx.x == 0 && threadIdx.x == 0) meta->S = unit;
+    inverse = 1.f / unit;
   }
-  if (Elem<T>::kScaled) raise(&meta->S, top);
+  for (int64_t c = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); c < g.C;
+       c += (int64_t)gridDim.x * 4) {
+    const bool hidden = Elem<T>::kScaled && masked(g.bias, c);
+#pragma unroll 4
+    for (int d = 4 * lane; d < g.dp; d += 256) {
+      float v[4];
+      load4(w + c * g.stride, d, g.D, wide, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] *= inverse;
+        // (a masked token may be larger than the others: its logits stay numbers)
+        if (hidden) v[e] = __builtin_amdgcn_fmed3f(v[e], -0x1p15f, 0x1p15f);
+      }
+      uint2 p[Elem<T>::PLANES];
+      Elem<T>::planes4(v, p);
+#pragma unroll
+      for (int s = 0; s < Elem<T>::PLANES; ++s)
+        *reinterpret_cast<uint2*>(g.out + c * Elem<T>::PLANES * g.dp +
+                                  place<Elem<T>::PLANES>(d) + s * kTurn) = p[s];
+    }
+  }
 }
 
 // float32: the planes of x_i m_i / T of the gathered rows.
@@ -394,6 +458,7 @@ template <int L>
 __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   static_assert(L == 16 || L == 64 || L == 256, "lanes of a row");
   __shared__ float lds[2][4];
+  lds_poison(lds, sizeof(lds));
   const int lane = threadIdx.x % L;
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
   if (at >= (f.idx ? f.meta->n : f.n)) return;
@@ -444,7 +509,6 @@ struct Kept {
   int32_t ldz;
   const int32_t* idx;  // rows of z, or NULL: gathered ones
   RowArgs row;
-  const float* s;
   int32_t C, cols;
   uint16_t* G;
   float* col;
@@ -458,15 +522,6 @@ __global__ void __launch_bounds__(256) kept_kernel(const Kept k) {
   const int64_t row0 = (int64_t)blockIdx.y * 64 + 16 * wave;
   const int c0 = blockIdx.x * 256 + 4 * lane;
   if ((int64_t)blockIdx.y * 64 >= up(meta.n, kStep)) return;
-  float scale[4] = {1.f, 1.f, 1.f, 1.f};
-  if (El::kScaled) {
-    const float top = 0x1p14f / top_unit(meta);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float s = k.s[min(c0 + e, k.C - 1)];
-      scale[e] = s > 0.f ? s * top : 0x1p14f;
-    }
-  }
   const float norm = El::kScaled ? 1.f : meta.inverse;
   float cs[4] = {0.f, 0.f, 0.f, 0.f};
   if (c0 < k.cols) {
@@ -485,7 +540,7 @@ __global__ void __launch_bounds__(256) kept_kernel(const Kept k) {
           if (c0 + e >= k.C) continue;
           v[e] = a * __builtin_amdgcn_exp2f((l[e] - lse) * kLog2e) - (t == e ? b : 0.f);
           cs[e] += v[e] * m;
-          if (El::kScaled) v[e] *= scale[e];
+          if (El::kScaled) v[e] *= 0x1p14f;
         }
       }
       uint2 p[El::PLANES];
@@ -498,6 +553,7 @@ __global__ void __launch_bounds__(256) kept_kernel(const Kept k) {
   }
   if (!k.col) return;
   __shared__ float4 sums[4][64];
+  lds_poison(sums, sizeof(sums));
   sums[wave][lane] = make_float4(cs[0], cs[1], cs[2], cs[3]);
   __syncthreads();
   if (wave == 0 && c0 < k.cols) {
@@ -525,7 +581,7 @@ __global__ void __launch_bounds__(256)
     if (from >= 0) {
       const float* p = g.acc + from * g.lda + d;
       for (int s = 0; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * g.acc_split);
-      scale = inv ? dx_scale<T>(g, meta, from) : dw_scale<T>(g, meta, (int)row);
+      scale = inv ? dx_scale<T>(g, meta, from) : dw_scale<T>(meta);
     }
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     if (from >= 0)
@@ -542,6 +598,7 @@ __global__ void __launch_bounds__(1024)
     columns_kernel(const float* col, int32_t ldg, const Meta* meta, int32_t rows, int32_t main,
                    int32_t rows_rest, T* db, int32_t n) {
   __shared__ float sums[16][64];
+  lds_poison(sums, sizeof(sums));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = blockIdx.x * 64 + lane;
   if (c >= main) rows = rows_rest;
@@ -561,6 +618,7 @@ __global__ void __launch_bounds__(1024)
 // ---- workspace
 
 constexpr int64_t kGradBytes = 256ll << 20;  // of the gradients of a piece's logits
+constexpr int64_t kMostStride = 1 << 22;      // of weights that are read where they are
 constexpr int32_t kFewRows = 64;             // that linear_few.hip takes
 
 // How a product is cut: tiles of 256 x 256, or smaller ones where those would leave CUs
@@ -620,7 +678,7 @@ struct Layout {
   Cut grad_all, w_all;         // (pieces but the last)
   Cut x;                       // ... and that which sums over them
   bool direct;                 // dx leaves its product's sums as it is
-  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, s, hit, part, px, pxm, pw, z, G, acc_x;
+  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, most, hit, part, px, pxm, pw, z, G, acc_x;
   int64_t acc_w, col, total;
 };
 
@@ -631,7 +689,9 @@ Layout plan(const Call& c) {
   const bool grads = c.dx || c.dw || c.db;
   L.np = up(c.n, kTile);
   L.dp = up(c.D, kStep);
-  L.copy_w = f32 || c.D % kStep != 0 || c.w_stride % 8 != 0 || (uintptr_t)c.w % 16 != 0;
+  // (the loads of a stage reach the 256 rows of a tile by 32-bit distances in bytes)
+  L.copy_w = f32 || c.D % kStep != 0 || c.w_stride % 8 != 0 || (uintptr_t)c.w % 16 != 0 ||
+             c.w_stride > kMostStride;
   // few rows are read where they are (16-byte aligned, of whole pieces of 16 bytes)
   const int64_t size = f32 ? 4 : 2;
   const bool read = c.D * size % 16 == 0 && c.w_stride * size % 16 == 0 &&
@@ -668,7 +728,7 @@ Layout plan(const Call& c) {
   L.lse = take(L.np * 4);
   if (f32) L.r = take(L.np * 4);
   if (f32) L.m = take(L.np * 4);
-  if (f32) L.s = take((int64_t)c.C * 4);
+  if (f32) L.most = take(kTops * 4);
   L.hit = take(L.np * 4);
   if (!c.lse) L.part = take(L.np * L.n_part * 8);
   if (L.gather) L.px = take(L.planes * L.np * L.dp * 2);
@@ -730,9 +790,15 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
                      a,      b,    lse, r, m, c.out_loss, c.out_lse,
                      c.x_stride, c.D, (int32_t)L.dp, u16(L.px),
                      L.direct ? c.dx : nullptr, c.dx_stride};
-  // (float32 gradients: it also clears what the others take maxima into)
-  if (L.gather && (groups != 1 || f32))
-    count_kernel<<<dim3((unsigned)(groups < 1 ? 1 : groups)), dim3(256), 0, st>>>(ga);
+  const Weights weights = {c.w_stride, c.D, (int32_t)L.dp, c.C,
+                           f32 ? static_cast<const float*>(c.bias) : nullptr,
+                           f32 ? flt(L.most) : nullptr, u16(L.pw)};
+  // (float32: it also clears what the others take maxima into)
+  if (L.gather && (groups != 1 || f32)) {
+    const bool tops = f32 && c.n > 0;
+    count_kernel<<<dim3((unsigned)(std::max<int64_t>(groups, 1) + (tops ? kTops : 0))), dim3(256), 0, st>>>(
+        ga, weights, tops ? static_cast<const float*>(c.w) : nullptr);
+  }
   if (L.gather) {
     const int rows = groups > 1 ? kRowsMany : kRowsOnly;
     const auto gather = groups > 1 ? &gather_kernel<T, kMany, kRowsMany> : &gather_kernel<T, kOnly, kRowsOnly>;
@@ -741,8 +807,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   }
   if (L.copy_w && c.n > 0)
     weights_kernel<T><<<dim3(c.C < 8192 ? (c.C + 3) / 4 : 2048), dim3(256), 0, st>>>(
-        static_cast<const T*>(c.w), c.w_stride, c.D, (int32_t)L.dp, c.C, u16(L.pw),
-        f32 ? flt(L.s) : nullptr, meta);
+        weights, static_cast<const T*>(c.w), meta);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
 
@@ -755,7 +820,6 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   g.bias = c.bias;
   g.C = c.C;
   g.row = {tgt, a, b, lse, r, m};
-  g.s = f32 ? flt(L.s) : nullptr;
   g.k = (int32_t)L.dp;
   g.splits = 1;
   g.Q = X;
@@ -820,7 +884,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     const Operand G = {u16(L.G), PL * L.ldg, (int32_t)L.np, n};
     float* col = c.db ? flt(L.col) : nullptr;
     if (L.kept && c.n > 0) {
-      const Kept k = {meta, flt(L.z), L.ldg, L.few ? idx : nullptr, g.row, g.s, c.C,
+      const Kept k = {meta, flt(L.z), L.ldg, L.few ? idx : nullptr, g.row, c.C,
                       (int32_t)up(c.C, kStep), u16(L.G), col};
       kept_kernel<T><<<dim3((c.C + 255) / 256, (unsigned)(L.np / 64)), dim3(256), 0, st>>>(k);
       e = hipGetLastError();

@@ -14,16 +14,18 @@
 // fourth is below 2^-24 of it. (Three bfloat16 planes hold as much but take six
 // products: a step of 2048 x 1024 features against 32,769 tokens took 3.4 ms with them.)
 // What float16 lacks is range: 2^-14 to 2^16, and absolute steps of 2^-24 below. So rows of x
-// and of w are divided by powers of two, r_i and s_c, that bring their largest value to
-// 2^14..2^15 (a value below 2^-16 of its row's largest loses precision, at most 2^-40 of
-// that; an entry of G below 2^-16 of its row's weight at most 2^-39 of that weight), and
+// are divided by powers of two r_i, and all of w by one, S, that bring their largest value
+// to 2^14..2^15. A value below 2^-16 of that largest loses precision, at most 2^-40 of it;
+// an entry of G below 2^-16 of its row's weight at most 2^-39 of that weight:
 //
-//   z_ic  = (x_i / r_i) (w_c / s_c) r_i s_c
-//   G'_ic = G_ic / m_i * s_c / S * 2^14,  m_i = max(|a_i|, |b_i|), S = max s_c
-//   dx_i  = G'_i (w / s) * m_i S 2^-14
-//   dw_c  = G'_c^T (x_i m_i / T) * T S / s_c 2^-14,  T a power of two for all rows
+//   z_ic  = (x_i / r_i) (w_c / S) r_i S
+//   G'_ic = G_ic / m_i * 2^14,  m_i = max(|a_i|, |b_i|)
+//   dx_i  = G'_i (w / S) * m_i S 2^-14
+//   dw_c  = G'_c^T (x_i m_i / T) * T 2^-14,  T a power of two for all rows
 //
-// so that a row's gradient is as exact as if it were alone, whatever the others weigh.
+// so that a row's gradient is as exact as if it were alone, whatever the others weigh. (With
+// a unit for each token G' would have to carry it too, and a token of small weights would
+// lose its gradient.) Tokens that the bias masks have no say in S, whatever they hold.
 //
 // Rows that take part (target not -1, weight not 0) are gathered first, so that the
 // others cost nothing and whatever they hold reaches no sum. Rows of the gathered
@@ -49,7 +51,8 @@ struct Meta {
   // the mean over a batch has, the target's entry p - 1 is then rounded near 1 and not
   // every row's by the same part of the weight (up to 2^-8, which no sum averages out).
   float scale, inverse;
-  uint32_t S, T;  // float32: bits of max s_c, and of the largest |x_i m_i|
+  float S;        // float32 only, as is
+  uint32_t T;     // the bits of the largest |x_i m_i|
 };
 
 // A matrix as 16-bit planes. Element (i, k), k the summed axis, lies in row i at value k,
@@ -85,7 +88,6 @@ struct Gemm {
   // statistics and gradients of the logits
   const void* bias;
   int32_t C, c0;   // tokens, and the first of P
-  const float* s;  // [C], float32 only
   RowArgs row;
   float2* part;    // [gathered row, n_part]: maximum, sum
   int32_t n_part;

@@ -37,7 +37,7 @@ struct Tiling {
   static constexpr int kOperandBytes = N * kStep * 2, kStageBytes = 2 * kOperandBytes;
   static constexpr int kStages = 512 / N;                    // 128 KB of them
   static constexpr int kSets = kStages + 1;                  // of Params
-  static constexpr int kParamBytes = 8 * N * 4, kColBytes = 4 * N * 4;
+  static constexpr int kParamBytes = 7 * N * 4, kColBytes = 4 * N * 4;
   static constexpr int kLdsBytes = kStages * kStageBytes + kSets * kParamBytes + kColBytes;
 };
 
@@ -276,30 +276,22 @@ __device__ __forceinline__ void gather16(uint2 a, uint2 b, uint2 c, uint2 d, uin
   *hi = make_uint4(x[2], y[2], x[3], y[3]);
 }
 
-// S; a token without weights has s_c = 0, which counts as S for its gradient.
-__device__ __forceinline__ float top_unit(const Meta& meta) {
-  return meta.S ? __uint_as_float(meta.S) : 1.f;
-}
-
-// What row q of a piece of dw is multiplied with.
+// What dw's sums are multiplied with.
 template <class T>
-__device__ __forceinline__ float dw_scale(const Gemm& g, const Meta& meta, int q) {
-  if (!Elem<T>::kScaled) return meta.scale;
-  const float top = top_unit(meta), s = g.s[g.c0 + q];
-  return (s > 0.f ? top / s : 1.f) * 0x1p-14f * unit_of(__uint_as_float(meta.T));
+__device__ __forceinline__ float dw_scale(const Meta& meta) {
+  return Elem<T>::kScaled ? 0x1p-14f * unit_of(__uint_as_float(meta.T)) : meta.scale;
 }
 
 // What gathered row q of dx is multiplied with.
 template <class T>
 __device__ __forceinline__ float dx_scale(const Gemm& g, const Meta& meta, int64_t q) {
-  return Elem<T>::kScaled ? g.row.m[q] * top_unit(meta) * 0x1p-14f : meta.scale;
+  return Elem<T>::kScaled ? g.row.m[q] * meta.S * 0x1p-14f : meta.scale;
 }
 
 // Per token and row of a tile, kept in LDS for the epilogue.
 template <int N>
 struct Params {
   uint32_t bias[N];  // float32, or bfloat16 in the low half
-  float s[N];
   int32_t target[N];
   float lse[N], a[N], b[N], r[N], m[N];
 };
@@ -370,7 +362,6 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
     constexpr int kPer = N / 64;
     if (wave < kPer) {
       const uint32_t c = min(g.c0 + t.p * N + 64 * wave + lane, g.C - 1), at = 256 * wave;
-      if (El::kScaled) four(g.s, c, offsetof(Params<N>, s) + at);
       if (g.bias && sizeof(T) == 4) four(g.bias, c, offsetof(Params<N>, bias) + at);
       if (g.bias && sizeof(T) == 2)
         load_lds2(to + offsetof(Params<N>, bias) + at, (const char*)g.bias, 2 * c);
@@ -424,17 +415,16 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
   f32x4 acc[FP][FQ];
   s16x8 pa[2][FP], qb[2][FQ];
   constexpr int kReadP = (TP ? 2 : 1) * FP, kReadQ = (TQ ? 2 : 1) * FQ;  // LDS reads
-  int frag_lane = lane;
   auto read_p = [&](int buf, int half) {
 #pragma unroll
     for (int i = 0; i < FP; ++i)
-      pa[half][i] = fragment<N, TP>(lds + buf * Ti::kStageBytes, wp + 16 * i, half, frag_lane);
+      pa[half][i] = fragment<N, TP>(lds + buf * Ti::kStageBytes, wp + 16 * i, half, lane);
   };
   auto read_q = [&](int buf, int half) {
 #pragma unroll
     for (int j = 0; j < FQ; ++j)
       qb[half][j] = fragment<N, TQ>(lds + buf * Ti::kStageBytes + Ti::kOperandBytes, wq + 16 * j,
-                                    half, frag_lane);
+                                    half, lane);
   };
   auto multiply = [&](int p, int q) {
 #pragma unroll
@@ -474,9 +464,6 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
     read_q(buf, 0);
     read_p(buf, 0);
     for (int s = 0; s < n_stage; ++s) {
-      // (made again in every stage: kept, the places of fragments left too few registers for
-      // two planes' products)
-      if (KIND == kStats && PL == 2 && N == 256) asm volatile("" : "+v"(frag_lane));
       // the first half's products while the second half is read ...
       read_q(buf, 1);
       read_p(buf, 1);
@@ -517,13 +504,11 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
 #pragma unroll
         for (int j = 0; j < FQ; ++j) r[j] = par.r[wq + 16 * j + lq];
 #pragma unroll
-        for (int i = 0; i < FP; ++i) {
-          const f32x4 s = *reinterpret_cast<const f32x4*>(&par.s[c_lane + 16 * i]);
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int j = 0; j < FQ; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * s[e] * r[j];
-        }
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * meta.S * r[j];
       }
       if (g.bias) {
 #pragma unroll
@@ -599,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       }
     }
     if (KIND == kLogitGrad) {
-      const float top = 0x1p14f / top_unit(meta), norm = El::kScaled ? 1.f : meta.inverse;
+      const float norm = El::kScaled ? 1.f : meta.inverse;
 #pragma unroll
       for (int j = 0; j < FQ; ++j) {
         const int at = wq + 16 * j + lq, row = q0 + at;
@@ -661,16 +646,6 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       constexpr int kF = FP < 4 ? FP : 4;
 #pragma unroll
       for (int part = 0; part < FP / kF; ++part) {
-        float to_f16[kF][4];
-        if (El::kScaled) {
-#pragma unroll
-          for (int i = 0; i < kF; ++i) {
-            const f32x4 s =
-                *reinterpret_cast<const f32x4*>(&par.s[c_lane + 64 * part + 16 * i]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) to_f16[i][e] = s[e] > 0.f ? s[e] * top : 0x1p14f;
-          }
-        }
 #pragma unroll
         for (int j = 0; j < FQ; ++j) {
           uint2 out[kF][El::PLANES];
@@ -680,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float x = acc[kF * part + i][j][e];
-              v[e] = El::kScaled ? x * to_f16[i][e] : x;
+              v[e] = El::kScaled ? x * 0x1p14f : x;
             }
             El::planes4(v, out[i]);
           }
@@ -724,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
             if (in && p0 + c_lane + 16 * i < g.lda) sums[4 * i] = acc[i][j];
           continue;
         }
-        const float scale = !in ? 0.f : KIND == kDx ? dx_scale<T>(g, meta, q) : dw_scale<T>(g, meta, q);
+        const float scale = !in ? 0.f : KIND == kDx ? dx_scale<T>(g, meta, q) : dw_scale<T>(meta);
         T* o = static_cast<T*>(g.out) + (KIND == kDx && in ? (int64_t)g.idx[q] : q) * g.ldo;
         if constexpr (sizeof(T) == 2 && FP >= 4) {
           if (wide) {

@@ -213,3 +213,12 @@ def test_captures_beside_an_eager_graph_are_refused(monkeypatch):
     linearops._mark((x, w, None))
     linearops._mark((x, w, None))  # further calls of one capture
     del loss
+
+
+def test_workspace_of_far_rows():
+    """Weights whose rows lie more than 2^22 values apart are copied."""
+    from paper_2608_21343_amd import capi
+    f = capi.LIB.tb_linear_xent_workspace_bytes
+    for grads in (0, 7):
+        near, far = (f(1, 1000, 640, 8193, P, stride, grads, 0) for stride in (1 << 22, (1 << 22) + 8))
+        assert 8193 * 640 * 2 <= far - near <= 8193 * 640 * 2 + 256
