@@ -29,6 +29,7 @@ struct Gather {
   uint16_t* out;
   void* dx;  // rows that are left out get 0 here; or NULL
   int64_t dx_stride;
+  int32_t blocks;  // workgroups that gather
 };
 
 // Rows of a count, in 256s, and rows that a workgroup gathers. Up to 2048 rows are one
@@ -256,11 +257,56 @@ __device__ __forceinline__ bool rows_wide(const T* x, int64_t stride) {
   return stride * sizeof(T) % 16 == 0 && (uintptr_t)x % 16 == 0;
 }
 
+// One of `blocks` workgroups: the weights' planes, one wave a row.
+template <class T>
+__device__ __forceinline__ void planes_of(const Weights& g, const T* w, Meta* meta, int block,
+                                          int blocks) {
+  const int lane = threadIdx.x & 63;
+  const bool wide = rows_wide(w, g.stride);
+  float inverse = 1.f;
+  if (Elem<T>::kScaled) {
+    int32_t none = 0;
+    float top = 0.f;
+    for (int i = threadIdx.x; i < kTops; i += 256) top = fmaxf(top, g.tops[i]);
+    join256(&none, &none, &top);
+    const float unit = unit_of(top);
+    if (block == 0 && threadIdx.x == 0) meta->S = unit;
+    inverse = 1.f / unit;
+  }
+  for (int64_t c = (int64_t)block * 4 + (threadIdx.x >> 6); c < g.C;
+       c += (int64_t)blocks * 4) {
+    const bool hidden = Elem<T>::kScaled && masked(g.bias, c);
+#pragma unroll 4
+    for (int d = 4 * lane; d < g.dp; d += 256) {
+      float v[4];
+      load4(w + c * g.stride, d, g.D, wide, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] *= inverse;
+        // (a masked token may be larger than the others: its logits stay numbers)
+        if (hidden) v[e] = __builtin_amdgcn_fmed3f(v[e], -0x1p15f, 0x1p15f);
+      }
+      uint2 p[Elem<T>::PLANES];
+      Elem<T>::planes4(v, p);
+#pragma unroll
+      for (int s = 0; s < Elem<T>::PLANES; ++s)
+        *reinterpret_cast<uint2*>(g.out + c * Elem<T>::PLANES * g.dp +
+                                  place<Elem<T>::PLANES>(d) + s * kTurn) = p[s];
+    }
+  }
+}
+
 // ROWS rows: their place among those that take part, their arguments and planes.
 // The rows before them are counted again up to the group's start, and groups by
-// their counts, so that no launch has to wait for a sum over all of them.
+// their counts, so that no launch has to wait for a sum over all of them. The workgroups
+// behind those of the rows make the weights' planes, where they are copied, meanwhile.
 template <class T, int EACH, int ROWS>
-__global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x) {
+__global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x, const Weights of,
+                                                      const T* w) {
+  if ((int)blockIdx.x >= g.blocks) {
+    planes_of(of, w, g.meta, blockIdx.x - g.blocks, gridDim.x - g.blocks);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row0 = (int64_t)blockIdx.x * ROWS;
   constexpr int64_t kGroup = 256 * EACH;
@@ -320,7 +366,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
       }
     }
   }
-  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
+  if ((int)blockIdx.x == g.blocks - 1 && threadIdx.x == 0) {
     // (no further, so that rows of far smaller weights keep their place in float32)
     top = fminf(fmaxf(top, 0x1p-24f), 0x1p24f);
     g.meta->n = all;
@@ -348,49 +394,11 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x)
     }
   }
   if (Elem<T>::kScaled && g.grads) raise(&g.meta->T, weighty);
-  if (blockIdx.x == gridDim.x - 1) {
+  if ((int)blockIdx.x == g.blocks - 1) {
     // the zeros behind the last row
     const int64_t row = Elem<T>::PLANES * g.dp, end = up(all, kStep) * row;
     for (int64_t i = all * row + 4 * threadIdx.x; i < end; i += 1024)
       *reinterpret_cast<uint2*>(g.out + i) = make_uint2(0, 0);
-  }
-}
-
-// The weights' planes, one wave a row.
-template <class T>
-__global__ void __launch_bounds__(256) weights_kernel(const Weights g, const T* w, Meta* meta) {
-  const int lane = threadIdx.x & 63;
-  const bool wide = rows_wide(w, g.stride);
-  float inverse = 1.f;
-  if (Elem<T>::kScaled) {
-    int32_t none = 0;
-    float top = 0.f;
-    for (int i = threadIdx.x; i < kTops; i += 256) top = fmaxf(top, g.tops[i]);
-    join256(&none, &none, &top);
-    const float unit = unit_of(top);
-    if (blockIdx.x == 0 && threadIdx.x == 0) meta->S = unit;
-    inverse = 1.f / unit;
-  }
-  for (int64_t c = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); c < g.C;
-       c += (int64_t)gridDim.x * 4) {
-    const bool hidden = Elem<T>::kScaled && masked(g.bias, c);
-#pragma unroll 4
-    for (int d = 4 * lane; d < g.dp; d += 256) {
-      float v[4];
-      load4(w + c * g.stride, d, g.D, wide, v);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] *= inverse;
-        // (a masked token may be larger than the others: its logits stay numbers)
-        if (hidden) v[e] = __builtin_amdgcn_fmed3f(v[e], -0x1p15f, 0x1p15f);
-      }
-      uint2 p[Elem<T>::PLANES];
-      Elem<T>::planes4(v, p);
-#pragma unroll
-      for (int s = 0; s < Elem<T>::PLANES; ++s)
-        *reinterpret_cast<uint2*>(g.out + c * Elem<T>::PLANES * g.dp +
-                                  place<Elem<T>::PLANES>(d) + s * kTurn) = p[s];
-    }
   }
 }
 
@@ -785,11 +793,13 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   float *a = flt(L.a), *b = flt(L.b), *lse = flt(L.lse);
   float *r = f32 ? flt(L.r) : nullptr, *m = f32 ? flt(L.m) : nullptr;
   const int64_t groups = (c.n + group_rows(c.n) - 1) / group_rows(c.n);
+  const int rows = groups > 1 ? kRowsMany : kRowsOnly;
   const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse,
                      grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
                      a,      b,    lse, r, m, c.out_loss, c.out_lse,
                      c.x_stride, c.D, (int32_t)L.dp, u16(L.px),
-                     L.direct ? c.dx : nullptr, c.dx_stride};
+                     L.direct ? c.dx : nullptr, c.dx_stride,
+                     (int32_t)std::max<int64_t>((c.n + rows - 1) / rows, 1)};
   const Weights weights = {c.w_stride, c.D, (int32_t)L.dp, c.C,
                            f32 ? static_cast<const float*>(c.bias) : nullptr,
                            f32 ? flt(L.most) : nullptr, u16(L.pw)};
@@ -800,14 +810,11 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
         ga, weights, tops ? static_cast<const float*>(c.w) : nullptr);
   }
   if (L.gather) {
-    const int rows = groups > 1 ? kRowsMany : kRowsOnly;
     const auto gather = groups > 1 ? &gather_kernel<T, kMany, kRowsMany> : &gather_kernel<T, kOnly, kRowsOnly>;
-    gather<<<dim3((unsigned)(c.n < 1 ? 1 : (c.n + rows - 1) / rows)), dim3(256), 0, st>>>(
-        ga, static_cast<const T*>(c.x));
+    const int more = !L.copy_w || c.n == 0 ? 0 : c.C < 8192 ? (c.C + 3) / 4 : 2048;
+    gather<<<dim3((unsigned)(ga.blocks + more)), dim3(256), 0, st>>>(
+        ga, static_cast<const T*>(c.x), weights, static_cast<const T*>(c.w));
   }
-  if (L.copy_w && c.n > 0)
-    weights_kernel<T><<<dim3(c.C < 8192 ? (c.C + 3) / 4 : 2048), dim3(256), 0, st>>>(
-        weights, static_cast<const T*>(c.w), meta);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
 
