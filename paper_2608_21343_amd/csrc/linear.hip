@@ -402,32 +402,42 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x,
   }
 }
 
-// float32: the planes of x_i m_i / T of the gathered rows.
-__global__ void __launch_bounds__(256)
-    weighted_kernel(const float* x, int64_t stride, int32_t D, int32_t dp, const int32_t* idx,
-                    const float* m, const Meta* meta, uint16_t* out) {
+// float32: the planes of x_i m_i / T of the gathered rows, by some workgroups behind those of
+// the rows' statistics or by a launch of its own.
+struct Weighted {
+  const float* x;
+  int64_t stride;
+  int32_t D, dp;
+  const int32_t* idx;
+  const float* m;
+  uint16_t* out;
+  int32_t blocks;
+};
+__device__ __forceinline__ void weighted_of(const Weighted& g, const Meta& meta, int block) {
   const int lane = threadIdx.x & 63;
-  const bool wide = rows_wide(x, stride);
-  const int64_t have = meta->n, rows = up(have, kStep);
-  const float inverse = 1.f / unit_of(__uint_as_float(meta->T));
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows;
-       i += (int64_t)gridDim.x * 4) {
-    const float* from = i < have ? x + (int64_t)idx[i] * stride : nullptr;
-    const float scale = i < have ? m[i] : 0.f;
-    for (int d = 4 * lane; d < dp; d += 256) {
+  const bool wide = rows_wide(g.x, g.stride);
+  const int64_t have = meta.n, rows = up(have, kStep);
+  const float inverse = 1.f / unit_of(__uint_as_float(meta.T));
+  for (int64_t i = (int64_t)block * 4 + (threadIdx.x >> 6); i < rows; i += (int64_t)g.blocks * 4) {
+    const float* from = i < have ? g.x + (int64_t)g.idx[i] * g.stride : nullptr;
+    const float scale = i < have ? g.m[i] : 0.f;
+    for (int d = 4 * lane; d < g.dp; d += 256) {
       float v[4] = {0.f, 0.f, 0.f, 0.f};
-      if (from && d < D) {
-        load4(from, d, D, wide, v);
+      if (from && d < g.D) {
+        load4(from, d, g.D, wide, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = v[e] * scale * inverse;
       }
       uint2 p[2];
       Elem<float>::planes4(v, p);
-      uint16_t* to = out + i * 2 * dp + place<2>(d);
+      uint16_t* to = g.out + i * 2 * g.dp + place<2>(d);
       *reinterpret_cast<uint2*>(to) = p[0];
       *reinterpret_cast<uint2*>(to + kTurn) = p[1];
     }
   }
+}
+__global__ void __launch_bounds__(256) weighted_kernel(const Weighted g, const Meta* meta) {
+  weighted_of(g, *meta, blockIdx.x);
 }
 
 // ---- what joins the tiles
@@ -463,12 +473,16 @@ __device__ __forceinline__ float over(float v, float* lds) {
 // L lanes a row: 16 for up to 128 parts (32,768 rows of 66: 7 us instead of 13 with a
 // wave each), or the workgroup for few rows with many parts.
 template <int L>
-__global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
+__global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Weighted g) {
+  if ((int)blockIdx.x < g.blocks) {
+    weighted_of(g, *f.meta, blockIdx.x);
+    return;
+  }
   static_assert(L == 16 || L == 64 || L == 256, "lanes of a row");
   __shared__ float lds[2][4];
   lds_poison(lds, sizeof(lds));
   const int lane = threadIdx.x % L;
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+  const int64_t at = ((int64_t)(blockIdx.x - g.blocks) * 256 + threadIdx.x) / L;
   if (at >= (f.idx ? f.meta->n : f.n)) return;
   const int64_t row = f.idx ? f.idx[at] : at, from = f.by_row ? row : at;
   const int32_t t = f.target[row];
@@ -508,8 +522,8 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f) {
   }
 }
 
-// The gradients of logits that are kept: 64 gathered rows by 256 tokens a workgroup, 16
-// rows a wave. The rows behind the last one, up to a multiple of kStep, get zeros, and so
+// The gradients of logits that are kept: ROWS gathered rows by 256 tokens a workgroup, a
+// quarter of them a wave. The rows behind the last one, up to a multiple of kStep, get zeros, and so
 // do the tokens.
 struct Kept {
   const Meta* meta;
@@ -522,19 +536,19 @@ struct Kept {
   float* col;
 };
 
-template <class T>
+template <class T, int ROWS>
 __global__ void __launch_bounds__(256) kept_kernel(const Kept k) {
   typedef Elem<T> El;
   const Meta meta = *k.meta;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row0 = (int64_t)blockIdx.y * 64 + 16 * wave;
+  const int64_t row0 = (int64_t)blockIdx.y * ROWS + ROWS / 4 * wave;
   const int c0 = blockIdx.x * 256 + 4 * lane;
-  if ((int64_t)blockIdx.y * 64 >= up(meta.n, kStep)) return;
+  if ((int64_t)blockIdx.y * ROWS >= up(meta.n, kStep)) return;
   const float norm = El::kScaled ? 1.f : meta.inverse;
   float cs[4] = {0.f, 0.f, 0.f, 0.f};
   if (c0 < k.cols) {
 #pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < ROWS / 4; ++i) {
       const int64_t at = row0 + i;
       float v[4] = {0.f, 0.f, 0.f, 0.f};
       if (at < meta.n) {
@@ -627,7 +641,12 @@ __global__ void __launch_bounds__(1024)
 
 constexpr int64_t kGradBytes = 256ll << 20;  // of the gradients of a piece's logits
 constexpr int64_t kMostStride = 1 << 22;      // of weights that are read where they are
-constexpr int32_t kFewRows = 64;             // that linear_few.hip takes
+// Rows that linear_few.hip takes. It reads the weights once for 16 bfloat16 rows and is bound
+// by that (16 rows of 1024 against 131,073 tokens 54 us, tiles 86; 32 rows 62 and 85; 64
+// rows 89 and 84), float32 ones without a copy of the weights (64 rows against 131,073
+// tokens 218 us, tiles with the copy 475). With gradients the copy is made in any case
+// (float32, 32,769 tokens: 16 rows 236 us, tiles 247; 64 rows 320 and 249).
+int32_t few_rows(bool f32, bool grads) { return grads ? 16 : f32 ? 64 : 32; }
 
 // How a product is cut: tiles of 256 x 256, or smaller ones where those would leave CUs
 // idle, and parts of the summed axis where that still leaves them idle. The costs are in
@@ -685,6 +704,7 @@ struct Layout {
   Strips stats, grad, w;       // of the products with tokens of their own ...
   Cut grad_all, w_all;         // (pieces but the last)
   Cut x;                       // ... and that which sums over them
+  int32_t kept_rows;           // of a workgroup that makes gradients of kept logits
   bool direct;                 // dx leaves its product's sums as it is
   int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, most, hit, part, px, pxm, pw, z, G, acc_x;
   int64_t acc_w, col, total;
@@ -705,7 +725,7 @@ Layout plan(const Call& c) {
   const bool read = c.D * size % 16 == 0 && c.w_stride * size % 16 == 0 &&
                     (uintptr_t)c.w % 16 == 0 && c.x_stride * size % 16 == 0 &&
                     (uintptr_t)c.x % 16 == 0;
-  L.few = !c.lse && read && c.n <= kFewRows;
+  L.few = !c.lse && read && c.n <= few_rows(f32, grads);
   // (the loss of few rows needs no copies)
   L.gather = grads || !L.few;
   L.copy_w = L.copy_w && L.gather;
@@ -754,6 +774,9 @@ Layout plan(const Call& c) {
     L.ldg = (int32_t)up(most, kTile);
     L.kept = !c.lse && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
     L.G = take(L.planes * L.np * L.ldg * 2);
+    // (by 16 rows where 64 would leave CUs idle: a step of 1511 bfloat16 rows of 336 against 612
+    // tokens 51 us by 64, 47 by 16; of 16,000 float32 rows of 512 against 1025 288 and 300)
+    L.kept_rows = up(c.n, 64) / 64 * ((c.C + 255) / 256) < 1024 ? 16 : 64;
     if (L.kept) L.z = take(L.np * L.ldg * 4);
     if (c.dx) {
       L.x = cut(L.dp, c.n, up(most, kStep) / kStep, stages, true);
@@ -769,7 +792,7 @@ Layout plan(const Call& c) {
     }
     L.grad = strips(last, c.n, L.dp / kStep, stages, false);
     L.grad_all = cut(L.piece, c.n, L.dp / kStep, stages, false);
-    if (c.db) L.col = take(L.np / 64 * L.ldg * 4);
+    if (c.db) L.col = take(L.np / (L.kept ? L.kept_rows : 64) * L.ldg * 4);
   }
   L.total = at;
   return L;
@@ -839,6 +862,12 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     hipError_t r = at(0, std::min(s.main, tokens), s.cut[0]);
     return r != hipSuccess || s.main >= tokens ? r : at(s.main, tokens - s.main, s.cut[1]);
   };
+  Weighted weighted = {};
+  if constexpr (f32) {
+    if (c.dw && c.n > 0)
+      weighted = {static_cast<const float*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, u16(L.pxm),
+                  (int32_t)(c.n < 8192 ? (c.n + 3) / 4 : 2048)};
+  }
   if (!c.lse && c.n > 0) {
     float2* part = reinterpret_cast<float2*>(ws + L.part);
     float *hit = flt(L.hit), *z = L.kept ? flt(L.z) : nullptr;
@@ -868,22 +897,20 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     const int lanes = L.n_part <= 128 ? 16 : c.n <= 1024 && L.n_part >= 256 ? 256 : 64;
     const auto finish =
         lanes == 16 ? &finish_kernel<16> : lanes == 64 ? &finish_kernel<64> : &finish_kernel<256>;
-    finish<<<dim3((unsigned)((c.n * lanes + 255) / 256)), dim3(256), 0, st>>>(f);
+    finish<<<dim3((unsigned)(weighted.blocks + (c.n * lanes + 255) / 256)), dim3(256), 0, st>>>(
+        f, weighted);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (!grads) return hipSuccess;
 
-  Operand XM = X;  // of dw
-  if constexpr (f32) {
-    if (c.dw && c.n > 0) {
-      XM.p = u16(L.pxm);
-      weighted_kernel<<<dim3(c.n < 8192 ? (c.n + 3) / 4 : 2048), dim3(256), 0, st>>>(
-          static_cast<const T*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, meta, u16(L.pxm));
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
+  if (c.lse && weighted.blocks) {
+    weighted_kernel<<<dim3(weighted.blocks), dim3(256), 0, st>>>(weighted, meta);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
+  Operand XM = X;  // of dw
+  if (f32) XM.p = u16(L.pxm);
   for (int32_t piece = 0; piece < L.pieces; ++piece) {
     const bool last = piece + 1 == L.pieces;
     const int32_t c0 = piece * L.piece, n = last ? c.C - c0 : L.piece;
@@ -893,7 +920,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (L.kept && c.n > 0) {
       const Kept k = {meta, flt(L.z), L.ldg, L.few ? idx : nullptr, g.row, c.C,
                       (int32_t)up(c.C, kStep), u16(L.G), col};
-      kept_kernel<T><<<dim3((c.C + 255) / 256, (unsigned)(L.np / 64)), dim3(256), 0, st>>>(k);
+      const auto make = L.kept_rows == 16 ? &kept_kernel<T, 16> : &kept_kernel<T, 64>;
+      make<<<dim3((c.C + 255) / 256, (unsigned)(up(c.n, 64) / L.kept_rows)), dim3(256), 0, st>>>(k);
       e = hipGetLastError();
     } else {
       e = over(grad, n, [&](int32_t first, int32_t n, const Cut& cut) {
@@ -912,8 +940,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     if (e != hipSuccess) return e;
     if (c.db) {
       columns_kernel<T><<<dim3((n + 63) / 64), dim3(1024), 0, st>>>(
-          col, L.ldg, meta, L.kept ? 64 : grad.cut[0].tile, grad.main,
-          L.kept ? 64 : grad.cut[1].tile, static_cast<T*>(c.db) + c0, n);
+          col, L.ldg, meta, L.kept ? L.kept_rows : grad.cut[0].tile, grad.main,
+          L.kept ? L.kept_rows : grad.cut[1].tile, static_cast<T*>(c.db) + c0, n);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

@@ -1,6 +1,6 @@
 // Logits of few rows: their statistics, and where they are kept the logits themselves.
 //
-// With up to 64 rows a layer's weights are read once and hardly used again, so the time
+// With up to 64 rows (32 in bfloat16) a layer's weights are read once and hardly used again, so the time
 // is that of reading them. A wave takes all rows of a group of 64 and its share of the
 // tokens, 64 at a time, straight from memory into the operands of the matrix
 // instructions: no LDS, no barriers, and every wave keeps several steps of loads in
@@ -202,11 +202,15 @@ void launch_few(const Few& f, hipStream_t st) {
       <<<dim3((f.parts + 3) / 4, (f.n + 16 * NQ - 1) / (16 * NQ)), dim3(256), 0, st>>>(f);
 }
 
+// More than 32 float32 rows: all of a wave with many tokens, or by 32 of twice as many waves
+// (64 rows of 1024 against 131,073 tokens 217 us and 241; of 512 against 4097 27 and 19).
 template <class T, int kP>
 void few_t(const Few& f, hipStream_t st) {
-  if (f.n <= 16) launch_few<T, kP, 1>(f, st);
-  else if (f.n <= 32) launch_few<T, kP, 2>(f, st);
-  else launch_few<T, kP, 4>(f, st);
+  if (f.n <= 16) return launch_few<T, kP, 1>(f, st);
+  if constexpr (sizeof(T) == 4 && kP == 4) {
+    if (f.n > 32) return launch_few<T, kP, 4>(f, st);
+  }
+  launch_few<T, kP, 2>(f, st);
 }
 
 }  // namespace
