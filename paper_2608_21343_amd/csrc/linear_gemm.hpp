@@ -288,6 +288,19 @@ __device__ __forceinline__ float dx_scale(const Gemm& g, const Meta& meta, int64
   return Elem<T>::kScaled ? g.row.m[q] * meta.S * 0x1p-14f : meta.scale;
 }
 
+// exp(z - base) = 2^(z log2(e) + by) (1 + off): the exponent by one operation, and the
+// rounding of `by`, the same for all z, once for their sum. far: the product with log2(e)
+// might overflow, so base has to be taken from z before (by and off are 0).
+struct Shift {
+  float by, off;
+  bool far;
+};
+__device__ __forceinline__ Shift shift_of(float base) {
+  const bool far = fabsf(base) > 0x1p100f;
+  const float by = far ? 0.f : -base * kLog2e;
+  return {by, far ? 0.f : __builtin_fmaf(-base, kLog2e, -by) * kLn2, far};
+}
+
 // Per token and row of a tile, kept in LDS for the epilogue.
 template <int N>
 struct Params {
@@ -457,10 +470,18 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
     const int p0 = tile.p * N, q0 = tile.q * N, n_stage = tile.steps;
     const Params<N>& par = params[turn];
     turn = turn == kSets - 1 ? 0 : turn + 1;
+    // (sums of bfloat16 operands begin at the bias)
+    constexpr bool kFromBias = kLogits && !El::kScaled;
 #pragma unroll
-    for (int i = 0; i < FP; ++i)
+    for (int i = 0; i < FP; ++i) {
+      f32x4 from = {0.f, 0.f, 0.f, 0.f};
+      if (kFromBias && g.bias) {
+        const uint4 b = *reinterpret_cast<const uint4*>(&par.bias[wp + 16 * i + 4 * (lane >> 4)]);
+        from = f32x4{low16(b.x), low16(b.y), low16(b.z), low16(b.w)};
+      }
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < FQ; ++j) acc[i][j] = from;
+    }
     read_q(buf, 0);
     read_p(buf, 0);
     for (int s = 0; s < n_stage; ++s) {
@@ -510,17 +531,12 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * meta.S * r[j];
       }
-      if (g.bias) {
+      if (El::kScaled && g.bias) {
 #pragma unroll
         for (int i = 0; i < FP; ++i) {
-          const uint4 b = *reinterpret_cast<const uint4*>(&par.bias[c_lane + 16 * i]);
-          const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+          const f32x4 b = *reinterpret_cast<const f32x4*>(&par.bias[c_lane + 16 * i]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float add = __uint_as_float(sizeof(T) == 4 ? w[e] : w[e] << 16);
-#pragma unroll
-            for (int j = 0; j < FQ; ++j) acc[i][j][e] += add;
-          }
+          for (int j = 0; j < FQ; ++j) acc[i][j] += b;
         }
       }
       if (g.c0 + p0 + N > g.C) {
@@ -570,13 +586,21 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
         m = fmaxf(m, __shfl_xor(m, 32));
         // (a NaN among the logits is no maximum, but it is in the sum)
         const float base = m == -__builtin_huge_valf() ? 0.f : m;
+        const Shift shift = shift_of(base);
+        if (__any(shift.far)) {
+#pragma unroll
+          for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] -= shift.far ? base : 0.f;
+        }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            sum[e] += __builtin_amdgcn_exp2f((acc[i][j][e] - base) * kLog2e);
+            sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, shift.by));
         float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        all = __builtin_fmaf(all, shift.off, all);
         all += __shfl_xor(all, 16);
         all += __shfl_xor(all, 32);
         if (row < meta.n && of_lane < 16)
@@ -589,17 +613,28 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       for (int j = 0; j < FQ; ++j) {
         const int at = wq + 16 * j + lq, row = q0 + at;
         const bool in = row < meta.n;
-        const float lse = par.lse[at], shift = -lse * kLog2e, a = par.a[at] * norm;
+        const float lse = par.lse[at];
+        float a = par.a[at] * norm;
+        Shift shift = {};
+        if constexpr (!El::kScaled) {  // (float32 has no registers left for it)
+          shift = shift_of(lse);
+          a = __builtin_fmaf(a, shift.off, a);
+          if (__any(shift.far)) {
+#pragma unroll
+            for (int i = 0; i < FP; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j][e] -= shift.far ? lse : 0.f;
+          }
+        }
         const int t = in ? par.target[at] - (g.c0 + p0 + c_lane) : -1;
         // G over the logits
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            // float32: the difference first, whose rounding is small where p is not
             const float z = acc[i][j][e];
             const float p = __builtin_amdgcn_exp2f(El::kScaled ? (z - lse) * kLog2e
-                                                               : __builtin_fmaf(z, kLog2e, shift));
+                                                               : __builtin_fmaf(z, kLog2e, shift.by));
             acc[i][j][e] = in ? a * p : 0.f;
           }
         if (__ballot(t >= 0 && t < N / 2 && (t & 12) == 0)) {

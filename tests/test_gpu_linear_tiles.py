@@ -122,6 +122,26 @@ def test_masked_tokens_hold_anything_finite(mask, n, dtype):
         check_all(step(c), want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [9, 40, 300])
+def test_every_token_masked_by_a_number(n, dtype):
+    """Logits that are all the same number near the type's lowest: loss log(V+1), and
+    gradients without a NaN."""
+    D, C = 96, 700
+    c = R.case(n, D, C, dtype, 8, device="cuda")
+    c["x"][:] = 0.0
+    c["bias"][:] = -3.0e38
+    want = math.log(C)
+    got = step(c)
+    two = grad(c, got["lse"], torch.ones(n, device="cuda"), None)
+    # 700 exponentials of 0 are exact, and so is their sum; the logarithm to two steps
+    assert float((got["loss"].double() - want).abs().max()) <= 4 * 2.0 ** -24 * want
+    assert bool((got["lse"].double() + 3.0e38 <= 2.0 ** -8 * 3.0e38).all())
+    for out in (got, two):
+        for name in ("dx", "dw", "db"):
+            assert bool(torch.isfinite(out[name]).all()), name
+
+
 def test_two_calls_at_once():
     cases = [R.case(n, 256, C, dtype, 2, device="cuda", gaps=True)
              for n, C, dtype in ((900, 4097, BF16), (700, 3001, F32))]
