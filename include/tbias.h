@@ -656,12 +656,18 @@ int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus
  * probability 0; a row without any other has lse -inf, loss +inf and gradient 0. A row
  * whose logits hold a NaN or +inf has NaN lse, loss and gradients.
  *
- * Rounding. Sums are float32. bfloat16 products are exact; the products of float32
- * operands are those of three bfloat16 planes each, to 2^-25 of the product (values
- * of 3.39e38 and more count as infinite). The gradients of the logits are rounded once
- * to dtype's precision, as they would be if they were kept (db is the sum of the
- * unrounded ones); the results are rounded once to dtype. Results are the same bits
- * for the same arguments.
+ * Rounding. Sums are float32. bfloat16 products are exact. A float32 operand is taken
+ * as the sum of two float16 values in units of a power of two: up to 2^-23 of it is lost, or
+ * 2^-39 of the largest value that shares its unit where that is more, which is the
+ * largest of its row of x, of all of w, and for dw of all rows of x times their largest
+ * |a_i|, |b_i|; products are exact to 2^-21. (Logits of few rows take three bfloat16
+ * values, 2^-25, without units.) So values 2^16 below the largest of their unit lose
+ * precision. A token whose bias is below -2^100 has no say in the unit, and counts as at
+ * most twice the largest of the others. The gradients of the logits are rounded once to
+ * dtype's precision, as they would be if they were kept (bfloat16: 2^-8 of each; float32:
+ * 2^-23 of each, or 2^-39 of the row's largest |a_i|, |b_i|); db is the sum of the unrounded
+ * ones. The results are rounded once to dtype. Results are the same bits for the same
+ * arguments; a loss alone may differ in its last bits from one that comes with gradients.
  *
  * tb_linear_xent_workspace_bytes - for a call with these arguments; grads: sum of 1
  *   (dx), 2 (dw) and 4 (db), 0 for the loss alone; with_lse: 1 for

@@ -11,6 +11,15 @@
 // that keeps its mean, from 16 bits that a hash makes of seed, step, tensor and place.
 // A second moment above 0 never becomes 0, which would make the next step a large one.
 //
+// What bounds it, in 235 million bfloat16 values of 290 tensors: with 32-bit states and copies
+// its bytes (28 a value, 1.35 ms, 4.9 TB/s; a large copy runs at 5.3), with 8-bit states (10 a
+// value) its instructions (0.62 ms, 3.8 TB/s), reading the moments their bytes (0.45 ms for 10
+// a value, 5.2 TB/s). Up to 52 tensors go into a launch, since their records fit its arguments, so that a
+// table need not be copied to the device first, which a captured graph could not do again.
+// A lane takes 8 values at a time, 16-byte loads at any address, the next ones in flight
+// while it works: without that 1.40 ms and 0.78. Loads and stores that leave the caches
+// alone were slower (1.66 ms; 5 million float32 values 38 us instead of 25).
+//
 // The moments' products and sums are rounded one by one, in float32, as the interface
 // states them, so the codes are the same wherever the same arithmetic runs.
 #include "adamw.hpp"

@@ -1,15 +1,15 @@
 // Logits of few rows: their statistics, and where they are kept the logits themselves.
 //
-// With up to 64 rows (32 in bfloat16) a layer's weights are read once and hardly used again, so the time
-// is that of reading them. A wave takes all rows of a group of 64 and its share of the
-// tokens, 64 at a time, straight from memory into the operands of the matrix
+// With up to 64 rows (32 in bfloat16) a layer's weights are read once and hardly used
+// again, so the time is that of reading them. A wave takes up to 16, 32 or 64 rows and its
+// share of the tokens, 64 at a time, straight from memory into the operands of the matrix
 // instructions: no LDS, no barriers, and every wave keeps several steps of loads in
 // flight. Waves begin at different places of their rows: in step they would ask for the
 // same part of every row, which the same memory channels hold (8 rows of 1024 bfloat16
-// against 131,073 tokens 57 us, 52 so; 268 MB at 5.2 TB/s). Tokens are dealt out in
-// units of 16: tiles of 256 took three rounds of the card's CUs for little more than two
-// rounds' worth. Layers of few tokens have a wave for each 16 of them, with up to eight
-// steps of loads in flight.
+// against 131,073 tokens 57 us, 45 so; 268 MB at 6.0 TB/s, 4.9 with nothing of them in a
+// cache). Tokens are dealt out in units of 16: tiles of 256 took three rounds of the card's
+// CUs for little more than two rounds' worth. Layers of few tokens have a wave for each 16 of
+// them, with up to eight steps of loads in flight.
 //
 // float32 operands are taken apart into three bfloat16 planes in registers (x, the
 // rounding of what x leaves, and once more): six products of them, to 2^-26 of the

@@ -1,7 +1,19 @@
-// The products of the linear cross entropy: tiles of 256 x 256 by eight waves of
-// 128 x 64, sums of 16 x 16 x 32 matrix instructions in registers, operands staged
-// through LDS by asynchronous 16-byte loads, two stages of 64 values of the summed
-// axis.
+// The products of the linear cross entropy: tiles of N x N (256, 128 or 64) by eight waves
+// of N / 2 x N / 4, sums of 16 x 16 x 32 matrix instructions in registers, operands staged
+// through LDS by asynchronous 16-byte loads, 512 / N stages of 64 values of the summed axis
+// (two planes: of 32).
+//
+// What bounds them is the matrix instructions. In tiles of 256 they are busy two thirds of
+// the time of a long sum (rocprofv3: 0.64 to 0.67 of all pipes' cycles, no bank conflicts in
+// LDS), at clocks that the card lowers to 1.6 to 1.8 GHz under such work. bfloat16 products
+// for 4096 rows of 2048 against 131,073 tokens: statistics 1.65 ms (1330 TFLOP/s; a library
+// product of that size 1380), dx 1.82, dw 1.67, gradients of the logits 1.87; float32 ones of
+// 2048 x 1024 against 32,769 run at 1190 to 1440 TFLOP/s of planes. The statistics of a short
+// sum (640 values) spend nearly half of their time in the exponentials: 32,768 rows
+// against 8193 tokens 320 us, 970 TFLOP/s.
+//
+// The sums of a tile of 256 take half of a wave's registers, so a CU holds one workgroup; in
+// tiles of 128 the LDS reads of the fragments take as long as the products.
 //
 // An operand whose rows run along the summed axis lies in LDS as [row, 64] with its
 // 16-byte pieces exchanged by row, so that the 16 rows of a fragment's read cover
@@ -128,7 +140,7 @@ __device__ __forceinline__ const char* uniform(const void* p) {
 // One 16-byte load of every lane, straight into LDS: lane l's piece goes to `to` + 16 l.
 // In assembly, because the compiler would wait for every load in flight before each
 // transposing read (it cannot tell the two stages apart): 693 TFLOP/s of dw instead of
-// %DW%. It has no result register; land() waits for it.
+// 880. It has no result register; land() waits for it.
 __device__ __forceinline__ void load_lds(uint32_t to, const char* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :

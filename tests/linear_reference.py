@@ -70,8 +70,9 @@ def case(n, D, C, dtype, seed=0, bias=True, weighted=False, gaps=False, device="
 def expected(c, d_loss=None, d_lse=None):
     """{name: (value, tolerance)} of a case's outputs.
 
-    Sums of k float32 products in any order are off by at most (k + 4) u of the sum of
-    their sizes (u = 2^-24; 4 for the planes of float32 operands and the bias). A logit
+    Sums of k float32 products in any order are off by at most (k + 9) u of the sum of
+    their sizes (u = 2^-24; 8 for the planes of float32 operands, which lose up to 2^-23
+    of each factor and 2^-22 of the product, and 1 for the bias). A logit
     that is off by e makes exp(z - lse) off by a factor of at most 1 + 4 e, and
     exponential, its argument and lse by another 2^-20 (arguments below 2^7 in units of
     log 2, half a step each). G is rounded to the type of the operands; the outputs
@@ -93,7 +94,7 @@ def expected(c, d_loss=None, d_lse=None):
     big = x.abs() @ w.abs().t()
     if bias is not None:
         big = big + torch.where(bias > -1e30, bias.abs(), 0.0)
-    ez = (D + 4) * u * big.amax(1)
+    ez = (D + 9) * u * big.amax(1)
     ok = (c["target"] >= 0) & (c["target"] < C)
     at = torch.where(ok, c["target"], 0).long()[:, None]
     hit = torch.gather(z, 1, at)[:, 0]
