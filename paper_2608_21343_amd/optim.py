@@ -18,8 +18,8 @@ class AdamW(torch.optim.Optimizer):
     rounded so that means are kept (the roundings follow from ``seed``).
     ``master`` keeps a float32 copy of bfloat16 parameters, which the steps
     update. ``capturable``: the number of the step lives on the device, so that a
-    captured graph of ``step`` can be replayed as a training loop; every
-    parameter then needs a gradient in every step, and a learning rate that
+    captured graph of ``step`` can be replayed as a training loop, once a first
+    step has made the states; every parameter then needs a gradient in every step, and a learning rate that
     changes is a device tensor of one float32. ``step(grad_scale=...)`` takes a device
     tensor of one float32 that multiplies the gradients, as clipping needs it."""
 
@@ -46,6 +46,9 @@ class AdamW(torch.optim.Optimizer):
         s = self.state[p]
         if s:
             return s
+        if torch.cuda.is_current_stream_capturing():
+            # (its replays would begin with empty states every time)
+            raise RuntimeError("the first step makes the states: run it before the capture")
         if group["state_bits"] == 8:
             units = (p.numel() + 255) // 256
             for name in ("exp_avg", "exp_avg_sq"):

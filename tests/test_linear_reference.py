@@ -215,6 +215,17 @@ def test_captures_beside_an_eager_graph_are_refused(monkeypatch):
     del loss
 
 
+def test_first_steps_are_not_captured(monkeypatch):
+    """States made inside a capture would be empty again in every replay."""
+    from paper_2608_21343_amd import optim
+    p = torch.zeros(3, requires_grad=True)
+    p.grad = torch.ones(3)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    for capturable in (False, True):
+        with pytest.raises(RuntimeError, match="before the capture"):
+            optim.AdamW([p], capturable=capturable).step()
+
+
 def test_workspace_of_far_rows():
     """Weights whose rows lie more than 2^22 values apart are copied."""
     from paper_2608_21343_amd import capi
