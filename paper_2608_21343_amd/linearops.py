@@ -44,15 +44,16 @@ def _args(x, w, target, bias, weight):
             None if weight is None else weight.contiguous())
 
 
-def _mark(leaves) -> None:
+def _mark(node) -> None:
     """A backward pass that is captured while a graph of an eager pass over the same
     leaves is alive would wait, inside the capture, for the stream of that pass
     (torch gives a leaf's accumulation the stream of its first use), and end the
-    process when the capture ends: such a call is refused here."""
+    process when the capture ends: such a call is refused here. The marks are on
+    the accumulations that follow ``node``, which live as long as a graph of theirs."""
     capturing = torch.cuda.is_current_stream_capturing()
-    for t in leaves:
-        if t is not None and t.requires_grad and t.is_leaf:
-            marks = torch.autograd.graph.get_gradient_edge(t).node.metadata
+    for leaf, _ in node.next_functions:
+        if leaf is not None and leaf.name() == "torch::autograd::AccumulateGrad":
+            marks = leaf.metadata
             if not capturing:
                 marks["tbias_eager"] = True
             elif marks.get("tbias_eager"):
@@ -98,8 +99,8 @@ def linear_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
     capture while the graph of an eager call with the same leaves is alive."""
     _constant(weight, "weight")
     out = _LinearXent.apply(x, w, target, bias, weight)
-    if out[0].requires_grad:  # (the graph keeps the leaves' nodes, and their marks)
-        _mark((x, w, bias))
+    if out[0].requires_grad:
+        _mark(out[0].grad_fn)
     return LinearLoss(*out)
 
 

@@ -203,16 +203,17 @@ def test_captures_beside_an_eager_graph_are_refused(monkeypatch):
     x, w = torch.zeros(3, requires_grad=True), torch.zeros(3)
     capturing = [False]
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
-    loss = (x * w).sum()
-    linearops._mark((x, w, None))
+    y = x * w
+    linearops._mark(y.grad_fn)
     capturing[0] = True
+    again = x * w
     with pytest.raises(RuntimeError, match="drop its losses"):
-        linearops._mark((x, w, None))
-    del loss
-    loss = (x * w).sum()
-    linearops._mark((x, w, None))
-    linearops._mark((x, w, None))  # further calls of one capture
-    del loss
+        linearops._mark(again.grad_fn)
+    del y, again
+    y = x * w
+    linearops._mark(y.grad_fn)
+    linearops._mark((x * w).grad_fn)  # further calls of one capture
+    del y
 
 
 def test_first_steps_are_not_captured(monkeypatch):
