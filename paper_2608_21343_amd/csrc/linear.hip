@@ -282,9 +282,10 @@ __device__ __forceinline__ void planes_of(const Weights& g, const T* w, Meta* me
       load4(w + c * g.stride, d, g.D, wide, v);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        v[e] *= inverse;
         // (a masked token may be larger than the others: its logits stay numbers)
-        if (hidden) v[e] = __builtin_amdgcn_fmed3f(v[e], -0x1p15f, 0x1p15f);
+        const bool bound = hidden && fabsf(v[e]) < __builtin_huge_valf();
+        v[e] *= inverse;
+        if (bound) v[e] = __builtin_amdgcn_fmed3f(v[e], -0x1p15f, 0x1p15f);
       }
       uint2 p[Elem<T>::PLANES];
       Elem<T>::planes4(v, p);

@@ -124,6 +124,23 @@ def test_masked_tokens_hold_anything_finite(mask, n, dtype):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n", [9, 40, 300])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_masked_tokens_that_are_not_finite(value, n, dtype):
+    """A mask does not hide a NaN: -inf and it, or an infinity of the other sign, are NaN."""
+    c = R.case(n, 96, 700, dtype, 8, device="cuda")
+    c["bias"][7] = -math.inf
+    c["target"][c["target"] == 7] = 1
+    c["w"][7] = value
+    z = c["x"].double() @ c["w"].double().t() + c["bias"].double()
+    bad = torch.isnan(z).any(1)
+    assert bool(bad.any())
+    for got in (step(c), step(c, ())):
+        assert bool((torch.isnan(got["loss"]) == bad).all())
+        assert bool((torch.isnan(got["lse"]) == bad).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [9, 40, 300])
 def test_every_token_masked_by_a_number(n, dtype):
     """Logits that are all the same number near the type's lowest: loss log(V+1), and
     gradients without a NaN."""
