@@ -93,11 +93,15 @@ __global__ void __launch_bounds__(256) few_kernel(const Few f) {
 #pragma unroll
     for (int p = 0; p < kP; ++p)
       w[p] = static_cast<const T*>(f.w) + min(c0 + 16 * p + lq, end - 1) * f.w_stride + lk;
-    f32x4 acc[kP][NQ];
+    // (the products of lower planes, or every other step's of up to 16 bfloat16 rows, on their
+    // own: in one sum all would round at the size of the whole. Losses of sums of 1536 float32
+    // values are off by 6e-7 so, by 1.5e-6 in one sum, in the same time; the second sum of more
+    // bfloat16 rows took a tenth longer, 67 us of 61, for its registers.)
+    f32x4 acc[kP][NQ], low[kP][NQ];
 #pragma unroll
     for (int p = 0; p < kP; ++p)
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) acc[p][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < NQ; ++q) acc[p][q] = low[p][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     Eight<T> a[kSets][kP], b[kSets][NQ];
     auto load = [&](int set, int step) {
       // every wave begins at another place of its rows
@@ -121,13 +125,14 @@ __global__ void __launch_bounds__(256) few_kernel(const Few f) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           if constexpr (PL == 3) {
-            acc[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[2], y[q][0], acc[p][q], 0, 0, 0);
-            acc[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[0], y[q][2], acc[p][q], 0, 0, 0);
-            acc[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[1], y[q][1], acc[p][q], 0, 0, 0);
-            acc[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[1], y[q][0], acc[p][q], 0, 0, 0);
-            acc[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[0], y[q][1], acc[p][q], 0, 0, 0);
+            low[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[2], y[q][0], low[p][q], 0, 0, 0);
+            low[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[0], y[q][2], low[p][q], 0, 0, 0);
+            low[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[1], y[q][1], low[p][q], 0, 0, 0);
+            low[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[1], y[q][0], low[p][q], 0, 0, 0);
+            low[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[0], y[q][1], low[p][q], 0, 0, 0);
           }
-          acc[p][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[0], y[q][0], acc[p][q], 0, 0, 0);
+          f32x4& sum = PL == 1 && NQ == 1 && set % 2 ? low[p][q] : acc[p][q];
+          sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[0], y[q][0], sum, 0, 0, 0);
         }
       }
     };
@@ -148,7 +153,7 @@ __global__ void __launch_bounds__(256) few_kernel(const Few f) {
         const float add = bias ? to_float(bias[min(c, f.C - 1)]) : 0.f;
 #pragma unroll
         for (int q = 0; q < NQ; ++q)
-          acc[p][q][e] = c < end ? acc[p][q][e] + add : -__builtin_huge_valf();
+          acc[p][q][e] = c < end ? acc[p][q][e] + low[p][q][e] + add : -__builtin_huge_valf();
       }
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
