@@ -684,13 +684,15 @@ int64_t tb_linear_xent_workspace_bytes(int32_t dtype, int64_t n_rows, int32_t wi
  * gradients of the sum of the losses in the same call (a training step).
  *
  *   out_loss, out_lse  device float[n_rows], or NULL
+ *   out_low            device float[n_rows], or NULL: what rounding to out_lse left of the
+ *                      log-sum-exp (0 where that is not finite)
  */
 int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype,
                    int64_t n_rows, int32_t width, int32_t v_plus_blank, int64_t x_stride,
                    int64_t w_stride, const int32_t* target, const float* weight,
-                   float* out_loss, float* out_lse, void* dx, int64_t dx_stride, void* dw,
-                   int64_t dw_stride, void* db, void* workspace, int64_t workspace_bytes,
-                   void* hip_stream);
+                   float* out_loss, float* out_lse, float* out_low, void* dx,
+                   int64_t dx_stride, void* dw, int64_t dw_stride, void* db, void* workspace,
+                   int64_t workspace_bytes, void* hip_stream);
 
 /*
  * tb_linear_xent_grad - the gradients of a scalar from its gradients with respect to
@@ -698,6 +700,8 @@ int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype
  * bias, target and weight.
  *
  *   lse            device float[n_rows]
+ *   lse_low        device float[n_rows], out_low of that call, or NULL (0): without it p is
+ *                  off by the rounding of lse, which shows where p - 1 is near 0
  *   d_loss, d_lse  device float[n_rows], or NULL (1 and 0)
  *
  * A row to which no gradient comes is left out as well.
@@ -705,8 +709,8 @@ int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype
 int tb_linear_xent_grad(const void* x, const void* w, const void* bias, int32_t dtype,
                         int64_t n_rows, int32_t width, int32_t v_plus_blank, int64_t x_stride,
                         int64_t w_stride, const int32_t* target, const float* weight,
-                        const float* lse, const float* d_loss, const float* d_lse, void* dx,
-                        int64_t dx_stride, void* dw, int64_t dw_stride, void* db,
+                        const float* lse, const float* lse_low, const float* d_loss,
+                        const float* d_lse, void* dx, int64_t dx_stride, void* dw, int64_t dw_stride, void* db,
                         void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /*

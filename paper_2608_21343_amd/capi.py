@@ -94,9 +94,9 @@ def _load() -> C.CDLL:
         "tb_token_logprobs_grad": [P, I32, I64, I32, I64, C.c_float, P, I32, P, P, P, P, I64, P,
                                    I64, P],
         "tb_distill": [P, I32, I64, I32, I64, C.c_float, P, P, I32, I32, P, P, P, I64, P, I64, P],
-        "tb_linear_xent": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, I64, P, I64, P, P,
+        "tb_linear_xent": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, I64, P, I64, P, P,
                            I64, P],
-        "tb_linear_xent_grad": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, I64, P,
+        "tb_linear_xent_grad": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, P, I64, P,
                                 I64, P, P, I64, P],
         "tb_adamw_step": [P, I32, I32, I32, C.c_double, C.c_double, C.c_double, C.c_double,
                           C.c_double, I64, P, P, P, C.c_uint32, P],
@@ -844,19 +844,20 @@ def _target(target, n: int):
 
 
 def tb_linear_xent(x, w, target, out_loss=None, out_lse=None, dx=None, dw=None, db=None,
-                   bias=None, weight=None, workspace=None, stream=None) -> None:
+                   bias=None, weight=None, workspace=None, stream=None, out_low=None) -> None:
     """x: [..., width] with evenly spaced rows; w: [V+1, width]; bias [V+1] or None;
-    target, weight, out_loss, out_lse: one value a row; dx, dw, db: like x, w, bias,
-    the gradients of the sum of the losses."""
+    target, weight, out_loss, out_lse, out_low: one value a row; dx, dw, db: like x, w,
+    bias, the gradients of the sum of the losses."""
     layer = _layer(x, w, bias)
     n = layer[4]
     _same_device(x, w=w, bias=bias, target=target, weight=weight, out_loss=out_loss,
-                 out_lse=out_lse, dx=dx, dw=dw, db=db, workspace=workspace)
+                 out_lse=out_lse, out_low=out_low, dx=dx, dw=dw, db=db, workspace=workspace)
     p_db = None if db is None else _like_bias(db, w)
     with _device_of(x, stream):
         ws, ws_bytes, keep = _linear_workspace(x, layer, dx, dw, db, 0, workspace, stream)
         _check(LIB.tb_linear_xent(*layer, _target(target, n), _one(weight, n, "weight"),
                                   _one(out_loss, n, "out_loss"), _one(out_lse, n, "out_lse"),
+                                  _one(out_low, n, "out_low"),
                                   *_like(dx, x, "dx"), *_like(dw, w, "dw"), p_db, ws, ws_bytes,
                                   _stream(stream)))
 
@@ -868,20 +869,22 @@ def _like_bias(db, w):
 
 
 def tb_linear_xent_grad(x, w, target, lse, d_loss=None, d_lse=None, dx=None, dw=None, db=None,
-                        bias=None, weight=None, workspace=None, stream=None) -> None:
-    """Gradients from those of loss and lse; lse: out_lse of tb_linear_xent for the
-    same layer and rows."""
+                        bias=None, weight=None, workspace=None, stream=None,
+                        lse_low=None) -> None:
+    """Gradients from those of loss and lse; lse and lse_low: out_lse and out_low (or
+    None) of tb_linear_xent for the same layer and rows."""
     layer = _layer(x, w, bias)
     n = layer[4]
-    _same_device(x, w=w, bias=bias, target=target, weight=weight, lse=lse, d_loss=d_loss,
-                 d_lse=d_lse, dx=dx, dw=dw, db=db, workspace=workspace)
+    _same_device(x, w=w, bias=bias, target=target, weight=weight, lse=lse, lse_low=lse_low,
+                 d_loss=d_loss, d_lse=d_lse, dx=dx, dw=dw, db=db, workspace=workspace)
     if lse is None:
         raise ValueError("lse is required")
     p_db = None if db is None else _like_bias(db, w)
     with _device_of(x, stream):
         ws, ws_bytes, keep = _linear_workspace(x, layer, dx, dw, db, 1, workspace, stream)
         _check(LIB.tb_linear_xent_grad(*layer, _target(target, n), _one(weight, n, "weight"),
-                                       _one(lse, n, "lse"), _one(d_loss, n, "d_loss"),
+                                       _one(lse, n, "lse"), _one(lse_low, n, "lse_low"),
+                                       _one(d_loss, n, "d_loss"),
                                        _one(d_lse, n, "d_lse"), *_like(dx, x, "dx"),
                                        *_like(dw, w, "dw"), p_db, ws, ws_bytes, _stream(stream)))
 

@@ -82,7 +82,9 @@ int linear_call(const linear::Call& c, void* workspace, int64_t workspace_bytes,
   if ((r = check_four(c.d_lse, "d_lse", false))) return r;
   if ((r = check_four(c.lse, "lse", false))) return r;
   if ((r = check_four(c.out_loss, "out_loss", false))) return r;
+  if ((r = check_four(c.lse_low, "lse_low", false))) return r;
   if ((r = check_four(c.out_lse, "out_lse", false))) return r;
+  if ((r = check_four(c.out_low, "out_low", false))) return r;
   if (c.dx && any && (r = check_matrix(c.dx, c.dtype, c.dx_stride, c.D, "dx"))) return r;
   if (c.dw && (r = check_matrix(c.dw, c.dtype, c.dw_stride, c.D, "dw"))) return r;
   if (c.db && !aligned(c.db, size)) return fail(TB_EINVAL, "db misaligned");
@@ -97,6 +99,7 @@ int linear_call(const linear::Call& c, void* workspace, int64_t workspace_bytes,
   };
   const Buf bufs[] = {{c.out_loss, c.n * 4, "out_loss"},
                       {c.out_lse, c.n * 4, "out_lse"},
+                      {c.out_low, c.n * 4, "out_low"},
                       {c.dx, rows(c.n, c.dx_stride), "dx"},
                       {c.dw, rows(c.C, c.dw_stride), "dw"},
                       {c.db, c.C * size, "db"},
@@ -107,9 +110,10 @@ int linear_call(const linear::Call& c, void* workspace, int64_t workspace_bytes,
                       {c.target, c.n * 4, "target"},
                       {c.weight, c.n * 4, "weight"},
                       {c.lse, c.n * 4, "lse"},
+                      {c.lse_low, c.n * 4, "lse_low"},
                       {c.d_loss, c.n * 4, "d_loss"},
                       {c.d_lse, c.n * 4, "d_lse"}};
-  if ((r = check_apart(bufs, 6))) return r;
+  if ((r = check_apart(bufs, 7))) return r;
   const hipError_t e = linear::run(c, workspace, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return hip_fail(e, what);
   return TB_OK;
@@ -145,30 +149,30 @@ extern "C" int64_t tb_linear_xent_workspace_bytes(int32_t dtype, int64_t n_rows,
 extern "C" int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype,
                               int64_t n_rows, int32_t width, int32_t v_plus_blank,
                               int64_t x_stride, int64_t w_stride, const int32_t* target,
-                              const float* weight, float* out_loss, float* out_lse, void* dx,
-                              int64_t dx_stride, void* dw, int64_t dw_stride, void* db,
+                              const float* weight, float* out_loss, float* out_lse,
+                              float* out_low, void* dx, int64_t dx_stride, void* dw, int64_t dw_stride, void* db,
                               void* workspace, int64_t workspace_bytes, void* hip_stream) {
-  if (!out_loss && !out_lse && !dx && !dw && !db)
+  if (!out_loss && !out_lse && !out_low && !dx && !dw && !db)
     return fail(TB_EINVAL, "every output is NULL");
   const linear::Call c = {x,      w,      bias,    dtype,   n_rows,   width,   v_plus_blank,
-                          x_stride, w_stride, target, weight, nullptr, nullptr, nullptr,
-                          out_loss, out_lse, dx, dw, db, dx_stride, dw_stride};
+                          x_stride, w_stride, target, weight, nullptr, nullptr, nullptr, nullptr,
+                          out_loss, out_lse, out_low, dx, dw, db, dx_stride, dw_stride};
   return linear_call(c, workspace, workspace_bytes, hip_stream, "linear_xent launch");
 }
 
 extern "C" int tb_linear_xent_grad(const void* x, const void* w, const void* bias, int32_t dtype,
                                    int64_t n_rows, int32_t width, int32_t v_plus_blank,
                                    int64_t x_stride, int64_t w_stride, const int32_t* target,
-                                   const float* weight, const float* lse, const float* d_loss,
-                                   const float* d_lse, void* dx, int64_t dx_stride, void* dw,
+                                   const float* weight, const float* lse, const float* lse_low,
+                                   const float* d_loss, const float* d_lse, void* dx, int64_t dx_stride, void* dw,
                                    int64_t dw_stride, void* db, void* workspace,
                                    int64_t workspace_bytes, void* hip_stream) {
   if (!dx && !dw && !db) return fail(TB_EINVAL, "dx, dw and db are all NULL");
   if (!lse && n_rows > 0) return fail(TB_EINVAL, "lse is NULL");
   static const float none = 0.f;  // (without rows nothing reads it)
   const linear::Call c = {x,      w,      bias,    dtype,   n_rows,   width,   v_plus_blank,
-                          x_stride, w_stride, target, weight, d_loss, d_lse, lse ? lse : &none,
-                          nullptr, nullptr, dx, dw, db, dx_stride, dw_stride};
+                          x_stride, w_stride, target, weight, d_loss, d_lse, lse ? lse : &none, lse_low,
+                          nullptr, nullptr, nullptr, dx, dw, db, dx_stride, dw_stride};
   return linear_call(c, workspace, workspace_bytes, hip_stream, "linear_xent_grad launch");
 }
 

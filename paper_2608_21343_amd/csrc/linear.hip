@@ -15,14 +15,14 @@ struct Gather {
   int64_t n;
   int32_t C;
   const int32_t* target;
-  const float *weight, *d_loss, *d_lse, *lse;
+  const float *weight, *d_loss, *d_lse, *lse, *lse_low;
   bool grads;
   Meta* meta;
   int32_t* counts;  // per group: rows that take part ...
   float* tops;      // ... and their largest finite |a|, |b|; NULL for a single group
   int32_t *idx, *inv, *tgt;
   float *a, *b, *lse_c, *r, *m;
-  float *out_loss, *out_lse;
+  float *out_loss, *out_lse, *out_low;
   // the features, and their planes
   int64_t stride;
   int32_t D, dp;
@@ -347,10 +347,14 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x,
         g.inv[r] = -1;
         if (g.out_loss) g.out_loss[r] = 0.f;
         if (g.out_lse) g.out_lse[r] = 0.f;
+        if (g.out_low) g.out_low[r] = 0.f;
       } else {
         float lse = g.lse ? g.lse[r] : 0.f;
         // an empty row (no token above -inf) has no gradient
         if (lse == -__builtin_huge_valf()) o.a = o.b = lse = 0.f;
+        // (exp(z - lse) has then the whole log-sum-exp in it: where p is near 1, p - 1 is
+        // as exact as p)
+        if (g.lse_low) o.a *= expf(-g.lse_low[r]);
         if (Elem<T>::kScaled) {
           float m = fmaxf(fabsf(o.a), fabsf(o.b));
           if (!(m > 0.f)) m = 1.f;  // (0 or NaN)
@@ -455,7 +459,7 @@ struct Finish {
   int32_t n, C;
   const float* weight;
   float *lse_c, *a, *b;
-  float *out_loss, *out_lse;
+  float *out_loss, *out_lse, *out_low;
 };
 
 // Maximum (or sum) over L lanes: part of a wave, or the four waves of a workgroup.
@@ -491,6 +495,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Weigh
   if (!f.idx && (t == -1 || weight == 0.f)) {
     if (lane == 0 && f.out_loss) f.out_loss[row] = 0.f;
     if (lane == 0 && f.out_lse) f.out_lse[row] = 0.f;
+    if (lane == 0 && f.out_low) f.out_low[row] = 0.f;
     return;
   }
   const float2* part = f.part + from * f.n_part;
@@ -506,11 +511,16 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Weigh
   }
   sum = over<L, false>(sum, lds[1]);
   if (lane != 0) return;
-  const float lse = base + logf(sum);
+  const float rest = logf(sum), lse = base + rest;
   if (f.out_lse) f.out_lse[row] = lse;
+  if (f.out_low) {
+    // what the rounding of that sum left, exactly
+    const float rounded = lse - base, low = (base - (lse - rounded)) + (rest - rounded);
+    f.out_low[row] = fabsf(lse) < __builtin_huge_valf() ? low : 0.f;
+  }
   if (f.out_loss) {
     // (the maximum first: a small loss keeps its digits; an empty row's is +inf)
-    float nll = lse == -__builtin_huge_valf() ? -lse : (base - f.hit[from]) + logf(sum);
+    float nll = lse == -__builtin_huge_valf() ? -lse : (base - f.hit[from]) + rest;
     if ((uint32_t)t >= (uint32_t)f.C) nll = __builtin_nanf("");
     f.out_loss[row] = f.weight ? weight * nll : nll;
   }
@@ -519,7 +529,9 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Weigh
     f.lse_c[at] = 0.f;
     f.a[at] = f.b[at] = 0.f;
   } else {
-    f.lse_c[at] = lse;
+    // a exp(z - lse), with nothing of lse rounded
+    f.lse_c[at] = base;
+    f.a[at] /= sum;
   }
 }
 
@@ -733,7 +745,7 @@ Layout plan(const Call& c) {
   const bool read = c.D * size % 16 == 0 && c.w_stride * size % 16 == 0 &&
                     (uintptr_t)c.w % 16 == 0 && c.x_stride * size % 16 == 0 &&
                     (uintptr_t)c.x % 16 == 0;
-  L.few = !c.lse && read && c.n <= few_rows(f32, grads);
+  L.few = read && c.n <= few_rows(f32, grads);
   // (the loss of few rows needs no copies)
   L.gather = grads || !L.few;
   L.copy_w = L.copy_w && L.gather;
@@ -766,7 +778,7 @@ Layout plan(const Call& c) {
   if (f32) L.m = take(L.np * 4);
   if (f32) L.most = take(kTops * 4);
   L.hit = take(L.np * 4);
-  if (!c.lse) L.part = take(L.np * L.n_part * 8);
+  if (!c.lse || L.few) L.part = take(L.np * L.n_part * 8);
   if (L.gather) L.px = take(L.planes * L.np * L.dp * 2);
   if (f32 && c.dw) L.pxm = take(L.planes * L.np * L.dp * 2);
   if (L.copy_w) L.pw = take(L.planes * c.C * L.dp * 2);
@@ -783,7 +795,7 @@ Layout plan(const Call& c) {
     // Logits that the statistics write and the gradients read again (float32, up to 256 MB)
     // cost less than another product: a step of 16,000 x 512 float32 against 1025 tokens 292
     // us instead of 313, of 300 x 1024 bfloat16 against 50,001 230 instead of 258.
-    L.kept = !c.lse && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
+    L.kept = (!c.lse || L.few) && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
     L.G = take(L.planes * L.np * L.ldg * 2);
     // (by 16 rows where 64 would leave CUs idle: a step of 1511 bfloat16 rows of 336 against 612
     // tokens 51 us by 64, 47 by 16; of 16,000 float32 rows of 512 against 1025 288 and 300)
@@ -828,9 +840,9 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   float *r = f32 ? flt(L.r) : nullptr, *m = f32 ? flt(L.m) : nullptr;
   const int64_t groups = (c.n + group_rows(c.n) - 1) / group_rows(c.n);
   const int rows = groups > 1 ? kRowsMany : kRowsOnly;
-  const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse,
+  const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse, c.lse_low,
                      grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
-                     a,      b,    lse, r, m, c.out_loss, c.out_lse,
+                     a,      b,    lse, r, m, c.out_loss, c.out_lse, c.out_low,
                      c.x_stride, c.D, (int32_t)L.dp, u16(L.px),
                      L.direct ? c.dx : nullptr, c.dx_stride,
                      (int32_t)std::max<int64_t>((c.n + rows - 1) / rows, 1)};
@@ -879,7 +891,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       weighted = {static_cast<const float*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, u16(L.pxm),
                   (int32_t)(c.n < 8192 ? (c.n + 3) / 4 : 2048)};
   }
-  if (!c.lse && c.n > 0) {
+  // (with lse at hand: the logits of few rows alone)
+  if ((!c.lse || (L.few && L.kept)) && c.n > 0) {
     float2* part = reinterpret_cast<float2*>(ws + L.part);
     float *hit = flt(L.hit), *z = L.kept ? flt(L.z) : nullptr;
     if (L.few) {
@@ -903,8 +916,10 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       });
     }
     if (e != hipSuccess) return e;
-    const Finish f = {meta,  part, L.n_part, hit,     L.gather ? idx : nullptr, c.target,
-                      L.few, (int32_t)c.n, c.C, c.weight, lse, a, b, c.out_loss, c.out_lse};
+  }
+  if (!c.lse && c.n > 0) {
+    const Finish f = {meta,  reinterpret_cast<float2*>(ws + L.part), L.n_part, flt(L.hit), L.gather ? idx : nullptr, c.target,
+                      L.few, (int32_t)c.n, c.C, c.weight, lse, a, b, c.out_loss, c.out_lse, c.out_low};
     const int lanes = L.n_part <= 128 ? 16 : c.n <= 1024 && L.n_part >= 256 ? 256 : 64;
     const auto finish =
         lanes == 16 ? &finish_kernel<16> : lanes == 64 ? &finish_kernel<64> : &finish_kernel<256>;

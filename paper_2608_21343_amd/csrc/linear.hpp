@@ -29,6 +29,11 @@
 // a unit for each token G' would have to carry it too, and a token of small weights would
 // lose its gradient.) Tokens that the bias masks have no say in S, whatever they hold.
 //
+// lse_i is the sum of a row's maximum and a logarithm, and its rounding would be a relative
+// error of p that shows in p - 1 where p is near 1. Where the statistics are of the same
+// call, a_i is divided by the sum and the maximum taken for lse_i; else the caller may hand
+// over what the rounding left.
+//
 // Rows that take part (target not -1, weight not 0) are gathered first, so that the
 // others cost nothing and whatever they hold reaches no sum. Rows of the gathered
 // matrix end at a multiple of 64 values, and its rows at one of 64, with zeros.
@@ -145,8 +150,8 @@ struct Call {
   int64_t x_stride, w_stride;
   const int32_t* target;
   const float *weight, *d_loss, *d_lse;
-  const float* lse;  // of an earlier call, or NULL: computed here
-  float *out_loss, *out_lse;
+  const float *lse, *lse_low;  // of an earlier call, or NULL: computed here
+  float *out_loss, *out_lse, *out_low;
   void *dx, *dw, *db;
   int64_t dx_stride, dw_stride;
 };

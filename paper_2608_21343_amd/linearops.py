@@ -66,15 +66,15 @@ class _LinearXent(torch.autograd.Function):
     def forward(ctx, x, w, target, bias, weight):
         x, w, target, bias, weight = _args(x, w, target, bias, weight)
         loss = torch.empty(target.shape, dtype=torch.float32, device=x.device)
-        lse = torch.empty_like(loss)
-        capi.tb_linear_xent(x, w, target, loss, lse, bias=bias, weight=weight)
+        lse, low = torch.empty_like(loss), torch.empty_like(loss)
+        capi.tb_linear_xent(x, w, target, loss, lse, bias=bias, weight=weight, out_low=low)
         ctx.set_materialize_grads(False)
-        ctx.save_for_backward(x, w, target, bias, weight, lse)
+        ctx.save_for_backward(x, w, target, bias, weight, lse, low)
         return loss, lse
 
     @staticmethod
     def backward(ctx, d_loss, d_lse):
-        x, w, target, bias, weight, lse = ctx.saved_tensors
+        x, w, target, bias, weight, lse, low = ctx.saved_tensors
         need_x, need_w, _, need_b, _ = ctx.needs_input_grad
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
         dw = torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None
@@ -83,7 +83,7 @@ class _LinearXent(torch.autograd.Function):
             d_loss = torch.zeros_like(lse)
         capi.tb_linear_xent_grad(x, w, target, lse, d_loss.contiguous(),
                                  None if d_lse is None else d_lse.contiguous(), dx, dw, db,
-                                 bias=bias, weight=weight)
+                                 bias=bias, weight=weight, lse_low=low)
         return tuple(None if g is None else _once(g) for g in (dx, dw, None, db, None))
 
 

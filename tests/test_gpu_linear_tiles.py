@@ -194,3 +194,34 @@ def test_small_losses_of_large_logits(dtype):
         # exponential's argument below 16 in units of log 2 (2^-21) and log 2's own rounding
         # (2^-20), its function and the logarithm (2^-22). Half a step of lse is 2^-14.
         assert float((loss - right).abs().max()) <= 80 * 2.0 ** -24 + right * 2.0 ** -19
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [9, 20, 70])
+def test_gradients_of_certain_rows(n, dtype):
+    """p - 1 keeps its digits where lse is large and p near 1, in one call and in two."""
+    from paper_2608_21343_amd import capi
+    D, C = 64, 600
+    c = R.case(n, D, C, dtype, 3, device="cuda", bias=False)
+    c["x"][:] = 0.0
+    c["x"][:, 0] = 1.0
+    c["w"][:] = 1008.0
+    c["w"][5] = 1024.0
+    c["target"][:] = 5
+    p = math.exp(-16.0) / (1 + (C - 1) * math.exp(-16.0))
+    want = torch.full((C,), p * n, dtype=torch.float64, device="cuda")
+    want[5] = -p * (C - 1) * n
+    # 1 / sum (or the exponential of lse's rest) and a times it: four roundings of half a step
+    # near 1 and as many of the sum of 64 tokens or fewer near 1; exponentials of -16 to 2^-19
+    # of themselves; n additions; the result's own rounding
+    tol = R.U[dtype] * want.abs() + 2.0 ** -18 * want.abs() + (n + 4) * 2.0 ** -24 * want.abs()
+    tol[5] += n * (4 + 68) * 2.0 ** -24
+    loss, lse, low = torch.empty((3, n), device="cuda")
+    out = {k: torch.empty(C, dtype=dtype, device="cuda") for k in ("one", "two")}
+    capi.tb_linear_xent(c["x"], c["w"], c["target"], loss, lse, db=out["one"], out_low=low)
+    capi.tb_linear_xent_grad(c["x"], c["w"], c["target"], lse, db=out["two"], lse_low=low)
+    for name, db in out.items():
+        assert bool(((db.double() - want).abs() <= tol).all()), name
+    exact = 1024.0 + math.log1p((C - 1) * math.exp(-16.0))
+    assert float((lse.double() + low.double() - exact).abs().max()) <= 72 * 2.0 ** -24
+    assert float(low.abs().max()) <= 2.0 ** -14  # half a step of lse
