@@ -664,9 +664,9 @@ int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus
  * values, 2^-25, without units.) So values 2^16 below the largest of their unit lose
  * precision. A token whose bias is below -2^100 has no say in the unit, and counts as at
  * most twice the largest of the others. The gradients of the logits are rounded once to
- * dtype's precision, as they would be if they were kept (bfloat16: 2^-8 of each; float32:
- * 2^-23 of each, or 2^-39 of the row's largest |a_i|, |b_i|); db is the sum of the unrounded
- * ones. The results are rounded once to dtype. Results are the same bits for the same
+ * dtype's precision, as they would be if they were kept (bfloat16: 2^-8 of each, in calls of
+ * up to 32 rows 2^-16; float32: 2^-23 of each, or 2^-39 of the row's largest |a_i|, |b_i|); db
+ * is the sum of the unrounded ones. The results are rounded once to dtype. Results are the same bits for the same
  * arguments; a loss alone may differ in its last bits from one that comes with gradients.
  *
  * tb_linear_xent_workspace_bytes - for a call with these arguments; grads: sum of 1

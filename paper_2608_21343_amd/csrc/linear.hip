@@ -30,6 +30,7 @@ struct Gather {
   void* dx;  // rows that are left out get 0 here; or NULL
   int64_t dx_stride;
   int32_t blocks;  // workgroups that gather
+  bool paired;     // every row's features twice, kPair rows apart
 };
 
 // Rows of a count, in 256s, and rows that a workgroup gathers. Up to 2048 rows are one
@@ -392,6 +393,9 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x,
     float most;
     const float unit = row_planes<T>(x + (row0 + i) * g.stride, g.D, g.dp, wide,
                                      g.out + (int64_t)at * Elem<T>::PLANES * g.dp, &most);
+    if (!Elem<T>::kScaled && g.paired)
+      row_planes<T>(x + (row0 + i) * g.stride, g.D, g.dp, wide,
+                    g.out + (int64_t)(at + kPair) * g.dp, &most);
     if (Elem<T>::kScaled && lane == 0) {
       g.r[at] = unit;
       const float with = most * g.m[at];  // (written by this workgroup)
@@ -401,9 +405,11 @@ __global__ void __launch_bounds__(256) gather_kernel(const Gather g, const T* x,
   if (Elem<T>::kScaled && g.grads) raise(&g.meta->T, weighty);
   if ((int)blockIdx.x == g.blocks - 1) {
     // the zeros behind the last row
-    const int64_t row = Elem<T>::PLANES * g.dp, end = up(all, kStep) * row;
-    for (int64_t i = all * row + 4 * threadIdx.x; i < end; i += 1024)
+    const int64_t row = Elem<T>::PLANES * g.dp, end = (g.paired ? kPair : up(all, kStep)) * row;
+    for (int64_t i = all * row + 4 * threadIdx.x; i < end; i += 1024) {
       *reinterpret_cast<uint2*>(g.out + i) = make_uint2(0, 0);
+      if (g.paired) *reinterpret_cast<uint2*>(g.out + kPair * row + i) = make_uint2(0, 0);
+    }
   }
 }
 
@@ -545,6 +551,7 @@ struct Kept {
   const int32_t* idx;  // rows of z, or NULL: gathered ones
   RowArgs row;
   int32_t C, cols;
+  bool paired;  // what the rounding of a row left goes kPair rows further on
   uint16_t* G;
   float* col;
 };
@@ -580,6 +587,17 @@ __global__ void __launch_bounds__(256) kept_kernel(const Kept k) {
       }
       uint2 p[El::PLANES];
       El::planes4(v, p);
+      if (!El::kScaled && k.paired) {
+        if (at >= kPair) continue;
+        float left[4] = {v[0] - low16(p[0].x), v[1] - high16(p[0].x), v[2] - low16(p[0].y),
+                         v[3] - high16(p[0].y)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!(fabsf(left[e]) < __builtin_huge_valf())) left[e] = 0.f;
+        uint2 q[El::PLANES];
+        El::planes4(left, q);
+        *reinterpret_cast<uint2*>(k.G + (at + kPair) * k.ldz + c0) = q[0];
+      }
 #pragma unroll
       for (int s = 0; s < El::PLANES; ++s)
         *reinterpret_cast<uint2*>(k.G + at * El::PLANES * k.ldz + place<El::PLANES>(c0) +
@@ -615,7 +633,10 @@ __global__ void __launch_bounds__(256)
     float scale = 0.f;
     if (from >= 0) {
       const float* p = g.acc + from * g.lda + d;
-      for (int s = 0; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * g.acc_split);
+      for (int s = 0; s < g.splits; ++s) {
+        v += *reinterpret_cast<const f32x4*>(p + s * g.acc_split);
+        if (g.paired) v += *reinterpret_cast<const f32x4*>(p + s * g.acc_split + kPair * g.lda);
+      }
       scale = inv ? dx_scale<T>(g, meta, from) : dw_scale<T>(meta);
     }
     float w[4] = {0.f, 0.f, 0.f, 0.f};
@@ -717,7 +738,7 @@ Strips strips(int64_t tokens, int64_t others, int64_t steps, int64_t stages, boo
 
 struct Layout {
   int64_t np, dp, planes;      // gathered rows and values a row, rounded up
-  bool copy_w, few, gather, kept;      // kept: the logits, from the statistics to their gradients
+  bool copy_w, few, gather, paired, kept;      // kept: the logits, from the statistics to their gradients
   int32_t n_part;
   // tokens of a piece of the vocabulary (of all but the last), and of a row of gradients
   int32_t piece, pieces, ldg;
@@ -778,7 +799,7 @@ Layout plan(const Call& c) {
   if (f32) L.m = take(L.np * 4);
   if (f32) L.most = take(kTops * 4);
   L.hit = take(L.np * 4);
-  if (!c.lse || L.few) L.part = take(L.np * L.n_part * 8);
+  if (!c.lse || L.few || c.n <= kPair) L.part = take(L.np * L.n_part * 8);
   if (L.gather) L.px = take(L.planes * L.np * L.dp * 2);
   if (f32 && c.dw) L.pxm = take(L.planes * L.np * L.dp * 2);
   if (L.copy_w) L.pw = take(L.planes * c.C * L.dp * 2);
@@ -795,7 +816,8 @@ Layout plan(const Call& c) {
     // Logits that the statistics write and the gradients read again (float32, up to 256 MB)
     // cost less than another product: a step of 16,000 x 512 float32 against 1025 tokens 292
     // us instead of 313, of 300 x 1024 bfloat16 against 50,001 230 instead of 258.
-    L.kept = (!c.lse || L.few) && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
+    L.paired = !f32 && L.pieces == 1 && c.n <= kPair;
+    L.kept = (!c.lse || L.few || L.paired) && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
     L.G = take(L.planes * L.np * L.ldg * 2);
     // (by 16 rows where 64 would leave CUs idle: a step of 1511 bfloat16 rows of 336 against 612
     // tokens 51 us by 64, 47 by 16; of 16,000 float32 rows of 512 against 1025 288 and 300)
@@ -803,7 +825,7 @@ Layout plan(const Call& c) {
     if (L.kept) L.z = take(L.np * L.ldg * 4);
     if (c.dx) {
       L.x = cut(L.dp, c.n, up(most, kStep) / kStep, stages, true);
-      L.direct = L.x.parts == 1;
+      L.direct = L.x.parts == 1 && !L.paired;
       if (!L.direct || L.pieces > 1) L.acc_x = take(L.x.parts * L.np * L.dp * 4);
     }
     if (c.dw) {
@@ -845,7 +867,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
                      a,      b,    lse, r, m, c.out_loss, c.out_lse, c.out_low,
                      c.x_stride, c.D, (int32_t)L.dp, u16(L.px),
                      L.direct ? c.dx : nullptr, c.dx_stride,
-                     (int32_t)std::max<int64_t>((c.n + rows - 1) / rows, 1)};
+                     (int32_t)std::max<int64_t>((c.n + rows - 1) / rows, 1), L.paired};
   const Weights weights = {c.w_stride, c.D, (int32_t)L.dp, c.C,
                            f32 ? static_cast<const float*>(c.bias) : nullptr,
                            f32 ? flt(L.most) : nullptr, u16(L.pw)};
@@ -891,8 +913,8 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       weighted = {static_cast<const float*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, u16(L.pxm),
                   (int32_t)(c.n < 8192 ? (c.n + 3) / 4 : 2048)};
   }
-  // (with lse at hand: the logits of few rows alone)
-  if ((!c.lse || (L.few && L.kept)) && c.n > 0) {
+  // (with lse at hand: the logits alone)
+  if ((!c.lse || L.kept) && c.n > 0) {
     float2* part = reinterpret_cast<float2*>(ws + L.part);
     float *hit = flt(L.hit), *z = L.kept ? flt(L.z) : nullptr;
     if (L.few) {
@@ -945,7 +967,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     float* col = c.db ? flt(L.col) : nullptr;
     if (L.kept && c.n > 0) {
       const Kept k = {meta, flt(L.z), L.ldg, L.few ? idx : nullptr, g.row, c.C,
-                      (int32_t)up(c.C, kStep), u16(L.G), col};
+                      (int32_t)up(c.C, kStep), L.paired, u16(L.G), col};
       const auto make = L.kept_rows == 16 ? &kept_kernel<T, 16> : &kept_kernel<T, 64>;
       make<<<dim3((c.C + 255) / 256, (unsigned)(up(c.n, 64) / L.kept_rows)), dim3(256), 0, st>>>(k);
       e = hipGetLastError();
@@ -989,6 +1011,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
       x.acc_split = L.np * L.dp;
       x.lda = (int32_t)L.dp;
       x.add = piece > 0;
+      x.paired = L.paired;
       e = f32 ? dx_f32(x, st) : dx_bf16(x, st);
       if (e != hipSuccess) return e;
     }
@@ -1029,6 +1052,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
     x.acc = flt(L.acc_x);
     x.acc_split = L.np * L.dp;
     x.lda = (int32_t)L.dp;
+    x.paired = L.paired;
     join_kernel<T><<<dim3(blocks(c.n * ((c.D + 3) / 4))), dim3(256), 0, st>>>(
         x, inv, static_cast<T*>(c.dx), c.dx_stride, c.n);
   }

@@ -732,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
 #pragma unroll
       for (int j = 0; j < FQ; ++j) {
         const int q = q0 + wq + 16 * j + lq;
-        const bool in = q < (KIND == kDx ? meta.n : g.n_q);
+        const bool in = q < (KIND != kDx ? g.n_q : g.paired ? 2 * kPair : meta.n);
         f32x4* sums = reinterpret_cast<f32x4*>(g.acc + tile.split * g.acc_split +
                                                (int64_t)q * g.lda + p0 + c_lane);
         if (g.add && in) {

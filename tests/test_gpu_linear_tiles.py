@@ -159,6 +159,28 @@ def test_every_token_masked_by_a_number(n, dtype):
             assert bool(torch.isfinite(out[name]).all()), name
 
 
+@pytest.mark.parametrize("n, D, C", [(1, 64, 300), (2, 127, 339), (16, 512, 1025), (17, 40, 65537),
+                                     (31, 320, 999), (32, 64, 70001)])
+def test_gradients_of_few_bfloat16_rows(n, D, C):
+    """Calls of up to 32 rows keep what rounding the logits' gradients left: 2^-16 of them is
+    lost and not 2^-8."""
+    some = n % 2 == 0
+    c = R.case(n, D, C, BF16, n + D, weighted=some, gaps=some, device="cuda")
+    weight = None if c["weight"] is None else c["weight"].double()
+    x = torch.where((c["target"] != -1)[:, None], c["x"].double(), 0.0)
+    w = c["w"].double()
+    _, lse, z = R.forward(x, w, c["target"], c["bias"].double(), weight)
+    G = R.logit_grad(z, lse, c["target"], weight).abs()
+    rounded = R.U[BF16] - 2.0 ** -16
+    want = R.expected(c)
+    for name, size in (("dx", G @ w.abs()), ("dw", G.t() @ x.abs())):
+        value, tol = want[name]
+        want[name] = (value, tol - rounded * size)
+    got = step(c)
+    check_all(got, want)
+    check_all(grad(c, got["lse"], torch.ones(n, device="cuda"), None), want)
+
+
 def test_two_calls_at_once():
     cases = [R.case(n, 256, C, dtype, 2, device="cuda", gaps=True)
              for n, C, dtype in ((900, 4097, BF16), (700, 3001, F32))]
