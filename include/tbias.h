@@ -703,6 +703,7 @@ int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype
  *   lse_low        device float[n_rows], out_low of that call, or NULL (0): without it p is
  *                  off by the rounding of lse, which shows where p - 1 is near 0
  *   d_loss, d_lse  device float[n_rows], or NULL (1 and 0)
+ *   d_loss_step    1, or 0: d_loss is one value for all rows (as the gradient of their sum)
  *
  * A row to which no gradient comes is left out as well.
  */
@@ -710,8 +711,9 @@ int tb_linear_xent_grad(const void* x, const void* w, const void* bias, int32_t 
                         int64_t n_rows, int32_t width, int32_t v_plus_blank, int64_t x_stride,
                         int64_t w_stride, const int32_t* target, const float* weight,
                         const float* lse, const float* lse_low, const float* d_loss,
-                        const float* d_lse, void* dx, int64_t dx_stride, void* dw, int64_t dw_stride, void* db,
-                        void* workspace, int64_t workspace_bytes, void* hip_stream);
+                        int32_t d_loss_step, const float* d_lse, void* dx, int64_t dx_stride,
+                        void* dw, int64_t dw_stride, void* db, void* workspace,
+                        int64_t workspace_bytes, void* hip_stream);
 
 /*
  * AdamW over many tensors in few launches. Per value, with float32 operations that are

@@ -96,8 +96,8 @@ def _load() -> C.CDLL:
         "tb_distill": [P, I32, I64, I32, I64, C.c_float, P, P, I32, I32, P, P, P, I64, P, I64, P],
         "tb_linear_xent": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, I64, P, I64, P, P,
                            I64, P],
-        "tb_linear_xent_grad": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, P, I64, P,
-                                I64, P, P, I64, P],
+        "tb_linear_xent_grad": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, I32, P, P,
+                                I64, P, I64, P, P, I64, P],
         "tb_adamw_step": [P, I32, I32, I32, C.c_double, C.c_double, C.c_double, C.c_double,
                           C.c_double, I64, P, P, P, C.c_uint32, P],
         "tb_adamw_moments": [P, I32, P, P, P],
@@ -773,8 +773,9 @@ class _device_of:
 
 
 def _same_device(first, **others) -> None:
+    index = first.get_device()
     for name, t in others.items():
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != index:
             raise ValueError(f"{name} is on {t.device}, x on {first.device}")
 
 
@@ -868,11 +869,21 @@ def _like_bias(db, w):
     return _dptr(db, w.dtype, "db")
 
 
+def _spread(t, n: int, name: str):
+    """(device pointer, step from row to row) of one value a row, or of one for all."""
+    if t is not None and n > 1 and t.numel() == n and not any(t.stride()):
+        if t.dtype is not _F32 or not t.is_cuda:
+            raise ValueError(f"{name} must be a float32 device tensor")
+        return t.data_ptr(), 0
+    return _one(t, n, name), 1
+
+
 def tb_linear_xent_grad(x, w, target, lse, d_loss=None, d_lse=None, dx=None, dw=None, db=None,
                         bias=None, weight=None, workspace=None, stream=None,
                         lse_low=None) -> None:
     """Gradients from those of loss and lse; lse and lse_low: out_lse and out_low (or
-    None) of tb_linear_xent for the same layer and rows."""
+    None) of tb_linear_xent for the same layer and rows. d_loss may be one value that
+    is expanded to all rows."""
     layer = _layer(x, w, bias)
     n = layer[4]
     _same_device(x, w=w, bias=bias, target=target, weight=weight, lse=lse, lse_low=lse_low,
@@ -884,8 +895,7 @@ def tb_linear_xent_grad(x, w, target, lse, d_loss=None, d_lse=None, dx=None, dw=
         ws, ws_bytes, keep = _linear_workspace(x, layer, dx, dw, db, 1, workspace, stream)
         _check(LIB.tb_linear_xent_grad(*layer, _target(target, n), _one(weight, n, "weight"),
                                        _one(lse, n, "lse"), _one(lse_low, n, "lse_low"),
-                                       _one(d_loss, n, "d_loss"),
-                                       _one(d_lse, n, "d_lse"), *_like(dx, x, "dx"),
+                                       *_spread(d_loss, n, "d_loss"), _one(d_lse, n, "d_lse"), *_like(dx, x, "dx"),
                                        *_like(dw, w, "dw"), p_db, ws, ws_bytes, _stream(stream)))
 
 

@@ -89,7 +89,8 @@ int linear_call(const linear::Call& c, void* workspace, int64_t workspace_bytes,
   if (c.dw && (r = check_matrix(c.dw, c.dtype, c.dw_stride, c.D, "dw"))) return r;
   if (c.db && !aligned(c.db, size)) return fail(TB_EINVAL, "db misaligned");
   if (!any && !c.dw && !c.db) return TB_OK;
-  const int64_t need = linear::workspace_bytes(c);
+  const linear::Layout plan = linear::plan(c);
+  const int64_t need = plan.total;
   if (!workspace || workspace_bytes < need)
     return fail(TB_ENOMEM, "workspace holds " + std::to_string(workspace ? workspace_bytes : 0) +
                                " bytes, the call needs " + std::to_string(need));
@@ -111,10 +112,10 @@ int linear_call(const linear::Call& c, void* workspace, int64_t workspace_bytes,
                       {c.weight, c.n * 4, "weight"},
                       {c.lse, c.n * 4, "lse"},
                       {c.lse_low, c.n * 4, "lse_low"},
-                      {c.d_loss, c.n * 4, "d_loss"},
+                      {c.d_loss, c.d_step ? c.n * 4 : 4, "d_loss"},
                       {c.d_lse, c.n * 4, "d_lse"}};
   if ((r = check_apart(bufs, 7))) return r;
-  const hipError_t e = linear::run(c, workspace, static_cast<hipStream_t>(hip_stream));
+  const hipError_t e = linear::run(c, plan, workspace, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return hip_fail(e, what);
   return TB_OK;
 }
@@ -155,7 +156,7 @@ extern "C" int tb_linear_xent(const void* x, const void* w, const void* bias, in
   if (!out_loss && !out_lse && !out_low && !dx && !dw && !db)
     return fail(TB_EINVAL, "every output is NULL");
   const linear::Call c = {x,      w,      bias,    dtype,   n_rows,   width,   v_plus_blank,
-                          x_stride, w_stride, target, weight, nullptr, nullptr, nullptr, nullptr,
+                          x_stride, w_stride, target, weight, nullptr, nullptr, 0, nullptr, nullptr,
                           out_loss, out_lse, out_low, dx, dw, db, dx_stride, dw_stride};
   return linear_call(c, workspace, workspace_bytes, hip_stream, "linear_xent launch");
 }
@@ -164,14 +165,16 @@ extern "C" int tb_linear_xent_grad(const void* x, const void* w, const void* bia
                                    int64_t n_rows, int32_t width, int32_t v_plus_blank,
                                    int64_t x_stride, int64_t w_stride, const int32_t* target,
                                    const float* weight, const float* lse, const float* lse_low,
-                                   const float* d_loss, const float* d_lse, void* dx, int64_t dx_stride, void* dw,
+                                   const float* d_loss, int32_t d_loss_step,
+                                   const float* d_lse, void* dx, int64_t dx_stride, void* dw,
                                    int64_t dw_stride, void* db, void* workspace,
                                    int64_t workspace_bytes, void* hip_stream) {
   if (!dx && !dw && !db) return fail(TB_EINVAL, "dx, dw and db are all NULL");
   if (!lse && n_rows > 0) return fail(TB_EINVAL, "lse is NULL");
+  if (d_loss_step != 0 && d_loss_step != 1) return fail(TB_EINVAL, "d_loss_step must be 0 or 1");
   static const float none = 0.f;  // (without rows nothing reads it)
   const linear::Call c = {x,      w,      bias,    dtype,   n_rows,   width,   v_plus_blank,
-                          x_stride, w_stride, target, weight, d_loss, d_lse, lse ? lse : &none, lse_low,
+                          x_stride, w_stride, target, weight, d_loss, d_lse, d_loss_step, lse ? lse : &none, lse_low,
                           nullptr, nullptr, nullptr, dx, dw, db, dx_stride, dw_stride};
   return linear_call(c, workspace, workspace_bytes, hip_stream, "linear_xent_grad launch");
 }

@@ -16,6 +16,7 @@ struct Gather {
   int32_t C;
   const int32_t* target;
   const float *weight, *d_loss, *d_lse, *lse, *lse_low;
+  int32_t d_step;
   bool grads;
   Meta* meta;
   int32_t* counts;  // per group: rows that take part ...
@@ -57,7 +58,7 @@ __device__ __forceinline__ Row row_of(const Gather& g, int64_t r) {
   o.a = o.b = w;
   bool keep = o.target != -1 && w != 0.f;
   if (g.grads) {
-    if (g.d_loss) o.b = w * g.d_loss[r];
+    if (g.d_loss) o.b = w * g.d_loss[r * g.d_step];
     o.a = o.b + (g.d_lse ? g.d_lse[r] : 0.f);
     // a row without a gradient is left out, unless its loss is asked for
     if (g.lse) keep = keep && (o.a != 0.f || o.b != 0.f);
@@ -692,10 +693,6 @@ int32_t few_rows(bool f32, bool grads) { return grads ? 16 : f32 ? 64 : 32; }
 // and in tiles of 256 alone: 1511 bfloat16 rows of 336 against 612 tokens 52 and 86 us, 1000
 // float32 rows of 512 against 4097 124 and 158, 16,000 against 1025 292 and 326; chosen so
 // and without parts: the last 292 and 400, 300 bfloat16 rows of 1024 against 50,001 230 and 490.
-struct Cut {
-  int32_t tile, parts;
-  double cost;
-};
 Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
   Cut best = {256, 1, 0};
   const struct {
@@ -722,10 +719,6 @@ Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
 // 1024 float32 against 32,769 tokens 1483 us, and 1666 without; of 2000 x 512 bfloat16
 // against 8193 165 and 182).
 constexpr int64_t kRest = 64;  // tokens that may be on their own
-struct Strips {
-  int32_t main;  // tokens of the first
-  Cut cut[2];
-};
 Strips strips(int64_t tokens, int64_t others, int64_t steps, int64_t stages, bool parts) {
   Strips s = {(int32_t)tokens, {cut(tokens, others, steps, stages, parts), {64, 1, 0}}};
   const int64_t rest = tokens % 256, main = tokens - rest;
@@ -736,20 +729,7 @@ Strips strips(int64_t tokens, int64_t others, int64_t steps, int64_t stages, boo
   return s;
 }
 
-struct Layout {
-  int64_t np, dp, planes;      // gathered rows and values a row, rounded up
-  bool copy_w, few, gather, paired, kept;      // kept: the logits, from the statistics to their gradients
-  int32_t n_part;
-  // tokens of a piece of the vocabulary (of all but the last), and of a row of gradients
-  int32_t piece, pieces, ldg;
-  Strips stats, grad, w;       // of the products with tokens of their own ...
-  Cut grad_all, w_all;         // (pieces but the last)
-  Cut x;                       // ... and that which sums over them
-  int32_t kept_rows;           // of a workgroup that makes gradients of kept logits
-  bool direct;                 // dx leaves its product's sums as it is
-  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, most, hit, part, px, pxm, pw, z, G, acc_x;
-  int64_t acc_w, col, total;
-};
+}  // namespace
 
 Layout plan(const Call& c) {
   Layout L = {};
@@ -843,15 +823,16 @@ Layout plan(const Call& c) {
   return L;
 }
 
+namespace {
+
 unsigned blocks(int64_t work) {
   const int64_t b = (work + 255) / 256;
   return (unsigned)(b < 1 ? 1 : b > 8192 ? 8192 : b);
 }
 
 template <class T>
-hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
+hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
   constexpr bool f32 = sizeof(T) == 4;
-  const Layout L = plan(c);
   const bool grads = c.dx || c.dw || c.db;
   Meta* meta = reinterpret_cast<Meta*>(ws + L.meta);
   auto i32 = [&](int64_t at) { return reinterpret_cast<int32_t*>(ws + at); };
@@ -862,7 +843,7 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
   float *r = f32 ? flt(L.r) : nullptr, *m = f32 ? flt(L.m) : nullptr;
   const int64_t groups = (c.n + group_rows(c.n) - 1) / group_rows(c.n);
   const int rows = groups > 1 ? kRowsMany : kRowsOnly;
-  const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse, c.lse_low,
+  const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse, c.lse_low, c.d_step,
                      grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
                      a,      b,    lse, r, m, c.out_loss, c.out_lse, c.out_low,
                      c.x_stride, c.D, (int32_t)L.dp, u16(L.px),
@@ -1061,20 +1042,19 @@ hipError_t run_t(const Call& c, char* ws, hipStream_t st) {
 
 }  // namespace
 
-int64_t workspace_bytes(const Call& c) { return plan(c).total; }
-
 int64_t most_workspace(Call c) {
-  // wherever x lies
+  // wherever x lies, which few rows' kernel goes by
   c.x_stride = c.w_stride;
   c.x = nullptr;
   const int64_t aligned = plan(c).total;
+  if (c.n > few_rows(true, false)) return aligned;
   c.x = reinterpret_cast<const void*>(1);
   return std::max(aligned, plan(c).total);
 }
 
-hipError_t run(const Call& c, void* workspace, hipStream_t st) {
+hipError_t run(const Call& c, const Layout& L, void* workspace, hipStream_t st) {
   char* ws = static_cast<char*>(workspace);
-  return c.dtype == TB_F32 ? run_t<float>(c, ws, st) : run_t<uint16_t>(c, ws, st);
+  return c.dtype == TB_F32 ? run_t<float>(c, L, ws, st) : run_t<uint16_t>(c, L, ws, st);
 }
 
 }  // namespace linear

@@ -156,17 +156,44 @@ struct Call {
   int64_t x_stride, w_stride;
   const int32_t* target;
   const float *weight, *d_loss, *d_lse;
+  int32_t d_step;    // from row to row of d_loss: 1, or 0 for one value
   const float *lse, *lse_low;  // of an earlier call, or NULL: computed here
   float *out_loss, *out_lse, *out_low;
   void *dx, *dw, *db;
   int64_t dx_stride, dw_stride;
 };
 
-// Bytes of workspace that a call needs, and that suffice for every x of its sizes; the
-// launches of a call.
-int64_t workspace_bytes(const Call& c);
+// How a product is cut into tiles, and in which parts of the summed axis.
+struct Cut {
+  int32_t tile, parts;
+  double cost;
+};
+// The tokens of a product: those in whole tiles of 256, and the few behind them.
+struct Strips {
+  int32_t main;  // tokens of the first
+  Cut cut[2];
+};
+// How a call is done, and where its buffers lie in the workspace.
+struct Layout {
+  int64_t np, dp, planes;      // gathered rows and values a row, rounded up
+  bool copy_w, few, gather, paired, kept;      // kept: the logits, from the statistics to their gradients
+  int32_t n_part;
+  // tokens of a piece of the vocabulary (of all but the last), and of a row of gradients
+  int32_t piece, pieces, ldg;
+  Strips stats, grad, w;       // of the products with tokens of their own ...
+  Cut grad_all, w_all;         // (pieces but the last)
+  Cut x;                       // ... and that which sums over them
+  int32_t kept_rows;           // of a workgroup that makes gradients of kept logits
+  bool direct;                 // dx leaves its product's sums as it is
+  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, most, hit, part, px, pxm, pw, z, G, acc_x;
+  int64_t acc_w, col, total;
+};
+
+// The plan of a call (its workspace: `total` bytes); the bytes that suffice for every x of
+// a call's sizes; the launches.
+Layout plan(const Call& c);
 int64_t most_workspace(Call c);
-hipError_t run(const Call& c, void* workspace, hipStream_t st);
+hipError_t run(const Call& c, const Layout& L, void* workspace, hipStream_t st);
 
 }  // namespace linear
 }  // namespace tbias

@@ -39,8 +39,8 @@ def _args(x, w, target, bias, weight):
         raise ValueError("target must be [...] for x [..., width]")
     if weight is not None and weight.shape != lead:
         raise ValueError("weight must be [...] for x [..., width]")
-    return (_even(x.detach(), "x"), _even(w.detach(), "w"), target.contiguous(),
-            None if bias is None else bias.detach().contiguous(),
+    return (_even(x, "x"), _even(w, "w"), target.contiguous(),
+            None if bias is None else bias.contiguous(),
             None if weight is None else weight.contiguous())
 
 
@@ -76,12 +76,14 @@ class _LinearXent(torch.autograd.Function):
     def backward(ctx, d_loss, d_lse):
         x, w, target, bias, weight, lse, low = ctx.saved_tensors
         need_x, need_w, _, need_b, _ = ctx.needs_input_grad
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
-        dw = torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None
+        dx = x.new_empty(x.shape) if need_x else None
+        dw = w.new_empty(w.shape) if need_w else None
         db = torch.empty_like(bias) if need_b else None
         if d_loss is None:
             d_loss = torch.zeros_like(lse)
-        capi.tb_linear_xent_grad(x, w, target, lse, d_loss.contiguous(),
+        elif any(d_loss.stride()):  # (a sum's gradient is one value, expanded)
+            d_loss = d_loss.contiguous()
+        capi.tb_linear_xent_grad(x, w, target, lse, d_loss,
                                  None if d_lse is None else d_lse.contiguous(), dx, dw, db,
                                  bias=bias, weight=weight, lse_low=low)
         return tuple(None if g is None else _once(g) for g in (dx, dw, None, db, None))
@@ -111,9 +113,7 @@ def linear_xent_step(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
     None without one) in one call."""
     x, w, target, bias, weight = _args(x, w, target, bias, weight)
     loss = torch.empty(target.shape, dtype=torch.float32, device=x.device)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
+    dx, dw = x.new_empty(x.shape), w.new_empty(w.shape)
     db = None if bias is None else torch.empty_like(bias)
-    capi.tb_linear_xent(x, w, target, loss, None, dx, dw, db, bias=bias,
-                        weight=None if weight is None else weight.detach())
+    capi.tb_linear_xent(x, w, target, loss, None, dx, dw, db, bias=bias, weight=weight)
     return loss, dx, dw, db

@@ -181,6 +181,18 @@ def test_gradients_of_few_bfloat16_rows(n, D, C):
     check_all(grad(c, got["lse"], torch.ones(n, device="cuda"), None), want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [1, 2, 300, 3000])
+def test_one_gradient_for_all_rows(n, dtype):
+    """A loss gradient that is one value, expanded: the same bits as one a row."""
+    c = R.case(n, 64, 300, dtype, 7, device="cuda", gaps=True)
+    lse = step(c, ())["lse"]
+    one = torch.full((1,), 0.75, device="cuda")
+    for name, value in grad(c, lse, one.expand(n), None).items():
+        again = grad(c, lse, one.repeat(n), None)[name]
+        assert bool((value == again).all()), name
+
+
 def test_two_calls_at_once():
     cases = [R.case(n, 256, C, dtype, 2, device="cuda", gaps=True)
              for n, C, dtype in ((900, 4097, BF16), (700, 3001, F32))]
