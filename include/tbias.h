@@ -672,8 +672,8 @@ int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus
  * tb_linear_xent_workspace_bytes - for a call with these arguments; grads: sum of 1
  *   (dx), 2 (dw) and 4 (db), 0 for the loss alone; with_lse: 1 for
  *   tb_linear_xent_grad, else 0. w is not read: its address and stride say whether its
- *   rows can be used where they are (16-byte aligned, width a multiple of 64,
- *   TB_BF16) or need a copy. -1 for arguments that the calls reject.
+ *   rows can be used where they are (16-byte aligned, up to 2^22 values apart, width a
+ *   multiple of 64, TB_BF16) or need a copy. -1 for arguments that the calls reject.
  */
 int64_t tb_linear_xent_workspace_bytes(int32_t dtype, int64_t n_rows, int32_t width,
                                        int32_t v_plus_blank, const void* w, int64_t w_stride,

@@ -94,8 +94,8 @@ def _load() -> C.CDLL:
         "tb_token_logprobs_grad": [P, I32, I64, I32, I64, C.c_float, P, I32, P, P, P, P, I64, P,
                                    I64, P],
         "tb_distill": [P, I32, I64, I32, I64, C.c_float, P, P, I32, I32, P, P, P, I64, P, I64, P],
-        "tb_linear_xent": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, I64, P, I64, P, P,
-                           I64, P],
+        "tb_linear_xent": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, P, I64, P, I64,
+                           P, P, I64, P],
         "tb_linear_xent_grad": [P, P, P, I32, I64, I32, I32, I64, I64, P, P, P, P, P, I32, P, P,
                                 I64, P, I64, P, P, I64, P],
         "tb_adamw_step": [P, I32, I32, I32, C.c_double, C.c_double, C.c_double, C.c_double,
@@ -895,7 +895,8 @@ def tb_linear_xent_grad(x, w, target, lse, d_loss=None, d_lse=None, dx=None, dw=
         ws, ws_bytes, keep = _linear_workspace(x, layer, dx, dw, db, 1, workspace, stream)
         _check(LIB.tb_linear_xent_grad(*layer, _target(target, n), _one(weight, n, "weight"),
                                        _one(lse, n, "lse"), _one(lse_low, n, "lse_low"),
-                                       *_spread(d_loss, n, "d_loss"), _one(d_lse, n, "d_lse"), *_like(dx, x, "dx"),
+                                       *_spread(d_loss, n, "d_loss"), _one(d_lse, n, "d_lse"),
+                                       *_like(dx, x, "dx"),
                                        *_like(dw, w, "dw"), p_db, ws, ws_bytes, _stream(stream)))
 
 

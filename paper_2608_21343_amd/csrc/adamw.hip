@@ -14,11 +14,11 @@
 // What bounds it, in 235 million bfloat16 values of 290 tensors: with 32-bit states and copies
 // its bytes (28 a value, 1.35 ms, 4.9 TB/s; a large copy runs at 5.3), with 8-bit states (10 a
 // value) its instructions (0.62 ms, 3.8 TB/s), reading the moments their bytes (0.45 ms for 10
-// a value, 5.2 TB/s). Up to 52 tensors go into a launch, since their records fit its arguments, so that a
-// table need not be copied to the device first, which a captured graph could not do again.
-// A lane takes 8 values at a time, 16-byte loads at any address, the next ones in flight
-// while it works: without that 1.40 ms and 0.78. Loads and stores that leave the caches
-// alone were slower (1.66 ms; 5 million float32 values 38 us instead of 25).
+// a value, 5.2 TB/s). Up to 52 tensors go into a launch, since their records fit its
+// arguments, so that a table need not be copied to the device first, which a captured graph
+// could not do again. A lane takes 8 values at a time, 16-byte loads at any address, the next
+// ones in flight while it works: without that 1.40 ms and 0.78. Loads and stores that leave
+// the caches alone were slower (1.66 ms; 5 million float32 values 38 us instead of 25).
 //
 // The moments' products and sums are rounded one by one, in float32, as the interface
 // states them, so the codes are the same wherever the same arithmetic runs.
@@ -216,7 +216,8 @@ __device__ __forceinline__ uint32_t encode_v(float v, float inverse, float rnd) 
   const int e = run_of<5>(root);
   const float low = floorf(__builtin_amdgcn_ldexpf(root, -e));
   const float over = __builtin_fmaf(-low, low, __builtin_amdgcn_ldexpf(y, -2 * e));
-  const uint32_t code = (e << 5) + (uint32_t)low + (over > __builtin_fmaf(2.f, low, 1.f) * rnd ? 1 : 0);
+  const bool up = over > __builtin_fmaf(2.f, low, 1.f) * rnd;
+  const uint32_t code = (e << 5) + (uint32_t)low + (up ? 1 : 0);
   return max(code, min(__float_as_uint(v), 1u));
 }
 

@@ -151,7 +151,8 @@ extern "C" int tb_linear_xent(const void* x, const void* w, const void* bias, in
                               int64_t n_rows, int32_t width, int32_t v_plus_blank,
                               int64_t x_stride, int64_t w_stride, const int32_t* target,
                               const float* weight, float* out_loss, float* out_lse,
-                              float* out_low, void* dx, int64_t dx_stride, void* dw, int64_t dw_stride, void* db,
+                              float* out_low, void* dx, int64_t dx_stride, void* dw,
+                              int64_t dw_stride, void* db,
                               void* workspace, int64_t workspace_bytes, void* hip_stream) {
   if (!out_loss && !out_lse && !out_low && !dx && !dw && !db)
     return fail(TB_EINVAL, "every output is NULL");
@@ -174,7 +175,8 @@ extern "C" int tb_linear_xent_grad(const void* x, const void* w, const void* bia
   if (d_loss_step != 0 && d_loss_step != 1) return fail(TB_EINVAL, "d_loss_step must be 0 or 1");
   static const float none = 0.f;  // (without rows nothing reads it)
   const linear::Call c = {x,      w,      bias,    dtype,   n_rows,   width,   v_plus_blank,
-                          x_stride, w_stride, target, weight, d_loss, d_lse, d_loss_step, lse ? lse : &none, lse_low,
+                          x_stride, w_stride, target, weight, d_loss, d_lse, d_loss_step,
+                          lse ? lse : &none, lse_low,
                           nullptr, nullptr, nullptr, dx, dw, db, dx_stride, dw_stride};
   return linear_call(c, workspace, workspace_bytes, hip_stream, "linear_xent_grad launch");
 }

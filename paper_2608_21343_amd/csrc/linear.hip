@@ -159,7 +159,8 @@ __device__ __forceinline__ void top_of(const Weights& g, const float* w, int at)
 }
 
 // Rows that take part; behind the groups of rows (float32) the weights' largest values.
-__global__ void __launch_bounds__(256) count_kernel(const Gather g, const Weights of, const float* w) {
+__global__ void __launch_bounds__(256)
+    count_kernel(const Gather g, const Weights of, const float* w) {
   const int groups = gridDim.x - (w ? kTops : 0);
   if ((int)blockIdx.x >= groups) {
     top_of(of, w, blockIdx.x - groups);
@@ -543,8 +544,8 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Weigh
 }
 
 // The gradients of logits that are kept: ROWS gathered rows by 256 tokens a workgroup, a
-// quarter of them a wave. The rows behind the last one, up to a multiple of kStep, get zeros, and so
-// do the tokens.
+// quarter of them a wave. The rows behind the last one, up to a multiple of kStep, get
+// zeros, and so do the tokens.
 struct Kept {
   const Meta* meta;
   const float* z;
@@ -723,7 +724,8 @@ Strips strips(int64_t tokens, int64_t others, int64_t steps, int64_t stages, boo
   Strips s = {(int32_t)tokens, {cut(tokens, others, steps, stages, parts), {64, 1, 0}}};
   const int64_t rest = tokens % 256, main = tokens - rest;
   if (rest == 0 || rest > kRest || main == 0) return s;
-  const Cut a = cut(main, others, steps, stages, parts), b = cut(rest, others, steps, stages, parts);
+  const Cut a = cut(main, others, steps, stages, parts);
+  const Cut b = cut(rest, others, steps, stages, parts);
   // (a launch of its own: 4 us)
   if (a.cost + b.cost + 3.0 < s.cut[0].cost) s = {(int32_t)main, {a, b}};
   return s;
@@ -791,7 +793,8 @@ Layout plan(const Call& c) {
     // (a few tokens more than whole tiles go with the last piece)
     L.piece = (int32_t)up(pieces == 1 ? c.C : (c.C - kRest + pieces - 1) / pieces, kTile);
     L.pieces = pieces == 1 ? 1 : (int32_t)((c.C - kRest + L.piece - 1) / L.piece);
-    const int32_t last = c.C - (L.pieces - 1) * L.piece, most = std::max(last, std::min(c.C, L.piece));
+    const int32_t last = c.C - (L.pieces - 1) * L.piece;
+    const int32_t most = std::max(last, std::min(c.C, L.piece));
     L.ldg = (int32_t)up(most, kTile);
     // Logits that the statistics write and the gradients read again (float32, up to 256 MB)
     // cost less than another product: a step of 16,000 x 512 float32 against 1025 tokens 292
@@ -843,7 +846,8 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
   float *r = f32 ? flt(L.r) : nullptr, *m = f32 ? flt(L.m) : nullptr;
   const int64_t groups = (c.n + group_rows(c.n) - 1) / group_rows(c.n);
   const int rows = groups > 1 ? kRowsMany : kRowsOnly;
-  const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,  c.d_lse, c.lse, c.lse_low, c.d_step,
+  const Gather ga = {c.n,    c.C,  c.target, c.weight,   c.d_loss,
+                     c.d_lse, c.lse, c.lse_low, c.d_step,
                      grads,  meta, i32(L.counts), flt(L.tops), idx, inv, tgt,
                      a,      b,    lse, r, m, c.out_loss, c.out_lse, c.out_low,
                      c.x_stride, c.D, (int32_t)L.dp, u16(L.px),
@@ -855,11 +859,13 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
   // (float32: it also clears what the others take maxima into)
   if (L.gather && (groups != 1 || f32)) {
     const bool tops = f32 && c.n > 0;
-    count_kernel<<<dim3((unsigned)(std::max<int64_t>(groups, 1) + (tops ? kTops : 0))), dim3(256), 0, st>>>(
+    const int64_t all = std::max<int64_t>(groups, 1) + (tops ? kTops : 0);
+    count_kernel<<<dim3((unsigned)all), dim3(256), 0, st>>>(
         ga, weights, tops ? static_cast<const float*>(c.w) : nullptr);
   }
   if (L.gather) {
-    const auto gather = groups > 1 ? &gather_kernel<T, kMany, kRowsMany> : &gather_kernel<T, kOnly, kRowsOnly>;
+    const auto gather = groups > 1 ? &gather_kernel<T, kMany, kRowsMany>
+                                   : &gather_kernel<T, kOnly, kRowsOnly>;
     const int more = !L.copy_w || c.n == 0 ? 0 : c.C < 8192 ? (c.C + 3) / 4 : 2048;
     gather<<<dim3((unsigned)(ga.blocks + more)), dim3(256), 0, st>>>(
         ga, static_cast<const T*>(c.x), weights, static_cast<const T*>(c.w));
@@ -891,8 +897,8 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
   Weighted weighted = {};
   if constexpr (f32) {
     if (c.dw && c.n > 0)
-      weighted = {static_cast<const float*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m, u16(L.pxm),
-                  (int32_t)(c.n < 8192 ? (c.n + 3) / 4 : 2048)};
+      weighted = {static_cast<const float*>(c.x), c.x_stride, c.D, (int32_t)L.dp, idx, m,
+                  u16(L.pxm), (int32_t)(c.n < 8192 ? (c.n + 3) / 4 : 2048)};
   }
   // (with lse at hand: the logits alone)
   if ((!c.lse || L.kept) && c.n > 0) {
@@ -921,8 +927,9 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   if (!c.lse && c.n > 0) {
-    const Finish f = {meta,  reinterpret_cast<float2*>(ws + L.part), L.n_part, flt(L.hit), L.gather ? idx : nullptr, c.target,
-                      L.few, (int32_t)c.n, c.C, c.weight, lse, a, b, c.out_loss, c.out_lse, c.out_low};
+    const Finish f = {meta, reinterpret_cast<float2*>(ws + L.part), L.n_part, flt(L.hit),
+                      L.gather ? idx : nullptr, c.target, L.few, (int32_t)c.n, c.C, c.weight,
+                      lse, a, b, c.out_loss, c.out_lse, c.out_low};
     const int lanes = L.n_part <= 128 ? 16 : c.n <= 1024 && L.n_part >= 256 ? 256 : 64;
     const auto finish =
         lanes == 16 ? &finish_kernel<16> : lanes == 64 ? &finish_kernel<64> : &finish_kernel<256>;

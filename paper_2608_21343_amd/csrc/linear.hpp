@@ -176,7 +176,8 @@ struct Strips {
 // How a call is done, and where its buffers lie in the workspace.
 struct Layout {
   int64_t np, dp, planes;      // gathered rows and values a row, rounded up
-  bool copy_w, few, gather, paired, kept;      // kept: the logits, from the statistics to their gradients
+  bool copy_w, few, gather, paired;
+  bool kept;                   // the logits, from the statistics to their gradients
   int32_t n_part;
   // tokens of a piece of the vocabulary (of all but the last), and of a row of gradients
   int32_t piece, pieces, ldg;
@@ -185,8 +186,8 @@ struct Layout {
   Cut x;                       // ... and that which sums over them
   int32_t kept_rows;           // of a workgroup that makes gradients of kept logits
   bool direct;                 // dx leaves its product's sums as it is
-  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, most, hit, part, px, pxm, pw, z, G, acc_x;
-  int64_t acc_w, col, total;
+  int64_t meta, counts, tops, idx, inv, tgt, a, b, lse, r, m, most, hit, part, px, pxm, pw;
+  int64_t z, G, acc_x, acc_w, col, total;
 };
 
 // The plan of a call (its workspace: `total` bytes); the bytes that suffice for every x of

@@ -660,7 +660,8 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
       }
       if (g.col) {
         // the tile's columns: over the lane's rows, 16 lanes, and the four waves through LDS
-        float* sums = reinterpret_cast<float*>(smem + kStages * Ti::kStageBytes + kSets * sizeof(Params<N>));
+        float* sums = reinterpret_cast<float*>(smem + kStages * Ti::kStageBytes +
+                                               kSets * sizeof(Params<N>));
         float m[FQ];
 #pragma unroll
         for (int j = 0; j < FQ; ++j) m[j] = El::kScaled ? par.m[wq + 16 * j + lq] : 1.f;

@@ -19,9 +19,10 @@ class AdamW(torch.optim.Optimizer):
     ``master`` keeps a float32 copy of bfloat16 parameters, which the steps
     update. ``capturable``: the number of the step lives on the device, so that a
     captured graph of ``step`` can be replayed as a training loop, once a first
-    step has made the states; every parameter then needs a gradient in every step, and a learning rate that
-    changes is a device tensor of one float32. ``step(grad_scale=...)`` takes a device
-    tensor of one float32 that multiplies the gradients, as clipping needs it."""
+    step has made the states; every parameter then needs a gradient in every step,
+    and a learning rate that changes is a device tensor of one float32.
+    ``step(grad_scale=...)`` takes a device tensor of one float32 that multiplies the
+    gradients, as clipping needs it."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, state_bits: int = 32, master: bool = False,

@@ -62,8 +62,8 @@ def xent(lib, **change):
 
 def xent_grad(lib, **change):
     a = dict(x=P, w=2 * P, bias=0, dtype=1, n=4, D=64, V1=100, xs=64, ws=64, target=3 * P,
-             weight=0, lse=4 * P, low=0, dl=0, dls=1, dlse=0, dx=7 * P, dxs=64, dw=0, dws=64, db=0, wk=9 * P,
-             wkb=BIG, st=0)
+             weight=0, lse=4 * P, low=0, dl=0, dls=1, dlse=0, dx=7 * P, dxs=64, dw=0,
+             dws=64, db=0, wk=9 * P, wkb=BIG, st=0)
     a.update(change)
     return lib.tb_linear_xent_grad(*a.values())
 
@@ -99,10 +99,13 @@ def test_refusals_of_either():
             (xent, dict(loss=0, lse=0), "every output"), (xent, dict(loss=4 * P + 2), "out_loss"),
             (xent, dict(lse=4 * P), "out_loss overlaps out_lse"),
             (xent, dict(wk=4 * P), "overlaps workspace"),
-            (xent, dict(low=5 * P + 2), "out_low"), (xent, dict(low=5 * P), "out_lse overlaps out_low"),
-            (xent_grad, dict(low=P + 2), "lse_low"), (xent_grad, dict(low=7 * P), "dx overlaps lse_low"),
+            (xent, dict(low=5 * P + 2), "out_low"),
+            (xent, dict(low=5 * P), "out_lse overlaps out_low"),
+            (xent_grad, dict(low=P + 2), "lse_low"),
+            (xent_grad, dict(low=7 * P), "dx overlaps lse_low"),
             (xent_grad, dict(dx=0), "all NULL"), (xent_grad, dict(lse=0), "lse is NULL"),
-            (xent_grad, dict(dls=2), "d_loss_step"), (xent_grad, dict(dl=7 * P, dls=0), "dx overlaps d_loss"),
+            (xent_grad, dict(dls=2), "d_loss_step"),
+            (xent_grad, dict(dl=7 * P, dls=0), "dx overlaps d_loss"),
             (xent_grad, dict(dl=P + 2), "d_loss"), (xent_grad, dict(dlse=P + 2), "d_lse"),
             (xent_grad, dict(dx=4 * P), "dx overlaps lse")):
         assert call(capi.LIB, **change) != 0
@@ -235,5 +238,6 @@ def test_workspace_of_far_rows():
     from paper_2608_21343_amd import capi
     f = capi.LIB.tb_linear_xent_workspace_bytes
     for grads in (0, 7):
-        near, far = (f(1, 1000, 640, 8193, P, stride, grads, 0) for stride in (1 << 22, (1 << 22) + 8))
+        near, far = (f(1, 1000, 640, 8193, P, stride, grads, 0)
+                     for stride in (1 << 22, (1 << 22) + 8))
         assert 8193 * 640 * 2 <= far - near <= 8193 * 640 * 2 + 256
