@@ -789,8 +789,8 @@ Layout plan(const Call& c) {
     // pieces of the vocabulary of about kGradBytes of gradients, of equal sizes
     const int64_t all = L.planes * L.np * 2 * c.C;
     int64_t pieces = (all + kGradBytes / 2) / kGradBytes;
-    pieces = pieces < 1 ? 1 : pieces;
-    // (a few tokens more than whole tiles go with the last piece)
+    // (a few tokens more than whole tiles go with the last piece, and none is without a tile)
+    pieces = std::max<int64_t>(std::min(pieces, (c.C - kRest + kTile - 1) / kTile), 1);
     L.piece = (int32_t)up(pieces == 1 ? c.C : (c.C - kRest + pieces - 1) / pieces, kTile);
     L.pieces = pieces == 1 ? 1 : (int32_t)((c.C - kRest + L.piece - 1) / L.piece);
     const int32_t last = c.C - (L.pieces - 1) * L.piece;

@@ -1,0 +1,26 @@
+"""The workspace of the output layer's calls: how a call is laid out is decided on the
+host, so no GPU is needed to ask for every size."""
+
+import itertools
+
+import pytest
+
+P = 1 << 20  # an aligned address that nothing reads
+F32, BF16 = 0, 1
+
+
+def need(dtype, n, D, C, grads, with_lse=0, w=P, stride=None):
+    from paper_2608_21343_amd import capi
+    return capi.LIB.tb_linear_xent_workspace_bytes(dtype, n, D, C, w, stride or D, grads, with_lse)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_every_size_has_a_plan(dtype):
+    """Few tokens with millions of rows, whose gradients take more than one piece, among them."""
+    tokens = [*range(2, 70), 127, 128, 129, 255, 256, 257, 300, 319, 320, 321, 383, 384, 385, 511,
+              512, 513, 576, 577, 1025, 4097, 32769, 131073, (1 << 20) - 255, 1 << 20]
+    rows = [0, 1, 2, 17, 33, 64, 65, 257, 4096, 70001, 350_000, 400_000, 800_000, 1_600_000,
+            3_500_000, 1 << 23, 1 << 24]
+    for C, n, D in itertools.product(tokens, rows, (1, 64, 513)):
+        for grads, with_lse in itertools.product((0, 1, 2, 4, 7), (0, 1)):
+            assert need(dtype, n, D, C, grads, with_lse) > 0, (n, D, C, grads, with_lse)
