@@ -799,7 +799,8 @@ Layout plan(const Call& c) {
     // Logits that the statistics write and the gradients read again (float32, up to 256 MB)
     // cost less than another product: a step of 16,000 x 512 float32 against 1025 tokens 292
     // us instead of 313, of 300 x 1024 bfloat16 against 50,001 230 instead of 258.
-    L.paired = !f32 && L.pieces == 1 && c.n <= kPair;
+    // (a call without rows has no place for a second set of them)
+    L.paired = !f32 && L.pieces == 1 && c.n > 0 && c.n <= kPair;
     L.kept = (!c.lse || L.few || L.paired) && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
     L.G = take(L.planes * L.np * L.ldg * 2);
     // (by 16 rows where 64 would leave CUs idle: a step of 1511 bfloat16 rows of 336 against 612
