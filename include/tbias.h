@@ -641,7 +641,8 @@ int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus
  *   x, w          device, row i at i * stride elements (stride >= width), aligned to
  *                 their type
  *   bias          device[V+1], or NULL (0)
- *   n_rows        in [0, 2^24]; width in [1, 2^16]; v_plus_blank in [2, TB_MAX_ROW]
+ *   n_rows        in [0, 2^24] (0: dw and db become 0, and every output may be NULL);
+ *                 width in [1, 2^16]; v_plus_blank in [2, TB_MAX_ROW]
  *   target        device int32[n_rows]; -1: the row is left out
  *   weight        device float[n_rows], or NULL (1); 0: the row is left out
  *   dx, dw, db    device, of type dtype, or NULL; rows of dx and dw at their strides,

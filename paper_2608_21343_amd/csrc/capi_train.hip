@@ -154,7 +154,7 @@ extern "C" int tb_linear_xent(const void* x, const void* w, const void* bias, in
                               float* out_low, void* dx, int64_t dx_stride, void* dw,
                               int64_t dw_stride, void* db,
                               void* workspace, int64_t workspace_bytes, void* hip_stream) {
-  if (!out_loss && !out_lse && !out_low && !dx && !dw && !db)
+  if (n_rows > 0 && !out_loss && !out_lse && !out_low && !dx && !dw && !db)
     return fail(TB_EINVAL, "every output is NULL");
   const linear::Call c = {x,      w,      bias,    dtype,   n_rows,   width,   v_plus_blank,
                           x_stride, w_stride, target, weight, nullptr, nullptr, 0, nullptr, nullptr,
@@ -170,7 +170,7 @@ extern "C" int tb_linear_xent_grad(const void* x, const void* w, const void* bia
                                    const float* d_lse, void* dx, int64_t dx_stride, void* dw,
                                    int64_t dw_stride, void* db, void* workspace,
                                    int64_t workspace_bytes, void* hip_stream) {
-  if (!dx && !dw && !db) return fail(TB_EINVAL, "dx, dw and db are all NULL");
+  if (n_rows > 0 && !dx && !dw && !db) return fail(TB_EINVAL, "dx, dw and db are all NULL");
   if (!lse && n_rows > 0) return fail(TB_EINVAL, "lse is NULL");
   if (d_loss_step != 0 && d_loss_step != 1) return fail(TB_EINVAL, "d_loss_step must be 0 or 1");
   static const float none = 0.f;  // (without rows nothing reads it)

@@ -24,3 +24,12 @@ def test_every_size_has_a_plan(dtype):
     for C, n, D in itertools.product(tokens, rows, (1, 64, 513)):
         for grads, with_lse in itertools.product((0, 1, 2, 4, 7), (0, 1)):
             assert need(dtype, n, D, C, grads, with_lse) > 0, (n, D, C, grads, with_lse)
+
+
+def test_calls_without_rows_need_no_output():
+    """The binding passes NULL for an output of no values."""
+    from paper_2608_21343_amd import capi
+    assert capi.LIB.tb_linear_xent(0, 2 * P, 0, 1, 0, 64, 100, 64, 64, 0, 0, 0, 0, 0, 0, 64, 0, 64,
+                                   0, 0, 0, 0) == 0
+    assert capi.LIB.tb_linear_xent_grad(0, 2 * P, 0, 1, 0, 64, 100, 64, 64, 0, 0, 0, 0, 0, 1, 0, 0,
+                                        64, 0, 64, 0, 0, 0, 0) == 0
