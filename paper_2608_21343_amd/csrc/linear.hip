@@ -816,8 +816,12 @@ Layout plan(const Call& c) {
       // (the last piece's cut: all others have whole tiles)
       L.w = strips(last, L.dp, L.np / kStep, stages, true);
       L.w_all = cut(L.piece, L.dp, L.np / kStep, stages, true);
-      const int32_t parts = std::max({L.w.cut[0].parts, L.w.cut[1].parts, L.w_all.parts});
-      if (parts > 1) L.acc_w = take(parts * (int64_t)L.ldg * L.dp * 4);
+      // (strip by strip: the one token behind whole tiles may be summed in many parts)
+      auto sums = [&](int64_t tokens, const Cut& cut) {
+        return cut.parts > 1 ? cut.parts * tokens * L.dp * 4 : 0;
+      };
+      L.acc_w = take(std::max({sums(L.w.main, L.w.cut[0]), sums(last - L.w.main, L.w.cut[1]),
+                               L.pieces > 1 ? sums(L.piece, L.w_all) : 0}));
     }
     L.grad = strips(last, c.n, L.dp / kStep, stages, false);
     L.grad_all = cut(L.piece, c.n, L.dp / kStep, stages, false);
@@ -1024,7 +1028,7 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
           return f32 ? dw_f32(w, st) : dw_bf16(w, st);
         }
         w.acc = flt(L.acc_w);
-        w.acc_split = (int64_t)L.ldg * L.dp;
+        w.acc_split = (int64_t)n * L.dp;
         w.lda = (int32_t)L.dp;
         const hipError_t r = f32 ? dw_f32(w, st) : dw_bf16(w, st);
         if (r != hipSuccess) return r;

@@ -52,3 +52,21 @@ def test_nothing_is_written_behind_the_workspace(n, D, C, dtype):
         capi.tb_linear_xent_grad(c["x"], c["w"], c["target"], lse, **out, bias=c["bias"],
                                  weight=c["weight"], workspace=ws)
         assert untouched(whole, need), (names, "gradients alone")
+
+
+@pytest.mark.parametrize("dtype, n, D, C", [(BF16, 4096, 256, 16385), (F32, 2048, 128, 8193),
+                                            (F32, 1500, 64, 4096 + 64), (BF16, 300, 64, 40001)])
+def test_sums_in_parts_stay_in_their_place(dtype, n, D, C):
+    """Tokens behind whole tiles whose dw is summed in parts."""
+    from paper_2608_21343_amd import capi
+    c = R.case(n, D, C, dtype, 2, device="cuda")
+    want = R.expected(c)
+    for names in (("dw",), ("dx", "dw", "db")):
+        grads = sum({"dx": 1, "dw": 2, "db": 4}[k] for k in names)
+        need = capi.tb_linear_xent_workspace_bytes(c["x"], c["w"], grads)
+        ws, whole = guarded(need, 255)
+        out, loss = outputs(c, names), torch.empty(n, device="cuda")
+        capi.tb_linear_xent(c["x"], c["w"], c["target"], loss, None, **out, bias=c["bias"],
+                            workspace=ws)
+        assert untouched(whole, need)
+        check_all(dict(out, loss=loss), want)

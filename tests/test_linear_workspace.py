@@ -33,3 +33,15 @@ def test_calls_without_rows_need_no_output():
                                    0, 0, 0, 0) == 0
     assert capi.LIB.tb_linear_xent_grad(0, 2 * P, 0, 1, 0, 64, 100, 64, 64, 0, 0, 0, 0, 0, 1, 0, 0,
                                         64, 0, 64, 0, 0, 0, 0) == 0
+
+
+@pytest.mark.parametrize("dtype, n, D, tokens", [
+    (BF16, 4096, 2048, 131072), (F32, 2048, 1024, 32768), (BF16, 16384, 1024, 8192),
+    (F32, 16000, 512, 1024)])
+@pytest.mark.parametrize("grads", [2, 3, 7])
+def test_a_token_behind_whole_tiles_takes_little(grads, dtype, n, D, tokens):
+    """The blank, one more than a multiple of 256: the copy of a token's weights, its parts of dw
+    (64 tokens in up to 64 parts), its gradients and their sums for every row."""
+    for with_lse in (0, 1):
+        even, odd = (need(dtype, n, D, C, grads, with_lse) for C in (tokens, tokens + 1))
+        assert odd <= even + 64 * 64 * D * 4 + 2 * 256 * n * 4 + (2 << 20)
