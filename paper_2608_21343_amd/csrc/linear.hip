@@ -694,7 +694,10 @@ int32_t few_rows(bool f32, bool grads) { return grads ? 16 : f32 ? 64 : 32; }
 // and in tiles of 256 alone: 1511 bfloat16 rows of 336 against 612 tokens 52 and 86 us, 1000
 // float32 rows of 512 against 4097 124 and 158, 16,000 against 1025 292 and 326; chosen so
 // and without parts: the last 292 and 400, 300 bfloat16 rows of 1024 against 50,001 230 and 490.
-Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
+// `full`: no tile of which less than half of P is there, since what a tile writes has its place
+// in memory (the gradients of 1,048,576 float32 rows against 50 tokens 256 MB, and 1 GB in
+// tiles of 256).
+Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts, bool full = false) {
   Cut best = {256, 1, 0};
   const struct {
     int32_t tile;
@@ -703,6 +706,7 @@ Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
   // parts are written and read once more, 7 MB in the time of a stage
   const double way = 8.0 * (double)p * (double)q / 7e6;
   for (const auto& s : sizes) {
+    if (full && s.tile >= 2 * up(p, kStep)) continue;
     const int64_t tiles = ((p + s.tile - 1) / s.tile) * ((q + s.tile - 1) / s.tile);
     for (int n = 1; n <= (parts ? 64 : 1) && n <= (steps + 3) / 4; ++n) {
       const double rounds = (double)((tiles * n + 255) / 256);
@@ -720,12 +724,13 @@ Cut cut(int64_t p, int64_t q, int64_t steps, int64_t stages, bool parts) {
 // 1024 float32 against 32,769 tokens 1483 us, and 1666 without; of 2000 x 512 bfloat16
 // against 8193 165 and 182).
 constexpr int64_t kRest = 64;  // tokens that may be on their own
-Strips strips(int64_t tokens, int64_t others, int64_t steps, int64_t stages, bool parts) {
-  Strips s = {(int32_t)tokens, {cut(tokens, others, steps, stages, parts), {64, 1, 0}}};
+Strips strips(int64_t tokens, int64_t others, int64_t steps, int64_t stages, bool parts,
+              bool full = false) {
+  Strips s = {(int32_t)tokens, {cut(tokens, others, steps, stages, parts, full), {64, 1, 0}}};
   const int64_t rest = tokens % 256, main = tokens - rest;
   if (rest == 0 || rest > kRest || main == 0) return s;
-  const Cut a = cut(main, others, steps, stages, parts);
-  const Cut b = cut(rest, others, steps, stages, parts);
+  const Cut a = cut(main, others, steps, stages, parts, full);
+  const Cut b = cut(rest, others, steps, stages, parts, full);
   // (a launch of its own: 4 us)
   if (a.cost + b.cost + 3.0 < s.cut[0].cost) s = {(int32_t)main, {a, b}};
   return s;
@@ -754,7 +759,7 @@ Layout plan(const Call& c) {
   L.copy_w = L.copy_w && L.gather;
   // products of planes that a step takes
   const int64_t stages = f32 ? 3 : 1;
-  L.stats = strips(c.C, c.n, L.dp / kStep, stages, false);
+  L.stats = strips(c.C, c.n, L.dp / kStep, stages, false, grads);
   L.n_part = few_parts(c.C);
   if (!L.few) {
     const int32_t main = L.stats.main, rest = c.C - main;
@@ -781,13 +786,20 @@ Layout plan(const Call& c) {
   if (f32) L.m = take(L.np * 4);
   if (f32) L.most = take(kTops * 4);
   L.hit = take(L.np * 4);
-  if (!c.lse || L.few || c.n <= kPair) L.part = take(L.np * L.n_part * 8);
+  if (!c.lse || L.few || c.n <= kPair) L.part = take(c.n * L.n_part * 8);
   if (L.gather) L.px = take(L.planes * L.np * L.dp * 2);
   if (f32 && c.dw) L.pxm = take(L.planes * L.np * L.dp * 2);
   if (L.copy_w) L.pw = take(L.planes * c.C * L.dp * 2);
   if (grads) {
-    // pieces of the vocabulary of about kGradBytes of gradients, of equal sizes
-    const int64_t all = L.planes * L.np * 2 * c.C;
+    // Logits that the statistics write and the gradients read again (float32, up to 256 MB)
+    // cost less than another product: a step of 16,000 x 512 float32 against 1025 tokens 292
+    // us instead of 313, of 300 x 1024 bfloat16 against 50,001 230 instead of 258.
+    const bool pair = !f32 && c.n > 0 && c.n <= kPair;  // (without rows there is nothing to keep)
+    L.kept = (!c.lse || L.few || pair) && c.n * up(c.C, kTile) * 4 <= kGradBytes;
+    // Pieces of the vocabulary of about kGradBytes of gradients, of equal sizes. Those of kept
+    // logits are made by 64 rows, others by tiles.
+    L.rows_g = L.kept ? up(c.n, kStep) : L.np;
+    const int64_t all = L.planes * L.rows_g * 2 * up(c.C, kStep);
     int64_t pieces = (all + kGradBytes / 2) / kGradBytes;
     // (a few tokens more than whole tiles go with the last piece, and none is without a tile)
     pieces = std::max<int64_t>(std::min(pieces, (c.C - kRest + kTile - 1) / kTile), 1);
@@ -795,22 +807,29 @@ Layout plan(const Call& c) {
     L.pieces = pieces == 1 ? 1 : (int32_t)((c.C - kRest + L.piece - 1) / L.piece);
     const int32_t last = c.C - (L.pieces - 1) * L.piece;
     const int32_t most = std::max(last, std::min(c.C, L.piece));
-    L.ldg = (int32_t)up(most, kTile);
-    // Logits that the statistics write and the gradients read again (float32, up to 256 MB)
-    // cost less than another product: a step of 16,000 x 512 float32 against 1025 tokens 292
-    // us instead of 313, of 300 x 1024 bfloat16 against 50,001 230 instead of 258.
-    // (a call without rows has no place for a second set of them)
-    L.paired = !f32 && L.pieces == 1 && c.n > 0 && c.n <= kPair;
-    L.kept = (!c.lse || L.few || L.paired) && L.pieces == 1 && c.n * L.ldg * 4 <= kGradBytes;
-    L.G = take(L.planes * L.np * L.ldg * 2);
+    L.kept = L.kept && L.pieces == 1;
+    if (!L.kept) L.rows_g = L.np;
+    L.paired = L.kept && pair;
+    L.grad = strips(last, c.n, L.dp / kStep, stages, false, true);
+    L.grad_all = cut(L.piece, c.n, L.dp / kStep, stages, false);
+    // (a row ends where the last tile that writes it does)
+    auto reach = [](const Strips& s, int32_t tokens) {
+      return (int32_t)(s.main < tokens ? s.main + up(tokens - s.main, s.cut[1].tile)
+                                       : up(tokens, s.cut[0].tile));
+    };
+    L.ldg = L.kept ? (int32_t)up(c.C, kStep) : reach(L.grad, last);
+    if (L.kept && !L.few) L.ldg = reach(L.stats, c.C);
+    if (L.pieces > 1) L.ldg = std::max(L.ldg, L.piece);
+    L.G = take(L.planes * L.rows_g * L.ldg * 2);
     // (by 16 rows where 64 would leave CUs idle: a step of 1511 bfloat16 rows of 336 against 612
     // tokens 51 us by 64, 47 by 16; of 16,000 float32 rows of 512 against 1025 288 and 300)
     L.kept_rows = up(c.n, 64) / 64 * ((c.C + 255) / 256) < 1024 ? 16 : 64;
-    if (L.kept) L.z = take(L.np * L.ldg * 4);
+    if (L.kept) L.z = take(c.n * L.ldg * 4);
     if (c.dx) {
       L.x = cut(L.dp, c.n, up(most, kStep) / kStep, stages, true);
       L.direct = L.x.parts == 1 && !L.paired;
-      if (!L.direct || L.pieces > 1) L.acc_x = take(L.x.parts * L.np * L.dp * 4);
+      L.rows_x = L.paired ? 2 * kPair : c.n;
+      if (!L.direct || L.pieces > 1) L.acc_x = take(L.x.parts * L.rows_x * L.dp * 4);
     }
     if (c.dw) {
       // (the last piece's cut: all others have whole tiles)
@@ -823,9 +842,7 @@ Layout plan(const Call& c) {
       L.acc_w = take(std::max({sums(L.w.main, L.w.cut[0]), sums(last - L.w.main, L.w.cut[1]),
                                L.pieces > 1 ? sums(L.piece, L.w_all) : 0}));
     }
-    L.grad = strips(last, c.n, L.dp / kStep, stages, false);
-    L.grad_all = cut(L.piece, c.n, L.dp / kStep, stages, false);
-    if (c.db) L.col = take(L.np / (L.kept ? L.kept_rows : 64) * L.ldg * 4);
+    if (c.db) L.col = take(L.rows_g / (L.kept ? L.kept_rows : 64) * L.ldg * 4);
   }
   L.total = at;
   return L;
@@ -956,7 +973,7 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
     const bool last = piece + 1 == L.pieces;
     const int32_t c0 = piece * L.piece, n = last ? c.C - c0 : L.piece;
     const Strips grad = last ? L.grad : Strips{n, {L.grad_all, L.grad_all}};
-    const Operand G = {u16(L.G), PL * L.ldg, (int32_t)L.np, n};
+    const Operand G = {u16(L.G), PL * L.ldg, (int32_t)L.rows_g, n};
     float* col = c.db ? flt(L.col) : nullptr;
     if (L.kept && c.n > 0) {
       const Kept k = {meta, flt(L.z), L.ldg, L.few ? idx : nullptr, g.row, c.C,
@@ -1001,7 +1018,7 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
         x.out = c.dx;
         x.ldo = c.dx_stride;
       }
-      x.acc_split = L.np * L.dp;
+      x.acc_split = L.rows_x * L.dp;
       x.lda = (int32_t)L.dp;
       x.add = piece > 0;
       x.paired = L.paired;
@@ -1043,7 +1060,7 @@ hipError_t run_t(const Call& c, const Layout& L, char* ws, hipStream_t st) {
     Gemm x = g;
     x.splits = L.x.parts;
     x.acc = flt(L.acc_x);
-    x.acc_split = L.np * L.dp;
+    x.acc_split = L.rows_x * L.dp;
     x.lda = (int32_t)L.dp;
     x.paired = L.paired;
     join_kernel<T><<<dim3(blocks(c.n * ((c.D + 3) / 4))), dim3(256), 0, st>>>(

@@ -176,6 +176,7 @@ struct Strips {
 // How a call is done, and where its buffers lie in the workspace.
 struct Layout {
   int64_t np, dp, planes;      // gathered rows and values a row, rounded up
+  int64_t rows_g, rows_x;      // rows of the logits' gradients, and of dx's sums
   bool copy_w, few, gather, paired;
   bool kept;                   // the logits, from the statistics to their gradients
   int32_t n_part;

@@ -568,6 +568,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
 #pragma unroll
         for (int j = 0; j < FQ; ++j) {
           const int64_t row = q0 + wq + 16 * j + lq;
+          if (row >= meta.n) continue;
 #pragma unroll
           for (int i = 0; i < FP; ++i)
             *reinterpret_cast<f32x4*>(g.z + row * g.ldg + p0 + c_lane + 16 * i) = acc[i][j];

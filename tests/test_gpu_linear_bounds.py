@@ -70,3 +70,25 @@ def test_sums_in_parts_stay_in_their_place(dtype, n, D, C):
                             workspace=ws)
         assert untouched(whole, need)
         check_all(dict(out, loss=loss), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n, D, C", [(70001, 8, 29), (70001, 8, 64), (70000, 8, 65), (9000, 70, 128),
+                                     (70001, 8, 129), (9000, 70, 320), (9000, 70, 321),
+                                     (1_600_000, 4, 64), (3000, 40, 1025), (300, 64, 50001)])
+def test_few_tokens_and_many_rows(n, D, C, dtype):
+    """Gradients in rows as long as the tokens need, in one piece and in several."""
+    from paper_2608_21343_amd import capi
+    c = R.case(n, D, C, dtype, 2, device="cuda", gaps=True)
+    want = R.expected(c)
+    need = capi.tb_linear_xent_workspace_bytes(c["x"], c["w"], 7)
+    ws, whole = guarded(need, 255)
+    out, loss, lse = outputs(c), *torch.empty((2, n), device="cuda")
+    capi.tb_linear_xent(c["x"], c["w"], c["target"], loss, lse, **out, bias=c["bias"], workspace=ws)
+    assert untouched(whole, need)
+    check_all(dict(out, loss=loss), want)
+    need = capi.tb_linear_xent_workspace_bytes(c["x"], c["w"], 7, True)
+    ws, whole = guarded(need, 255)
+    capi.tb_linear_xent_grad(c["x"], c["w"], c["target"], lse, **out, bias=c["bias"], workspace=ws)
+    assert untouched(whole, need)
+    check_all(out, want)
