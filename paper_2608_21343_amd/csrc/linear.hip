@@ -679,12 +679,16 @@ __global__ void __launch_bounds__(1024)
 // 256 MB 7.4 ms, of 128 8.4, of 64 10.2), and of logits that are kept.
 constexpr int64_t kGradBytes = 256ll << 20;
 constexpr int64_t kMostStride = 1 << 22;      // of weights that are read where they are
-// Rows that linear_few.hip takes. It reads the weights once for 16 bfloat16 rows and is bound
-// by that (16 rows of 1024 against 131,073 tokens 54 us, tiles 86; 32 rows 62 and 85; 64
-// rows 89 and 84), float32 ones without a copy of the weights (64 rows against 131,073
-// tokens 218 us, tiles with the copy 475). With gradients the copy is made in any case
-// (float32, 32,769 tokens: 16 rows 236 us, tiles 247; 64 rows 320 and 249).
-int32_t few_rows(bool f32, bool grads) { return grads ? 16 : f32 ? 64 : 32; }
+// Rows that linear_few.hip takes, whatever a call returns: its logits differ in their last
+// bits from those of the tiles, so a call that gives lse and the one that takes it, and a call's
+// statistics and gradients, go by one rule (their logits are always kept: 64 rows against 2^20
+// tokens are 256 MB). It reads the weights once for 16 bfloat16 rows and is bound by that (16
+// rows of 1024 against 131,073 tokens 54 us, tiles 86; 32 rows 62 and 85; 64 rows 89 and 84),
+// float32 ones without a copy of the weights (64 rows against 131,073 tokens 218 us, tiles
+// with the copy 475). With gradients the copy is made in any case: steps and backward passes
+// of 17 to 64 float32 rows take up to a quarter longer than with tiles' logits (32,769
+// tokens: 32 rows 254 us and 236, 64 rows 306 and 243), bfloat16 ones up to a tenth.
+int32_t few_rows(bool f32) { return f32 ? 64 : 32; }
 
 // How a product is cut: tiles of 256 x 256, or smaller ones where those would leave CUs
 // idle, and parts of the summed axis where that still leaves them idle. The costs are in
@@ -753,7 +757,7 @@ Layout plan(const Call& c) {
   const bool read = c.D * size % 16 == 0 && c.w_stride * size % 16 == 0 &&
                     (uintptr_t)c.w % 16 == 0 && c.x_stride * size % 16 == 0 &&
                     (uintptr_t)c.x % 16 == 0;
-  L.few = read && c.n <= few_rows(f32, grads);
+  L.few = read && c.n <= few_rows(f32);
   // (the loss of few rows needs no copies)
   L.gather = grads || !L.few;
   L.copy_w = L.copy_w && L.gather;
@@ -1076,7 +1080,7 @@ int64_t most_workspace(Call c) {
   c.x_stride = c.w_stride;
   c.x = nullptr;
   const int64_t aligned = plan(c).total;
-  if (c.n > few_rows(true, false)) return aligned;
+  if (c.n > few_rows(true)) return aligned;
   c.x = reinterpret_cast<const void*>(1);
   return std::max(aligned, plan(c).total);
 }

@@ -32,3 +32,55 @@ def test_a_batch_without_rows(shape, dtype):
     loss, dx, dw, db = linear_xent_step(x.detach(), c["w"], target, c["bias"])
     assert loss.shape == shape and dx.shape == x.shape and not dw.any() and not db.any()
     capi.tb_linear_xent(x.detach(), c["w"], target, loss)
+
+
+@pytest.mark.parametrize("dtype, n", [(F32, 9), (F32, 16), (F32, 17), (F32, 32), (F32, 33),
+                                      (F32, 64), (F32, 65), (BF16, 9), (BF16, 16), (BF16, 17),
+                                      (BF16, 32), (BF16, 33)])
+def test_both_passes_see_the_same_logits(dtype, n):
+    """Rows that are nearly certain, of values whose logits depend on how they are summed:
+    lse has to be that of the logits which the backward pass makes, or p - 1 is their
+    difference.
+
+    float32: 1 + 2^-12 + 2^-23 takes 24 bits; two float16 planes hold 23 of them, so 1024
+    of them are short by 2^-13, of all tokens alike. Among each other the logits may be off by
+    e = 2^-5 + 2^-13: the target's sum is of multiples of 2^-12 below 2^11, exact in any order;
+    the others' is of 1024 products 2^-12 (1 - 2^-6) of the lower plane besides, and if each is
+    added on its own, each addition rounds by half a step of a sum below 1024, 2^-15.
+    bfloat16: 32 sums of 32 products, each 3/8 of a step of a sum of 1024, which a sum that
+    begins at the bias drops and one to which the bias is added keeps, for all tokens alike;
+    e = 2^-12, a rounding or two of half a step of 1024, 2^-14 each."""
+    from paper_2608_21343_amd.linearops import linear_xent
+    D, C, at = 1024, 1025, 5
+    if dtype == F32:
+        x = torch.full((n, D), 1 + 2.0 ** -12 + 2.0 ** -23, device="cuda")
+        w = torch.full((C, D), 1 - 2.0 ** -6, device="cuda")
+        w[at] = 1.0
+        b = torch.zeros(C, device="cuda")
+    else:
+        x = torch.full((n, D), 3 * 2.0 ** -11, dtype=dtype, device="cuda")
+        w = torch.full((C, D), 2.0 ** -10, dtype=dtype, device="cuda")
+        b = torch.full((C,), 1024.0, dtype=dtype, device="cuda")
+        b[at] = 1040.0
+    target = torch.full((n,), at, dtype=torch.int32, device="cuda")
+    z = x[:1].double() @ w.double().t() + b.double()
+    p = torch.softmax(z, 1)[0]
+    G = p * n
+    rest = 1 - p[at]
+    G[at] = -(p.sum() - p[at]) * n
+    assert 1e-5 < float(rest) < 1e-3
+    leaves = [t.requires_grad_() for t in (x, w, b)]
+    _, dw, db = torch.autograd.grad(linear_xent(*leaves[:2], target, b).loss.sum(), leaves)
+    # the logits' differences (e^2e - 1, below 4 e), exponentials of -16 to 2^-19 of themselves,
+    # n additions; for the target's entry roundings near 1 besides: four of a, and of the sum of
+    # the 64 tokens beside it
+    e = 2.0 ** -12 if dtype == BF16 else 2.0 ** -5 + 2.0 ** -13
+    tol = G.abs() * (4 * e + 2.0 ** -18 + (n + 4) * 2.0 ** -24)
+    tol[at] += n * (4 + 68) * 2.0 ** -24
+    off = (db.double() - G).abs()
+    assert bool((off <= tol + R.U[dtype] * G.abs()).all()), (off / G.abs()).max()
+    # (x is one value; G's own rounding is a part of b with many bfloat16 rows, of G with others)
+    one = float(x[0, 0].detach())
+    planes = R.U[dtype] if dtype == BF16 else 2.0 ** -21
+    off = (dw.double() - G[:, None] * one).abs()
+    assert bool((off <= one * (tol + (planes + R.U[dtype]) * G.abs())[:, None]).all()), off.max()
