@@ -65,6 +65,11 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def step(self, closure=None, grad_scale=None):
+        if torch.cuda.is_current_stream_capturing() and not all(
+                group["capturable"] for group in self.param_groups):
+            # (a graph would hold this step's bias corrections and roundings)
+            raise RuntimeError("a step is captured of capturable groups alone, and its states "
+                               "are made before the capture")
         loss = None
         if closure is not None:
             with torch.enable_grad():
