@@ -75,6 +75,8 @@ class AdamW(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         for at, group in enumerate(self.param_groups):
+            if "step_dev" in group and not group["capturable"]:
+                self._count_on_host(group)
             # one call for the tensors of a device and type that are equally far
             calls = {}
             for p in group["params"]:
@@ -93,16 +95,35 @@ class AdamW(torch.optim.Optimizer):
                            grad_scale)
         return loss
 
+    def _counter(self, group, device):
+        """The number of a capturable group's steps so far, on a device."""
+        counters = group.setdefault("step_dev", {})
+        if device not in counters:
+            if torch.cuda.is_current_stream_capturing():
+                # (its replays would count from the same number every time)
+                raise RuntimeError("the first capturable step makes its counter: run it before "
+                                   "the capture")
+            steps = {self.state[p]["step"] for p in group["params"]}
+            if len(steps) != 1:
+                raise RuntimeError("parameters that have made different numbers of steps cannot "
+                                   "become capturable")
+            counters[device] = torch.full((1,), steps.pop(), dtype=torch.int64, device=device)
+        return counters[device]
+
+    def _count_on_host(self, group):
+        """Of a group that was capturable: its states take over the number of its steps."""
+        counters = group.pop("step_dev")
+        for p in group["params"]:
+            if p in self.state and p.device in counters:
+                self.state[p]["step"] = int(counters[p.device])
+
     def _call(self, group, at, device, step, params, states, grad_scale):
         lr, lr_dev, step_dev = group["lr"], None, None
         if isinstance(lr, torch.Tensor):
             lr, lr_dev = 0.0, lr.reshape(1)
         if group["capturable"]:
-            counters = group.setdefault("step_dev", {})
-            if device not in counters:
-                counters[device] = torch.zeros(1, dtype=torch.int64, device=device)
             # (the tensors of a device share it: the first call of a step counts)
-            step_dev = counters[device]
+            step_dev = self._counter(group, device)
             if params[0] is next(p for p in group["params"] if p.device == device):
                 step_dev.add_(1)
             step = 1
@@ -124,6 +145,16 @@ class AdamW(torch.optim.Optimizer):
 
     def load_state_dict(self, state_dict):
         super().load_state_dict(state_dict)
+        # counters and rates on the device were saved with their group, under the devices of then
+        for group in self.param_groups:
+            devices = {p.device for p in group["params"]}
+            counters = group.pop("step_dev", None)
+            if counters:
+                steps = max(int(t) for t in counters.values())  # (they are the same on all)
+                group["step_dev"] = {d: torch.full((1,), steps, dtype=torch.int64, device=d)
+                                     for d in devices}
+            if isinstance(group["lr"], torch.Tensor) and len(devices) == 1:
+                group["lr"] = group["lr"].to(*devices)
         # the states keep their own types (torch casts them to the parameter's)
         saved = [i for g in state_dict["param_groups"] for i in g["params"]]
         mine = [p for g in self.param_groups for p in g["params"]]

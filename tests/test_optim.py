@@ -44,3 +44,61 @@ def test_only_capturable_steps_are_captured(calls, monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
     opt.step()
     assert len(calls) == done + 2
+
+
+@pytest.fixture
+def steps(monkeypatch):
+    made = []
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(optim.capi, "tb_adamw_step",
+                        lambda param, *a, step, step_dev, **how: made.append(
+                            step if step_dev is None else (int(step_dev), step_dev.device)))
+    return made
+
+
+def test_counters_resume_on_their_parameters_device(steps, tmp_path):
+    """A state dict of other devices than those of the parameters: the counter goes on."""
+    one, two = leaf(), leaf(5)
+    opt = optim.AdamW([one, two], lr=torch.tensor(1e-3), capturable=True)
+    for _ in range(2):
+        opt.step()
+    saved = opt.state_dict()
+    here = torch.device("cpu")
+    group = saved["param_groups"][0]
+    assert group["step_dev"][here].tolist() == [2]
+    other = dict(saved, param_groups=[dict(group, step_dev={
+        torch.device("meta"): group["step_dev"][here].clone()})])
+    torch.save(saved, tmp_path / "state.pt")
+    for state in (saved, other, torch.load(tmp_path / "state.pt", map_location="cpu",
+                                           weights_only=True)):
+        again = optim.AdamW([leaf(), leaf(5)], capturable=True)
+        again.load_state_dict(state)
+        steps.clear()
+        again.step()
+        assert steps == [(3, here)]
+        assert again.param_groups[0]["step_dev"].keys() == {here}
+    assert group["step_dev"][here].tolist() == [2]  # the saved one stays
+
+
+def test_capturable_may_change(steps, monkeypatch):
+    """The number of steps goes along, both ways."""
+    one, two = leaf(), leaf(5)
+    opt = optim.AdamW([one, two])
+    for _ in range(3):
+        opt.step()
+    opt.param_groups[0]["capturable"] = True
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="before the capture"):
+        opt.step()
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    opt.step()
+    opt.step()
+    opt.param_groups[0]["capturable"] = False
+    opt.step()
+    assert steps == [1, 2, 3, (4, one.device), (5, one.device), 6]
+    one.grad = None
+    opt.step()
+    one.grad = torch.ones(3)
+    opt.param_groups[0]["capturable"] = True
+    with pytest.raises(RuntimeError, match="different numbers"):
+        opt.step()
