@@ -9,6 +9,7 @@ Gradients are not themselves differentiable: a second derivative raises an error
 
 from __future__ import annotations
 
+import weakref
 from typing import NamedTuple, Optional
 
 import torch
@@ -44,21 +45,45 @@ def _args(x, w, target, bias, weight):
             None if weight is None else weight.contiguous())
 
 
+class _Eager:
+    """An eager call whose graph is alive: it lies in the metadata of the call's node
+    and names the nodes that follow."""
+
+    def __init__(self, node):
+        self.inputs = [n for n, _ in node.next_functions if n is not None]
+
+
+_eager = weakref.WeakSet()
+
+
+def _leaves(nodes) -> set:
+    """The accumulations that a backward pass through these nodes reaches."""
+    seen, todo = set(), list(nodes)
+    while todo:
+        node = todo.pop()
+        if node not in seen:
+            seen.add(node)
+            todo += [n for n, _ in node.next_functions if n is not None]
+    return {n for n in seen if n.name() == "torch::autograd::AccumulateGrad"}
+
+
 def _mark(node) -> None:
     """A backward pass that is captured while a graph of an eager pass over the same
     leaves is alive would wait, inside the capture, for the stream of that pass
-    (torch gives a leaf's accumulation the stream of its first use), and end the
-    process when the capture ends: such a call is refused here. The marks are on
-    the accumulations that follow ``node``, which live as long as a graph of theirs."""
-    capturing = torch.cuda.is_current_stream_capturing()
-    for leaf, _ in node.next_functions:
-        if leaf is not None and leaf.name() == "torch::autograd::AccumulateGrad":
-            marks = leaf.metadata
-            if not capturing:
-                marks["tbias_eager"] = True
-            elif marks.get("tbias_eager"):
-                raise RuntimeError("a graph of an eager pass over this layer is alive: drop its "
-                                   "losses before the capture")
+    (torch gives a leaf's accumulation the stream of its first use). Where that is
+    the default stream, which no capture may wait for, the process would end with the
+    capture: such a call is refused here, however far behind the call the leaves
+    are. Only a call that is captured looks that far."""
+    if not torch.cuda.is_current_stream_capturing():
+        if not (torch.cuda.is_initialized() and capi._stream(None)):  # (0: the default one)
+            call = node.metadata["tbias_eager"] = _Eager(node)
+            _eager.add(call)
+        return
+    mine = _leaves([node])
+    for call in list(_eager):
+        if not mine.isdisjoint(_leaves(call.inputs)):
+            raise RuntimeError("a graph of an eager pass over this layer is alive: drop its "
+                               "losses before the capture")
 
 
 class _LinearXent(torch.autograd.Function):
@@ -98,7 +123,8 @@ def linear_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
     ``weight`` [...] multiplies the losses; rows of weight 0 or without a target
     are left out (loss and lse 0). Differentiable with respect to x, w and bias;
     a weight that requires a gradient is refused, and so is a call under graph
-    capture while the graph of an eager call with the same leaves is alive."""
+    capture while the graph of an eager call on the default stream is alive that
+    shares a leaf with it (one on another stream, as a capture is warmed up on, may be)."""
     _constant(weight, "weight")
     out = _LinearXent.apply(x, w, target, bias, weight)
     if out[0].requires_grad:

@@ -84,3 +84,51 @@ def test_both_passes_see_the_same_logits(dtype, n):
     planes = R.U[dtype] if dtype == BF16 else 2.0 ** -21
     off = (dw.double() - G[:, None] * one).abs()
     assert bool((off <= one * (tol + (planes + R.U[dtype]) * G.abs())[:, None]).all()), off.max()
+
+
+def layer(n=100, dtype=BF16):
+    """Features and float32 weights that are cast for the call, and a pass through it."""
+    from paper_2608_21343_amd.linearops import linear_xent
+    c = R.case(n, 64, 500, dtype, 16, device="cuda")
+    x = c["x"].float().requires_grad_()
+    w = c["w"].float().requires_grad_()
+
+    def run():
+        loss = linear_xent(x.to(dtype), w.to(dtype), c["target"], c["bias"]).loss.sum()
+        return (loss, *torch.autograd.grad(loss, (x, w)))
+
+    return run
+
+
+def test_a_capture_beside_an_eager_loss_is_refused():
+    """The leaves lie behind casts; the loss is of the default stream."""
+    run = layer()
+    loss = run()[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError, match="drop its losses"):
+            run()
+    del loss
+
+
+def test_a_capture_beside_its_warm_up():
+    """The usual recipe: some passes on a side stream, whose last loss is still in scope."""
+    run = layer()
+    want = [t.detach().clone() for t in run()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            loss, dx, dw = run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for _ in range(3):
+        for t in out[1:]:
+            t.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(bool((a == b).all()) for a, b in zip(out[1:], want[1:]))
+        run()
+    assert torch.isfinite(loss)
