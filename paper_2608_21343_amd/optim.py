@@ -27,17 +27,26 @@ class AdamW(torch.optim.Optimizer):
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, state_bits: int = 32, master: bool = False,
                  capturable: bool = False, seed: int = 0):
-        if state_bits not in (8, 32):
-            raise ValueError("state_bits must be 8 or 32")
-        if isinstance(lr, torch.Tensor) and (lr.numel() != 1 or lr.dtype != torch.float32):
-            raise ValueError("a learning rate on the device is one float32")
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay,
                                       state_bits=state_bits, master=master,
                                       capturable=capturable, seed=seed))
 
     def add_param_group(self, group):
         super().add_param_group(group)
-        for p in self.param_groups[-1]["params"]:
+        try:
+            self._check(self.param_groups[-1])
+        except ValueError:
+            self.param_groups.pop()  # (a group that is refused leaves nothing behind)
+            raise
+
+    @staticmethod
+    def _check(group):
+        if group["state_bits"] not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        lr = group["lr"]
+        if isinstance(lr, torch.Tensor) and (lr.numel() != 1 or lr.dtype != torch.float32):
+            raise ValueError("a learning rate on the device is one float32")
+        for p in group["params"]:
             if p.dtype not in (torch.float32, torch.bfloat16):
                 raise ValueError("parameters must be float32 or bfloat16")
             if not p.is_contiguous():

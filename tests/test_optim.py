@@ -102,3 +102,22 @@ def test_capturable_may_change(steps, monkeypatch):
     opt.param_groups[0]["capturable"] = True
     with pytest.raises(RuntimeError, match="different numbers"):
         opt.step()
+
+
+@pytest.mark.parametrize("group, message", [
+    (dict(params=[torch.zeros(4, dtype=torch.float16)]), "float32 or bfloat16"),
+    (dict(params=[torch.zeros(4, 6).t()]), "contiguous"),
+    (dict(params=[torch.zeros(4)], state_bits=4), "state_bits"),
+    (dict(params=[torch.zeros(4)], lr=torch.zeros(2)), "learning rate"),
+])
+def test_a_group_that_is_refused_leaves_nothing(group, message, calls):
+    group["params"][0].requires_grad_()
+    kept = leaf()
+    opt = optim.AdamW([kept])
+    with pytest.raises(ValueError, match=message):
+        opt.add_param_group(group)
+    assert len(opt.param_groups) == 1
+    opt.step()
+    assert len(calls) == 1 and calls[0]["param"][0] is kept
+    with pytest.raises(ValueError, match=message):
+        optim.AdamW([group])
