@@ -632,7 +632,7 @@ __global__ void __launch_bounds__(256)
     const int d = (int)(at - row * each) * 4;
     const int64_t from = inv ? inv[row] : row;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    float scale = 0.f;
+    Scale scale = {0.f, 0};
     if (from >= 0) {
       const float* p = g.acc + from * g.lda + d;
       for (int s = 0; s < g.splits; ++s) {
@@ -644,7 +644,7 @@ __global__ void __launch_bounds__(256)
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     if (from >= 0)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = v[e] * scale;
+      for (int e = 0; e < 4; ++e) w[e] = scaled<T>(v[e], scale);
     store4(out + row * ldo + d, w, wide, g.D - d);
   }
 }

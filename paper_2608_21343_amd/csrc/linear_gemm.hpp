@@ -288,16 +288,37 @@ __device__ __forceinline__ void gather16(uint2 a, uint2 b, uint2 c, uint2 d, uin
   *hi = make_uint4(x[2], y[2], x[3], y[3]);
 }
 
-// What dw's sums are multiplied with.
+// What sums are multiplied with: by 2^e. Units may be as large or small as their values, so
+// a product of two of them could leave float32's range where the result does not.
+struct Scale {
+  float by;
+  int e;
+};
+__device__ __forceinline__ int exponent_of(float unit) {  // of a power of two
+  return (int)(__float_as_uint(unit) >> 23 & 255) - 127;
+}
+__device__ __forceinline__ float power_of(int e) {
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
 template <class T>
-__device__ __forceinline__ float dw_scale(const Meta& meta) {
-  return Elem<T>::kScaled ? 0x1p-14f * unit_of(__uint_as_float(meta.T)) : meta.scale;
+__device__ __forceinline__ float scaled(float v, const Scale& s) {
+  return Elem<T>::kScaled ? __builtin_amdgcn_ldexpf(v * s.by, s.e) : v * s.by;
 }
 
-// What gathered row q of dx is multiplied with.
+// Of dw.
 template <class T>
-__device__ __forceinline__ float dx_scale(const Gemm& g, const Meta& meta, int64_t q) {
-  return Elem<T>::kScaled ? g.row.m[q] * meta.S * 0x1p-14f : meta.scale;
+__device__ __forceinline__ Scale dw_scale(const Meta& meta) {
+  if (!Elem<T>::kScaled) return {meta.scale, 0};
+  return {1.f, exponent_of(unit_of(__uint_as_float(meta.T))) - 14};
+}
+
+// Of gathered row q of dx.
+template <class T>
+__device__ __forceinline__ Scale dx_scale(const Gemm& g, const Meta& meta, int64_t q) {
+  if (!Elem<T>::kScaled) return {meta.scale, 0};
+  const float m = g.row.m[q];
+  return {__builtin_amdgcn_frexp_mantf(m),
+          __builtin_amdgcn_frexp_expf(m) + exponent_of(meta.S) - 14};
 }
 
 // exp(z - base) = 2^(z log2(e) + by) (1 + off): the exponent by one operation, and the
@@ -533,15 +554,20 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
     const int c_lane = wp + lp;  // first token of the lane in the tile, of 4 in every 16
     if (kLogits) {
       if (El::kScaled) {
+        // in two steps, each with about half of S's exponent: with all of it one could
+        // overflow on the way to a logit that does not
+        const int e_s = exponent_of(meta.S), half = e_s / 2;
+        const float first = power_of(half), second = power_of(e_s - half);
         float r[FQ];
 #pragma unroll
-        for (int j = 0; j < FQ; ++j) r[j] = par.r[wq + 16 * j + lq];
+        for (int j = 0; j < FQ; ++j)
+          r[j] = fminf(par.r[wq + 16 * j + lq] * second, 0x1p127f);  // (times 0 it is 0)
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int j = 0; j < FQ; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * meta.S * r[j];
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * first * r[j];
       }
       if (El::kScaled && g.bias) {
 #pragma unroll
@@ -748,7 +774,8 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
             if (in && p0 + c_lane + 16 * i < g.lda) sums[4 * i] = acc[i][j];
           continue;
         }
-        const float scale = !in ? 0.f : KIND == kDx ? dx_scale<T>(g, meta, q) : dw_scale<T>(meta);
+        Scale scale = {0.f, 0};
+        if (in) scale = KIND == kDx ? dx_scale<T>(g, meta, q) : dw_scale<T>(meta);
         T* o = static_cast<T*>(g.out) + (KIND == kDx && in ? (int64_t)g.idx[q] : q) * g.ldo;
         if constexpr (sizeof(T) == 2 && FP >= 4) {
           if (wide) {
@@ -757,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
               uint2 out[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const f32x4 v = acc[4 * part + i][j] * scale;
+                const f32x4 v = acc[4 * part + i][j] * scale.by;
                 out[i] = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
               }
               uint4 lo, hi;
@@ -773,8 +800,9 @@ __global__ void __launch_bounds__(kThreads, 2) gemm_kernel(const Gemm g) {
 #pragma unroll
           for (int i = 0; i < FP; ++i) {
             const int d = p0 + c_lane + 16 * i;
-            const float v[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale, acc[i][j][2] * scale,
-                                acc[i][j][3] * scale};
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = scaled<T>(acc[i][j][e], scale);
             store4(o + d, v, wide, g.D - d);
           }
         }
