@@ -51,3 +51,16 @@ def test_logits_of_a_million(n):
     got = step(c, ())
     check_all(got, {k: want[k] for k in ("loss", "lse")})
     assert bool(torch.isfinite(got["loss"]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, torch.bfloat16])
+@pytest.mark.parametrize("n", [9, 40, 300])
+def test_lse_of_tokens_that_are_all_masked_by_a_number(n, dtype):
+    """It is that number, from either side, alone and beside gradients."""
+    c = R.case(n, 96, 700, dtype, 8, device="cuda")
+    c["x"][:] = 0.0
+    c["bias"][:] = -3.0e38
+    want = c["bias"][0].double()
+    for got in (step(c), step(c, ())):
+        # (log 700 is far below half a step of it)
+        assert float((got["lse"].double() - want).abs().max()) <= 2.0 ** -24 * float(want.abs())
