@@ -658,23 +658,28 @@ int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus
  * whose logits hold a NaN or +inf has NaN lse, loss and gradients.
  *
  * Rounding. Sums are float32. bfloat16 products are exact. A float32 operand is taken
- * as the sum of two float16 values in units of a power of two: up to 2^-23 of it is lost, or
- * 2^-39 of the largest value that shares its unit where that is more, which is the
- * largest of its row of x, of all of w, and for dw of all rows of x times their largest
- * |a_i|, |b_i|; products are exact to 2^-21. (Logits of few rows take three bfloat16
- * values, 2^-25, without units.) So values 2^16 below the largest of their unit lose
- * precision. A token whose bias is below -2^100 has no say in the unit, and counts as at
- * most twice the largest of the others. The gradients of the logits are rounded once to
+ * as the sum of two float16 values in units of a power of two (2^-110 and above): up to
+ * 2^-23 of it is lost, or 2^-39 of the largest value that shares its unit, or 2^-135, where
+ * that is more. It shares its unit with its row of x, with all of w, and for dw with all rows of
+ * x times their largest |a_i|, |b_i|; products are exact to 2^-21. (Logits of few rows take
+ * three bfloat16 values, 2^-25, without units.) So values 2^16 below the largest of their
+ * unit lose precision. A token whose bias is below -2^100 has no say in the unit, and counts as
+ * at most twice the largest of the others. The gradients of the logits are rounded once to
  * dtype's precision, as they would be if they were kept (bfloat16: 2^-8 of each, in calls of
- * up to 32 rows 2^-16; float32: 2^-23 of each, or 2^-39 of the row's largest |a_i|, |b_i|); db
- * is the sum of the unrounded ones. The results are rounded once to dtype. Results are the same bits for the same
- * arguments; a loss alone may differ in its last bits from one that comes with gradients.
+ * up to 32 rows 2^-16; float32: 2^-23 of each, or 2^-39 of the row's largest |a_i|, |b_i|);
+ * db is the sum of the unrounded ones. The results are rounded once to dtype. Results are the
+ * same bits for the same arguments; a loss alone may differ in its last bits from one that
+ * comes with gradients.
  *
  * tb_linear_xent_workspace_bytes - for a call with these arguments; grads: sum of 1
  *   (dx), 2 (dw) and 4 (db), 0 for the loss alone; with_lse: 1 for
  *   tb_linear_xent_grad, else 0. w is not read: its address and stride say whether its
  *   rows can be used where they are (16-byte aligned, up to 2^22 values apart, width a
- *   multiple of 64, TB_BF16) or need a copy. -1 for arguments that the calls reject.
+ *   multiple of 64, TB_BF16) or need a copy. Besides that copy the call takes 2 bytes a value
+ *   of x (TB_F32: 4, with dw 8; n_rows rounded up to 256, widths to 64), 8 for every 32 to
+ *   128 tokens of a row, up to 256 MB for logits that are kept, and with gradients 384 MB for
+ *   those of a piece's logits, or 256 tokens and up to 64 behind them in whole tiles for all
+ *   rows (2 bytes each, TB_F32: 4) where that is more. -1 for arguments that the calls reject.
  */
 int64_t tb_linear_xent_workspace_bytes(int32_t dtype, int64_t n_rows, int32_t width,
                                        int32_t v_plus_blank, const void* w, int64_t w_stride,
@@ -698,7 +703,8 @@ int tb_linear_xent(const void* x, const void* w, const void* bias, int32_t dtype
 /*
  * tb_linear_xent_grad - the gradients of a scalar from its gradients with respect to
  * loss and lse (a backward pass). lse is what tb_linear_xent gave for the same x, w,
- * bias, target and weight.
+ * bias, target and weight, where they lie: logits of up to 64 rows come from another kernel
+ * where x and w are 16-byte aligned, and lse has to be that of the same logits.
  *
  *   lse            device float[n_rows]
  *   lse_low        device float[n_rows], out_low of that call, or NULL (0): without it p is

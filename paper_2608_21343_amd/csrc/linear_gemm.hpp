@@ -6,14 +6,16 @@
 // What bounds them is the matrix instructions. In tiles of 256 they are busy two thirds of
 // the time of a long sum (rocprofv3: 0.64 to 0.67 of all pipes' cycles, no bank conflicts in
 // LDS), at clocks that the card lowers to 1.6 to 1.8 GHz under such work. bfloat16 products
-// for 4096 rows of 2048 against 131,073 tokens: statistics 1.65 ms (1330 TFLOP/s; a library
-// product of that size 1380), dx 1.82, dw 1.67, gradients of the logits 1.87; float32 ones of
-// 2048 x 1024 against 32,769 run at 1190 to 1440 TFLOP/s of planes. The statistics of a short
-// sum (640 values) spend nearly half of their time in the exponentials: 32,768 rows
-// against 8193 tokens 320 us, 970 TFLOP/s.
+// for 4096 rows of 2048 against 131,073 tokens, traced: statistics 1.69 ms (1300 TFLOP/s; a
+// library product of that size 1380), dx 1.82, dw 1.71, gradients of the logits 1.87; float32 ones
+// of 2048 x 1024 against 32,769 at 1060 to 1220 TFLOP/s of planes in a traced pass, which is
+// a seventh longer than an untraced one. The statistics of a short sum (640 values) spend nearly
+// half of their time in the exponentials: 32,768 rows, a tenth left out, against 8193 tokens
+// 313 us traced, 990 TFLOP/s (untraced the whole call takes 316).
 //
-// The sums of a tile of 256 take half of a wave's registers, so a CU holds one workgroup; in
-// tiles of 128 the LDS reads of the fragments take as long as the products.
+// A CU holds one workgroup: the sums of a tile of 256 take half of a wave's registers, and
+// smaller tiles have more stages in the same 128 KB of LDS. In tiles of 128 the LDS reads of
+// the fragments take as long as the products.
 //
 // An operand whose rows run along the summed axis lies in LDS as [row, 64] with its
 // 16-byte pieces exchanged by row, so that the 16 rows of a fragment's read cover
