@@ -676,10 +676,12 @@ int tb_distill(const void* logits, int32_t dtype, int64_t n_rows, int32_t v_plus
  *   tb_linear_xent_grad, else 0. w is not read: its address and stride say whether its
  *   rows can be used where they are (16-byte aligned, up to 2^22 values apart, width a
  *   multiple of 64, TB_BF16) or need a copy. Besides that copy the call takes 2 bytes a value
- *   of x (TB_F32: 4, with dw 8; n_rows rounded up to 256, widths to 64), 8 for every 32 to
+ *   of x (TB_F32: 4, with dw 8; n_rows rounded up to 256, widths to 64), 8 for every 16 to
  *   128 tokens of a row, up to 256 MB for logits that are kept, and with gradients 384 MB for
  *   those of a piece's logits, or 256 tokens and up to 64 behind them in whole tiles for all
- *   rows (2 bytes each, TB_F32: 4) where that is more. -1 for arguments that the calls reject.
+ *   rows (2 bytes each, TB_F32: 4) where that is more, their sums for every 16 to 256 rows, and
+ *   sums of dx and dw in parts of up to 256 MB each (with several pieces 4 bytes a value of dx).
+ *   -1 for arguments that the calls reject.
  */
 int64_t tb_linear_xent_workspace_bytes(int32_t dtype, int64_t n_rows, int32_t width,
                                        int32_t v_plus_blank, const void* w, int64_t w_stride,

@@ -92,3 +92,24 @@ def test_few_tokens_and_many_rows(n, D, C, dtype):
     capi.tb_linear_xent_grad(c["x"], c["w"], c["target"], lse, **out, bias=c["bias"], workspace=ws)
     assert untouched(whole, need)
     check_all(out, want)
+
+
+@pytest.mark.parametrize("dtype, n", [(F32, 64), (F32, 65), (BF16, 32), (BF16, 1)])
+def test_the_largest_vocabulary(dtype, n):
+    """The most logits that few rows keep, and one row more."""
+    from paper_2608_21343_amd import capi
+    c = R.case(n, 16, 1 << 20, dtype, 2, device="cuda")
+    want = R.expected(c)
+    need = capi.tb_linear_xent_workspace_bytes(c["x"], c["w"], 7)
+    ws, whole = guarded(need, 255)
+    out, loss, lse, low = outputs(c), *torch.empty((3, n), device="cuda")
+    capi.tb_linear_xent(c["x"], c["w"], c["target"], loss, lse, **out, bias=c["bias"],
+                        out_low=low, workspace=ws)
+    assert untouched(whole, need)
+    check_all(dict(out, loss=loss), want)
+    need = capi.tb_linear_xent_workspace_bytes(c["x"], c["w"], 7, True)
+    ws, whole = guarded(need, 255)
+    capi.tb_linear_xent_grad(c["x"], c["w"], c["target"], lse, **out, bias=c["bias"],
+                             lse_low=low, workspace=ws)
+    assert untouched(whole, need)
+    check_all(out, want)
